@@ -51,6 +51,67 @@ class Plan(ctypes.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class RotaryOperand(ctypes.Structure):
+    """grkan_rotary_t"""
+
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+        ("batch", ctypes.c_int64),
+        ("tokens", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+        ("batch_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("position_batch_stride", ctypes.c_int64),
+        ("position_token_stride", ctypes.c_int64),
+        ("positions_dtype", ctypes.c_int),
+    ]
+
+
+class Attention(ctypes.Structure):
+    """grkan_attention_t"""
+
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("key_lengths", ctypes.c_void_p),
+        ("key_mask", ctypes.c_void_p),
+        ("batch", ctypes.c_int64),
+        ("queries", ctypes.c_int64),
+        ("keys", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("key_lengths_64", ctypes.c_int32),
+        ("q_batch_stride", ctypes.c_int64),
+        ("q_token_stride", ctypes.c_int64),
+        ("q_head_stride", ctypes.c_int64),
+        ("k_batch_stride", ctypes.c_int64),
+        ("k_token_stride", ctypes.c_int64),
+        ("k_head_stride", ctypes.c_int64),
+        ("v_batch_stride", ctypes.c_int64),
+        ("v_token_stride", ctypes.c_int64),
+        ("v_head_stride", ctypes.c_int64),
+        ("mask_batch_stride", ctypes.c_int64),
+        ("mask_key_stride", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+    ]
+
+    @classmethod
+    def of(cls, q, k, v, key_lengths=None, key_mask=None, scale: float = 1.0):
+        """The description of a call on these tensors (which have to outlive it)."""
+        def at(t):
+            return None if t is None else t.data_ptr()
+
+        mask = (key_mask.stride(0), key_mask.stride(1)) if key_mask is not None else (0, 0)
+        wide = key_lengths is not None and key_lengths.element_size() == 8
+        return cls(at(q), at(k), at(v), at(key_lengths), at(key_mask), q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2],
+                   q.shape[3], int(wide), *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *mask, scale)
+
+
 def load_library():
     """Load libgrkan.so (built in-tree by paper_2505_13813_amd/build.py)."""
     global _lib
@@ -127,6 +188,22 @@ def load_library():
     lib.grkan_linear_pack_w.restype = ctypes.c_int
     lib.grkan_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, ctypes.c_int, vp]
     lib.grkan_bwd_noalloc.restype = ctypes.c_int
+    lib.grkan_rms_norm_fwd.argtypes = [vp] * 6 + [i64, i32, i64, i64, ctypes.c_float, ctypes.c_int, ctypes.c_int, vp]
+    lib.grkan_rms_norm_fwd.restype = ctypes.c_int
+    lib.grkan_rms_norm_bwd_workspace_bytes.argtypes = [i64, i32, ctypes.c_int]
+    lib.grkan_rms_norm_bwd_workspace_bytes.restype = sz
+    lib.grkan_rms_norm_bwd.argtypes = [vp] * 7 + [sz, i64, i32, i64, i64, i64, ctypes.c_float, ctypes.c_int, ctypes.c_int, vp]
+    lib.grkan_rms_norm_bwd.restype = ctypes.c_int
+    lib.grkan_rotary.argtypes = [ctypes.POINTER(RotaryOperand), i32, vp, vp, i32, i32, i32, i32, i32, ctypes.c_int, vp]
+    lib.grkan_rotary.restype = ctypes.c_int
+    lib.grkan_attention_lse_count.argtypes = [ctypes.POINTER(Attention)]
+    lib.grkan_attention_lse_count.restype = sz
+    lib.grkan_attention_workspace_bytes.argtypes = [ctypes.POINTER(Attention), i32]
+    lib.grkan_attention_workspace_bytes.restype = sz
+    lib.grkan_attention_fwd.argtypes = [ctypes.POINTER(Attention), vp, vp, vp, sz, ctypes.c_int, vp]
+    lib.grkan_attention_fwd.restype = ctypes.c_int
+    lib.grkan_attention_bwd.argtypes = [ctypes.POINTER(Attention), vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, sz, ctypes.c_int, vp]
+    lib.grkan_attention_bwd.restype = ctypes.c_int
     lib.grkan_alg1_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, vp]
     lib.grkan_alg1_bwd.restype = ctypes.c_int
     _lib = lib

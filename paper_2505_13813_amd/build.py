@@ -11,15 +11,17 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libgrkan.so"
 SOURCES = [CSRC / "grkan_kernels.hip", CSRC / "grkan_plan.cpp", CSRC / "grkan_alg1_baseline.hip",
            CSRC / "grkan_linear.hip", CSRC / "grkan_linear_grad.hip", CSRC / "grkan_hidden.hip",
-           CSRC / "grkan_product.hip", CSRC / "grkan_block.hip"]
+           CSRC / "grkan_product.hip", CSRC / "grkan_block.hip", CSRC / "grkan_norm.hip", CSRC / "grkan_rotary.hip",
+           CSRC / "grkan_attention.hip", CSRC / "grkan_attention_bwd.hip"]
 HEADERS = [CSRC / "grkan_walk.h", CSRC / "grkan_plan.h", CSRC / "grkan_elem.h", CSRC / "grkan_tile.h", CSRC / "grkan_stage2.h",
+           CSRC / "grkan_vector.h", CSRC / "grkan_attention.h",
            PKG.parent / "include" / "grkan.h",
-           PKG.parent / "include" / "grkan_alg1.h"]
+           PKG.parent / "include" / "grkan_alg1.h", PKG.parent / "include" / "grkan_transformer.h"]
 
 # the C++ autograd route of the PyTorch front end: host code only, over the C ABI of the library above
 NATIVE = PKG / "_native.so"
-NATIVE_SOURCES = [CSRC / "grkan_torch.cpp"]
-NATIVE_HEADERS = [PKG.parent / "include" / "grkan.h"]
+NATIVE_SOURCES = [CSRC / "grkan_torch.cpp", CSRC / "grkan_transformer_torch.cpp"]
+NATIVE_HEADERS = [CSRC / "grkan_torch.h", PKG.parent / "include" / "grkan.h", PKG.parent / "include" / "grkan_transformer.h"]
 
 # packed-fp32 code generation is switched off on purpose (hipcc flag, device side)
 HIPCC_FLAGS = [

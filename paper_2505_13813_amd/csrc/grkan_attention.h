@@ -1,0 +1,251 @@
+// What the cross attention's kernels share: arguments, tiles of rows in LDS, and operands of the matrix instructions from them.
+//
+// The queries of the heads that read one key head are one list of rows: row r is query r / group of head r mod group, so that every
+// product has as many rows as the heads allow, with one query too.
+//
+// All products run in 32 x 32 x 16 matrix instructions, arranged so that the probabilities never leave the registers: the scores
+// are formed transposed, S^T = K Q^T, and a lane then holds sixteen keys of one row (keys 8 (i / 4) + 4 (lane / 32) + i mod 4);
+// the order of the keys in a contraction is free as long as both operands agree, and in this one the lane's probabilities are
+// the second operand of V^T P^T as they lie.  V^T comes from V's rows in LDS by transposing reads, numbered the same way.
+#ifndef GRKAN_ATTENTION_H_
+#define GRKAN_ATTENTION_H_
+
+#include "../../include/grkan_transformer.h"
+#include "grkan_tile.h"
+
+namespace grkan {
+namespace attention {
+
+using namespace tile;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// [batch, token, head, channel]; strides in bytes
+struct Operand {
+    uint64_t at;
+    int64_t batch, token, head;
+};
+
+struct Args {
+    Operand q, k, v, dout;
+    const void *lengths;
+    const uint8_t *mask;
+    int64_t mask_batch, mask_key;
+    int64_t keys, rows; // rows: queries x group
+    int32_t batch, kv_heads, group, dim;
+    int32_t lengths_64;
+    float c; // scale x log2(e)
+    float scale;
+    char *out;              // dq in the backward pass
+    char *dk, *dv;
+    float *lse;             // [batch, kv_heads, rows]
+    float *partial;         // [splits][batch, kv_heads][rows][dim], then the splits' lse [splits][batch, kv_heads][rows]
+    // backward: of each row, padded to whole tiles of 64, its lse and sum over channels of dout out; the largest |dout| of each 64
+    float *row_lse, *row_delta, *row_most;
+    int32_t padded;         // rows with the padding
+    int32_t splits, tiles_per_split;
+    int32_t row_tiles, key_tiles; // workgroups of a key head over rows, over keys
+    int32_t work, per_xcd;
+};
+
+template <typename IO> struct Matrix;
+template <> struct Matrix<__bf16> {
+    static __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t two(float a, float b) { return pack(a, b); }
+    static __device__ __forceinline__ float first(uint32_t w) { return low(w); }
+    static __device__ __forceinline__ float second(uint32_t w) { return high(w); }
+};
+template <> struct Matrix<_Float16> {
+    static __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t two(float a, float b)
+    {
+        f32x2 v;
+        v[0] = a;
+        v[1] = b;
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    }
+    static __device__ __forceinline__ float first(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
+    static __device__ __forceinline__ float second(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
+};
+
+// Row r of a key head's list: query r / group of its head r mod group.
+__device__ __forceinline__ int64_t row_offset(uint32_t row, uint32_t group, int64_t token, int64_t head)
+{
+    if (group == 1)
+        return (int64_t)row * token;
+    const uint32_t query = row / group;
+    return (int64_t)query * token + (int64_t)(row - query * group) * head;
+}
+
+// Where loads of rows and channels that are not there read: zeros, so that nothing that lies in memory behind them (NaN times a
+// probability of zero is NaN) gets into a product.
+static __device__ const uint4 kZeros[16] __attribute__((aligned(256))) = {};
+
+// The 16-byte pieces of a row are permuted in LDS, piece p of row r at slot p ^ swizzle(r), so that both kinds of reads hit all banks:
+// one piece of eight rows one behind the other, and two adjacent pieces of four rows.
+template <int DP> __device__ __forceinline__ constexpr uint32_t swizzle(uint32_t row)
+{
+    return DP == 128 ? 2u * (row & 7u) : DP == 64 ? 2u * ((row >> 1) & 3u) : 2u * ((row >> 2) & 1u);
+}
+
+// 16 bytes a lane from its own address to LDS bytes lds_at + 16 lane .. (as load_to_lds, with addresses instead of offsets)
+__device__ __forceinline__ void load_to_lds_at(uint64_t address, uint32_t lds_at)
+{
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds_at), "v"(address) : "memory");
+}
+
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Tiles of ROWS tokens (keys) by WAVES wavefronts: `q`-th load of this wavefront.
+template <int DP, int ROWS, int WAVES> struct TileLoads {
+    static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = (kLoads + WAVES - 1) / WAVES;
+    static constexpr uint32_t kBytes = ROWS * DP * 2u;
+    static_assert(ROWS * kChunks % 64 == 0, "");
+
+    uint32_t offset[kMine], bit[kMine]; // from the tile's first row; the row, or 64: no such channels
+    int first;
+
+    __device__ __forceinline__ TileLoads(int wave, int lane, int64_t token_stride, int32_t dim) : first(wave)
+    {
+#pragma unroll
+        for (int q = 0; q < kMine; ++q) {
+            const uint32_t e = (uint32_t)(first + q * WAVES) * 64u + (uint32_t)lane;
+            const uint32_t row = e / kChunks, chunk = (e % kChunks) ^ swizzle<DP>(row);
+            offset[q] = row * (uint32_t)token_stride + chunk * 16u;
+            bit[q] = chunk * 8u < (uint32_t)dim ? row : 64u;
+        }
+    }
+
+    // base: the tile's first row (the same in all lanes); word: which rows are valid; whole: all of them, and all channels
+    __device__ __forceinline__ void issue(uint64_t base, uint64_t word, bool whole, uint32_t lds_at) const
+    {
+#pragma unroll
+        for (int q = 0; q < kMine; ++q) {
+            const int u = first + q * WAVES;
+            if ((q + 1) * WAVES <= kLoads || u < kLoads) {
+                if (whole) {
+                    load_to_lds(uniform_u64(base), offset[q], lds_at + (uint32_t)u * 1024u);
+                } else {
+                    const bool there = bit[q] < 64u && ((word >> (bit[q] & 63u)) & 1u);
+                    load_to_lds_at(there ? base + offset[q] : reinterpret_cast<uint64_t>(kZeros), lds_at + (uint32_t)u * 1024u);
+                }
+            }
+        }
+    }
+};
+
+// First operand from a tile's rows: lane l has row 32 block + l mod 32, channels 16 step + 8 (l / 32) ..
+template <int DP> struct RowOperand {
+    uint32_t at[DP / 16];
+    __device__ __forceinline__ explicit RowOperand(int lane)
+    {
+        const uint32_t row = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+            at[s] = row * DP * 2u + (((uint32_t)(2 * s) + h) ^ swizzle<DP>(row)) * 16u;
+    }
+    __device__ __forceinline__ u32x4 read(uint32_t tile, int block, int step) const
+    {
+        return lds_read16(tile + at[step] + (uint32_t)block * 32u * DP * 2u);
+    }
+};
+
+// First operand from a tile's columns: lane l has channel 32 part + l mod 32 and, of the sixteen rows 32 block + 16 t .., those that the
+// lane's sums hold: 4 (l / 32) .. + 3 and 8 + 4 (l / 32) .. + 3
+template <int DP> struct ColumnOperand {
+    uint32_t at[DP / 32];
+    __device__ __forceinline__ explicit ColumnOperand(int lane)
+    {
+        const uint32_t i = (uint32_t)lane & 15u, part16 = ((uint32_t)lane >> 4) & 1u, h = (uint32_t)lane >> 5;
+        const uint32_t row = 4u * h + (i >> 2);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+            at[d] = row * DP * 2u + ((4u * d + 2u * part16 + ((i & 3u) >> 1)) ^ swizzle<DP>(row)) * 16u + (i & 1u) * 8u;
+    }
+    __device__ __forceinline__ u32x4 read(uint32_t tile, int block, int t, int part) const
+    {
+        const uint32_t from = tile + at[part] + (uint32_t)(32 * block + 16 * t) * DP * 2u;
+        const u32x2 a = __builtin_bit_cast(u32x2, lds_read_transposed(from)), b = __builtin_bit_cast(u32x2, lds_read_transposed(from + 8u * DP * 2u));
+        u32x4 r;
+        r[0] = a[0];
+        r[1] = a[1];
+        r[2] = b[0];
+        r[3] = b[1];
+        return r;
+    }
+};
+
+// The same of both halves of a wavefront (lanes l and l + 32 hold parts of one row).
+__device__ __forceinline__ float halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+__device__ __forceinline__ int64_t keys_of(const Args &a, int32_t b)
+{
+    if (!a.lengths)
+        return a.keys;
+    const int64_t n = a.lengths_64 ? static_cast<const int64_t *>(a.lengths)[b] : (int64_t) static_cast<const int32_t *>(a.lengths)[b];
+    return n < 0 ? 0 : n < a.keys ? n : a.keys;
+}
+
+// Which keys of a batch entry are valid, 64 to a word.  With a mask, lane i keeps word first + i, and the words are made 64 at a time.
+struct ValidKeys {
+    const uint8_t *mask;
+    int64_t stride, count;
+    int64_t first;
+    uint64_t mine;
+
+    __device__ __forceinline__ ValidKeys(const Args &a, int32_t b, int64_t count_)
+        : mask(a.mask ? a.mask + (int64_t)b * a.mask_batch : nullptr), stride(a.mask_key), count(count_), first(-64), mine(0)
+    {
+    }
+    // word w: keys 64 w .. (asked in rising order, by all lanes)
+    __device__ __forceinline__ uint64_t word(int64_t w)
+    {
+        const int64_t left = count - 64 * w;
+        const uint64_t below = left >= 64 ? ~(uint64_t)0 : left > 0 ? ((uint64_t)1 << left) - 1u : 0u;
+        if (!mask)
+            return below;
+        if (w - first >= 64) {
+            const int lane = (int)threadIdx.x & 63;
+            first = w;
+#pragma unroll 8
+            for (int i = 0; i < 64; ++i) {
+                const int64_t key = 64 * (w + i) + lane;
+                const uint8_t m = key < count ? mask[key * stride] : (uint8_t)0;
+                const uint64_t found = __ballot(m != 0);
+                mine = i == lane ? found : mine;
+            }
+        }
+        const int from = (int)(w - first);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, from);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), from);
+        return below & (((uint64_t)hi << 32) | lo);
+    }
+};
+
+// Workgroups go round-robin over the 8 XCDs; each gets a run of work items, whose keys and values its L2 fetches once.
+__device__ __forceinline__ int32_t work_item(const Args &a) { return ((int32_t)blockIdx.x & 7) * a.per_xcd + ((int32_t)blockIdx.x >> 3); }
+
+// host
+grkan_status_t fill(const grkan_attention_t *a, grkan_dtype_t io, Args *to); // checks and arguments (grkan_attention.hip)
+bool allow_lds(const void *kernel, size_t bytes);
+
+} // namespace attention
+} // namespace grkan
+#endif // GRKAN_ATTENTION_H_

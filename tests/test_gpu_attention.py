@@ -1,0 +1,417 @@
+"""GPU tests of cross attention, forward and backward, against the formulas in 64 bits.
+
+Bounds.  u: a rounding to the 16-bit type.  A score is a float32 sum of dim products: its error moves a probability by at most
+    delta = 2^-20 + 2 (dim + 4) 2^-24 scale |q| |k|     relative
+(the exponential, the row's statistics, the sum).  A probability is rounded once more for the product with v, and the result once:
+    |out - exact| <= u |out| + (u + delta) P |v|.
+S' = P (D - delta_row) is rounded once for its products; D is a float32 sum, delta_row is formed of the rounded out.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+# batch, queries, keys, heads, key heads, dim
+SHAPES = [(1, 1, 1, 1, 1, 8), (2, 1, 5, 2, 1, 64), (3, 1, 1000, 8, 2, 128), (2, 1, 4099, 4, 4, 64), (1, 3, 129, 6, 2, 80),
+          (2, 8, 700, 8, 2, 96), (1, 32, 64, 1, 1, 32), (2, 33, 64, 2, 2, 64), (1, 128, 128, 3, 3, 64), (2, 197, 197, 3, 3, 64),
+          (1, 130, 577, 6, 6, 128), (2, 45, 300, 12, 3, 72), (1, 300, 65, 4, 1, 24), (2, 64, 31, 2, 2, 104), (1, 700, 1300, 2, 1, 128),
+          (1, 1030, 40, 5, 5, 40), (1, 17, 9000, 2, 2, 64), (2, 257, 1025, 2, 1, 96), (1, 4500, 70, 2, 2, 32)]
+MASKS = ["none", "lengths", "mask", "both"]
+
+
+def _type(torch, dtype):
+    return {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+
+
+def _rand(torch, gen, dtype, *shape, std=1.0):
+    return (torch.randn(*shape, device="cuda:0", generator=gen) * std).to(_type(torch, dtype))
+
+
+def _operands(torch, shape, dtype, masks, seed=0, poison=True):
+    """q, k, v (of one projection), lengths, mask and the valid keys [batch, keys].  With `poison`, NaN and infinities where keys are not
+    valid."""
+    batch, queries, keys, heads, kv, dim = shape
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(1000 * seed + queries + keys)
+    q = _rand(torch, gen, dtype, batch, queries, heads, dim, std=1.5)
+    both = _rand(torch, gen, dtype, batch, keys, 2, kv, dim)
+    valid = torch.ones(batch, keys, dtype=torch.bool, device="cuda:0")
+    lengths = mask = None
+    if masks in ("lengths", "both"):
+        lengths = torch.randint(0, keys + 1, (batch,), generator=gen, device="cuda:0")
+        lengths[0] = keys if batch == 1 else min(keys, 1)
+        valid &= torch.arange(keys, device="cuda:0") < lengths[:, None]
+    if masks in ("mask", "both"):
+        mask = torch.rand(batch, keys, generator=gen, device="cuda:0") < 0.6
+        if batch > 1:
+            mask[1] = False
+        if batch > 2:
+            mask[2, : keys // 2] = False
+        valid &= mask
+    if poison and not bool(valid.all()):
+        bad = torch.tensor([math.nan, math.inf, -math.inf], device="cuda:0").to(both.dtype)
+        which = torch.randint(0, 3, both.shape, generator=gen, device="cuda:0")
+        both = torch.where(valid[:, :, None, None, None], both, bad[which])
+    return q, both[:, :, 0], both[:, :, 1], lengths, mask, valid
+
+
+def _heads(t, group):
+    """[batch, tokens, heads, dim] as float64 [batch, heads x group, tokens, dim]."""
+    return t.double().transpose(1, 2).repeat_interleave(group, 1)
+
+
+def _formulas(torch, q, k, v, valid, scale, dtype, dout=None):
+    """Exact results and their bounds, each a list of (exact, bound) in the layout of the outputs."""
+    u, dim, group = UNIT[dtype], q.shape[-1], q.shape[2] // k.shape[2]
+    k, v = (torch.where(valid[:, :, None, None], t, 0) for t in (k, v))
+    Q, K, V = _heads(q, 1), _heads(k, group), _heads(v, group)
+    S = Q @ K.transpose(-1, -2) * scale
+    ok = valid[:, None, None, :]
+    S = S.masked_fill(~ok, -math.inf)
+    most = S.amax(-1, keepdim=True) if S.shape[-1] else torch.zeros_like(S.sum(-1, keepdim=True))
+    P = torch.exp(S - torch.where(most > -math.inf, most, 0.0))
+    total = P.sum(-1, keepdim=True)
+    P = P / torch.where(total > 0, total, 1.0)
+    delta = 2.0 ** -20 + 2 * (dim + 4) * 2.0 ** -24 * scale * (Q.abs() @ K.abs().transpose(-1, -2))
+    # (a row's statistics move with its scores)
+    delta = delta + (P * delta).sum(-1, keepdim=True)
+    O = P @ V
+    # float16: probabilities below 2^-24 of the largest round to steps of that
+    small = 2.0 ** -24 if dtype == "f16" else 0.0
+
+    def back(t, to):
+        return t.transpose(1, 2) if to == t.shape[1] else t.unflatten(1, (to, group)).sum(2).transpose(1, 2)
+
+    def found(exact, bound, to):
+        e = back(exact, to)
+        return e, u * e.abs() + back(bound, to) + (2.0 ** -25 if dtype == "f16" else 0.0)
+
+    H, G = q.shape[2], k.shape[2]
+    out = found(O, ((u + delta) * P + small) @ V.abs(), H)
+    if dout is None:
+        return [out]
+    dO = _heads(dout, 1)
+    D = dO @ V.transpose(-1, -2)
+    row = (dO * O).sum(-1, keepdim=True)
+    dS = P * (D - row)
+    # of D, of delta_row (the rounded out), of the rounding to 16 bits (float16: in steps of 2^-24 where |dO| is 1/8)
+    e_row = (dO.abs() * (u * O.abs() + ((u + delta) * P + small) @ V.abs())).sum(-1, keepdim=True)
+    E = (u + delta) * dS.abs() + P * ((dim + 4) * 2.0 ** -23 * (dO.abs() @ V.abs().transpose(-1, -2)) + e_row)
+    if dtype == "f16":
+        E = E + 2.0 ** -22 * dO.abs().amax()
+    E = torch.where(ok, E, 0.0)
+    return [out, found(dS @ K * scale, E @ K.abs() * scale, H),
+            found(dS.transpose(-1, -2) @ Q * scale, E.transpose(-1, -2) @ Q.abs() * scale, G),
+            found(P.transpose(-1, -2) @ dO, torch.where(ok, (u + delta) * P + small, 0.0).transpose(-1, -2) @ dO.abs(), G)]
+
+
+def _assert_within(got, wanted, label):
+    for name, g, (exact, bound) in zip(("out", "dq", "dk", "dv"), got, wanted):
+        assert g.shape == exact.shape and g.is_contiguous()
+        off = (g.double() - exact).abs() - bound
+        assert bool((off <= 0).all()), (label, name, float(off.max()), float((g.double() - exact).abs().max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("masks", MASKS)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_and_backward(shape, masks, dtype):
+    """Every element within its bound, with NaN and infinities in the keys that are not valid; zeros for rows without a valid key and
+    for the gradients of keys that are not; the same bits again, and from the forward pass without a gradient."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    print(shape, masks, dtype, flush=True)
+    q, k, v, lengths, mask, valid = _operands(torch, shape, dtype, masks)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(5)
+    dout = _rand(torch, gen, dtype, *q.shape)
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+
+    def both():
+        out = cross_attention(*leaves, key_lengths=lengths, key_mask=mask)
+        return (out.detach(),) + torch.autograd.grad(out, leaves, dout)
+
+    got = both()
+    _assert_within(got, _formulas(torch, q, k, v, valid, shape[-1] ** -0.5, dtype, dout), (shape, masks, dtype))
+    assert all(torch.equal(a, b) for a, b in zip(got, both()))
+    assert torch.equal(got[0], cross_attention(q, k, v, key_lengths=lengths, key_mask=mask))
+    empty = ~valid.any(1)
+    assert (got[0][empty] == 0).all() and (got[1][empty] == 0).all()
+    assert (got[2][~valid] == 0).all() and (got[3][~valid] == 0).all()
+
+
+@pytest.mark.parametrize("shape", [(2, 0, 5, 2, 1, 64), (2, 5, 0, 2, 1, 64), (0, 5, 5, 2, 2, 64)])
+def test_nothing(shape):
+    """No queries, no keys, no batch: empty results and zeros."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, shape, "bf16", "none")
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    out = cross_attention(*leaves)
+    assert out.shape == q.shape and (out == 0).all()
+    for g, t in zip(torch.autograd.grad(out, leaves, torch.ones_like(out)), leaves):
+        assert g.shape == t.shape and (g == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scores_that_rise_and_fall(dtype):
+    """Rows whose scores rise by thousands over the keys, fall, are all low, or are all the same: the running maximum."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, (1, 40, 1500, 1, 1, 64), dtype, "none")
+    k = k.clone()
+    q = q.clone()
+    ramp = torch.linspace(-1, 1, 1500, device="cuda:0")
+    k[..., 0] = ramp[None, :, None].to(k.dtype)
+    q[:, :10, :, 0] = 3000.0
+    q[:, 10:20, :, 0] = -3000.0
+    q[:, 20:25] = 0.0
+    k[..., 1] = 30.0
+    q[:, 25:30, :, 1] = -400.0
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(6)
+    dout = _rand(torch, gen, dtype, *q.shape)
+    valid = torch.ones(1, 1500, dtype=torch.bool, device="cuda:0")
+    for scale in (0.125, 1.0):
+        out = cross_attention(*leaves, scale=scale)
+        got = (out.detach(),) + torch.autograd.grad(out, leaves, dout)
+        _assert_within(got, _formulas(torch, q, k, v, valid, scale, dtype, dout), scale)
+
+
+@pytest.mark.parametrize("size", [1e-6, 1e-4, 1.0, 300.0])
+def test_small_and_large_upstream_gradients_in_float16(size):
+    """float16 gradients of a small loss keep their precision: the sums' bounds scale with |dout|.  (The results themselves are float16:
+    below 2^-14 in steps of 2^-24, which `_formulas` allows.)"""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    shape = (1, 150, 500, 2, 1, 64)
+    q, k, v, _, _, valid = _operands(torch, shape, "f16", "none")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(7)
+    dout = _rand(torch, gen, "f16", *q.shape, std=size)
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    out = cross_attention(*leaves)
+    got = (out.detach(),) + torch.autograd.grad(out, leaves, dout)
+    _assert_within(got, _formulas(torch, q, k, v, valid, 0.125, "f16", dout), size)
+
+
+def test_layouts():
+    """Heads before tokens, views into larger tensors, broadcast keys, addresses off 16 bytes (copied): the same bits."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(8)
+    wide = _rand(torch, gen, "bf16", 2, 4, 90, 3 * 72)
+    q = wide[..., 8:72].transpose(1, 2)
+    k, v = (wide[:, :2, 10:, s:s + 64].transpose(1, 2) for s in (72, 144))
+    shared = [t[:1].expand(2, -1, -1, -1) for t in (k, v)]
+    off = [wide[:, :2, :70, s:s + 64].transpose(1, 2) for s in (3, 77)]
+    apart = q.transpose(2, 3).contiguous().transpose(2, 3)
+    assert apart.stride(-1) != 1
+    mask = torch.rand(2, 160, generator=gen, device="cuda:0")[:, ::2] < 0.7
+    for a, b, c, m in ((q, k, v, mask), (q, *shared, mask[:1]), (q, *off, mask[:, :70]), (apart, k, v, None)):
+        leaves = [t.detach().requires_grad_() for t in (a, b, c)]
+        dense = [t.detach().contiguous().requires_grad_() for t in (a, b, c)]
+        out = cross_attention(*leaves, key_mask=m)
+        want = cross_attention(*dense, key_mask=None if m is None else m.expand(2, -1).contiguous())
+        assert torch.equal(out, want)
+        dout = _rand(torch, gen, "bf16", 2, 4, 90, 64).transpose(1, 2)
+        for x, y in zip(torch.autograd.grad(out, leaves, dout), torch.autograd.grad(want, dense, dout.contiguous())):
+            assert torch.equal(x, y)
+
+
+def test_lengths_out_of_range_are_clamped():
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, (4, 40, 100, 2, 2, 64), "bf16", "none")
+    for dtype in (torch.int32, torch.int64):
+        n = torch.tensor([-5, 100, 1000, 7], dtype=dtype, device="cuda:0")
+        got = cross_attention(q, k, v, key_lengths=n)
+        assert torch.equal(got, cross_attention(q, k, v, key_lengths=n.clamp(0, 100))) and (got[0] == 0).all()
+
+
+def test_gradient_against_differences():
+    """The gradients along a direction, against a central difference of the formula in 64 bits: off by the roundings of the
+    gradients, whose bounds add up along the direction, and 1e-6 for the difference itself."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    shape = (2, 60, 90, 4, 2, 64)
+    q, k, v, lengths, mask, valid = _operands(torch, shape, "bf16", "mask", seed=3, poison=False)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(9)
+    dout = _rand(torch, gen, "bf16", *q.shape)
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    out = cross_attention(*leaves, key_mask=mask)
+    grads = torch.autograd.grad(out, leaves, dout)
+    to = [torch.randn(t.shape, device="cuda:0", generator=gen, dtype=torch.float64) for t in leaves]
+
+    def loss(step):
+        a, b, c = (t.detach().double() + step * d for t, d in zip(leaves, to))
+        (o, _), = _formulas(torch, a, b, c, valid, 0.125, "bf16")
+        return (o * dout.double()).sum()
+
+    want = (loss(1e-4) - loss(-1e-4)) / 2e-4
+    got = sum((g.double() * t).sum() for g, t in zip(grads, to))
+    bounds = _formulas(torch, q, k, v, valid, 0.125, "bf16", dout)[1:]
+    allowed = sum((b * t.abs()).sum() for (_, b), t in zip(bounds, to))
+    assert (got - want).abs() <= allowed + 1e-6 * want.abs()
+    # (the bound is one for the worst case; along a random direction the roundings mostly cancel)
+    size = sum((g.double() * t).square().sum() for g, t in zip(grads, to)).sqrt()
+    assert (got - want).abs() <= 0.05 * size
+
+
+def test_long_cache_past_32_bits():
+    """Keys of one batch entry further than 2^32 bytes from its first: single tokens and many rows, forward and backward."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    keys, token = 4200, 524288 + 64  # elements between two keys: 4.4 GB in all
+    memory = torch.empty(keys * token, dtype=torch.bfloat16, device="cuda:0")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(10)
+    view = memory.as_strided((1, keys, 2, 1, 64), (keys * token, token, 64, 64, 1))
+    view.copy_(_rand(torch, gen, "bf16", 1, keys, 2, 1, 64))
+    k, v = view[:, :, 0], view[:, :, 1]
+    dense = [t.contiguous() for t in (k, v)]
+    for queries in (1, 50):
+        q = _rand(torch, gen, "bf16", 1, queries, 2, 64)
+        assert torch.equal(cross_attention(q, k, v), cross_attention(q, *dense))
+        dout = _rand(torch, gen, "bf16", *q.shape)
+        a, b = [q, k, v], [q, *dense]
+        for leaves in (a, b):
+            leaves[:] = [t.detach().requires_grad_() for t in leaves]
+        x = torch.autograd.grad(cross_attention(*a), a, dout)
+        y = torch.autograd.grad(cross_attention(*b), b, dout)
+        assert all(torch.equal(s, t) for s, t in zip(x, y))
+
+
+def test_refusals():
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, (2, 5, 9, 4, 2, 64), "bf16", "none")
+    n, m = torch.tensor([3, 4], device="cuda:0"), torch.ones(2, 9, dtype=torch.bool, device="cuda:0")
+    bad = [((q.cpu(), k, v), ValueError), ((q, k.cpu(), v), ValueError), ((q.float(), k.float(), v.float()), TypeError), ((q, k.half(), v), TypeError),
+           ((q[0], k, v), ValueError), ((q, k, v[:, :8]), ValueError), ((q[:1], k, v), ValueError), ((q[:, :, :3], k, v), ValueError),
+           ((q[..., :60], k[..., :60], v[..., :60]), ValueError), ((q[..., :56], k, v), ValueError),
+           ((q.repeat(1, 1, 1, 3), k.repeat(1, 1, 1, 3), v.repeat(1, 1, 1, 3)), ValueError), ((q, k, v, n.float()), TypeError),
+           ((q, k, v, n[:1]), ValueError), ((q, k, v, n.cpu()), ValueError), ((q, k, v, None, m.int()), TypeError),
+           ((q, k, v, None, m[:, :8]), ValueError), ((q, k, v, None, m.cpu()), ValueError), ((q, k, v, None, None, 0.0), ValueError),
+           ((q, k, v, None, None, -1.0), ValueError), ((q, k, v, None, None, math.inf), ValueError)]
+    for args, error in bad:
+        with pytest.raises(error):
+            cross_attention(*args)
+    with pytest.raises(NotImplementedError):
+        torch.func.vmap(cross_attention)(q[None], k[None], v[None])
+    out = cross_attention(q.requires_grad_(), k, v)
+    g, = torch.autograd.grad(out, q, torch.ones_like(out), create_graph=True)
+    with pytest.raises(RuntimeError, match="not differentiable twice"):
+        g.sum().backward()
+
+
+def test_only_some_operands_recorded_and_in_place_writes():
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, (2, 50, 90, 4, 2, 64), "bf16", "none")
+    every = [t.detach().requires_grad_() for t in (q, k, v)]
+    dout = torch.ones_like(q)
+    want = torch.autograd.grad(cross_attention(*every), every, dout)
+    for i in range(3):
+        leaves = [t.detach() for t in (q, k, v)]
+        leaves[i].requires_grad_()
+        assert torch.equal(torch.autograd.grad(cross_attention(*leaves), leaves[i], dout)[0], want[i])
+    out = cross_attention(*every)
+    with torch.no_grad():
+        every[1].add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        torch.autograd.grad(out, every, dout)
+
+
+def test_guarded_outputs():
+    """Nothing is written past the outputs, at sizes that end inside tiles (through the C interface)."""
+    import ctypes
+
+    import torch
+
+    from paper_2505_13813_amd import binding
+
+    lib = binding.load_library()
+    for shape in ((1, 3, 70, 6, 2, 40), (2, 77, 90, 2, 2, 72), (1, 1, 3000, 4, 2, 128)):
+        q, k, v, lengths, mask, valid = _operands(torch, shape, "bf16", "lengths")
+        k, v = k.contiguous(), v.contiguous()
+        a = binding.Attention.of(q, k, v, lengths, None, shape[-1] ** -0.5)
+        size = {"out": q.numel(), "dq": q.numel(), "dk": k.numel(), "dv": v.numel()}
+        held = {n: torch.full((c + 64,), 7.0, dtype=torch.bfloat16, device="cuda:0") for n, c in size.items()}
+        lse = torch.full((q.shape[0] * q.shape[1] * q.shape[2] + 64,), 7.0, device="cuda:0")
+        stream = torch.cuda.current_stream().cuda_stream
+        for back in (0, 1):
+            need = lib.grkan_attention_workspace_bytes(ctypes.byref(a), back)
+            ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda:0")
+            if not back:
+                st = lib.grkan_attention_fwd(ctypes.byref(a), held["out"].data_ptr(), lse.data_ptr(), ws.data_ptr(), need, binding.GRKAN_BF16, stream)
+            else:
+                dout = torch.randn_like(q)
+                st = lib.grkan_attention_bwd(ctypes.byref(a), held["out"].data_ptr(), lse.data_ptr(), dout.data_ptr(), *dout.stride()[:3],
+                                             held["dq"].data_ptr(), held["dk"].data_ptr(), held["dv"].data_ptr(), ws.data_ptr(), need,
+                                             binding.GRKAN_BF16, stream)
+            assert st == 0
+            torch.cuda.synchronize()
+            assert (ws[need:] == 7).all()
+        for n, c in size.items():
+            assert (held[n][c:] == 7).all() and not (held[n][:c] == 7).any()
+        assert (lse[-64:] == 7).all()
+
+
+def test_on_another_stream_and_in_a_graph():
+    """On a stream of its own behind work there; captured with its backward pass' kernels, and replayed three times with eager calls
+    between."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    for shape in ((2, 100, 700, 4, 2, 64), (4, 1, 3000, 8, 2, 128)):
+        q, k, v, lengths, mask, _ = _operands(torch, shape, "bf16", "lengths")
+        want = cross_attention(q, k, v, lengths)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = cross_attention(q * 1.0, k, v, lengths)
+        side.synchronize()
+        assert torch.equal(got, want)
+        held = [t.clone().requires_grad_() for t in (q, k, v)]
+        dout = torch.ones_like(q)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = cross_attention(*held, lengths)
+            grads = torch.autograd.grad(out, held, dout)
+        for n in range(3):
+            with torch.no_grad():
+                held[0].copy_(q * (n + 1))
+            graph.replay()
+            torch.cuda.synchronize()
+            eager = [t.detach().clone().requires_grad_() for t in held]
+            again = cross_attention(*eager, lengths)
+            assert torch.equal(out, again)
+            assert all(torch.equal(a, b) for a, b in zip(grads, torch.autograd.grad(again, eager, dout)))
