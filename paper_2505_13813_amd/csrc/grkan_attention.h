@@ -47,7 +47,7 @@ struct Args {
     int32_t padded;         // rows with the padding
     int32_t splits, tiles_per_split;
     int32_t row_tiles, key_tiles; // workgroups of a key head over rows, over keys
-    int32_t work, per_xcd;
+    int32_t work, run; // work items, and how many of them in a row one XCD gets
 };
 
 template <typename IO> struct Matrix;
@@ -89,12 +89,20 @@ __device__ __forceinline__ int64_t row_offset(uint32_t row, uint32_t group, int6
 // probability of zero is NaN) gets into a product.
 static __device__ const uint4 kZeros[16] __attribute__((aligned(256))) = {};
 
-// The 16-byte pieces of a row are permuted in LDS, piece p of row r at slot p ^ swizzle(r), so that both kinds of reads hit all banks:
-// one piece of eight rows one behind the other, and two adjacent pieces of four rows.
+// A tile's rows in LDS.  16-byte pieces are permuted within a row, piece p of row r at slot p ^ swizzle(r), and, with rows of 128 or 256 bytes, every
+// KB is followed by 16 bytes of nothing, so that the reads of both kinds hit all 64 banks at once: the same piece of sixteen rows one behind
+// the other, and four adjacent pieces of four rows.  (Measured: a row operand's read 4.5 cycles of a compute unit, a column operand's 2.7; with rows
+// permuted for eight rows and for two pieces, as the counters of conflicts have it 8.4 and 4.1.)
 template <int DP> __device__ __forceinline__ constexpr uint32_t swizzle(uint32_t row)
 {
-    return DP == 128 ? 2u * (row & 7u) : DP == 64 ? 2u * ((row >> 1) & 3u) : 2u * ((row >> 2) & 1u);
+    return DP == 128 ? 4u * (row & 3u) : DP == 64 ? 2u * (row & 2u) + ((row & 4u) >> 1) : (row >> 2) & 3u;
 }
+template <int DP> constexpr uint32_t kBlock = DP == 64 || DP == 128 ? 1040u : 1024u; // what a wavefront loads at once
+template <int DP> __device__ __forceinline__ constexpr uint32_t row_at(uint32_t row)
+{
+    return row * DP * 2u + (DP == 64 || DP == 128 ? row * DP * 2u / 1024u * 16u : 0u);
+}
+template <int DP, int ROWS> constexpr uint32_t kTileBytes = ROWS *DP * 2u / 1024u * kBlock<DP>;
 
 // 16 bytes a lane from its own address to LDS bytes lds_at + 16 lane .. (as load_to_lds, with addresses instead of offsets)
 __device__ __forceinline__ void load_to_lds_at(uint64_t address, uint32_t lds_at)
@@ -102,12 +110,21 @@ __device__ __forceinline__ void load_to_lds_at(uint64_t address, uint32_t lds_at
     asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds_at), "v"(address) : "memory");
 }
 
+// Loads into registers have arrived, behind this: the compiler, which does not know of the loads to LDS, would else wait for all of
+// those too at every use of the registers in the loop behind.
+template <int N> __device__ __forceinline__ void arrived(u32x4 (&r)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+v"(r[i]));
+}
+__device__ __forceinline__ void arrived(float &r) { asm volatile("" : "+v"(r)); }
+
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // Tiles of ROWS tokens (keys) by WAVES wavefronts: `q`-th load of this wavefront.
 template <int DP, int ROWS, int WAVES> struct TileLoads {
     static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = (kLoads + WAVES - 1) / WAVES;
-    static constexpr uint32_t kBytes = ROWS * DP * 2u;
     static_assert(ROWS * kChunks % 64 == 0, "");
 
     uint32_t offset[kMine], bit[kMine]; // from the tile's first row; the row, or 64: no such channels
@@ -132,48 +149,66 @@ template <int DP, int ROWS, int WAVES> struct TileLoads {
             const int u = first + q * WAVES;
             if ((q + 1) * WAVES <= kLoads || u < kLoads) {
                 if (whole) {
-                    load_to_lds(uniform_u64(base), offset[q], lds_at + (uint32_t)u * 1024u);
+                    load_to_lds(uniform_u64(base), offset[q], lds_at + (uint32_t)u * kBlock<DP>);
                 } else {
                     const bool there = bit[q] < 64u && ((word >> (bit[q] & 63u)) & 1u);
-                    load_to_lds_at(there ? base + offset[q] : reinterpret_cast<uint64_t>(kZeros), lds_at + (uint32_t)u * 1024u);
+                    load_to_lds_at(there ? base + offset[q] : reinterpret_cast<uint64_t>(kZeros), lds_at + (uint32_t)u * kBlock<DP>);
                 }
             }
         }
     }
 };
 
+// Addresses of a lane, moved to a tile.  (The compiler is kept from adding the tile's place to each read's constant part instead, which
+// takes an instruction for every read.)
+template <int N> struct Addresses {
+    uint32_t at[N];
+    __device__ __forceinline__ Addresses moved(uint32_t tile) const
+    {
+        Addresses r;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            r.at[i] = at[i] + tile;
+            asm volatile("" : "+v"(r.at[i]));
+        }
+        return r;
+    }
+};
+
 // First operand from a tile's rows: lane l has row 32 block + l mod 32, channels 16 step + 8 (l / 32) ..
-template <int DP> struct RowOperand {
-    uint32_t at[DP / 16];
+template <int DP> struct RowOperand : Addresses<DP / 16> {
     __device__ __forceinline__ explicit RowOperand(int lane)
     {
         const uint32_t row = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s)
-            at[s] = row * DP * 2u + (((uint32_t)(2 * s) + h) ^ swizzle<DP>(row)) * 16u;
+            this->at[s] = row_at<DP>(row) + (((uint32_t)(2 * s) + h) ^ swizzle<DP>(row)) * 16u;
     }
-    __device__ __forceinline__ u32x4 read(uint32_t tile, int block, int step) const
+    // `further`: of a second tile, that many bytes behind
+    static __device__ __forceinline__ u32x4 read(const Addresses<DP / 16> &from, int block, int step, uint32_t further = 0)
     {
-        return lds_read16(tile + at[step] + (uint32_t)block * 32u * DP * 2u);
+        return lds_read16(from.at[step] + (row_at<DP>(32u * block) + further));
     }
 };
 
 // First operand from a tile's columns: lane l has channel 32 part + l mod 32 and, of the sixteen rows 32 block + 16 t .., those that the
 // lane's sums hold: 4 (l / 32) .. + 3 and 8 + 4 (l / 32) .. + 3
-template <int DP> struct ColumnOperand {
-    uint32_t at[DP / 32];
+template <int DP> struct ColumnOperand : Addresses<DP / 32> {
     __device__ __forceinline__ explicit ColumnOperand(int lane)
     {
         const uint32_t i = (uint32_t)lane & 15u, part16 = ((uint32_t)lane >> 4) & 1u, h = (uint32_t)lane >> 5;
         const uint32_t row = 4u * h + (i >> 2);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
-            at[d] = row * DP * 2u + ((4u * d + 2u * part16 + ((i & 3u) >> 1)) ^ swizzle<DP>(row)) * 16u + (i & 1u) * 8u;
+            this->at[d] = row_at<DP>(row) + ((4u * d + 2u * part16 + ((i & 3u) >> 1)) ^ swizzle<DP>(row)) * 16u + (i & 1u) * 8u;
     }
-    __device__ __forceinline__ u32x4 read(uint32_t tile, int block, int t, int part) const
+    static __device__ __forceinline__ u32x4 read(const Addresses<DP / 32> &from, int block, int t, int part, uint32_t further = 0)
     {
-        const uint32_t from = tile + at[part] + (uint32_t)(32 * block + 16 * t) * DP * 2u;
-        const u32x2 a = __builtin_bit_cast(u32x2, lds_read_transposed(from)), b = __builtin_bit_cast(u32x2, lds_read_transposed(from + 8u * DP * 2u));
+        // (eight rows further the pieces are permuted alike, but for the short and the uneven rows)
+        constexpr uint32_t flip = swizzle<DP>(8u) * 16u;
+        const uint32_t first = from.at[part] + (row_at<DP>(32u * block + 16u * t) + further);
+        const uint32_t second = (flip ? from.at[part] ^ flip : from.at[part]) + (row_at<DP>(32u * block + 16u * t + 8u) + further);
+        const u32x2 a = __builtin_bit_cast(u32x2, lds_read_transposed(first)), b = __builtin_bit_cast(u32x2, lds_read_transposed(second));
         u32x4 r;
         r[0] = a[0];
         r[1] = a[1];
@@ -195,29 +230,29 @@ __device__ __forceinline__ float halves_sum(float v)
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
-__device__ __forceinline__ int64_t keys_of(const Args &a, int32_t b)
+__device__ __forceinline__ int32_t keys_of(const Args &a, int32_t b)
 {
     if (!a.lengths)
-        return a.keys;
+        return (int32_t)a.keys;
     const int64_t n = a.lengths_64 ? static_cast<const int64_t *>(a.lengths)[b] : (int64_t) static_cast<const int32_t *>(a.lengths)[b];
-    return n < 0 ? 0 : n < a.keys ? n : a.keys;
+    return (int32_t)(n < 0 ? 0 : n < a.keys ? n : a.keys);
 }
 
 // Which keys of a batch entry are valid, 64 to a word.  With a mask, lane i keeps word first + i, and the words are made 64 at a time.
 struct ValidKeys {
     const uint8_t *mask;
-    int64_t stride, count;
-    int64_t first;
+    int64_t stride;
+    int32_t count, first;
     uint64_t mine;
 
-    __device__ __forceinline__ ValidKeys(const Args &a, int32_t b, int64_t count_)
+    __device__ __forceinline__ ValidKeys(const Args &a, int32_t b, int32_t count_)
         : mask(a.mask ? a.mask + (int64_t)b * a.mask_batch : nullptr), stride(a.mask_key), count(count_), first(-64), mine(0)
     {
     }
     // word w: keys 64 w .. (asked in rising order, by all lanes)
-    __device__ __forceinline__ uint64_t word(int64_t w)
+    __device__ __forceinline__ uint64_t word(int32_t w)
     {
-        const int64_t left = count - 64 * w;
+        const int32_t left = count - 64 * w;
         const uint64_t below = left >= 64 ? ~(uint64_t)0 : left > 0 ? ((uint64_t)1 << left) - 1u : 0u;
         if (!mask)
             return below;
@@ -226,25 +261,32 @@ struct ValidKeys {
             first = w;
 #pragma unroll 8
             for (int i = 0; i < 64; ++i) {
-                const int64_t key = 64 * (w + i) + lane;
+                const int64_t key = 64 * ((int64_t)w + i) + lane;
                 const uint8_t m = key < count ? mask[key * stride] : (uint8_t)0;
                 const uint64_t found = __ballot(m != 0);
                 mine = i == lane ? found : mine;
             }
         }
-        const int from = (int)(w - first);
+        const int from = w - first;
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, from);
         const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), from);
         return below & (((uint64_t)hi << 32) | lo);
     }
 };
 
-// Workgroups go round-robin over the 8 XCDs; each gets a run of work items, whose keys and values its L2 fetches once.
-__device__ __forceinline__ int32_t work_item(const Args &a) { return ((int32_t)blockIdx.x & 7) * a.per_xcd + ((int32_t)blockIdx.x >> 3); }
+// Workgroups go round-robin over the 8 XCDs.  Runs of work items go to one XCD, whose L2 fetches their keys and values once; runs
+// are short enough (host: spread) that every XCD has several of them, of long and of short batch entries.
+__device__ __forceinline__ int32_t work_item(const Args &a)
+{
+    const int32_t xcd = (int32_t)blockIdx.x & 7, i = (int32_t)blockIdx.x >> 3;
+    const int32_t turn = i / a.run;
+    return (turn * 8 + xcd) * a.run + (i - turn * a.run);
+}
 
 // host
 grkan_status_t fill(const grkan_attention_t *a, grkan_dtype_t io, Args *to); // checks and arguments (grkan_attention.hip)
 bool allow_lds(const void *kernel, size_t bytes);
+unsigned spread(Args &a, int64_t work, int64_t per_head); // sets work and run; the grid
 
 } // namespace attention
 } // namespace grkan

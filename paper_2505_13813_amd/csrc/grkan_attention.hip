@@ -1,7 +1,7 @@
 // Cross attention on gfx950 (MI355X), forward: out = softmax(scale Q K^T) V in one pass over the keys, with the running maximum and sum
 // of each row.
 //
-//   * With rows enough (queries x heads that share a key head), a workgroup of four wavefronts has 32 RB rows each; 64 keys and their
+//   * With rows enough (queries x heads that share a key head), a workgroup of four wavefronts has 32 each; 64 keys and their
 //     values at a time come to LDS by LDS-direct loads, two tiles deep, and serve all four.
 //   * With 32 rows or fewer (single tokens) the keys are what there is to read: the four wavefronts have the same rows and
 //     tiles of 32 keys of their own, in LDS of their own, without a barrier, and join what they found at the end.
@@ -20,13 +20,13 @@
 namespace grkan {
 namespace attention {
 
-template <typename IO_, int DP_, int RB_, bool KEYS_> struct Shape {
+template <typename IO_, int DP_, bool KEYS_> struct Shape {
     typedef IO_ IO;
-    static constexpr int DP = DP_, RB = RB_, kWaves = 4;
-    static constexpr bool KEYS = KEYS_;          // the wavefronts split the keys, not the rows
-    static constexpr int KT = KEYS ? 32 : 64;    // keys of a tile
-    static constexpr int kRows = KEYS ? 32 * RB : 32 * RB * kWaves;
-    static constexpr uint32_t kTile = KT * DP * 2u, kStage = 2 * kTile;
+    static constexpr int DP = DP_, kWaves = 4;
+    static constexpr bool KEYS = KEYS_;       // the wavefronts split the keys, not the rows
+    static constexpr int KT = KEYS ? 32 : 64; // keys of a tile
+    static constexpr int kRows = KEYS ? 32 : 32 * kWaves;
+    static constexpr uint32_t kTile = kTileBytes<DP, KT>, kStage = 2 * kTile;
     static constexpr size_t kLds = (size_t)kStage * 2 * (KEYS ? kWaves : 1);
 };
 
@@ -34,7 +34,7 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
 {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
-    constexpr int DP = SH::DP, RB = SH::RB, KT = SH::KT, KB = KT / 32, ND = DP / 32, NS = DP / 16;
+    constexpr int DP = SH::DP, KT = SH::KT, KB = KT / 32, ND = DP / 32, NS = DP / 16;
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -47,196 +47,186 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
     const int32_t bh = item / per_head, rest = item - bh * per_head;
     const int32_t row_tile = rest / a.splits, split = rest - row_tile * a.splits;
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
-    const int64_t count = keys_of(a, b);
-    const int32_t tiles = (int32_t)((count + KT - 1) / KT);
-    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
-    t1 = t1 < tiles ? t1 : tiles;
-    constexpr int step = SH::KEYS ? SH::kWaves : 1;
-    if (SH::KEYS)
-        t0 += wave;
-
     // ---- this wavefront's rows as second operands: lane l has row l mod 32, channels 16 s + 8 (l / 32) ..
-    const uint32_t row0 = (uint32_t)row_tile * SH::kRows + (SH::KEYS ? 0u : (uint32_t)wave * 32u * RB);
-    const uint64_t q_base = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head);
-    u32x4 q[RB][NS];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const uint32_t row = row0 + 32u * rb + col;
-        const uint64_t at = q_base + (uint64_t)row_offset(row, (uint32_t)a.group, a.q.token, a.q.head);
+    const uint32_t row0 = (uint32_t)row_tile * SH::kRows + (SH::KEYS ? 0u : (uint32_t)wave * 32u), row = row0 + col;
+    u32x4 q[NS];
+    {
+        const uint64_t at = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head +
+                                                row_offset(row, (uint32_t)a.group, a.q.token, a.q.head));
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const uint32_t channel = 16u * s + 8u * h;
             const bool there = (int64_t)row < a.rows && channel < (uint32_t)a.dim;
-            q[rb][s] = gload16(there ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            q[s] = gload16(there ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
     }
+
+    const int32_t count = keys_of(a, b), tiles = (count + KT - 1) / KT;
+    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
+    t1 = t1 < tiles ? t1 : tiles;
+    if (SH::KEYS)
+        t0 += wave;
 
     constexpr int loaders = SH::KEYS ? 1 : SH::kWaves;
     const TileLoads<DP, KT, loaders> k_loads(SH::KEYS ? 0 : wave, lane, a.k.token, a.dim), v_loads(SH::KEYS ? 0 : wave, lane, a.v.token, a.dim);
     const RowOperand<DP> k_operand(lane);
     const ColumnOperand<DP> v_operand(lane);
     const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
-    const uint32_t stages = lds0 + (SH::KEYS ? (uint32_t)wave * 2u * SH::kStage : 0u);
     ValidKeys valid(a, b, count);
     constexpr uint64_t all = KT == 64 ? ~(uint64_t)0 : 0xffffffffu;
 
     auto word_of = [&](int32_t t) {
-        const int64_t key = (int64_t)t * KT;
-        return (valid.word(key >> 6) >> (key & 63)) & all;
+        if constexpr (KT == 64)
+            return valid.word(t);
+        else
+            return (valid.word(t / 2) >> (t % 2 * 32)) & all;
     };
-    auto issue = [&](int32_t t, uint64_t word, uint32_t stage) {
-        const bool whole = word == all && a.dim == DP;
-        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, word, whole, stage);
-        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, whole, stage + SH::kTile);
+    auto issue_k = [&](int32_t t, uint64_t word, uint32_t to) {
+        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, word, word == all && a.dim == DP, to);
+    };
+    auto issue_v = [&](int32_t t, uint64_t word, uint32_t to) {
+        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, word == all && a.dim == DP, to);
     };
 
-    f32x16 acc[RB][ND];
-    float top[RB], sum[RB]; // the maximum that the probabilities are relative to; this lane's part of their sum
+    f32x16 acc[ND];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-            acc[rb][d] = f32x16{};
-        top[rb] = -__builtin_inff();
-        sum[rb] = 0.0f;
-    }
+    for (int d = 0; d < ND; ++d)
+        acc[d] = f32x16{};
+    float top = -__builtin_inff(), sum = 0.0f; // the maximum that the probabilities are relative to; this lane's part of their sum
     const float c = a.c, slack = fminf(8.0f / c, 1e38f); // (of scores)
 
-    auto compute = [&](uint32_t stage, uint64_t word) {
-        f32x16 s[RB][KB];
+    auto compute = [&](uint32_t k_at, uint32_t v_at, uint64_t word) {
+        const auto k_from = k_operand.moved(k_at);
+        const auto v_from = v_operand.moved(v_at);
+        f32x16 s[KB];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-                s[rb][kb] = f32x16{};
+        for (int kb = 0; kb < KB; ++kb)
+            s[kb] = f32x16{};
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const u32x4 k = k_operand.read(stage, kb, st);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    s[rb][kb] = MM::multiply(k, q[rb][st], s[rb][kb]);
+                const u32x4 k = RowOperand<DP>::read(k_from, kb, st);
+                s[kb] = MM::multiply(k, q[st], s[kb]);
             }
-        if (word != all) {
+        if (word != all) { // keys that are not valid: minus infinity
             const uint64_t mine = word >> (4u * h);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const uint32_t bits = (uint32_t)(mine >> (32 * kb));
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool there = (bits >> (8 * (i / 4) + i % 4)) & 1u;
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        s[rb][kb][i] = there ? s[rb][kb][i] : -__builtin_inff();
-                }
+                for (int i = 0; i < 16; ++i)
+                    s[kb][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[kb][i] : -__builtin_inff();
             }
         }
-        uint32_t p[RB][KB][8];
+        uint32_t p[KB][8];
+        float most = s[0][0];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            float most = s[rb][0][0];
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+            for (int i = 0; i < 16; ++i)
+                most = fmaxf(most, s[kb][i]);
+        most = halves_max(most);
+        if (__ballot(most > top + slack) != 0) {
+            const float next = fmaxf(top, most);
+            const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - next) * c) : 1.0f;
+            top = next;
+            sum *= by;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    most = fmaxf(most, s[rb][kb][i]);
-            most = halves_max(most);
-            if (__ballot(most > top[rb] + slack) != 0) {
-                const float next = fmaxf(top[rb], most);
-                const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top[rb] - next) * c) : 1.0f;
-                top[rb] = next;
-                sum[rb] *= by;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[rb][d][i] *= by;
-            }
-            const float less = top[rb] > -__builtin_inff() ? top[rb] * c : 0.0f;
-            float part = 0.0f;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[rb][kb][i], c, -less)), y = __builtin_amdgcn_exp2f(fmaf(s[rb][kb][i + 1], c, -less));
-                    part += x + y;
-                    p[rb][kb][i / 2] = MM::two(x, y);
-                }
-            sum[rb] += part;
+                    acc[d][i] *= by;
         }
+        const float less = top > -__builtin_inff() ? top * c : 0.0f;
+        float part = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -less)), y = __builtin_amdgcn_exp2f(fmaf(s[kb][i + 1], c, -less));
+                part += x + y;
+                p[kb][i / 2] = MM::two(x, y);
+            }
+        sum += part;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    const u32x4 v = v_operand.read(stage + SH::kTile, kb, t, d);
+                    const u32x4 v = ColumnOperand<DP>::read(v_from, kb, t, d);
+                    u32x4 w;
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        u32x4 w;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            w[j] = p[rb][kb][4 * t + j];
-                        acc[rb][d] = MM::multiply(v, w, acc[rb][d]);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = p[kb][4 * t + j];
+                    acc[d] = MM::multiply(v, w, acc[d]);
                 }
     };
 
     if constexpr (SH::KEYS) {
+        // tiles t0, t0 + 4, .. of this wavefront's own: loads of the next in flight while one is computed
         constexpr int kAhead = 2 * TileLoads<DP, KT, 1>::kMine;
+        const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage;
         uint32_t at = 0;
         uint64_t word = 0;
         if (t0 < t1) {
             word = word_of(t0);
-            issue(t0, word, stages);
+            issue_k(t0, word, stages);
+            issue_v(t0, word, stages + SH::kTile);
         }
-        for (int32_t t = t0; t < t1; t += step) {
+        arrived(q);
+        for (int32_t t = t0; t < t1; t += SH::kWaves) {
             uint64_t next = 0;
-            if (t + step < t1) {
-                next = word_of(t + step);
-                issue(t + step, next, stages + (at ^ SH::kStage));
+            if (t + SH::kWaves < t1) {
+                next = word_of(t + SH::kWaves);
+                issue_k(t + SH::kWaves, next, stages + (at ^ SH::kStage));
+                issue_v(t + SH::kWaves, next, stages + (at ^ SH::kStage) + SH::kTile);
                 wait_loads<kAhead>();
             } else {
                 wait_loads<0>();
             }
-            compute(stages + at, word);
+            compute(stages + at, stages + at + SH::kTile, word);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
             at ^= SH::kStage;
             word = next;
         }
     } else {
+        const uint32_t ks = lds0, vs = lds0 + 2 * SH::kTile;
+        const bool works = (int64_t)row0 < a.rows; // (a wavefront without rows loads for the others)
         uint32_t at = 0;
         uint64_t word = 0;
         if (t0 < t1) {
             word = word_of(t0);
-            issue(t0, word, stages);
+            issue_k(t0, word, ks);
+            issue_v(t0, word, vs);
         }
+        arrived(q);
         for (int32_t t = t0; t < t1; ++t) {
             const uint64_t next = t + 1 < t1 ? word_of(t + 1) : 0;
             wait_loads<0>();
-            barrier(); // all wavefronts' loads of this tile are there, and all are done with the tile before
-            if (t + 1 < t1)
-                issue(t + 1, next, stages + (at ^ SH::kStage));
-            compute(stages + at, word);
-            at ^= SH::kStage;
+            barrier();
+            if (t + 1 < t1) {
+                issue_k(t + 1, next, ks + (at ^ SH::kTile));
+                issue_v(t + 1, next, vs + (at ^ SH::kTile));
+            }
+            if (works)
+                compute(ks + at, vs + at, word);
+            at ^= SH::kTile;
             word = next;
         }
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-        sum[rb] = halves_sum(sum[rb]);
+    sum = halves_sum(sum);
 
     if constexpr (SH::KEYS) {
         // the four wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order
-        static_assert(RB == 1, "");
-        float *const joined = reinterpret_cast<float *>(smem);             // [wave][channel][32 rows]
-        float *const stats = joined + SH::kWaves * DP * 32;                // [wave][2][32 rows]
+        float *const joined = reinterpret_cast<float *>(smem); // [wave][channel][32 rows]
+        float *const stats = joined + SH::kWaves * DP * 32;    // [wave][2][32 rows]
         wait_loads<0>();
         barrier();
         if (h == 0) {
-            stats[wave * 64 + col] = top[0];
-            stats[wave * 64 + 32 + col] = sum[0];
+            stats[wave * 64 + col] = top;
+            stats[wave * 64 + 32 + col] = sum;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier();
@@ -250,96 +240,67 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
             const float m = stats[w * 64 + col];
             total += m > -__builtin_inff() ? stats[w * 64 + 32 + col] * __builtin_amdgcn_exp2f((m - most) * c) : 0.0f;
         }
-        const float by = top[0] > -__builtin_inff() ? __builtin_amdgcn_exp2f((top[0] - most) * c) : 0.0f;
+        const float by = top > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - most) * c) : 0.0f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                joined[(wave * DP + 32 * d + 8 * (i / 4) + 4 * (int)h + i % 4) * 32 + (int)col] = acc[0][d][i] * by;
+                joined[(wave * DP + 32 * d + 8 * (i / 4) + 4 * (int)h + i % 4) * 32 + (int)col] = acc[d][i] * by;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier();
-        // wavefront w writes channels DP / 4 w ..
-        top[0] = most;
-        sum[0] = total;
-    }
-
-    // ---- out: lane l has channels 32 d + 8 (i / 4) + 4 (l / 32) .. of row l mod 32
+        top = most;
+        sum = total;
+        if (wave >= ND)
+            return; // wavefront w writes channels 32 w ..
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const uint32_t row = row0 + 32u * rb + col;
-        if ((int64_t)row >= a.rows)
-            continue;
-        const float inv = sum[rb] > 0.0f || sum[rb] != sum[rb] ? 1.0f / sum[rb] : 0.0f;
-        const float l2 = sum[rb] == 0.0f ? -__builtin_inff() : top[rb] * c + __builtin_amdgcn_logf(sum[rb]);
-        auto four = [&](int d, int g, float (&o)[4]) {
-            if constexpr (SH::KEYS) {
-                const float *const joined = reinterpret_cast<const float *>(smem);
+        for (int d = 0; d < ND; ++d)
+            if (d == wave) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int at = (32 * d + 8 * g + 4 * (int)h + j) * 32 + (int)col;
-                    o[j] = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < SH::kWaves; ++w)
-                        o[j] += joined[w * DP * 32 + at];
+                for (int i = 0; i < 16; ++i) {
+                    const float *const from = joined + (32 * d + 8 * (i / 4) + 4 * (int)h + i % 4) * 32 + (int)col;
+                    acc[d][i] = ((from[0] + from[DP * 32]) + from[2 * DP * 32]) + from[3 * DP * 32];
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    o[j] = acc[rb][d][4 * g + j];
             }
+    }
+    // ---- out: lane l has channels 32 d + 8 (i / 4) + 4 (l / 32) .. of row l mod 32
+    const bool split_up = a.splits > 1;
+    const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
+    char *const out0 = a.out + 2 * ((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim);
+    if ((int64_t)row >= a.rows)
+        return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float l2 = sum == 0.0f ? -__builtin_inff() : top * c + __builtin_amdgcn_logf(sum);
+    const int64_t line = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row;
+    char *const out = split_up ? reinterpret_cast<char *>(a.partial + line * a.dim)
+                               : out0 + 2 * row_offset(row, (uint32_t)a.group, heads_dim, a.dim);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        if (SH::KEYS && d != wave)
+            continue;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int channel = 32 * d + 8 * g + 4 * (int)h;
+            if (channel >= a.dim)
+                continue;
+            f32x4 o;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                o[j] *= inv;
-        };
-        if (SH::KEYS && wave >= ND)
-            continue;
-        if (a.splits == 1) {
-            const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
-            const int64_t first = (int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim;
-            char *const out = a.out + (first + row_offset(row, (uint32_t)a.group, heads_dim, a.dim)) * 2;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                if (SH::KEYS && d % SH::kWaves != wave)
-                    continue;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int channel = 32 * d + 8 * g + 4 * (int)h;
-                    if (channel < a.dim) {
-                        float o[4];
-                        four(d, g, o);
-                        u32x2 w;
-                        w[0] = MM::two(o[0], o[1]);
-                        w[1] = MM::two(o[2], o[3]);
-                        *reinterpret_cast<u32x2 *>(out + channel * 2) = w;
-                    }
-                }
+                o[j] = acc[d][4 * g + j] * inv;
+            if (split_up) {
+                *reinterpret_cast<f32x4 *>(out + channel * 4) = o;
+            } else {
+                u32x2 w;
+                w[0] = MM::two(o[0], o[1]);
+                w[1] = MM::two(o[2], o[3]);
+                *reinterpret_cast<u32x2 *>(out + channel * 2) = w;
             }
-            if (a.lse && h == 0 && (!SH::KEYS || wave == 0))
-                a.lse[(int64_t)bh * a.rows + row] = sum[rb] == 0.0f ? __builtin_inff() : l2;
-        } else {
-            const int64_t at = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row;
-            float *const out = a.partial + at * a.dim;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                if (SH::KEYS && d % SH::kWaves != wave)
-                    continue;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int channel = 32 * d + 8 * g + 4 * (int)h;
-                    if (channel < a.dim) {
-                        float o[4];
-                        four(d, g, o);
-                        f32x4 w;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            w[j] = o[j];
-                        *reinterpret_cast<f32x4 *>(out + channel) = w;
-                    }
-                }
-            }
-            if (h == 0 && (!SH::KEYS || wave == 0))
-                a.partial[(int64_t)a.splits * a.batch * a.kv_heads * a.rows * a.dim + at] = l2;
         }
+    }
+    if (h == 0 && (!SH::KEYS || wave == 0)) {
+        if (split_up)
+            a.partial[(int64_t)a.splits * a.batch * a.kv_heads * a.rows * a.dim + line] = l2;
+        else if (a.lse)
+            a.lse[line] = sum == 0.0f ? __builtin_inff() : l2;
     }
 }
 
@@ -406,6 +367,15 @@ bool allow_lds(const void *kernel, size_t bytes)
     return true;
 }
 
+unsigned spread(Args &a, int64_t work, int64_t per_head)
+{
+    int64_t run = work / 64 < per_head ? work / 64 : per_head;
+    run = run > 1 ? run : 1;
+    a.work = (int32_t)work;
+    a.run = (int32_t)run;
+    return (unsigned)((work + 8 * run - 1) / (8 * run) * 8 * run);
+}
+
 static bool fine_operand(const void *p, int64_t batch, int64_t token, int64_t head)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (batch | token | head) % 8 == 0;
@@ -469,8 +439,8 @@ template <class SH> static Variant variant() { return Variant{forward_kernel<SH>
 template <typename IO, int DP> static Variant pick(int64_t rows)
 {
     if (rows <= 32)
-        return variant<Shape<IO, DP, 1, true>>();
-    return variant<Shape<IO, DP, 1, false>>();
+        return variant<Shape<IO, DP, true>>();
+    return variant<Shape<IO, DP, false>>();
 }
 template <typename IO> static Variant pick(int32_t dim, int64_t rows)
 {
@@ -545,18 +515,17 @@ extern "C" grkan_status_t grkan_attention_fwd(const grkan_attention_t *at, void 
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return GRKAN_ERR_WORKSPACE;
     const int64_t work = (int64_t)a.batch * a.kv_heads * a.row_tiles * a.splits;
-    if (work > INT32_MAX - 8)
+    if (work > INT32_MAX / 2)
         return GRKAN_ERR_UNSUPPORTED;
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.partial = static_cast<float *>(workspace);
-    a.work = (int32_t)work;
-    a.per_xcd = (int32_t)((work + 7) / 8);
+    const unsigned grid = attention::spread(a, work, (int64_t)a.row_tiles * a.splits);
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)a.per_xcd * 8u), dim3(256), args, v.lds, stream) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3(grid), dim3(256), args, v.lds, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     if (a.splits > 1) {
         const int64_t lanes = (int64_t)a.batch * a.kv_heads * a.rows * (a.dim / 8), blocks = (lanes + 255) / 256;

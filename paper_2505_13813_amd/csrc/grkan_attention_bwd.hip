@@ -21,7 +21,6 @@ constexpr int kRowTile = 64;
 // Tiles of ROWS rows of the list: as TileLoads, but a row's place is its query's and its head's.
 template <int DP, int ROWS, int WAVES> struct RowLoads {
     static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = (kLoads + WAVES - 1) / WAVES;
-    static constexpr uint32_t kBytes = ROWS * DP * 2u;
     static_assert(kLoads % WAVES == 0, "");
     uint32_t row[kMine], chunk[kMine]; // chunk: its bytes, or ~0: no such channels
     int first;
@@ -41,7 +40,7 @@ template <int DP, int ROWS, int WAVES> struct RowLoads {
         const bool whole = a.group == 1 && a.dim == DP && (int64_t)row0 + ROWS <= a.rows;
 #pragma unroll
         for (int q = 0; q < kMine; ++q) {
-            const uint32_t to = lds_at + (uint32_t)(first + q * WAVES) * 1024u;
+            const uint32_t to = lds_at + (uint32_t)(first + q * WAVES) * kBlock<DP>;
             if (whole) {
                 load_to_lds(uniform_u64(base + (uint64_t)row0 * (uint64_t)o.token), row[q] * (uint32_t)o.token + chunk[q], to);
             } else {
@@ -135,21 +134,24 @@ template <typename IO> __device__ __forceinline__ float gradient_scale(const Arg
     }
 }
 
-template <typename IO_, int DP_, int B_, int WAVES_PER_SIMD_> struct BackShape {
+// ROWS: of a stage of the keys' kernel.  V_LDS: that kernel reads V from LDS at every use; its registers hold K and the sums alone.
+template <typename IO_, int DP_, int ROWS_, bool V_LDS_, int PER_> struct BackShape {
     typedef IO_ IO;
-    static constexpr int DP = DP_, B = B_, PER = WAVES_PER_SIMD_, kWaves = 4;
-    static constexpr int kOwn = 32 * B * kWaves; // keys or rows of a workgroup
-    static constexpr uint32_t kTile = kRowTile * DP * 2u;
-    // key kernel: Q, dO, lse, delta of 64 rows; row kernel: K, V of 64 keys
-    static constexpr uint32_t kKeyStage = 2 * kTile + 2 * kRowTile * 4u, kRowStage = 2 * kTile;
+    static constexpr int DP = DP_, ROWS = ROWS_, PER = PER_, kWaves = 4;
+    static constexpr bool V_LDS = V_LDS_;
+    static constexpr int kOwn = 32 * kWaves; // keys or rows of a workgroup
+    // keys' kernel: Q, dO, lse, delta of ROWS rows; queries' kernel: K, V of 64 keys
+    static constexpr uint32_t kRowsTile = kTileBytes<DP, ROWS>, kKeyStage = 2 * kRowsTile + 2 * ROWS * 4u;
+    static constexpr uint32_t kKeysTile = kTileBytes<DP, 64>, kRowStage = 2 * kKeysTile;
+    static constexpr size_t kKeyLds = 2 * (size_t)kKeyStage + (V_LDS ? 2 * (size_t)kKeysTile : 0), kRowLds = 2 * (size_t)kRowStage;
 };
 
-// dK and dV of 32 B keys a wavefront.
+// dK and dV of 32 keys a wavefront.
 template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(const Args a)
 {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
-    constexpr int DP = SH::DP, B = SH::B, ND = DP / 32, NS = DP / 16;
+    constexpr int DP = SH::DP, ROWS = SH::ROWS, ND = DP / 32, NS = DP / 16;
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -161,173 +163,170 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     const int32_t bh = item / per_head, rest = item - bh * per_head;
     const int32_t key_tile = rest / a.splits, split = rest - key_tile * a.splits;
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
-    const int64_t count = keys_of(a, b);
-    const int64_t key0 = (int64_t)key_tile * SH::kOwn + wave * 32 * B; // this wavefront's
+    const int32_t count = keys_of(a, b);
+    const int64_t key0 = (int64_t)key_tile * SH::kOwn + wave * 32, key = key0 + col; // this wavefront's and this lane's
 
     // ---- keys and values as second operands: lane l has key l mod 32, channels 16 s + 8 (l / 32) ..
-    u32x4 k[B][NS], v[B][NS];
-    bool valid[B];
+    u32x4 k[NS], v[SH::V_LDS ? 1 : NS];
+    const bool valid = key < count && (!a.mask || a.mask[(int64_t)b * a.mask_batch + key * a.mask_key] != 0);
     const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
 #pragma unroll
-    for (int kb = 0; kb < B; ++kb) {
-        const int64_t key = key0 + 32 * kb + col;
-        valid[kb] = key < count && (!a.mask || a.mask[(int64_t)b * a.mask_batch + key * a.mask_key] != 0);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const uint32_t channel = 16u * s + 8u * h;
-            const bool there = valid[kb] && channel < (uint32_t)a.dim;
-            k[kb][s] = gload16(there ? k_base + (uint64_t)key * (uint64_t)a.k.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
-            v[kb][s] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
-        }
+    for (int s = 0; s < NS; ++s) {
+        const uint32_t channel = 16u * s + 8u * h;
+        const bool there = valid && channel < (uint32_t)a.dim;
+        k[s] = gload16(there ? k_base + (uint64_t)key * (uint64_t)a.k.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        if constexpr (!SH::V_LDS)
+            v[s] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
     }
 
-    f32x16 dk[B][ND], dv[B][ND];
+    f32x16 dk[ND], dv[ND];
 #pragma unroll
-    for (int kb = 0; kb < B; ++kb)
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            dk[kb][d] = f32x16{};
-            dv[kb][d] = f32x16{};
-        }
+    for (int d = 0; d < ND; ++d) {
+        dk[d] = f32x16{};
+        dv[d] = f32x16{};
+    }
 
-    const RowLoads<DP, kRowTile, SH::kWaves> loads(wave, lane, a.dim);
+    const RowLoads<DP, ROWS, SH::kWaves> loads(wave, lane, a.dim);
     const RowOperand<DP> row_operand(lane);
     const ColumnOperand<DP> column_operand(lane);
     const uint64_t q_base = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head);
     const uint64_t d_base = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
-    const int32_t tiles = a.padded / kRowTile;
+    const int32_t tiles = (int32_t)((a.rows + ROWS - 1) / ROWS);
     int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
     t1 = t1 < tiles ? t1 : tiles;
-    // (no key of this workgroup is valid by its length: nothing to add)
-    if ((int64_t)key_tile * SH::kOwn >= count)
+    if ((int64_t)key_tile * SH::kOwn >= count) // no valid key in the workgroup: nothing to add
         t1 = t0;
+    const bool works = key0 < count; // (a wavefront without keys loads for the others)
     const float up = gradient_scale<IO>(a, bh), c = a.c;
 
     auto issue = [&](int32_t t, uint32_t stage) {
-        const uint32_t row0 = (uint32_t)t * kRowTile;
+        const uint32_t row0 = (uint32_t)t * ROWS;
         loads.issue(a.q, q_base, row0, a, stage);
-        loads.issue(a.dout, d_base, row0, a, stage + SH::kTile);
-        if (wave < 2) {
+        loads.issue(a.dout, d_base, row0, a, stage + SH::kRowsTile);
+        // (the rows' statistics are padded to whole tiles of 64)
+        if (wave < 2 && lane < ROWS) {
             const float *const from = (wave ? a.row_delta : a.row_lse) + (int64_t)bh * a.padded + row0;
-            load_words_to_lds(uniform_u64(reinterpret_cast<uint64_t>(from)), (uint32_t)lane * 4u, stage + 2 * SH::kTile + (uint32_t)wave * kRowTile * 4u);
+            load_words_to_lds(uniform_u64(reinterpret_cast<uint64_t>(from)), (uint32_t)lane * 4u, stage + 2 * SH::kRowsTile + (uint32_t)wave * ROWS * 4u);
         }
     };
 
+    const uint32_t stages = lds0 + (SH::V_LDS ? 2 * SH::kKeysTile : 0u);
     uint32_t at = 0;
-    if (t0 < t1)
-        issue(t0, lds0);
+    if (t0 < t1) {
+        if constexpr (SH::V_LDS) {
+            const TileLoads<DP, 64, SH::kWaves> v_loads(wave, lane, a.v.token, a.dim);
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const int64_t first = (int64_t)key_tile * SH::kOwn + 64 * part, mine = first + lane;
+                const bool there = mine < count && (!a.mask || a.mask[(int64_t)b * a.mask_batch + mine * a.mask_key] != 0);
+                v_loads.issue(v_base + (uint64_t)first * (uint64_t)a.v.token, __ballot(there), false, lds0 + (uint32_t)part * SH::kKeysTile);
+            }
+        }
+        issue(t0, stages);
+    }
+    arrived(k);
+    if constexpr (!SH::V_LDS)
+        arrived(v);
+    const auto v_rows = row_operand.moved(lds0 + (uint32_t)wave * row_at<DP>(32u));
     for (int32_t t = t0; t < t1; ++t) {
         wait_loads<0>();
         barrier();
         if (t + 1 < t1)
-            issue(t + 1, lds0 + (at ^ SH::kKeyStage));
-        const uint32_t stage = lds0 + at, stats = stage + 2 * SH::kTile;
+            issue(t + 1, stages + (at ^ SH::kKeyStage));
+        const uint32_t stage = stages + at;
+        at ^= SH::kKeyStage;
+        if (!works)
+            continue;
+        const auto rows = row_operand.moved(stage);
+        const auto columns = column_operand.moved(stage);
+        uint32_t stats = stage + 2 * SH::kRowsTile + 16u * h;
 #pragma unroll
-        for (int rb = 0; rb < kRowTile / 32; ++rb) {
-            f32x16 s[B], d[B];
+        for (int rb = 0; rb < ROWS / 32; ++rb) {
+            f32x16 p = {}, d = {};
 #pragma unroll
-            for (int kb = 0; kb < B; ++kb) {
-                s[kb] = f32x16{};
-                d[kb] = f32x16{};
-            }
-#pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                const u32x4 q = row_operand.read(stage, rb, st);
-#pragma unroll
-                for (int kb = 0; kb < B; ++kb)
-                    s[kb] = MM::multiply(q, k[kb][st], s[kb]);
-            }
-#pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                const u32x4 o = row_operand.read(stage + SH::kTile, rb, st);
-#pragma unroll
-                for (int kb = 0; kb < B; ++kb)
-                    d[kb] = MM::multiply(o, v[kb][st], d[kb]);
-            }
-            uint32_t p[B][8], g[B][8];
+            for (int st = 0; st < NS; ++st)
+                p = MM::multiply(RowOperand<DP>::read(rows, rb, st), k[st], p);
+            u32x4 w[2];
 #pragma unroll
             for (int quad = 0; quad < 4; ++quad) {
-                const uint32_t place = stats + (32u * rb + 8u * quad + 4u * h) * 4u;
-                const f32x4 lse = __builtin_bit_cast(f32x4, lds_read16(place)), delta = __builtin_bit_cast(f32x4, lds_read16(place + kRowTile * 4u));
+                const f32x4 lse = __builtin_bit_cast(f32x4, lds_read16(stats + (32u * rb + 8u * quad) * 4u));
 #pragma unroll
-                for (int kb = 0; kb < B; ++kb) {
-                    float x[4], y[4];
+                for (int j = 0; j < 4; ++j)
+                    p[4 * quad + j] = __builtin_amdgcn_exp2f(fmaf(p[4 * quad + j], c, -lse[j]));
+                w[quad / 2][2 * (quad % 2)] = MM::two(p[4 * quad], p[4 * quad + 1]);
+                w[quad / 2][2 * (quad % 2) + 1] = MM::two(p[4 * quad + 2], p[4 * quad + 3]);
+            }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = __builtin_amdgcn_exp2f(fmaf(s[kb][4 * quad + j], c, -lse[j]));
-                        y[j] = x[j] * fmaf(d[kb][4 * quad + j], up, -delta[j] * up);
-                    }
-                    p[kb][2 * quad] = MM::two(x[0], x[1]);
-                    p[kb][2 * quad + 1] = MM::two(x[2], x[3]);
-                    g[kb][2 * quad] = MM::two(y[0], y[1]);
-                    g[kb][2 * quad + 1] = MM::two(y[2], y[3]);
-                }
+            for (int st = 0; st < NS; ++st) {
+                u32x4 value;
+                if constexpr (SH::V_LDS)
+                    value = RowOperand<DP>::read(v_rows, 0, st);
+                else
+                    value = v[st];
+                d = MM::multiply(RowOperand<DP>::read(rows, rb, st, SH::kRowsTile), value, d);
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int part = 0; part < ND; ++part) {
-                    const u32x4 o = column_operand.read(stage + SH::kTile, rb, half, part), q = column_operand.read(stage, rb, half, part);
+                for (int part = 0; part < ND; ++part)
+                    dv[part] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, part, SH::kRowsTile), w[half], dv[part]);
 #pragma unroll
-                    for (int kb = 0; kb < B; ++kb) {
-                        u32x4 w, z;
+            for (int quad = 0; quad < 4; ++quad) {
+                const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(stats + (ROWS + 32u * rb + 8u * quad) * 4u));
+                float y[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            w[j] = p[kb][4 * half + j];
-                            z[j] = g[kb][4 * half + j];
-                        }
-                        dv[kb][part] = MM::multiply(o, w, dv[kb][part]);
-                        dk[kb][part] = MM::multiply(q, z, dk[kb][part]);
-                    }
-                }
+                for (int j = 0; j < 4; ++j)
+                    y[j] = p[4 * quad + j] * fmaf(d[4 * quad + j], up, -delta[j] * up);
+                w[quad / 2][2 * (quad % 2)] = MM::two(y[0], y[1]);
+                w[quad / 2][2 * (quad % 2) + 1] = MM::two(y[2], y[3]);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int part = 0; part < ND; ++part)
+                    dk[part] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, part), w[half], dk[part]);
         }
-        at ^= SH::kKeyStage;
     }
 
+    if (key >= a.keys)
+        return;
     const float by = a.scale / up;
+    const int64_t line = ((int64_t)b * a.keys + key) * a.kv_heads + kvh, all = (int64_t)a.batch * a.keys * a.kv_heads;
 #pragma unroll
-    for (int kb = 0; kb < B; ++kb) {
-        const int64_t key = key0 + 32 * kb + col;
-        if (key >= a.keys)
-            continue;
-        const int64_t line = ((int64_t)b * a.keys + key) * a.kv_heads + kvh;
-        const int64_t all = (int64_t)a.batch * a.keys * a.kv_heads;
+    for (int part = 0; part < ND; ++part)
 #pragma unroll
-        for (int part = 0; part < ND; ++part)
+        for (int g = 0; g < 4; ++g) {
+            const int channel = 32 * part + 8 * g + 4 * (int)h;
+            if (channel >= a.dim)
+                continue;
+            f32x4 x, y;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int channel = 32 * part + 8 * g + 4 * (int)h;
-                if (channel < a.dim) {
-                    f32x4 x, y;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = valid[kb] ? dk[kb][part][4 * g + j] * by : 0.0f;
-                        y[j] = valid[kb] ? dv[kb][part][4 * g + j] : 0.0f;
-                    }
-                    if (a.splits == 1) {
-                        u32x2 w, z;
-                        w[0] = MM::two(x[0], x[1]);
-                        w[1] = MM::two(x[2], x[3]);
-                        z[0] = MM::two(y[0], y[1]);
-                        z[1] = MM::two(y[2], y[3]);
-                        *reinterpret_cast<u32x2 *>(a.dk + (line * a.dim + channel) * 2) = w;
-                        *reinterpret_cast<u32x2 *>(a.dv + (line * a.dim + channel) * 2) = z;
-                    } else {
-                        float *const to = a.partial + ((int64_t)split * all + line) * a.dim + channel;
-                        *reinterpret_cast<f32x4 *>(to) = x;
-                        *reinterpret_cast<f32x4 *>(to + (int64_t)a.splits * all * a.dim) = y;
-                    }
-                }
+            for (int j = 0; j < 4; ++j) {
+                x[j] = valid ? dk[part][4 * g + j] * by : 0.0f;
+                y[j] = valid ? dv[part][4 * g + j] : 0.0f;
             }
-    }
+            if (a.splits == 1) {
+                u32x2 u, z;
+                u[0] = MM::two(x[0], x[1]);
+                u[1] = MM::two(x[2], x[3]);
+                z[0] = MM::two(y[0], y[1]);
+                z[1] = MM::two(y[2], y[3]);
+                *reinterpret_cast<u32x2 *>(a.dk + (line * a.dim + channel) * 2) = u;
+                *reinterpret_cast<u32x2 *>(a.dv + (line * a.dim + channel) * 2) = z;
+            } else {
+                float *const to = a.partial + ((int64_t)split * all + line) * a.dim + channel;
+                *reinterpret_cast<f32x4 *>(to) = x;
+                *reinterpret_cast<f32x4 *>(to + (int64_t)a.splits * all * a.dim) = y;
+            }
+        }
 }
 
-// dQ of 32 B rows a wavefront.
-template <class SH> __global__ __launch_bounds__(256, SH::PER) void queries_kernel(const Args a)
+// dQ of 32 rows a wavefront.
+template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(const Args a)
 {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
-    constexpr int DP = SH::DP, B = SH::B, ND = DP / 32, NS = DP / 16, KT = kRowTile;
+    constexpr int DP = SH::DP, ND = DP / 32, NS = DP / 16, KT = 64;
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -339,37 +338,34 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void queries_kern
     const int32_t bh = item / per_head, rest = item - bh * per_head;
     const int32_t row_tile = rest / a.splits, split = rest - row_tile * a.splits;
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
-    const int64_t count = keys_of(a, b);
-    const int32_t tiles = (int32_t)((count + KT - 1) / KT);
-    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
-    t1 = t1 < tiles ? t1 : tiles;
 
-    const uint32_t row0 = (uint32_t)row_tile * SH::kOwn + (uint32_t)wave * 32u * B;
-    const uint64_t q_base = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head);
-    const uint64_t d_base = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
-    const float up = gradient_scale<IO>(a, bh), c = a.c;
-    u32x4 q[B][NS], o[B][NS];
-    float lse[B], delta[B];
-    f32x16 dq[B][ND];
-#pragma unroll
-    for (int rb = 0; rb < B; ++rb) {
-        const uint32_t row = row0 + 32u * rb + col;
-        const bool row_there = (int64_t)row < a.rows;
-        const int64_t qo = row_offset(row, (uint32_t)a.group, a.q.token, a.q.head), oo = row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head);
+    const uint32_t row0 = (uint32_t)row_tile * SH::kOwn + (uint32_t)wave * 32u, row = row0 + col;
+    const bool there = (int64_t)row < a.rows, works = (int64_t)row0 < a.rows;
+    u32x4 q[NS], o[NS];
+    {
+        const uint64_t q_at = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head +
+                                                  row_offset(row, (uint32_t)a.group, a.q.token, a.q.head));
+        const uint64_t o_at = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head +
+                                                     row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head));
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const uint32_t channel = 16u * s + 8u * h;
-            const bool there = row_there && channel < (uint32_t)a.dim;
-            q[rb][s] = gload16(there ? q_base + (uint64_t)qo + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
-            o[rb][s] = gload16(there ? d_base + (uint64_t)oo + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            const bool loaded = there && channel < (uint32_t)a.dim;
+            q[s] = gload16(loaded ? q_at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            o[s] = gload16(loaded ? o_at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
-        lse[rb] = row_there ? a.row_lse[(int64_t)bh * a.padded + row] : __builtin_inff();
-        delta[rb] = row_there ? a.row_delta[(int64_t)bh * a.padded + row] * up : 0.0f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-            dq[rb][d] = f32x16{};
     }
+    const float up = gradient_scale<IO>(a, bh), c = a.c;
+    float lse = there ? a.row_lse[(int64_t)bh * a.padded + row] : __builtin_inff();
+    float delta = there ? a.row_delta[(int64_t)bh * a.padded + row] * up : 0.0f;
+    f32x16 dq[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+        dq[d] = f32x16{};
 
+    const int32_t count = keys_of(a, b), tiles = (count + KT - 1) / KT;
+    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
+    t1 = t1 < tiles ? t1 : tiles;
     const TileLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
     const RowOperand<DP> row_operand(lane);
     const ColumnOperand<DP> column_operand(lane);
@@ -378,7 +374,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void queries_kern
     auto issue = [&](int32_t t, uint64_t word, uint32_t stage) {
         const bool whole = word == ~(uint64_t)0 && a.dim == DP;
         k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, word, whole, stage);
-        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, whole, stage + SH::kTile);
+        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, whole, stage + SH::kKeysTile);
     };
 
     uint32_t at = 0;
@@ -387,100 +383,78 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void queries_kern
         word = valid.word(t0);
         issue(t0, word, lds0);
     }
+    arrived(q);
+    arrived(o);
+    arrived(lse);
+    arrived(delta);
     for (int32_t t = t0; t < t1; ++t) {
-        const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0;
+        const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0, now = word;
         wait_loads<0>();
         barrier();
         if (t + 1 < t1)
             issue(t + 1, next, lds0 + (at ^ SH::kRowStage));
-        const uint32_t stage = lds0 + at;
-#pragma unroll
-        for (int kb = 0; kb < KT / 32; ++kb) {
-            f32x16 s[B], d[B];
-#pragma unroll
-            for (int rb = 0; rb < B; ++rb) {
-                s[rb] = f32x16{};
-                d[rb] = f32x16{};
-            }
-#pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                const u32x4 k = row_operand.read(stage, kb, st);
-#pragma unroll
-                for (int rb = 0; rb < B; ++rb)
-                    s[rb] = MM::multiply(k, q[rb][st], s[rb]);
-            }
-#pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                const u32x4 v = row_operand.read(stage + SH::kTile, kb, st);
-#pragma unroll
-                for (int rb = 0; rb < B; ++rb)
-                    d[rb] = MM::multiply(v, o[rb][st], d[rb]);
-            }
-            uint32_t g[B][8];
-#pragma unroll
-            for (int rb = 0; rb < B; ++rb) {
-                float y[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    y[i] = __builtin_amdgcn_exp2f(fmaf(s[rb][i], c, -lse[rb])) * fmaf(d[rb][i], up, -delta[rb]);
-                if (word != ~(uint64_t)0) {
-                    const uint32_t bits = (uint32_t)((word >> (32 * kb)) >> (4u * h));
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        y[i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? y[i] : 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; i += 2)
-                    g[rb][i / 2] = MM::two(y[i], y[i + 1]);
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int part = 0; part < ND; ++part) {
-                    const u32x4 k = column_operand.read(stage, kb, half, part);
-#pragma unroll
-                    for (int rb = 0; rb < B; ++rb) {
-                        u32x4 z;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            z[j] = g[rb][4 * half + j];
-                        dq[rb][part] = MM::multiply(k, z, dq[rb][part]);
-                    }
-                }
-        }
+        const auto rows = row_operand.moved(lds0 + at);
+        const auto columns = column_operand.moved(lds0 + at);
         at ^= SH::kRowStage;
         word = next;
+        if (!works)
+            continue;
+#pragma unroll
+        for (int kb = 0; kb < KT / 32; ++kb) {
+            f32x16 s = {}, d = {};
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+                s = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], s);
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+                d = MM::multiply(RowOperand<DP>::read(rows, kb, st, SH::kKeysTile), o[st], d);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * fmaf(d[i], up, -delta);
+            if (now != ~(uint64_t)0) {
+                const uint32_t bits = (uint32_t)((now >> (32 * kb)) >> (4u * h));
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[i] : 0.0f;
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                u32x4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = MM::two(s[8 * half + 2 * j], s[8 * half + 2 * j + 1]);
+#pragma unroll
+                for (int part = 0; part < ND; ++part)
+                    dq[part] = MM::multiply(ColumnOperand<DP>::read(columns, kb, half, part), w, dq[part]);
+            }
+        }
     }
 
+    if (!there)
+        return;
     const float by = a.scale / up;
     const int64_t heads = (int64_t)a.kv_heads * a.group, all = (int64_t)a.batch * a.kv_heads * a.rows;
+    const int64_t line = (int64_t)b * (a.rows / a.group) * heads + (int64_t)kvh * a.group + row_offset(row, (uint32_t)a.group, heads, 1);
 #pragma unroll
-    for (int rb = 0; rb < B; ++rb) {
-        const uint32_t row = row0 + 32u * rb + col;
-        if ((int64_t)row >= a.rows)
-            continue;
-        const int64_t line = (int64_t)b * (a.rows / a.group) * heads + (int64_t)kvh * a.group + row_offset(row, (uint32_t)a.group, heads, 1);
+    for (int part = 0; part < ND; ++part)
 #pragma unroll
-        for (int part = 0; part < ND; ++part)
+        for (int g = 0; g < 4; ++g) {
+            const int channel = 32 * part + 8 * g + 4 * (int)h;
+            if (channel >= a.dim)
+                continue;
+            f32x4 x;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int channel = 32 * part + 8 * g + 4 * (int)h;
-                if (channel < a.dim) {
-                    f32x4 x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        x[j] = dq[rb][part][4 * g + j] * by;
-                    if (a.splits == 1) {
-                        u32x2 w;
-                        w[0] = MM::two(x[0], x[1]);
-                        w[1] = MM::two(x[2], x[3]);
-                        *reinterpret_cast<u32x2 *>(a.out + (line * a.dim + channel) * 2) = w;
-                    } else {
-                        *reinterpret_cast<f32x4 *>(a.partial + ((int64_t)split * all + line) * a.dim + channel) = x;
-                    }
-                }
+            for (int j = 0; j < 4; ++j)
+                x[j] = dq[part][4 * g + j] * by;
+            if (a.splits == 1) {
+                u32x2 w;
+                w[0] = MM::two(x[0], x[1]);
+                w[1] = MM::two(x[2], x[3]);
+                *reinterpret_cast<u32x2 *>(a.out + (line * a.dim + channel) * 2) = w;
+            } else {
+                *reinterpret_cast<f32x4 *>(a.partial + ((int64_t)split * all + line) * a.dim + channel) = x;
             }
-    }
+        }
 }
 
 // The sum of the splits' parts, eight elements a lane.
@@ -511,22 +485,22 @@ template <typename IO> __global__ __launch_bounds__(256) void sum_kernel(const f
 typedef void (*Kernel)(Args);
 struct BackVariant {
     Kernel keys, queries;
-    int own_keys, own_rows;
+    int own, rows; // keys or rows of a workgroup; rows of a stage of the keys' kernel
     size_t keys_lds, queries_lds;
 };
-template <class KS, class QS> static BackVariant back_variant()
+template <class SH> static BackVariant back_variant()
 {
-    return BackVariant{keys_kernel<KS>, queries_kernel<QS>, KS::kOwn, QS::kOwn, 2 * (size_t)KS::kKeyStage, 2 * (size_t)QS::kRowStage};
+    return BackVariant{keys_kernel<SH>, queries_kernel<SH>, SH::kOwn, SH::ROWS, SH::kKeyLds, SH::kRowLds};
 }
 template <typename IO> static BackVariant pick(int32_t dim)
 {
     if (dim <= 32)
-        return back_variant<BackShape<IO, 32, 1, 2>, BackShape<IO, 32, 1, 2>>();
+        return back_variant<BackShape<IO, 32, 64, false, 2>>();
     if (dim <= 64)
-        return back_variant<BackShape<IO, 64, 1, 2>, BackShape<IO, 64, 1, 2>>();
+        return back_variant<BackShape<IO, 64, 64, false, 2>>();
     if (dim <= 96)
-        return back_variant<BackShape<IO, 96, 1, 2>, BackShape<IO, 96, 1, 2>>();
-    return back_variant<BackShape<IO, 128, 1, 1>, BackShape<IO, 128, 1, 2>>();
+        return back_variant<BackShape<IO, 96, 64, false, 2>>();
+    return back_variant<BackShape<IO, 128, 32, true, 2>>();
 }
 
 // How many workgroups share the walk of one: enough to give each compute unit two, four tiles each at least.
@@ -556,9 +530,9 @@ static BackPlan back_plan(const Args &a, grkan_dtype_t io)
     const int64_t heads = (int64_t)a.batch * a.kv_heads;
     const int32_t padded = (int32_t)((a.rows + kRowTile - 1) / kRowTile) * kRowTile;
     p.keys.padded = p.queries.padded = padded;
-    p.keys.key_tiles = (int32_t)((a.keys + p.v.own_keys - 1) / p.v.own_keys);
-    p.queries.row_tiles = (int32_t)((a.rows + p.v.own_rows - 1) / p.v.own_rows);
-    split(heads * p.keys.key_tiles, padded / kRowTile, p.keys);
+    p.keys.key_tiles = (int32_t)((a.keys + p.v.own - 1) / p.v.own);
+    p.queries.row_tiles = (int32_t)((a.rows + p.v.own - 1) / p.v.own);
+    split(heads * p.keys.key_tiles, (a.rows + p.v.rows - 1) / p.v.rows, p.keys);
     split(heads * p.queries.row_tiles, (a.keys + kRowTile - 1) / kRowTile, p.queries);
     p.stats = (size_t)heads * (size_t)padded * 2 + (((size_t)heads * (size_t)(padded / kRowTile) + 3) & ~(size_t)3);
     // (one after the other: they share the memory)
@@ -582,7 +556,7 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
     const int64_t key_work = heads * k.key_tiles * k.splits, row_work = heads * q.row_tiles * q.splits;
     const int64_t key_elements = (int64_t)k.batch * k.keys * k.kv_heads * k.dim, row_elements = heads * k.rows * k.dim;
     const int64_t key_blocks = (key_elements / 8 + 255) / 256, row_blocks = (row_elements / 8 + 255) / 256;
-    if (rows_grid > INT32_MAX || key_work > INT32_MAX - 8 || row_work > INT32_MAX - 8 || (k.splits > 1 && key_blocks > INT32_MAX) ||
+    if (rows_grid > INT32_MAX || key_work > INT32_MAX / 2 || row_work > INT32_MAX / 2 || (k.splits > 1 && key_blocks > INT32_MAX) ||
         (q.splits > 1 && row_blocks > INT32_MAX))
         return GRKAN_ERR_UNSUPPORTED;
     if (!allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) || !allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))
@@ -590,10 +564,9 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
     if (rows_grid > 0)
         rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
     if (key_work > 0) {
-        k.work = (int32_t)key_work;
-        k.per_xcd = (int32_t)((key_work + 7) / 8);
+        const unsigned grid = spread(k, key_work, (int64_t)k.key_tiles * k.splits);
         void *args[] = {&k};
-        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3((unsigned)k.per_xcd * 8u), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
+        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3(grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
             return GRKAN_ERR_LAUNCH;
         if (k.splits > 1) {
             sum_kernel<IO><<<dim3((unsigned)key_blocks), 256, 0, stream>>>(k.partial, k.splits, key_elements, k.dk);
@@ -601,10 +574,9 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
         }
     }
     if (row_work > 0) {
-        q.work = (int32_t)row_work;
-        q.per_xcd = (int32_t)((row_work + 7) / 8);
+        const unsigned grid = spread(q, row_work, (int64_t)q.row_tiles * q.splits);
         void *args[] = {&q};
-        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.queries), dim3((unsigned)q.per_xcd * 8u), dim3(256), args, p.v.queries_lds, stream) != hipSuccess)
+        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.queries), dim3(grid), dim3(256), args, p.v.queries_lds, stream) != hipSuccess)
             return GRKAN_ERR_LAUNCH;
         if (q.splits > 1)
             sum_kernel<IO><<<dim3((unsigned)row_blocks), 256, 0, stream>>>(q.partial, q.splits, row_elements, q.out);
