@@ -45,6 +45,7 @@ struct Args {
     // backward: of each row, padded to whole tiles of 64, its lse and sum over channels of dout out; the largest |dout| of each 64
     float *row_lse, *row_delta, *row_most;
     int32_t padded;         // rows with the padding
+    int32_t even_q, even_dout; // places of a tile's rows in q and dout in 32 bits
     int32_t splits, tiles_per_split;
     int32_t row_tiles, key_tiles; // workgroups of a key head over rows, over keys
     int32_t work, run; // work items, and how many of them in a row one XCD gets
@@ -122,39 +123,49 @@ __device__ __forceinline__ void arrived(float &r) { asm volatile("" : "+v"(r)); 
 
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
-// Tiles of ROWS tokens (keys) by WAVES wavefronts: `q`-th load of this wavefront.
+// Tiles of ROWS tokens (keys) by WAVES wavefronts, a KB at a time.  Loops, not rows of loads: a kernel that is over in microseconds waits for
+// its own code, which comes to every compute unit with the launch (the first keys of 1,024, 128 channels, were under way after 4 us of a wavefront's
+// life with the loads written out).
 template <int DP, int ROWS, int WAVES> struct TileLoads {
-    static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = (kLoads + WAVES - 1) / WAVES;
-    static_assert(ROWS * kChunks % 64 == 0, "");
+    static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = kLoads / WAVES;
+    // loads kEach WAVES apart differ by whole tokens alone: the pieces of a row are permuted alike in both
+    static constexpr int kEach = DP == 96 ? 3 : 1, kTurns = kMine / kEach;
+    static constexpr uint32_t kTokens = (uint32_t)(kEach * WAVES * 64 / kChunks); // between them
+    static_assert(kMine * WAVES == kLoads && kTurns * kEach == kMine && kEach * WAVES * 64 % kChunks == 0, "");
 
-    uint32_t offset[kMine], bit[kMine]; // from the tile's first row; the row, or 64: no such channels
-    int first;
+    uint32_t offset[kEach], row[kEach]; // of the first turn: bytes from the tile's first row; the row, or 64: no such channels
+    uint32_t first;
 
-    __device__ __forceinline__ TileLoads(int wave, int lane, int64_t token_stride, int32_t dim) : first(wave)
+    __device__ __forceinline__ TileLoads(int wave, int lane, int64_t token_stride, int32_t dim) : first((uint32_t)wave)
     {
 #pragma unroll
-        for (int q = 0; q < kMine; ++q) {
-            const uint32_t e = (uint32_t)(first + q * WAVES) * 64u + (uint32_t)lane;
-            const uint32_t row = e / kChunks, chunk = (e % kChunks) ^ swizzle<DP>(row);
-            offset[q] = row * (uint32_t)token_stride + chunk * 16u;
-            bit[q] = chunk * 8u < (uint32_t)dim ? row : 64u;
+        for (int q = 0; q < kEach; ++q) {
+            const uint32_t e = (first + (uint32_t)(q * WAVES)) * 64u + (uint32_t)lane;
+            const uint32_t r = e / kChunks, chunk = (e % kChunks) ^ swizzle<DP>(r);
+            offset[q] = r * (uint32_t)token_stride + chunk * 16u;
+            row[q] = chunk * 8u < (uint32_t)dim ? r : 64u;
         }
     }
 
     // base: the tile's first row (the same in all lanes); word: which rows are valid; whole: all of them, and all channels
-    __device__ __forceinline__ void issue(uint64_t base, uint64_t word, bool whole, uint32_t lds_at) const
+    __device__ __forceinline__ void issue(uint64_t base, int64_t token_stride, uint64_t word, bool whole, uint32_t lds_at) const
     {
+        const uint64_t step = (uint64_t)token_stride * kTokens;
+        uint32_t to = lds_at + first * kBlock<DP>;
+#pragma unroll 1
+        for (int turn = 0; turn < kTurns; ++turn) {
 #pragma unroll
-        for (int q = 0; q < kMine; ++q) {
-            const int u = first + q * WAVES;
-            if ((q + 1) * WAVES <= kLoads || u < kLoads) {
+            for (int q = 0; q < kEach; ++q) {
                 if (whole) {
-                    load_to_lds(uniform_u64(base), offset[q], lds_at + (uint32_t)u * kBlock<DP>);
+                    load_to_lds(uniform_u64(base), offset[q], to);
                 } else {
-                    const bool there = bit[q] < 64u && ((word >> (bit[q] & 63u)) & 1u);
-                    load_to_lds_at(there ? base + offset[q] : reinterpret_cast<uint64_t>(kZeros), lds_at + (uint32_t)u * kBlock<DP>);
+                    const bool there = row[q] < 64u && ((word >> (row[q] & 63u)) & 1u);
+                    load_to_lds_at(there ? base + offset[q] : reinterpret_cast<uint64_t>(kZeros), to);
                 }
+                to += WAVES * kBlock<DP>;
             }
+            base += step;
+            word >>= kTokens;
         }
     }
 };
@@ -286,6 +297,7 @@ __device__ __forceinline__ int32_t work_item(const Args &a)
 // host
 grkan_status_t fill(const grkan_attention_t *a, grkan_dtype_t io, Args *to); // checks and arguments (grkan_attention.hip)
 bool allow_lds(const void *kernel, size_t bytes);
+bool in_offsets(int64_t token_stride, int64_t head_stride, int64_t heads);    // of a tile, in elements of 2 bytes
 unsigned spread(Args &a, int64_t work, int64_t per_head); // sets work and run; the grid
 
 } // namespace attention

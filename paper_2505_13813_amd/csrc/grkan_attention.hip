@@ -3,9 +3,10 @@
 //
 //   * With rows enough (queries x heads that share a key head), a workgroup of four wavefronts has 32 each; 64 keys and their
 //     values at a time come to LDS by LDS-direct loads, two tiles deep, and serve all four.
+//     Where the workgroups would not fill the chip, the keys are split over several, and a second launch joins them.
 //   * With 32 rows or fewer (single tokens) the keys are what there is to read: the four wavefronts have the same rows and
-//     tiles of 32 keys of their own, in LDS of their own, without a barrier, and join what they found at the end.
-//   * Where the workgroups would not fill the chip, the keys are split over several, and a second launch joins them.
+//     tiles of 32 keys of their own, in LDS of their own, without a barrier, and join what they found at the end.  All the keys are dealt
+//     out evenly to a workgroup on each compute unit, and a second launch joins the parts.
 //
 // The maximum of a row is raised only where a score passes it by more than 2^8 in the exponent: the probabilities are then at most 256,
 // which neither 16-bit type minds, and the accumulators are scaled in few of the tiles instead of in most.
@@ -20,36 +21,17 @@
 namespace grkan {
 namespace attention {
 
-template <typename IO_, int DP_, bool KEYS_> struct Shape {
-    typedef IO_ IO;
-    static constexpr int DP = DP_, kWaves = 4;
-    static constexpr bool KEYS = KEYS_;       // the wavefronts split the keys, not the rows
-    static constexpr int KT = KEYS ? 32 : 64; // keys of a tile
-    static constexpr int kRows = KEYS ? 32 : 32 * kWaves;
-    static constexpr uint32_t kTile = kTileBytes<DP, KT>, kStage = 2 * kTile;
-    static constexpr size_t kLds = (size_t)kStage * 2 * (KEYS ? kWaves : 1);
-};
-
-template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(const Args a)
-{
-    using IO = typename SH::IO;
+// 32 rows of a wavefront: their queries, the running maximum and sum, and the sum of the weighted values.
+template <typename IO, int DP, int KT> struct Rows {
     using MM = Matrix<IO>;
-    constexpr int DP = SH::DP, KT = SH::KT, KB = KT / 32, ND = DP / 32, NS = DP / 16;
-    extern __shared__ __align__(256) char smem[];
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
+    static constexpr int KB = KT / 32, ND = DP / 32, NS = DP / 16;
+    static constexpr uint64_t kAll = KT == 64 ? ~(uint64_t)0 : 0xffffffffu;
 
-    const int32_t item = work_item(a);
-    if (item >= a.work)
-        return;
-    const int32_t per_head = a.row_tiles * a.splits;
-    const int32_t bh = item / per_head, rest = item - bh * per_head;
-    const int32_t row_tile = rest / a.splits, split = rest - row_tile * a.splits;
-    const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
-    // ---- this wavefront's rows as second operands: lane l has row l mod 32, channels 16 s + 8 (l / 32) ..
-    const uint32_t row0 = (uint32_t)row_tile * SH::kRows + (SH::KEYS ? 0u : (uint32_t)wave * 32u), row = row0 + col;
-    u32x4 q[NS];
+    u32x4 q[NS];   // second operands: lane l has row l mod 32, channels 16 s + 8 (l / 32) ..
+    f32x16 acc[ND]; // lane l has channels 32 d + 8 (i / 4) + 4 (l / 32) + i mod 4 of row l mod 32
+    float top, sum; // the maximum that the probabilities are relative to; this lane's part of their sum
+
+    __device__ __forceinline__ void load(const Args &a, int32_t b, int32_t kvh, uint32_t row, uint32_t h)
     {
         const uint64_t at = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head +
                                                 row_offset(row, (uint32_t)a.group, a.q.token, a.q.head));
@@ -60,44 +42,18 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
             q[s] = gload16(there ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
     }
-
-    const int32_t count = keys_of(a, b), tiles = (count + KT - 1) / KT;
-    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
-    t1 = t1 < tiles ? t1 : tiles;
-    if (SH::KEYS)
-        t0 += wave;
-
-    constexpr int loaders = SH::KEYS ? 1 : SH::kWaves;
-    const TileLoads<DP, KT, loaders> k_loads(SH::KEYS ? 0 : wave, lane, a.k.token, a.dim), v_loads(SH::KEYS ? 0 : wave, lane, a.v.token, a.dim);
-    const RowOperand<DP> k_operand(lane);
-    const ColumnOperand<DP> v_operand(lane);
-    const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
-    ValidKeys valid(a, b, count);
-    constexpr uint64_t all = KT == 64 ? ~(uint64_t)0 : 0xffffffffu;
-
-    auto word_of = [&](int32_t t) {
-        if constexpr (KT == 64)
-            return valid.word(t);
-        else
-            return (valid.word(t / 2) >> (t % 2 * 32)) & all;
-    };
-    auto issue_k = [&](int32_t t, uint64_t word, uint32_t to) {
-        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, word, word == all && a.dim == DP, to);
-    };
-    auto issue_v = [&](int32_t t, uint64_t word, uint32_t to) {
-        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, word == all && a.dim == DP, to);
-    };
-
-    f32x16 acc[ND];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
-        acc[d] = f32x16{};
-    float top = -__builtin_inff(), sum = 0.0f; // the maximum that the probabilities are relative to; this lane's part of their sum
-    const float c = a.c, slack = fminf(8.0f / c, 1e38f); // (of scores)
+        for (int d = 0; d < ND; ++d)
+            acc[d] = f32x16{};
+        top = -__builtin_inff();
+        sum = 0.0f;
+    }
 
-    auto compute = [&](uint32_t k_at, uint32_t v_at, uint64_t word) {
-        const auto k_from = k_operand.moved(k_at);
-        const auto v_from = v_operand.moved(v_at);
+    // One tile of keys.  word: which of them are valid; c: of the scores, in powers of 2
+    __device__ __forceinline__ void take(const Addresses<NS> &k_from, const Addresses<ND> &v_from, uint64_t word, float c, uint32_t h)
+    {
         f32x16 s[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -105,11 +61,9 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const u32x4 k = RowOperand<DP>::read(k_from, kb, st);
-                s[kb] = MM::multiply(k, q[st], s[kb]);
-            }
-        if (word != all) { // keys that are not valid: minus infinity
+            for (int kb = 0; kb < KB; ++kb)
+                s[kb] = MM::multiply(RowOperand<DP>::read(k_from, kb, st), q[st], s[kb]);
+        if (word != kAll) { // keys that are not valid: minus infinity
             const uint64_t mine = word >> (4u * h);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
@@ -119,7 +73,6 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
                     s[kb][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[kb][i] : -__builtin_inff();
             }
         }
-        uint32_t p[KB][8];
         float most = s[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -127,18 +80,21 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
             for (int i = 0; i < 16; ++i)
                 most = fmaxf(most, s[kb][i]);
         most = halves_max(most);
-        if (__ballot(most > top + slack) != 0) {
+        if (__ballot(most > top + fminf(8.0f / c, 1e38f)) != 0) {
             const float next = fmaxf(top, most);
-            const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - next) * c) : 1.0f;
+            if (__ballot(top > -__builtin_inff()) != 0) { // (else there is nothing to scale yet)
+                const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - next) * c) : 1.0f;
+                sum *= by;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        acc[d][i] *= by;
+            }
             top = next;
-            sum *= by;
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    acc[d][i] *= by;
         }
         const float less = top > -__builtin_inff() ? top * c : 0.0f;
+        uint32_t p[KB][8];
         float part = 0.0f;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -152,159 +108,168 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                u32x4 w;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const u32x4 v = ColumnOperand<DP>::read(v_from, kb, t, d);
-                    u32x4 w;
+                for (int j = 0; j < 4; ++j)
+                    w[j] = p[kb][4 * t + j];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        w[j] = p[kb][4 * t + j];
-                    acc[d] = MM::multiply(v, w, acc[d]);
-                }
-    };
-
-    if constexpr (SH::KEYS) {
-        // tiles t0, t0 + 4, .. of this wavefront's own: loads of the next in flight while one is computed
-        constexpr int kAhead = 2 * TileLoads<DP, KT, 1>::kMine;
-        const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage;
-        uint32_t at = 0;
-        uint64_t word = 0;
-        if (t0 < t1) {
-            word = word_of(t0);
-            issue_k(t0, word, stages);
-            issue_v(t0, word, stages + SH::kTile);
-        }
-        arrived(q);
-        for (int32_t t = t0; t < t1; t += SH::kWaves) {
-            uint64_t next = 0;
-            if (t + SH::kWaves < t1) {
-                next = word_of(t + SH::kWaves);
-                issue_k(t + SH::kWaves, next, stages + (at ^ SH::kStage));
-                issue_v(t + SH::kWaves, next, stages + (at ^ SH::kStage) + SH::kTile);
-                wait_loads<kAhead>();
-            } else {
-                wait_loads<0>();
-            }
-            compute(stages + at, stages + at + SH::kTile, word);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
-            at ^= SH::kStage;
-            word = next;
-        }
-    } else {
-        const uint32_t ks = lds0, vs = lds0 + 2 * SH::kTile;
-        const bool works = (int64_t)row0 < a.rows; // (a wavefront without rows loads for the others)
-        uint32_t at = 0;
-        uint64_t word = 0;
-        if (t0 < t1) {
-            word = word_of(t0);
-            issue_k(t0, word, ks);
-            issue_v(t0, word, vs);
-        }
-        arrived(q);
-        for (int32_t t = t0; t < t1; ++t) {
-            const uint64_t next = t + 1 < t1 ? word_of(t + 1) : 0;
-            wait_loads<0>();
-            barrier();
-            if (t + 1 < t1) {
-                issue_k(t + 1, next, ks + (at ^ SH::kTile));
-                issue_v(t + 1, next, vs + (at ^ SH::kTile));
-            }
-            if (works)
-                compute(ks + at, vs + at, word);
-            at ^= SH::kTile;
-            word = next;
-        }
-    }
-    sum = halves_sum(sum);
-
-    if constexpr (SH::KEYS) {
-        // the four wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order
-        float *const joined = reinterpret_cast<float *>(smem); // [wave][channel][32 rows]
-        float *const stats = joined + SH::kWaves * DP * 32;    // [wave][2][32 rows]
-        wait_loads<0>();
-        barrier();
-        if (h == 0) {
-            stats[wave * 64 + col] = top;
-            stats[wave * 64 + 32 + col] = sum;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        barrier();
-        float most = -__builtin_inff();
-#pragma unroll
-        for (int w = 0; w < SH::kWaves; ++w)
-            most = fmaxf(most, stats[w * 64 + col]);
-        float total = 0.0f;
-#pragma unroll
-        for (int w = 0; w < SH::kWaves; ++w) {
-            const float m = stats[w * 64 + col];
-            total += m > -__builtin_inff() ? stats[w * 64 + 32 + col] * __builtin_amdgcn_exp2f((m - most) * c) : 0.0f;
-        }
-        const float by = top > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - most) * c) : 0.0f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                joined[(wave * DP + 32 * d + 8 * (i / 4) + 4 * (int)h + i % 4) * 32 + (int)col] = acc[d][i] * by;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        barrier();
-        top = most;
-        sum = total;
-        if (wave >= ND)
-            return; // wavefront w writes channels 32 w ..
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-            if (d == wave) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float *const from = joined + (32 * d + 8 * (i / 4) + 4 * (int)h + i % 4) * 32 + (int)col;
-                    acc[d][i] = ((from[0] + from[DP * 32]) + from[2 * DP * 32]) + from[3 * DP * 32];
-                }
+                for (int d = 0; d < ND; ++d)
+                    acc[d] = MM::multiply(ColumnOperand<DP>::read(v_from, kb, t, d), w, acc[d]);
             }
     }
-    // ---- out: lane l has channels 32 d + 8 (i / 4) + 4 (l / 32) .. of row l mod 32
-    const bool split_up = a.splits > 1;
-    const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
-    char *const out0 = a.out + 2 * ((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim);
-    if ((int64_t)row >= a.rows)
-        return;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const float l2 = sum == 0.0f ? -__builtin_inff() : top * c + __builtin_amdgcn_logf(sum);
-    const int64_t line = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row;
-    char *const out = split_up ? reinterpret_cast<char *>(a.partial + line * a.dim)
-                               : out0 + 2 * row_offset(row, (uint32_t)a.group, heads_dim, a.dim);
+};
+
+// Channels 32 d .. of a row, as the sums lie in the lanes: of the output, or as they are to a row of float32
+template <typename IO> __device__ __forceinline__ void store_channels(const f32x16 &sums, int d, float by, const Args &a, char *out, bool wide, uint32_t h)
+{
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-        if (SH::KEYS && d != wave)
+    for (int g = 0; g < 4; ++g) {
+        const int channel = 32 * d + 8 * g + 4 * (int)h;
+        if (channel >= a.dim)
             continue;
+        f32x4 o;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int channel = 32 * d + 8 * g + 4 * (int)h;
-            if (channel >= a.dim)
-                continue;
-            f32x4 o;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                o[j] = acc[d][4 * g + j] * inv;
-            if (split_up) {
-                *reinterpret_cast<f32x4 *>(out + channel * 4) = o;
-            } else {
-                u32x2 w;
-                w[0] = MM::two(o[0], o[1]);
-                w[1] = MM::two(o[2], o[3]);
-                *reinterpret_cast<u32x2 *>(out + channel * 2) = w;
-            }
+        for (int j = 0; j < 4; ++j)
+            o[j] = sums[4 * g + j] * by;
+        if (wide) {
+            *reinterpret_cast<f32x4 *>(out + channel * 4) = o;
+        } else {
+            u32x2 w;
+            w[0] = Matrix<IO>::two(o[0], o[1]);
+            w[1] = Matrix<IO>::two(o[2], o[3]);
+            *reinterpret_cast<u32x2 *>(out + channel * 2) = w;
         }
-    }
-    if (h == 0 && (!SH::KEYS || wave == 0)) {
-        if (split_up)
-            a.partial[(int64_t)a.splits * a.batch * a.kv_heads * a.rows * a.dim + line] = l2;
-        else if (a.lse)
-            a.lse[line] = sum == 0.0f ? __builtin_inff() : l2;
     }
 }
 
-// out of the splits' rows, each the mean over its own keys, by the share of the sum that each has: dim / 8 lanes a row, eight channels each
+// Where row r of a key head goes in the output.
+__device__ __forceinline__ char *out_row(const Args &a, int32_t b, int32_t kvh, uint32_t row)
+{
+    const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
+    return a.out + 2 * ((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim +
+                        row_offset(row, (uint32_t)a.group, heads_dim, a.dim));
+}
+
+// log2 of a row's sum as the splits keep it; the caller's lse has an infinity for a row without a valid key
+__device__ __forceinline__ float log2_sum(float top, float sum, float c)
+{
+    return sum == 0.0f ? -__builtin_inff() : top * c + __builtin_amdgcn_logf(sum);
+}
+__device__ __forceinline__ float lse_of(float l2) { return l2 == -__builtin_inff() ? __builtin_inff() : l2; }
+
+// ------------------------------------------------------------------------------------------------ many rows
+
+template <typename IO_, int DP_> struct Shape {
+    typedef IO_ IO;
+    static constexpr int DP = DP_, KT = 64, kWaves = 4, kRows = 32 * kWaves;
+    static constexpr uint32_t kTile = kTileBytes<DP, KT>;
+    static constexpr size_t kLds = 4 * (size_t)kTile; // K and V, two of each
+};
+
+template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(const Args a)
+{
+    constexpr int DP = SH::DP, KT = SH::KT;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
+
+    const int32_t item = work_item(a);
+    if (item >= a.work)
+        return;
+    const int32_t per_head = a.row_tiles * a.splits;
+    const int32_t bh = item / per_head, rest = item - bh * per_head;
+    const int32_t row_tile = rest / a.splits, split = rest - row_tile * a.splits;
+    const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
+    const uint32_t row0 = (uint32_t)row_tile * SH::kRows + (uint32_t)wave * 32u, row = row0 + col;
+    const bool works = (int64_t)row0 < a.rows; // (a wavefront without rows loads for the others)
+    Rows<typename SH::IO, DP, KT> rows;
+    rows.load(a, b, kvh, row, h);
+    rows.clear();
+
+    const int32_t count = keys_of(a, b), tiles = (count + KT - 1) / KT;
+    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
+    t1 = t1 < tiles ? t1 : tiles;
+    const TileLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
+    const RowOperand<DP> k_operand(lane);
+    const ColumnOperand<DP> v_operand(lane);
+    const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
+    ValidKeys valid(a, b, count);
+    // (each part of the loop is in the code once, the first tile's loads too)
+    arrived(rows.q);
+    uint32_t at = SH::kTile;
+    uint64_t word = 0;
+#pragma unroll 1
+    for (int32_t t = t0 - 1; t < t1; ++t) {
+        const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0;
+        if (t >= t0) {
+            wait_loads<0>();
+            barrier(); // all wavefronts' loads of this tile are there, and all are done with the tile before
+        }
+        if (t + 1 < t1) {
+            const bool whole = next == ~(uint64_t)0 && a.dim == DP;
+            const uint32_t to = lds0 + (at ^ SH::kTile);
+            k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
+            v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + 2 * SH::kTile);
+        }
+        if (t >= t0 && works)
+            rows.take(k_operand.moved(lds0 + at), v_operand.moved(lds0 + at + 2 * SH::kTile), word, a.c, h);
+        at ^= SH::kTile;
+        word = next;
+    }
+    if ((int64_t)row >= a.rows)
+        return;
+
+    const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum, l2 = log2_sum(rows.top, sum, a.c);
+    const bool wide = a.splits > 1;
+    const int64_t line = ((int64_t)split * a.batch * a.kv_heads + bh) * a.rows + row;
+    char *const out = wide ? reinterpret_cast<char *>(a.partial + line * a.dim) : out_row(a, b, kvh, row);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+        store_channels<typename SH::IO>(rows.acc[d], d, inv, a, out, wide, h);
+    if (h == 0) {
+        if (wide)
+            a.partial[(int64_t)a.splits * a.batch * a.kv_heads * a.rows * a.dim + line] = l2;
+        else if (a.lse)
+            a.lse[line] = lse_of(l2);
+    }
+}
+
+// A row's parts p of `parts`, each the mean over its own keys, by the share of the sum that each has: eight channels of it, rounded to `out`.
+// values(p), stats(p): a part's channels and log2 of its sum
+template <typename IO, typename Values, typename Stats>
+__device__ __forceinline__ float join_parts(int32_t parts, Values &&values, Stats &&stats, char *out)
+{
+    float most = -__builtin_inff();
+#pragma unroll 8
+    for (int32_t p = 0; p < parts; ++p)
+        most = fmaxf(most, stats(p));
+    const float less = most == -__builtin_inff() ? 0.0f : most;
+    float total = 0.0f, o[8] = {};
+#pragma unroll 8
+    for (int32_t p = 0; p < parts; ++p) {
+        // (a part without a valid key has a share of 0 and a row of zeros)
+        const float share = __builtin_amdgcn_exp2f(stats(p) - less);
+        total += share;
+        const f32x4 *const from = reinterpret_cast<const f32x4 *>(values(p));
+        const f32x4 x = from[0], y = from[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            o[j] += share * x[j];
+            o[4 + j] += share * y[j];
+        }
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = Matrix<IO>::two(o[2 * j] * inv, o[2 * j + 1] * inv);
+    *reinterpret_cast<u32x4 *>(out) = w;
+    return total == 0.0f ? __builtin_inff() : most + __builtin_amdgcn_logf(total);
+}
+
+// out of the splits' rows: dim / 8 lanes a row
 template <typename IO> __global__ __launch_bounds__(256) void join_kernel(const Args a)
 {
     const int64_t all = (int64_t)a.batch * a.kv_heads * a.rows;
@@ -314,37 +279,282 @@ template <typename IO> __global__ __launch_bounds__(256) void join_kernel(const 
     if (line >= all)
         return;
     const float *const stats = a.partial + (int64_t)a.splits * all * a.dim;
-    float most = -__builtin_inff();
-    for (int32_t s = 0; s < a.splits; ++s)
-        most = fmaxf(most, stats[s * all + line]);
-    float total = 0.0f, o[8] = {};
-    for (int32_t s = 0; s < a.splits; ++s) {
-        const float l2 = stats[s * all + line];
-        if (l2 == -__builtin_inff())
-            continue; // no valid key in this split
-        const float share = __builtin_amdgcn_exp2f(l2 - most);
-        total += share;
-        const f32x4 *const from = reinterpret_cast<const f32x4 *>(a.partial + (s * all + line) * a.dim + 8u * piece);
-        const f32x4 x = from[0], y = from[1];
+    const int64_t bh = line / a.rows;
+    const int32_t b = (int32_t)(bh / a.kv_heads), kvh = (int32_t)(bh - (int64_t)b * a.kv_heads);
+    const float lse = join_parts<IO>(
+        a.splits, [&](int32_t p) { return a.partial + (p * all + line) * a.dim + 8u * piece; }, [&](int32_t p) { return stats[p * all + line]; },
+        out_row(a, b, kvh, (uint32_t)(line - bh * a.rows)) + 16u * piece);
+    if (a.lse && piece == 0)
+        a.lse[line] = lse;
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+
+// The keys of all key heads one behind the other, in groups of 128, are dealt out evenly to the workers: worker w of W has groups
+// w G / W .. (w + 1) G / W, G all of them; where a worker's run ends inside a key head, the next one's begins.  So all have the same to
+// read, whatever the batch entries' lengths are.  A worker's part of key head bh is in slot bh + w of the workspace (no two are
+// in the same: from one part to the next, bh or w rises).
+constexpr int kGroup = 128, kWorkers = 256;
+
+// (Everything in 32 bits: the host lets no more than 2^30 groups come here.)
+struct Deal {
+    int32_t total, workers; // G, and W: as many as the host asked for, but none without a group
+    int32_t quotient, rest; // of G by W
+    // batch entry b, its keys, the groups of one of its key heads, and the group that its first one begins with
+    int32_t b, count, groups, begin;
+    int32_t mine, up_to; // of entry `lane`, where 64 are all: its keys; the groups up to and with it, of one key head each
+
+    __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + kGroup - 1) / kGroup; }
+
+    // keys of entry first + lane (0 behind the last), and the running sum of the groups
+    __device__ __forceinline__ static void scan(const Args &a, int32_t first, int32_t &keys, int32_t &sum)
+    {
+        const int32_t lane = (int32_t)threadIdx.x & 63, entry = first + lane;
+        keys = entry < a.batch ? keys_of(a, entry) : 0;
+        sum = groups_of(keys);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            o[j] += share * x[j];
-            o[4 + j] += share * y[j];
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t o = __shfl_up(sum, d);
+            sum += lane >= d ? o : 0;
         }
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const int64_t bh = line / a.rows;
-    const uint32_t row = (uint32_t)(line - bh * a.rows);
-    const int32_t b = (int32_t)(bh / a.kv_heads), kvh = (int32_t)(bh - (int64_t)b * a.kv_heads);
-    const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
-    const int64_t first = (int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim;
-    u32x4 w;
+
+    __device__ __forceinline__ explicit Deal(const Args &a)
+    {
+        if (!a.lengths) {
+            total = groups_of((int32_t)a.keys) * a.kv_heads * a.batch;
+        } else {
+            scan(a, 0, mine, up_to);
+            total = __builtin_amdgcn_readlane(up_to, 63);
+            for (int32_t first = 64; first < a.batch; first += 64) {
+                int32_t keys, sum;
+                scan(a, first, keys, sum);
+                total += __builtin_amdgcn_readlane(sum, 63);
+            }
+            total *= a.kv_heads;
+        }
+        workers = total < a.splits ? total : a.splits;
+        quotient = workers ? total / workers : 0;
+        rest = total - quotient * workers;
+    }
+    // worker w's first group, w G / W
+    __device__ __forceinline__ int32_t first_of(int32_t w) const { return w * quotient + w * rest / workers; }
+    // the worker that has group x
+    __device__ __forceinline__ int32_t worker_of(int32_t x) const
+    {
+        int32_t w = (int32_t)((float)x * ((float)workers / (float)total));
+        w = w < workers ? w : workers - 1;
+        while (first_of(w) > x)
+            --w;
+        while (first_of(w + 1) <= x)
+            ++w;
+        return w;
+    }
+    // Sets b, count, groups and begin: to the entry that holds group x, or to `entry`.
+    __device__ __forceinline__ void find(const Args &a, int32_t x, int32_t entry = -1)
+    {
+        if (!a.lengths) {
+            count = (int32_t)a.keys;
+            groups = groups_of(count);
+            b = entry >= 0 ? entry : x / (groups * a.kv_heads);
+            begin = b * groups * a.kv_heads;
+            return;
+        }
+        int32_t before = 0; // groups of a key head each, of the entries in front
+        for (int32_t first = 0;; first += 64) {
+            if (first)
+                scan(a, first, mine, up_to);
+            const int32_t lane = (int32_t)threadIdx.x & 63;
+            const uint64_t found = __ballot(entry >= 0 ? first + lane == entry : (before + up_to) * a.kv_heads > x);
+            if (found || first + 64 >= a.batch) {
+                const int at = found ? __builtin_ctzll(found) : 63;
+                b = first + at;
+                count = __builtin_amdgcn_readlane(mine, at);
+                groups = groups_of(count);
+                begin = (before + __builtin_amdgcn_readlane(up_to, at) - groups) * a.kv_heads;
+                return;
+            }
+            before += __builtin_amdgcn_readlane(up_to, 63);
+        }
+    }
+};
+
+template <typename IO_, int DP_> struct TokenShape {
+    typedef IO_ IO;
+    static constexpr int DP = DP_, KT = 32, kWaves = 4;
+    static constexpr uint32_t kTile = kTileBytes<DP, KT>, kStage = 2 * kTile;
+    static constexpr size_t kLds = (size_t)kStage * 2 * kWaves;
+    static_assert(kGroup % (KT * kWaves) == 0, "");
+    static_assert(((DP + 4) * 32 * kWaves + 64 * kWaves) * sizeof(float) <= kLds, ""); // what the wavefronts join
+};
+
+// With a.splits workers; 0: each has one key head by itself and writes the output.
+template <class SH> __global__ __launch_bounds__(64 * SH::kWaves, 2) void tokens_kernel(const Args a)
+{
+    constexpr int DP = SH::DP, KT = SH::KT, ND = DP / 32;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t row = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
+    const bool shared = a.splits > 0;
+    const int32_t worker = (int32_t)blockIdx.x;
+
+    const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
+    const RowOperand<DP> k_operand(lane);
+    const ColumnOperand<DP> v_operand(lane);
+    const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage;
+    const float c = a.c;
+
+    // groups [g0, g1) of a key head; the part's place in `out`
+    auto part = [&](int32_t b, int32_t kvh, int32_t count, int32_t g0, int32_t g1) {
+        Rows<typename SH::IO, DP, KT> rows;
+        rows.load(a, b, kvh, row, h);
+        rows.clear();
+        constexpr int kTiles = kGroup / KT;
+        const int32_t tiles = (count + KT - 1) / KT, t0 = g0 * kTiles + wave, t1 = g1 * kTiles < tiles ? g1 * kTiles : tiles;
+        const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
+        ValidKeys valid(a, b, count);
+        auto word_of = [&](int32_t t) { return (valid.word(t / 2) >> (t % 2 * 32)) & rows.kAll; };
+        // Tiles t0, t0 + kWaves, .. of this wavefront's own, without a barrier: the loads of the next are in flight while one is computed with.
+        // (Each part of the loop is in the code once, the first tile's loads too.)
+        constexpr int kAhead = 2 * TileLoads<DP, KT, 1>::kMine, kStep = SH::kWaves;
+        arrived(rows.q);
+        uint32_t at = SH::kStage;
+        uint64_t word = 0;
+#pragma unroll 1
+        for (int32_t t = t0 - kStep; t < t1; t += kStep) {
+            const bool more = t + kStep < t1;
+            const uint64_t next = more ? word_of(t + kStep) : 0;
+            if (more) {
+                const bool whole = next == rows.kAll && a.dim == DP;
+                const uint32_t to = stages + (at ^ SH::kStage);
+                k_loads.issue(k_base + (uint64_t)(t + kStep) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
+                v_loads.issue(v_base + (uint64_t)(t + kStep) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + SH::kTile);
+            }
+            if (t >= t0) {
+                if (more)
+                    wait_loads<kAhead>();
+                else
+                    wait_loads<0>();
+                rows.take(k_operand.moved(stages + at), v_operand.moved(stages + at + SH::kTile), word, c, h);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
+            }
+            at ^= SH::kStage;
+            word = next;
+        }
+
+        // the wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order
+        constexpr int kPitch = DP + 4; // of a row's channels
+        float *const joined = reinterpret_cast<float *>(smem);         // [wave][32 rows][channel]
+        float *const stats = joined + SH::kWaves * 32 * kPitch;        // [wave][2][32 rows]
+        const float mine = halves_sum(rows.sum);
+        wait_loads<0>();
+        barrier();
+        if (h == 0) {
+            stats[wave * 64 + row] = rows.top;
+            stats[wave * 64 + 32 + row] = mine;
+        }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        w[j] = Matrix<IO>::two(o[2 * j] * inv, o[2 * j + 1] * inv);
-    *reinterpret_cast<u32x4 *>(a.out + (first + row_offset(row, (uint32_t)a.group, heads_dim, a.dim)) * 2 + 16u * piece) = w;
-    if (a.lse && piece == 0)
-        a.lse[line] = total == 0.0f ? __builtin_inff() : most + __builtin_amdgcn_logf(total);
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = rows.acc[d][4 * g + j];
+                *reinterpret_cast<f32x4 *>(joined + (wave * 32 + (int)row) * kPitch + 32 * d + 8 * g + 4 * (int)h) = o;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier();
+        float top = -__builtin_inff(), sum = 0.0f, by[SH::kWaves];
+#pragma unroll
+        for (int w = 0; w < SH::kWaves; ++w)
+            top = fmaxf(top, stats[w * 64 + row]);
+#pragma unroll
+        for (int w = 0; w < SH::kWaves; ++w) {
+            const float m = stats[w * 64 + row];
+            by[w] = m > -__builtin_inff() ? __builtin_amdgcn_exp2f((m - top) * c) : 0.0f;
+            sum += stats[w * 64 + 32 + row] * by[w];
+        }
+        const int64_t bh = (int64_t)b * a.kv_heads + kvh, slot = bh + worker;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum, l2 = log2_sum(top, sum, c);
+        if ((int64_t)row < a.rows) { // wavefront w writes channels 32 w .., 32 (w + kWaves) ..
+            char *const out = shared ? reinterpret_cast<char *>(a.partial + (slot * a.rows + row) * a.dim) : out_row(a, b, kvh, row);
+#pragma unroll 1
+            for (int d = wave; d < ND; d += SH::kWaves) {
+                f32x16 all;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 o = {};
+#pragma unroll
+                    for (int w = 0; w < SH::kWaves; ++w) {
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(joined + (w * 32 + (int)row) * kPitch + 32 * d + 8 * g + 4 * (int)h);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[j] += x[j] * by[w];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        all[4 * g + j] = o[j];
+                }
+                store_channels<typename SH::IO>(all, d, inv, a, out, shared, h);
+            }
+            if (h == 0 && wave == 0) {
+                if (shared)
+                    a.partial[((int64_t)a.batch * a.kv_heads + a.splits) * a.rows * a.dim + slot * a.rows + row] = l2;
+                else if (a.lse)
+                    a.lse[bh * a.rows + row] = lse_of(l2);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier(); // (the next part's tiles come where the joined rows were)
+    };
+
+    if (!shared) {
+        const int32_t b = worker / a.kv_heads, count = keys_of(a, b);
+        part(b, worker - b * a.kv_heads, count, 0, Deal::groups_of(count));
+        return;
+    }
+    Deal deal(a);
+    if (worker >= deal.workers)
+        return;
+    int32_t x = deal.first_of(worker);
+    const int32_t end = deal.first_of(worker + 1);
+    deal.find(a, x);
+    while (x < end) {
+        const int32_t kvh = (x - deal.begin) / deal.groups, g0 = x - deal.begin - kvh * deal.groups;
+        const int32_t g1 = end - x < deal.groups - g0 ? g0 + end - x : deal.groups;
+        part(deal.b, kvh, deal.count, g0, g1);
+        x += g1 - g0;
+        if (x < end && x == deal.begin + deal.groups * a.kv_heads) { // the next entry with keys
+            deal.begin = x;
+            do {
+                deal.count = keys_of(a, ++deal.b);
+                deal.groups = Deal::groups_of(deal.count);
+            } while (deal.groups == 0);
+        }
+    }
+}
+
+// out of the workers' parts: a workgroup for each key head, dim / 8 lanes a row
+template <typename IO> __global__ __launch_bounds__(256) void join_tokens_kernel(const Args a)
+{
+    const int32_t bh = (int32_t)blockIdx.x, b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
+    Deal deal(a);
+    deal.find(a, -1, b);
+    const int32_t x0 = deal.begin + kvh * deal.groups;
+    const int32_t w0 = deal.groups ? deal.worker_of(x0) : 0, parts = deal.groups ? deal.worker_of(x0 + deal.groups - 1) - w0 + 1 : 0;
+    const uint32_t pieces = (uint32_t)a.dim / 8u;
+    const float *const stats = a.partial + ((int64_t)a.batch * a.kv_heads + a.splits) * a.rows * a.dim;
+    for (uint32_t i = threadIdx.x; i < (uint32_t)a.rows * pieces; i += 256) {
+        const uint32_t row = i / pieces, piece = i - row * pieces;
+        auto line = [&](int32_t p) { return ((int64_t)bh + w0 + p) * a.rows + row; };
+        const float lse = join_parts<IO>(
+            parts, [&](int32_t p) { return a.partial + line(p) * a.dim + 8u * piece; }, [&](int32_t p) { return stats[line(p)]; },
+            out_row(a, b, kvh, row) + 16u * piece);
+        if (a.lse && piece == 0)
+            a.lse[(int64_t)bh * a.rows + row] = lse;
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -381,6 +591,13 @@ static bool fine_operand(const void *p, int64_t batch, int64_t token, int64_t he
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (batch | token | head) % 8 == 0;
 }
 
+bool in_offsets(int64_t token_stride, int64_t head_stride, int64_t heads)
+{
+    // 64 tokens and the heads of a group, in bytes, in 32 bits
+    const int64_t most = (int64_t)1 << 30;
+    return token_stride >= 0 && head_stride >= 0 && token_stride <= (most - 256) / 64 && head_stride <= (most - 256) / heads;
+}
+
 grkan_status_t fill(const grkan_attention_t *at, grkan_dtype_t io, Args *to)
 {
     if (!at)
@@ -396,9 +613,8 @@ grkan_status_t fill(const grkan_attention_t *at, grkan_dtype_t io, Args *to)
     const int64_t most = (int64_t)1 << 31;
     if (at->batch >= most || at->keys > most - 256 || at->queries >= most || at->queries * group >= most - 256 || at->batch * at->kv_heads >= most)
         return GRKAN_ERR_UNSUPPORTED;
-    for (const int64_t stride : {at->q_token_stride, at->k_token_stride, at->v_token_stride})
-        if (stride < 0 || stride > (most - 512) / 128)
-            return GRKAN_ERR_UNSUPPORTED;
+    if (!in_offsets(at->k_token_stride, 0, 1) || !in_offsets(at->v_token_stride, 0, 1))
+        return GRKAN_ERR_UNSUPPORTED;
     if ((at->queries > 0 && at->batch > 0 && !at->q) || (at->keys > 0 && at->batch > 0 && (!at->k || !at->v)))
         return GRKAN_ERR_NULL;
     if (!fine_operand(at->q, at->q_batch_stride, at->q_token_stride, at->q_head_stride) ||
@@ -429,34 +645,40 @@ grkan_status_t fill(const grkan_attention_t *at, grkan_dtype_t io, Args *to)
 
 typedef void (*Kernel)(Args);
 struct Variant {
-    Kernel kernel;
-    int rows, keys; // of a workgroup, of a tile
-    bool splits_keys;
+    Kernel kernel, join;
+    bool few; // rows
+    int rows, keys, threads; // of a workgroup: rows, keys at a time
     size_t lds;
 };
-template <class SH> static Variant variant() { return Variant{forward_kernel<SH>, SH::kRows, SH::KT, SH::KEYS, SH::kLds}; }
 
 template <typename IO, int DP> static Variant pick(int64_t rows)
 {
     if (rows <= 32)
-        return variant<Shape<IO, DP, true>>();
-    return variant<Shape<IO, DP, false>>();
+        return Variant{tokens_kernel<TokenShape<IO, DP>>, join_tokens_kernel<IO>, true, 32, kGroup, 64 * TokenShape<IO, DP>::kWaves, TokenShape<IO, DP>::kLds};
+    return Variant{forward_kernel<Shape<IO, DP>>, join_kernel<IO>, false, Shape<IO, DP>::kRows, Shape<IO, DP>::KT, 256, Shape<IO, DP>::kLds};
 }
 template <typename IO> static Variant pick(int32_t dim, int64_t rows)
 {
     return dim <= 32 ? pick<IO, 32>(rows) : dim <= 64 ? pick<IO, 64>(rows) : dim <= 96 ? pick<IO, 96>(rows) : pick<IO, 128>(rows);
 }
 
-// The kernel, its grid and how the keys are split.
+// The kernel, and how the keys are split.
 static Variant plan(Args &a, grkan_dtype_t io)
 {
     const Variant v = io == GRKAN_BF16 ? pick<__bf16>(a.dim, a.rows) : pick<_Float16>(a.dim, a.rows);
+    const int64_t heads = (int64_t)a.batch * a.kv_heads, tiles = (a.keys + v.keys - 1) / v.keys;
+    if (v.few) {
+        // A worker on every compute unit, with 256 keys at least; none where a key head each does as well: 1,024 of them, or all short
+        // (the second launch takes as long as 1,024 keys one behind the other).
+        const int64_t most = heads * tiles / 2;
+        a.splits = heads >= 1024 || tiles <= 8 || most <= heads || heads * tiles >= (int64_t)1 << 30 ? 0 : (int32_t)(most < kWorkers ? most : kWorkers);
+        return v;
+    }
     a.row_tiles = (int32_t)((a.rows + v.rows - 1) / v.rows);
-    const int64_t base = (int64_t)a.batch * a.kv_heads * a.row_tiles, tiles = (a.keys + v.keys - 1) / v.keys;
-    // as many as give each compute unit two workgroups, each with four tiles for a wavefront at least
-    const int64_t most = tiles / (v.splits_keys ? 16 : 4);
+    // as many as give each compute unit two workgroups, each with four tiles at least
+    const int64_t base = heads * a.row_tiles;
     int64_t splits = base > 0 && base < 384 ? 512 / base : 1;
-    splits = splits < most ? splits : most;
+    splits = splits < tiles / 4 ? splits : tiles / 4;
     splits = splits > 1 ? splits : 1;
     a.tiles_per_split = (int32_t)((tiles + splits - 1) / splits);
     if (a.tiles_per_split < 1)
@@ -467,9 +689,12 @@ static Variant plan(Args &a, grkan_dtype_t io)
     return v;
 }
 
-static size_t forward_bytes(const Args &a)
+// of the parts, where there are any
+static size_t forward_bytes(const Args &a, const Variant &v)
 {
-    return a.splits > 1 ? (size_t)a.splits * (size_t)a.batch * (size_t)a.kv_heads * (size_t)a.rows * (size_t)(a.dim + 1) * sizeof(float) : 0;
+    const size_t heads = (size_t)a.batch * (size_t)a.kv_heads;
+    const size_t parts = v.few ? (a.splits > 0 ? heads + (size_t)a.splits : 0) : a.splits > 1 ? heads * (size_t)a.splits : 0;
+    return parts * (size_t)a.rows * (size_t)(a.dim + 1) * sizeof(float);
 }
 
 size_t backward_bytes(const Args &a); // grkan_attention_bwd.hip
@@ -493,8 +718,7 @@ extern "C" size_t grkan_attention_workspace_bytes(const grkan_attention_t *at, i
         return 0;
     if (backward)
         return attention::backward_bytes(a);
-    attention::plan(a, GRKAN_BF16);
-    return attention::forward_bytes(a);
+    return attention::forward_bytes(a, attention::plan(a, GRKAN_BF16));
 }
 
 extern "C" grkan_status_t grkan_attention_fwd(const grkan_attention_t *at, void *out, float *lse, void *workspace, size_t workspace_bytes,
@@ -511,32 +735,24 @@ extern "C" grkan_status_t grkan_attention_fwd(const grkan_attention_t *at, void 
     if (reinterpret_cast<uintptr_t>(out) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
         return GRKAN_ERR_ALIGN;
     const attention::Variant v = attention::plan(a, io);
-    const size_t need = attention::forward_bytes(a);
+    const size_t need = attention::forward_bytes(a, v);
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return GRKAN_ERR_WORKSPACE;
-    const int64_t work = (int64_t)a.batch * a.kv_heads * a.row_tiles * a.splits;
-    if (work > INT32_MAX / 2)
+    const int64_t heads = (int64_t)a.batch * a.kv_heads, work = v.few ? (a.splits > 0 ? a.splits : heads) : heads * a.row_tiles * a.splits;
+    const int64_t join = !need ? 0 : v.few ? heads : (heads * a.rows * (a.dim / 8) + 255) / 256;
+    if (work > INT32_MAX / 2 || join > INT32_MAX)
         return GRKAN_ERR_UNSUPPORTED;
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.partial = static_cast<float *>(workspace);
-    const unsigned grid = attention::spread(a, work, (int64_t)a.row_tiles * a.splits);
+    const unsigned grid = v.few ? (unsigned)work : attention::spread(a, work, (int64_t)a.row_tiles * a.splits);
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3(grid), dim3(256), args, v.lds, stream) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3(grid), dim3((unsigned)v.threads), args, v.lds, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
-    if (a.splits > 1) {
-        const int64_t lanes = (int64_t)a.batch * a.kv_heads * a.rows * (a.dim / 8), blocks = (lanes + 255) / 256;
-        if (blocks > INT32_MAX)
-            return GRKAN_ERR_UNSUPPORTED;
-        if (io == GRKAN_BF16)
-            attention::join_kernel<__bf16><<<dim3((unsigned)blocks), 256, 0, stream>>>(a);
-        else
-            attention::join_kernel<_Float16><<<dim3((unsigned)blocks), 256, 0, stream>>>(a);
-        if (hipGetLastError() != hipSuccess)
-            return GRKAN_ERR_LAUNCH;
-    }
+    if (join > 0 && hipLaunchKernel(reinterpret_cast<const void *>(v.join), dim3((unsigned)join), dim3(256), args, 0, stream) != hipSuccess)
+        return GRKAN_ERR_LAUNCH;
     return GRKAN_OK;
 }

@@ -18,34 +18,45 @@ namespace attention {
 
 constexpr int kRowTile = 64;
 
-// Tiles of ROWS rows of the list: as TileLoads, but a row's place is its query's and its head's.
+// Tiles of ROWS rows of the list: as TileLoads, but a row's place is its query's and its head's.  Where a tile holds whole queries, the
+// places in it are the same in every tile; elsewhere they are computed anew for each.
 template <int DP, int ROWS, int WAVES> struct RowLoads {
-    static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = (kLoads + WAVES - 1) / WAVES;
+    static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = kLoads / WAVES;
     static_assert(kLoads % WAVES == 0, "");
-    uint32_t row[kMine], chunk[kMine]; // chunk: its bytes, or ~0: no such channels
+    uint32_t offset[kMine], row[kMine], chunk[kMine]; // chunk: its bytes, or ~0: no such channels
     int first;
+    bool even;
+    uint64_t base, advance; // (even) of a tile
 
-    __device__ __forceinline__ RowLoads(int wave, int lane, int32_t dim) : first(wave)
+    __device__ __forceinline__ RowLoads(int wave, int lane, const Operand &o, uint64_t base_, bool even_, const Args &a)
+        : first(wave), even(even_), base(base_)
     {
+        const uint32_t group = (uint32_t)a.group;
+        advance = even ? (uint64_t)(ROWS / group) * (uint64_t)o.token : 0;
 #pragma unroll
         for (int q = 0; q < kMine; ++q) {
             const uint32_t e = (uint32_t)(first + q * WAVES) * 64u + (uint32_t)lane;
             row[q] = e / kChunks;
             const uint32_t c = (e % kChunks) ^ swizzle<DP>(row[q]);
-            chunk[q] = c * 8u < (uint32_t)dim ? c * 16u : ~0u;
+            chunk[q] = c * 8u < (uint32_t)a.dim ? c * 16u : ~0u;
+            offset[q] = (uint32_t)row_offset(row[q], group, o.token, o.head) + c * 16u;
         }
     }
-    __device__ __forceinline__ void issue(const Operand &o, uint64_t base, uint32_t row0, const Args &a, uint32_t lds_at) const
+    __device__ __forceinline__ void issue(const Operand &o, int32_t t, const Args &a, uint32_t lds_at) const
     {
-        const bool whole = a.group == 1 && a.dim == DP && (int64_t)row0 + ROWS <= a.rows;
+        const uint32_t row0 = (uint32_t)t * ROWS;
+        const uint64_t tile = base + (uint64_t)(uint32_t)t * advance;
+        const bool whole = even && a.dim == DP && (int64_t)row0 + ROWS <= a.rows;
 #pragma unroll
         for (int q = 0; q < kMine; ++q) {
             const uint32_t to = lds_at + (uint32_t)(first + q * WAVES) * kBlock<DP>;
             if (whole) {
-                load_to_lds(uniform_u64(base + (uint64_t)row0 * (uint64_t)o.token), row[q] * (uint32_t)o.token + chunk[q], to);
+                load_to_lds(uniform_u64(tile), offset[q], to);
             } else {
-                const bool there = (int64_t)row0 + row[q] < a.rows && chunk[q] != ~0u;
-                const uint64_t at = base + (uint64_t)row_offset(row0 + row[q], (uint32_t)a.group, o.token, o.head) + chunk[q];
+                uint32_t r = row[q];
+                keep_in_loop(r);
+                const bool there = (int64_t)row0 + r < a.rows && chunk[q] != ~0u;
+                const uint64_t at = even ? tile + offset[q] : base + (uint64_t)row_offset(row0 + r, (uint32_t)a.group, o.token, o.head) + chunk[q];
                 load_to_lds_at(there ? at : reinterpret_cast<uint64_t>(kZeros), to);
             }
         }
@@ -186,11 +197,12 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
         dv[d] = f32x16{};
     }
 
-    const RowLoads<DP, ROWS, SH::kWaves> loads(wave, lane, a.dim);
     const RowOperand<DP> row_operand(lane);
     const ColumnOperand<DP> column_operand(lane);
     const uint64_t q_base = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head);
     const uint64_t d_base = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
+    const RowLoads<DP, ROWS, SH::kWaves> q_loads(wave, lane, a.q, q_base, a.even_q && ROWS % a.group == 0, a),
+        d_loads(wave, lane, a.dout, d_base, a.even_dout && ROWS % a.group == 0, a);
     const int32_t tiles = (int32_t)((a.rows + ROWS - 1) / ROWS);
     int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
     t1 = t1 < tiles ? t1 : tiles;
@@ -201,8 +213,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
 
     auto issue = [&](int32_t t, uint32_t stage) {
         const uint32_t row0 = (uint32_t)t * ROWS;
-        loads.issue(a.q, q_base, row0, a, stage);
-        loads.issue(a.dout, d_base, row0, a, stage + SH::kRowsTile);
+        q_loads.issue(a.q, t, a, stage);
+        d_loads.issue(a.dout, t, a, stage + SH::kRowsTile);
         // (the rows' statistics are padded to whole tiles of 64)
         if (wave < 2 && lane < ROWS) {
             const float *const from = (wave ? a.row_delta : a.row_lse) + (int64_t)bh * a.padded + row0;
@@ -211,31 +223,33 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     };
 
     const uint32_t stages = lds0 + (SH::V_LDS ? 2 * SH::kKeysTile : 0u);
-    uint32_t at = 0;
-    if (t0 < t1) {
-        if constexpr (SH::V_LDS) {
+    uint32_t at = SH::kKeyStage;
+    if constexpr (SH::V_LDS) {
+        if (t0 < t1) {
             const TileLoads<DP, 64, SH::kWaves> v_loads(wave, lane, a.v.token, a.dim);
-#pragma unroll
+#pragma unroll 1
             for (int part = 0; part < 2; ++part) {
                 const int64_t first = (int64_t)key_tile * SH::kOwn + 64 * part, mine = first + lane;
                 const bool there = mine < count && (!a.mask || a.mask[(int64_t)b * a.mask_batch + mine * a.mask_key] != 0);
-                v_loads.issue(v_base + (uint64_t)first * (uint64_t)a.v.token, __ballot(there), false, lds0 + (uint32_t)part * SH::kKeysTile);
+                v_loads.issue(v_base + (uint64_t)first * (uint64_t)a.v.token, a.v.token, __ballot(there), false, lds0 + (uint32_t)part * SH::kKeysTile);
             }
         }
-        issue(t0, stages);
     }
     arrived(k);
     if constexpr (!SH::V_LDS)
         arrived(v);
     const auto v_rows = row_operand.moved(lds0 + (uint32_t)wave * row_at<DP>(32u));
-    for (int32_t t = t0; t < t1; ++t) {
-        wait_loads<0>();
-        barrier();
+#pragma unroll 1
+    for (int32_t t = t0 - 1; t < t1; ++t) {
+        if (t >= t0) {
+            wait_loads<0>();
+            barrier();
+        }
         if (t + 1 < t1)
             issue(t + 1, stages + (at ^ SH::kKeyStage));
         const uint32_t stage = stages + at;
         at ^= SH::kKeyStage;
-        if (!works)
+        if (t < t0 || !works)
             continue;
         const auto rows = row_operand.moved(stage);
         const auto columns = column_operand.moved(stage);
@@ -371,36 +385,34 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
     const ColumnOperand<DP> column_operand(lane);
     const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
     ValidKeys valid(a, b, count);
-    auto issue = [&](int32_t t, uint64_t word, uint32_t stage) {
-        const bool whole = word == ~(uint64_t)0 && a.dim == DP;
-        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, word, whole, stage);
-        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, word, whole, stage + SH::kKeysTile);
-    };
-
-    uint32_t at = 0;
-    uint64_t word = 0;
-    if (t0 < t1) {
-        word = valid.word(t0);
-        issue(t0, word, lds0);
-    }
     arrived(q);
     arrived(o);
     arrived(lse);
     arrived(delta);
-    for (int32_t t = t0; t < t1; ++t) {
+    uint32_t at = SH::kRowStage;
+    uint64_t word = 0;
+#pragma unroll 1
+    for (int32_t t = t0 - 1; t < t1; ++t) {
         const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0, now = word;
-        wait_loads<0>();
-        barrier();
-        if (t + 1 < t1)
-            issue(t + 1, next, lds0 + (at ^ SH::kRowStage));
+        if (t >= t0) {
+            wait_loads<0>();
+            barrier();
+        }
+        if (t + 1 < t1) {
+            const bool whole = next == ~(uint64_t)0 && a.dim == DP;
+            const uint32_t to = lds0 + (at ^ SH::kRowStage);
+            k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
+            v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + SH::kKeysTile);
+        }
         const auto rows = row_operand.moved(lds0 + at);
         const auto columns = column_operand.moved(lds0 + at);
         at ^= SH::kRowStage;
         word = next;
-        if (!works)
+        if (t < t0 || !works)
             continue;
 #pragma unroll
         for (int kb = 0; kb < KT / 32; ++kb) {
+            fence_schedule(); // (the two halves mixed take more registers than there are)
             f32x16 s = {}, d = {};
 #pragma unroll
             for (int st = 0; st < NS; ++st)
@@ -497,7 +509,7 @@ template <typename IO> static BackVariant pick(int32_t dim)
     if (dim <= 32)
         return back_variant<BackShape<IO, 32, 64, false, 2>>();
     if (dim <= 64)
-        return back_variant<BackShape<IO, 64, 64, false, 2>>();
+        return back_variant<BackShape<IO, 64, 32, true, 3>>();
     if (dim <= 96)
         return back_variant<BackShape<IO, 96, 64, false, 2>>();
     return back_variant<BackShape<IO, 128, 32, true, 2>>();
@@ -607,8 +619,6 @@ extern "C" grkan_status_t grkan_attention_bwd(const grkan_attention_t *at, const
     if ((address(out) | address(dout) | address(dq) | address(dk) | address(dv)) % 16 != 0 || address(lse) % 4 != 0 ||
         (dout_batch_stride | dout_token_stride | dout_head_stride) % 8 != 0)
         return GRKAN_ERR_ALIGN;
-    if (dout_token_stride < 0 || dout_token_stride > (((int64_t)1 << 31) - 512) / 128)
-        return GRKAN_ERR_UNSUPPORTED;
     attention::BackPlan p = attention::back_plan(a, io);
     const size_t need = (p.stats + p.partial) * sizeof(float);
     if (need && (!workspace || workspace_bytes < need || address(workspace) % 16 != 0))
@@ -616,6 +626,8 @@ extern "C" grkan_status_t grkan_attention_bwd(const grkan_attention_t *at, const
     const size_t padded = (size_t)a.batch * (size_t)a.kv_heads * (size_t)p.keys.padded;
     for (attention::Args *to : {&p.keys, &p.queries}) {
         to->dout = attention::Operand{address(dout), dout_batch_stride * 2, dout_token_stride * 2, dout_head_stride * 2};
+        to->even_q = attention::in_offsets(at->q_token_stride, at->q_head_stride, a.group);
+        to->even_dout = attention::in_offsets(dout_token_stride, dout_head_stride, a.group);
         to->lse = const_cast<float *>(lse);
         to->row_lse = static_cast<float *>(workspace);
         to->row_delta = to->row_lse + padded;

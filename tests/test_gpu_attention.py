@@ -363,8 +363,8 @@ def test_guarded_outputs():
         k, v = k.contiguous(), v.contiguous()
         a = binding.Attention.of(q, k, v, lengths, None, shape[-1] ** -0.5)
         size = {"out": q.numel(), "dq": q.numel(), "dk": k.numel(), "dv": v.numel()}
-        held = {n: torch.full((c + 64,), 7.0, dtype=torch.bfloat16, device="cuda:0") for n, c in size.items()}
-        lse = torch.full((q.shape[0] * q.shape[1] * q.shape[2] + 64,), 7.0, device="cuda:0")
+        held = {n: torch.full((c + 64,), math.nan, dtype=torch.bfloat16, device="cuda:0") for n, c in size.items()}
+        lse = torch.full((q.shape[0] * q.shape[1] * q.shape[2] + 64,), math.nan, device="cuda:0")
         stream = torch.cuda.current_stream().cuda_stream
         for back in (0, 1):
             need = lib.grkan_attention_workspace_bytes(ctypes.byref(a), back)
@@ -380,8 +380,8 @@ def test_guarded_outputs():
             torch.cuda.synchronize()
             assert (ws[need:] == 7).all()
         for n, c in size.items():
-            assert (held[n][c:] == 7).all() and not (held[n][:c] == 7).any()
-        assert (lse[-64:] == 7).all()
+            assert held[n][c:].isnan().all() and not held[n][:c].isnan().any()
+        assert lse[-64:].isnan().all() and not lse[:-64].isnan().any()
 
 
 def test_on_another_stream_and_in_a_graph():
