@@ -123,13 +123,13 @@ __device__ __forceinline__ void arrived(float &r) { asm volatile("" : "+v"(r)); 
 
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
-// Tiles of ROWS tokens (keys) by WAVES wavefronts, a KB at a time.  Loops, not rows of loads: a kernel that is over in microseconds waits for
-// its own code, which comes to every compute unit with the launch (the first keys of 1,024, 128 channels, were under way after 4 us of a wavefront's
-// life with the loads written out).
+// Tiles of ROWS tokens (keys) by WAVES wavefronts, a KB at a time.  Where one wavefront loads a tile by itself, in a loop: that kernel is over in
+// microseconds, and waits for its own code, which comes to every compute unit with the launch (its first loads are out after 2.2 us of a wavefront's
+// life; with eight loads written out 4.7).  Where four do, written out: 220 us in the place of 242 for 2 x 4096 x 4001 of 16 heads of 128.
 template <int DP, int ROWS, int WAVES> struct TileLoads {
     static constexpr int kChunks = DP / 8, kLoads = ROWS * kChunks / 64, kMine = kLoads / WAVES;
     // loads kEach WAVES apart differ by whole tokens alone: the pieces of a row are permuted alike in both
-    static constexpr int kEach = DP == 96 ? 3 : 1, kTurns = kMine / kEach;
+    static constexpr int kEach = WAVES > 1 ? kMine : DP == 96 ? 3 : 1, kTurns = kMine / kEach;
     static constexpr uint32_t kTokens = (uint32_t)(kEach * WAVES * 64 / kChunks); // between them
     static_assert(kMine * WAVES == kLoads && kTurns * kEach == kMine && kEach * WAVES * 64 % kChunks == 0, "");
 
@@ -164,8 +164,10 @@ template <int DP, int ROWS, int WAVES> struct TileLoads {
                 }
                 to += WAVES * kBlock<DP>;
             }
-            base += step;
-            word >>= kTokens;
+            if constexpr (kTurns > 1) {
+                base += step;
+                word >>= kTokens;
+            }
         }
     }
 };
@@ -284,6 +286,26 @@ struct ValidKeys {
         return below & (((uint64_t)hi << 32) | lo);
     }
 };
+
+// What is added to the scores of a tile's keys, in LDS: 0, or minus infinity where a key is not valid.  The matrix instructions start from it, so that
+// a mask takes no vector instruction for each score (a bit test, a comparison, a selection and a wait).
+__device__ __forceinline__ void write_cover(uint32_t at, uint64_t word, int lane)
+{
+    *(__attribute__((address_space(3))) float *)(uintptr_t)(at + 4u * (uint32_t)lane) = (word >> lane) & 1u ? 0.0f : -__builtin_inff();
+}
+// of 32 keys, as the scores lie in the lanes
+__device__ __forceinline__ f32x16 read_cover(uint32_t at, int block, uint32_t h)
+{
+    f32x16 r;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 c = __builtin_bit_cast(f32x4, lds_read16(at + (32u * block + 8u * g + 4u * h) * 4u));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            r[4 * g + j] = c[j];
+    }
+    return r;
+}
 
 // Workgroups go round-robin over the 8 XCDs.  Runs of work items go to one XCD, whose L2 fetches their keys and values once; runs
 // are short enough (host: spread) that every XCD has several of them, of long and of short batch entries.

@@ -51,27 +51,29 @@ template <typename IO, int DP, int KT> struct Rows {
         sum = 0.0f;
     }
 
-    // One tile of keys.  word: which of them are valid; c: of the scores, in powers of 2
-    __device__ __forceinline__ void take(const Addresses<NS> &k_from, const Addresses<ND> &v_from, uint64_t word, float c, uint32_t h)
+    // One tile of keys.  word: which of them are valid, and cover what write_cover left of that, where it is not all; c: of the scores, in powers
+    // of 2
+    __device__ __forceinline__ void take(const Addresses<NS> &k_from, const Addresses<ND> &v_from, uint64_t word, uint32_t cover, float c, uint32_t h)
     {
         f32x16 s[KB];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-            s[kb] = f32x16{};
-#pragma unroll
-        for (int st = 0; st < NS; ++st)
+        if (word != kAll) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                s[kb] = MM::multiply(RowOperand<DP>::read(k_from, kb, st), q[st], s[kb]);
-        if (word != kAll) { // keys that are not valid: minus infinity
-            const uint64_t mine = word >> (4u * h);
+                s[kb] = read_cover(cover, kb, h);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const uint32_t bits = (uint32_t)(mine >> (32 * kb));
+            for (int st = 0; st < NS; ++st)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[kb][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[kb][i] : -__builtin_inff();
-            }
+                for (int kb = 0; kb < KB; ++kb)
+                    s[kb] = MM::multiply(RowOperand<DP>::read(k_from, kb, st), q[st], s[kb]);
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                s[kb] = f32x16{};
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    s[kb] = MM::multiply(RowOperand<DP>::read(k_from, kb, st), q[st], s[kb]);
         }
         float most = s[0][0];
 #pragma unroll
@@ -82,15 +84,13 @@ template <typename IO, int DP, int KT> struct Rows {
         most = halves_max(most);
         if (__ballot(most > top + fminf(8.0f / c, 1e38f)) != 0) {
             const float next = fmaxf(top, most);
-            if (__ballot(top > -__builtin_inff()) != 0) { // (else there is nothing to scale yet)
-                const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - next) * c) : 1.0f;
-                sum *= by;
+            const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - next) * c) : 1.0f;
+            sum *= by;
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[d][i] *= by;
-            }
+                for (int i = 0; i < 16; ++i)
+                    acc[d][i] *= by;
             top = next;
         }
         const float less = top > -__builtin_inff() ? top * c : 0.0f;
@@ -164,7 +164,8 @@ template <typename IO_, int DP_> struct Shape {
     typedef IO_ IO;
     static constexpr int DP = DP_, KT = 64, kWaves = 4, kRows = 32 * kWaves;
     static constexpr uint32_t kTile = kTileBytes<DP, KT>;
-    static constexpr size_t kLds = 4 * (size_t)kTile; // K and V, two of each
+    static constexpr uint32_t kCover = 4 * kTile; // behind K and V, two of each
+    static constexpr size_t kLds = kCover + 2 * KT * 4;
 };
 
 template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(const Args a)
@@ -183,7 +184,6 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
     const int32_t row_tile = rest / a.splits, split = rest - row_tile * a.splits;
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
     const uint32_t row0 = (uint32_t)row_tile * SH::kRows + (uint32_t)wave * 32u, row = row0 + col;
-    const bool works = (int64_t)row0 < a.rows; // (a wavefront without rows loads for the others)
     Rows<typename SH::IO, DP, KT> rows;
     rows.load(a, b, kvh, row, h);
     rows.clear();
@@ -196,28 +196,40 @@ template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(con
     const ColumnOperand<DP> v_operand(lane);
     const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
     ValidKeys valid(a, b, count);
-    // (each part of the loop is in the code once, the first tile's loads too)
+    auto issue = [&](int32_t t, uint64_t word, uint32_t at) {
+        const bool all = word == ~(uint64_t)0, whole = all && a.dim == DP;
+        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, word, whole, lds0 + at);
+        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, word, whole, lds0 + at + 2 * SH::kTile);
+        if (!all && wave == 0)
+            write_cover(lds0 + SH::kCover + (at ? KT * 4u : 0u), word, lane);
+    };
     arrived(rows.q);
-    uint32_t at = SH::kTile;
-    uint64_t word = 0;
-#pragma unroll 1
-    for (int32_t t = t0 - 1; t < t1; ++t) {
-        const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0;
-        if (t >= t0) {
+    // (a wavefront without rows loads for the others; two loops, as one with a condition in it would copy the sums in every pass)
+    auto walk = [&](auto works) {
+        uint32_t at = 0;
+        uint64_t word = 0;
+        if (t0 < t1) {
+            word = valid.word(t0);
+            issue(t0, word, 0);
+        }
+        for (int32_t t = t0; t < t1; ++t) {
+            const uint64_t next = t + 1 < t1 ? valid.word(t + 1) : 0;
             wait_loads<0>();
             barrier(); // all wavefronts' loads of this tile are there, and all are done with the tile before
+            if (t + 1 < t1)
+                issue(t + 1, next, at ^ SH::kTile);
+            if constexpr (decltype(works)::value)
+                rows.take(k_operand.moved(lds0 + at), v_operand.moved(lds0 + at + 2 * SH::kTile), word,
+                          lds0 + SH::kCover + (at ? KT * 4u : 0u), a.c, h);
+            at ^= SH::kTile;
+            word = next;
         }
-        if (t + 1 < t1) {
-            const bool whole = next == ~(uint64_t)0 && a.dim == DP;
-            const uint32_t to = lds0 + (at ^ SH::kTile);
-            k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
-            v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + 2 * SH::kTile);
-        }
-        if (t >= t0 && works)
-            rows.take(k_operand.moved(lds0 + at), v_operand.moved(lds0 + at + 2 * SH::kTile), word, a.c, h);
-        at ^= SH::kTile;
-        word = next;
+    };
+    if ((int64_t)row0 >= a.rows) {
+        walk(std::false_type{});
+        return;
     }
+    walk(std::true_type{});
     if ((int64_t)row >= a.rows)
         return;
 
@@ -383,13 +395,14 @@ template <typename IO_, int DP_> struct TokenShape {
     typedef IO_ IO;
     static constexpr int DP = DP_, KT = 32, kWaves = 4;
     static constexpr uint32_t kTile = kTileBytes<DP, KT>, kStage = 2 * kTile;
-    static constexpr size_t kLds = (size_t)kStage * 2 * kWaves;
+    static constexpr uint32_t kCover = kStage * 2 * kWaves; // behind the tiles, two of each wavefront
+    static constexpr size_t kLds = kCover + 2 * KT * 4 * kWaves;
     static_assert(kGroup % (KT * kWaves) == 0, "");
     static_assert(((DP + 4) * 32 * kWaves + 64 * kWaves) * sizeof(float) <= kLds, ""); // what the wavefronts join
 };
 
 // With a.splits workers; 0: each has one key head by itself and writes the output.
-template <class SH> __global__ __launch_bounds__(64 * SH::kWaves, 2) void tokens_kernel(const Args a)
+template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void tokens_kernel(const Args a)
 {
     constexpr int DP = SH::DP, KT = SH::KT, ND = DP / 32;
     extern __shared__ __align__(256) char smem[];
@@ -402,7 +415,7 @@ template <class SH> __global__ __launch_bounds__(64 * SH::kWaves, 2) void tokens
     const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
     const RowOperand<DP> k_operand(lane);
     const ColumnOperand<DP> v_operand(lane);
-    const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage;
+    const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage, covers = lds0 + SH::kCover + (uint32_t)wave * 2u * KT * 4u;
     const float c = a.c;
 
     // groups [g0, g1) of a key head; the part's place in `out`
@@ -430,13 +443,15 @@ template <class SH> __global__ __launch_bounds__(64 * SH::kWaves, 2) void tokens
                 const uint32_t to = stages + (at ^ SH::kStage);
                 k_loads.issue(k_base + (uint64_t)(t + kStep) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
                 v_loads.issue(v_base + (uint64_t)(t + kStep) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + SH::kTile);
+                if (next != rows.kAll && lane < KT)
+                    write_cover(covers + (at ? 0u : KT * 4u), next, lane);
             }
             if (t >= t0) {
                 if (more)
                     wait_loads<kAhead>();
                 else
                     wait_loads<0>();
-                rows.take(k_operand.moved(stages + at), v_operand.moved(stages + at + SH::kTile), word, c, h);
+                rows.take(k_operand.moved(stages + at), v_operand.moved(stages + at + SH::kTile), word, covers + (at ? KT * 4u : 0u), c, h);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
             }
             at ^= SH::kStage;

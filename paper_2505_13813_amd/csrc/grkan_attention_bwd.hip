@@ -153,8 +153,8 @@ template <typename IO_, int DP_, int ROWS_, bool V_LDS_, int PER_> struct BackSh
     static constexpr int kOwn = 32 * kWaves; // keys or rows of a workgroup
     // keys' kernel: Q, dO, lse, delta of ROWS rows; queries' kernel: K, V of 64 keys
     static constexpr uint32_t kRowsTile = kTileBytes<DP, ROWS>, kKeyStage = 2 * kRowsTile + 2 * ROWS * 4u;
-    static constexpr uint32_t kKeysTile = kTileBytes<DP, 64>, kRowStage = 2 * kKeysTile;
-    static constexpr size_t kKeyLds = 2 * (size_t)kKeyStage + (V_LDS ? 2 * (size_t)kKeysTile : 0), kRowLds = 2 * (size_t)kRowStage;
+    static constexpr uint32_t kKeysTile = kTileBytes<DP, 64>, kRowStage = 2 * kKeysTile, kCover = 2 * kRowStage; // and behind two of those what covers keys
+    static constexpr size_t kKeyLds = 2 * (size_t)kKeyStage + (V_LDS ? 2 * (size_t)kKeysTile : 0), kRowLds = kCover + 2 * 64 * 4;
 };
 
 // dK and dV of 32 keys a wavefront.
@@ -403,7 +403,10 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
             const uint32_t to = lds0 + (at ^ SH::kRowStage);
             k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, next, whole, to);
             v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, next, whole, to + SH::kKeysTile);
+            if (next != ~(uint64_t)0 && wave == 0)
+                write_cover(lds0 + SH::kCover + (at ? 0u : KT * 4u), next, lane);
         }
+        const uint32_t cover = lds0 + SH::kCover + (at ? KT * 4u : 0u);
         const auto rows = row_operand.moved(lds0 + at);
         const auto columns = column_operand.moved(lds0 + at);
         at ^= SH::kRowStage;
@@ -413,22 +416,24 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
 #pragma unroll
         for (int kb = 0; kb < KT / 32; ++kb) {
             fence_schedule(); // (the two halves mixed take more registers than there are)
-            f32x16 s = {}, d = {};
+            f32x16 s, d = {};
+            if (now != ~(uint64_t)0) {
+                s = read_cover(cover, kb, h);
 #pragma unroll
-            for (int st = 0; st < NS; ++st)
-                s = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], s);
+                for (int st = 0; st < NS; ++st)
+                    s = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], s);
+            } else {
+                s = f32x16{};
+#pragma unroll
+                for (int st = 0; st < NS; ++st)
+                    s = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], s);
+            }
 #pragma unroll
             for (int st = 0; st < NS; ++st)
                 d = MM::multiply(RowOperand<DP>::read(rows, kb, st, SH::kKeysTile), o[st], d);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * fmaf(d[i], up, -delta);
-            if (now != ~(uint64_t)0) {
-                const uint32_t bits = (uint32_t)((now >> (32 * kb)) >> (4u * h));
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[i] : 0.0f;
-            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 u32x4 w;
