@@ -144,8 +144,12 @@ template <class SH, typename W, bool RESIDUAL, bool EIGHT> __global__ __launch_b
         }
         sum = row_sum<SH>(sum, shared, slot);
         const float s = rsqrtf(sum / (float)a.D + a.eps);
-        float q = 0.0f, pre = 1.0f;
+        // To 8 bits: y / scale = 448 h w / max |h w| does not depend on s, and of 16-bit numbers the product h w is exact; the factor's
+        // remainder is kept too, so that nothing but the last step rounds.  (h in units of s rounded to a power of 2, so that its products
+        // stay in range.)
+        float unit = 1.0f, factor = 0.0f, remainder = 0.0f;
         if constexpr (EIGHT) {
+            unit = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) & 0x7f800000u);
             // magnitudes as whole numbers: a NaN is the largest
             uint32_t most = 0;
 #pragma unroll
@@ -155,18 +159,22 @@ template <class SH, typename W, bool RESIDUAL, bool EIGHT> __global__ __launch_b
                     widen<IO, VEC>(xs[i], f);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const uint32_t b = __builtin_bit_cast(uint32_t, f[e] * s * w[i][e]) & 0x7fffffffu;
+                        const uint32_t b = __builtin_bit_cast(uint32_t, f[e] * unit * w[i][e]) & 0x7fffffffu;
                         most = b > most ? b : most;
                     }
                 }
             }
-            const float amax = __builtin_bit_cast(float, row_max<SH>(most, shared, slot));
+            const float largest = __builtin_bit_cast(float, row_max<SH>(most, shared, slot)), amax = largest * (s / unit);
             const float scale = amax < __builtin_inff() ? amax / kMost8 : __builtin_nanf("");
-            // (448 / amax would overflow for the smallest)
-            pre = amax < 0x1p-80f ? 0x1p100f : 1.0f;
-            q = amax > 0.0f || amax != amax ? kMost8 / (amax * pre) : 0.0f;
-            if (amax == __builtin_inff())
-                q = __builtin_nanf("");
+            if (scale != scale) {
+                factor = scale;
+            } else if (largest > 0.0f) {
+                if (largest < 0x1p-80f) // (448 / largest would overflow for the smallest)
+                    unit *= 0x1p100f;
+                const float m = largest < 0x1p-80f ? largest * 0x1p100f : largest;
+                factor = kMost8 / m;
+                remainder = fmaf(-factor, m, kMost8) / m;
+            }
             if (threadIdx.x % (64 * SH::WAVES) == 0)
                 a.scale[row] = scale;
         }
@@ -180,13 +188,16 @@ template <class SH, typename W, bool RESIDUAL, bool EIGHT> __global__ __launch_b
                 widen<IO, VEC>(xs[i], f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    f[e] = f[e] * s * w[i][e];
+                    f[e] = EIGHT ? f[e] * unit * w[i][e] : f[e] * s * w[i][e];
                 if constexpr (EIGHT) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        f[e] = fmaf(f[e], factor, f[e] * remainder);
                     typedef uint8_t bytes_t __attribute__((ext_vector_type(VEC), aligned(1)));
                     uint8_t b[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; e += 2) {
-                        const uint32_t two = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[e] * pre * q, e + 1 < VEC ? f[e + 1] * pre * q : 0.0f, 0, false);
+                        const uint32_t two = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[e], e + 1 < VEC ? f[e + 1] : 0.0f, 0, false);
                         b[e] = (uint8_t)two;
                         if (e + 1 < VEC)
                             b[e + 1] = (uint8_t)(two >> 8);
@@ -328,7 +339,7 @@ template <typename W> __global__ __launch_bounds__(1024) void columns_kernel(con
     const int32_t c = (int32_t)blockIdx.x * 16 + lane;
     float v = 0.0f;
     if (c < D) {
-#pragma unroll 8
+#pragma unroll 16
         for (int32_t r = slice; r < count; r += 64)
             v += partial[(int64_t)r * D + c];
     }
@@ -389,10 +400,14 @@ static Variant choose(int32_t D, grkan_dtype_t io, grkan_dtype_t wt, int which, 
     return wt == GRKAN_F32 ? choose<_Float16, float>(D, which, residual) : choose<_Float16, _Float16>(D, which, residual);
 }
 
-// Workgroups: each keeps its weights (and the weights' gradient) for all the rows it visits.
-static int64_t grid_of(const Variant &v, int64_t rows, bool backward)
+// Workgroups.  Forward: nearly one for each row or four (of a row below a KB two or more, which the start of a workgroup is worth); us with
+// 2,048 / 16,384 of them: 25,216 x 768 in bfloat16 with a residual 32.7 / 28.0, 16,384 x 4096 103 / 87, 40,000 x 768 in float32 88 / 82;
+// 60,000 x 192 20.6 / 24.6.  Backward: each keeps its columns' sums for all the rows it visits, and writes them; 512 / 1,024 / 1,536 of them:
+// 25,216 x 768 34 / 27 / 34, 16,384 x 4096 116 / 87 / 104, 8,192 x 8192 115 / 124 / 134.
+static int64_t grid_of(const Variant &v, int64_t rows, int32_t D, grkan_dtype_t io, bool backward)
 {
-    const int64_t most = backward ? (v.threads > 256 ? 256 : 1024) : (v.threads > 256 ? 512 : 2048);
+    const int64_t bytes = (int64_t)D * (io == GRKAN_F32 ? 4 : 2);
+    const int64_t most = backward ? (v.threads > 256 ? 256 : bytes > 8192 ? 512 : 1024) : bytes < 1024 ? 2048 : 16384;
     const int64_t need = (rows + v.rows - 1) / v.rows;
     return need < most ? need : most;
 }
@@ -443,7 +458,7 @@ extern "C" grkan_status_t grkan_rms_norm_fwd(const void *x, const void *residual
     a.D = D;
     a.eps = eps;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)norm::grid_of(v, rows, false)), dim3((unsigned)v.threads), args,
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)norm::grid_of(v, rows, D, io, false)), dim3((unsigned)v.threads), args,
                         0, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     return GRKAN_OK;
@@ -454,7 +469,7 @@ extern "C" size_t grkan_rms_norm_bwd_workspace_bytes(int64_t rows, int32_t D, gr
     if (norm::check(rows, D, io, GRKAN_F32) != GRKAN_OK)
         return 0;
     const norm::Variant v = norm::choose(D, io, GRKAN_F32, 2, false);
-    const int64_t grid = norm::grid_of(v, rows, true);
+    const int64_t grid = norm::grid_of(v, rows, D, io, true);
     return (size_t)(grid > 0 ? grid : 1) * (size_t)D * sizeof(float);
 }
 
@@ -472,7 +487,7 @@ extern "C" grkan_status_t grkan_rms_norm_bwd(const void *h, const void *dy, cons
         norm::misaligned(weight, weight_dtype) || norm::misaligned(dweight, weight_dtype))
         return GRKAN_ERR_ALIGN;
     const norm::Variant v = norm::choose(D, io, weight_dtype, 2, dh != nullptr);
-    const int64_t grid = norm::grid_of(v, rows, true);
+    const int64_t grid = norm::grid_of(v, rows, D, io, true);
     if (!workspace || workspace_bytes < (size_t)grid * (size_t)D * sizeof(float) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
         return GRKAN_ERR_WORKSPACE;
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);

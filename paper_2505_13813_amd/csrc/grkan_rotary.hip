@@ -24,6 +24,7 @@ struct Tensor {
     int64_t tokens, all_tokens; // of a batch entry, of all
     int64_t batch_stride, token_stride, head_stride, position_batch_stride, position_token_stride;
     int32_t heads, positions_dtype, per_block; // per_block: tokens of a workgroup
+    uint32_t by_heads; // 2^32 / heads, rounded up (below: by chunks): quotients of small numbers by the high half of a product; 0: of one
 };
 
 struct Args {
@@ -32,6 +33,7 @@ struct Args {
     const double *frequencies;
     const int32_t *axis;
     int32_t pairs, axes, dim;
+    uint32_t chunks, by_chunks; // items of 2 VP channels a head
     float sign; // of the angle
 };
 
@@ -65,42 +67,61 @@ template <typename IO, int VP, bool INTERLEAVED> __global__ __launch_bounds__(kT
     }
     __syncthreads();
 
-    const uint32_t chunks = (uint32_t)a.dim / (2 * VP), rotated = pairs / VP, heads = (uint32_t)t.heads;
-    const uint32_t items = tokens * heads * chunks;
+    // Items in turns of kAtOnce a lane, whose loads are all out before the first is used.
+    constexpr int kAtOnce = 2;
+    const uint32_t heads = (uint32_t)t.heads, rotated = pairs / VP, items = tokens * heads * a.chunks;
     IO *const out = reinterpret_cast<IO *>(t.out) + token0 * t.heads * a.dim;
-    for (uint32_t i = threadIdx.x; i < items; i += kThreads) {
-        const uint32_t line = i / chunks, c = i - line * chunks, k = line / heads, h = line - k * heads;
-        const int64_t token = token0 + k, b = token / t.tokens;
-        const IO *const x = reinterpret_cast<const IO *>(t.x) + b * t.batch_stride + (token - b * t.tokens) * t.token_stride + h * t.head_stride;
-        // where the item's two vectors are
-        const bool turns = c < rotated;
-        const uint32_t from = turns && !INTERLEAVED ? c * VP : c * 2 * VP, to = turns && !INTERLEAVED ? pairs + from : from + VP;
-        float f[2 * VP], lo[VP], hi[VP];
-        widen<IO, VP>(load<IO, VP>(x + from), lo);
-        widen<IO, VP>(load<IO, VP>(x + to), hi);
+    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += kThreads * kAtOnce) {
+        typename Raw<IO, VP>::type first[kAtOnce], second[kAtOnce];
+        uint32_t from[kAtOnce], to[kAtOnce], angle[kAtOnce]; // the vectors' channels; the first of the item's angles, or ~0: copied
+        uint32_t line[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-            f[e] = lo[e];
-            f[VP + e] = hi[e];
+        for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t i = i0 + (uint32_t)u * kThreads;
+            if (u > 0 && i >= items)
+                continue;
+            line[u] = a.by_chunks ? __umulhi(i, a.by_chunks) : i;
+            const uint32_t c = i - line[u] * a.chunks, k = t.by_heads ? __umulhi(line[u], t.by_heads) : line[u], h = line[u] - k * heads;
+            const int64_t token = token0 + k, b = t.tokens == t.all_tokens ? 0 : token / t.tokens;
+            const IO *const x = reinterpret_cast<const IO *>(t.x) + b * t.batch_stride + (token - b * t.tokens) * t.token_stride + h * t.head_stride;
+            const bool turns = c < rotated;
+            from[u] = turns && !INTERLEAVED ? c * VP : c * 2 * VP;
+            to[u] = turns && !INTERLEAVED ? pairs + from[u] : from[u] + VP;
+            angle[u] = turns ? k * pairs + c * VP : ~0u;
+            first[u] = load<IO, VP>(x + from[u]);
+            second[u] = load<IO, VP>(x + to[u]);
         }
-        if (turns) {
-            const float *const cs = turned + 2 * (k * pairs + c * VP);
 #pragma unroll
-            for (int j = 0; j < VP; ++j) {
-                const int ia = INTERLEAVED ? 2 * j : j, ib = INTERLEAVED ? 2 * j + 1 : VP + j;
-                const float p = f[ia], q = f[ib], co = cs[2 * j], si = cs[2 * j + 1];
-                f[ia] = p * co - q * si;
-                f[ib] = p * si + q * co;
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (u > 0 && i0 + (uint32_t)u * kThreads >= items)
+                continue;
+            float f[2 * VP], lo[VP], hi[VP];
+            widen<IO, VP>(first[u], lo);
+            widen<IO, VP>(second[u], hi);
+#pragma unroll
+            for (int e = 0; e < VP; ++e) {
+                f[e] = lo[e];
+                f[VP + e] = hi[e];
             }
-        }
+            if (angle[u] != ~0u) {
+                const float *const cs = turned + 2 * angle[u];
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-            lo[e] = f[e];
-            hi[e] = f[VP + e];
+                for (int j = 0; j < VP; ++j) {
+                    const int ia = INTERLEAVED ? 2 * j : j, ib = INTERLEAVED ? 2 * j + 1 : VP + j;
+                    const float p = f[ia], q = f[ib], co = cs[2 * j], si = cs[2 * j + 1];
+                    f[ia] = p * co - q * si;
+                    f[ib] = p * si + q * co;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < VP; ++e) {
+                lo[e] = f[e];
+                hi[e] = f[VP + e];
+            }
+            IO *const o = out + (int64_t)line[u] * a.dim;
+            store<IO, VP>(o + from[u], narrow<IO, VP>(lo));
+            store<IO, VP>(o + to[u], narrow<IO, VP>(hi));
         }
-        IO *const o = out + (int64_t)line * a.dim;
-        store<IO, VP>(o + from, narrow<IO, VP>(lo));
-        store<IO, VP>(o + to, narrow<IO, VP>(hi));
     }
 }
 
@@ -168,12 +189,15 @@ extern "C" grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t co
         if ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.out)) % element != 0 ||
             reinterpret_cast<uintptr_t>(t.positions) % (t.positions_dtype == GRKAN_POSITIONS_I64 ? 8 : 4) != 0)
             return GRKAN_ERR_ALIGN;
+        // n / d = high half of n ceil(2^32 / d) where n d < 2^32
+        const uint64_t chunks = (uint64_t)(dim / (2 * vp)), one = (uint64_t)t.heads * chunks;
         // Four items a lane where there are tokens enough for two workgroups on every compute unit
-        const int64_t items = (int64_t)t.heads * (dim / (2 * vp));
-        int64_t per = 4 * rotary::kThreads / items;
+        int64_t per = 4 * rotary::kThreads / (int64_t)one;
         per = per < all / 512 ? per : all / 512;
         per = per < rotary::kMostAngles / (pairs > 0 ? pairs : 1) ? per : rotary::kMostAngles / (pairs > 0 ? pairs : 1);
         per = per > 1 ? per : 1;
+        if ((uint64_t)per * one * (chunks > (uint64_t)t.heads ? chunks : (uint64_t)t.heads) >> 32)
+            return GRKAN_ERR_UNSUPPORTED;
         rotary::Tensor &to = a.t[i];
         to.x = static_cast<const char *>(t.x);
         to.out = static_cast<char *>(t.out);
@@ -188,6 +212,7 @@ extern "C" grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t co
         to.heads = t.heads;
         to.positions_dtype = t.positions_dtype;
         to.per_block = (int32_t)per;
+        to.by_heads = t.heads > 1 ? (uint32_t)((((uint64_t)1 << 32) + (uint64_t)t.heads - 1) / (uint64_t)t.heads) : 0;
         most_tokens = per > most_tokens ? (int32_t)per : most_tokens;
         blocks += (all + per - 1) / per;
         if (i == 0)
@@ -202,6 +227,8 @@ extern "C" grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t co
     a.pairs = pairs;
     a.axes = axes;
     a.dim = dim;
+    a.chunks = (uint32_t)(dim / (2 * vp));
+    a.by_chunks = a.chunks > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.chunks - 1) / a.chunks) : 0;
     a.sign = inverse ? -1.0f : 1.0f;
     void *args[] = {&a};
     if (hipLaunchKernel(reinterpret_cast<const void *>(rotary::choose(io, vp, interleaved != 0)), dim3((unsigned)blocks), dim3(rotary::kThreads),
