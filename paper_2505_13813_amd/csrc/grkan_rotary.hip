@@ -191,8 +191,10 @@ extern "C" grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t co
             return GRKAN_ERR_ALIGN;
         // n / d = high half of n ceil(2^32 / d) where n d < 2^32
         const uint64_t chunks = (uint64_t)(dim / (2 * vp)), one = (uint64_t)t.heads * chunks;
-        // Four items a lane where there are tokens enough for two workgroups on every compute unit
-        int64_t per = 4 * rotary::kThreads / (int64_t)one;
+        // Two items a lane, all out at once, where there are tokens enough for two workgroups on
+        // every compute unit (us with 1 / 2 / 4 / 8 items: 128 images of 196 tokens, 12 + 12 heads
+        // of 64, 29 / 28 / 31 / 34; two videos of 14,720, 16 + 4 heads of 128, 57 / 55 / 60 / 68).
+        int64_t per = 2 * rotary::kThreads / (int64_t)one;
         per = per < all / 512 ? per : all / 512;
         per = per < rotary::kMostAngles / (pairs > 0 ? pairs : 1) ? per : rotary::kMostAngles / (pairs > 0 ? pairs : 1);
         per = per > 1 ? per : 1;
