@@ -46,8 +46,9 @@ struct Args {
     float *row_lse, *row_delta, *row_most;
     int32_t padded;         // rows with the padding
     int32_t even_q, even_dout; // places of a tile's rows in q and dout in 32 bits
-    int32_t splits, tiles_per_split;
+    int32_t splits, tiles_per_split; // (splits: the workers, where the groups of keys are dealt out; the most parts, in the keys' gradients)
     int32_t row_tiles, key_tiles; // workgroups of a key head over rows, over keys
+    int32_t at_once;       // workgroups of the keys' gradients that the device holds
     int32_t work, run; // work items, and how many of them in a row one XCD gets
 };
 
@@ -306,6 +307,93 @@ __device__ __forceinline__ f32x16 read_cover(uint32_t at, int block, uint32_t h)
     }
     return r;
 }
+
+// The keys of all key heads one behind the other, in groups of 128 that do not reach over a head's end: who deals them out evenly to its
+// workers gives all the same to do, whatever the batch entries' lengths are.
+// (Everything in 32 bits: the host lets no more than 2^30 groups come here.)
+constexpr int kGroup = 128;
+struct Deal {
+    int32_t total, workers; // G, and W: as many as the host asked for, but none without a group
+    int32_t quotient, rest; // of G by W
+    // batch entry b, its keys, the groups of one of its key heads, and the group that its first one begins with
+    int32_t b, count, groups, begin;
+    int32_t mine, up_to; // of entry `lane`: its keys; the groups up to and with it, of one key head each
+
+    __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + kGroup - 1) / kGroup; }
+
+    // keys of entry first + lane (0 behind the last), and the running sum of the groups
+    __device__ __forceinline__ static void scan(const Args &a, int32_t first, int32_t &keys, int32_t &sum)
+    {
+        const int32_t lane = (int32_t)threadIdx.x & 63, entry = first + lane;
+        keys = entry < a.batch ? keys_of(a, entry) : 0;
+        sum = groups_of(keys);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t o = __shfl_up(sum, d);
+            sum += lane >= d ? o : 0;
+        }
+    }
+
+    __device__ __forceinline__ explicit Deal(const Args &a)
+    {
+        if (!a.lengths) {
+            total = groups_of((int32_t)a.keys) * a.kv_heads * a.batch;
+        } else {
+            scan(a, 0, mine, up_to);
+            total = __builtin_amdgcn_readlane(up_to, 63);
+            for (int32_t first = 64; first < a.batch; first += 64) {
+                int32_t keys, sum;
+                scan(a, first, keys, sum);
+                total += __builtin_amdgcn_readlane(sum, 63);
+            }
+            total *= a.kv_heads;
+        }
+        workers = total < a.splits ? total : a.splits;
+        quotient = workers ? total / workers : 0;
+        rest = total - quotient * workers;
+    }
+    // worker w's first group, w G / W
+    __device__ __forceinline__ int32_t first_of(int32_t w) const { return w * quotient + w * rest / workers; }
+    // the worker that has group x
+    __device__ __forceinline__ int32_t worker_of(int32_t x) const
+    {
+        int32_t w = (int32_t)((float)x * ((float)workers / (float)total));
+        w = w < workers ? w : workers - 1;
+        while (first_of(w) > x)
+            --w;
+        while (first_of(w + 1) <= x)
+            ++w;
+        return w;
+    }
+    // Sets b, count, groups and begin: to the entry that holds group x, or to `entry`.
+    __device__ __forceinline__ void find(const Args &a, int32_t x, int32_t entry = -1)
+    {
+        if (!a.lengths) {
+            count = (int32_t)a.keys;
+            groups = groups_of(count);
+            b = entry >= 0 ? entry : x / (groups * a.kv_heads);
+            begin = b * groups * a.kv_heads;
+            return;
+        }
+        int32_t before = 0; // groups of a key head each, of the entries in front
+        for (int32_t first = 0;; first += 64) {
+            int32_t keys = mine, sum = up_to;
+            if (first)
+                scan(a, first, keys, sum);
+            const int32_t lane = (int32_t)threadIdx.x & 63;
+            const uint64_t found = __ballot(entry >= 0 ? first + lane == entry : (before + sum) * a.kv_heads > x);
+            if (found || first + 64 >= a.batch) {
+                const int at = found ? __builtin_ctzll(found) : 63;
+                b = first + at;
+                count = __builtin_amdgcn_readlane(keys, at);
+                groups = groups_of(count);
+                begin = (before + __builtin_amdgcn_readlane(sum, at) - groups) * a.kv_heads;
+                return;
+            }
+            before += __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+};
 
 // Workgroups go round-robin over the 8 XCDs.  Runs of work items go to one XCD, whose L2 fetches their keys and values once; runs
 // are short enough (host: spread) that every XCD has several of them, of long and of short batch entries.

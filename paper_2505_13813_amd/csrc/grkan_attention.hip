@@ -302,94 +302,9 @@ template <typename IO> __global__ __launch_bounds__(256) void join_kernel(const 
 
 // ------------------------------------------------------------------------------------------------ few rows
 
-// The keys of all key heads one behind the other, in groups of 128, are dealt out evenly to the workers: worker w of W has groups
-// w G / W .. (w + 1) G / W, G all of them; where a worker's run ends inside a key head, the next one's begins.  So all have the same to
-// read, whatever the batch entries' lengths are.  A worker's part of key head bh is in slot bh + w of the workspace (no two are
+// Worker w of W has groups w G / W .. (w + 1) G / W, G all of them (Deal): all have the same to read.  A worker's part of key head bh is in slot bh + w of the workspace (no two are
 // in the same: from one part to the next, bh or w rises).
-constexpr int kGroup = 128, kWorkers = 256;
-
-// (Everything in 32 bits: the host lets no more than 2^30 groups come here.)
-struct Deal {
-    int32_t total, workers; // G, and W: as many as the host asked for, but none without a group
-    int32_t quotient, rest; // of G by W
-    // batch entry b, its keys, the groups of one of its key heads, and the group that its first one begins with
-    int32_t b, count, groups, begin;
-    int32_t mine, up_to; // of entry `lane`, where 64 are all: its keys; the groups up to and with it, of one key head each
-
-    __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + kGroup - 1) / kGroup; }
-
-    // keys of entry first + lane (0 behind the last), and the running sum of the groups
-    __device__ __forceinline__ static void scan(const Args &a, int32_t first, int32_t &keys, int32_t &sum)
-    {
-        const int32_t lane = (int32_t)threadIdx.x & 63, entry = first + lane;
-        keys = entry < a.batch ? keys_of(a, entry) : 0;
-        sum = groups_of(keys);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t o = __shfl_up(sum, d);
-            sum += lane >= d ? o : 0;
-        }
-    }
-
-    __device__ __forceinline__ explicit Deal(const Args &a)
-    {
-        if (!a.lengths) {
-            total = groups_of((int32_t)a.keys) * a.kv_heads * a.batch;
-        } else {
-            scan(a, 0, mine, up_to);
-            total = __builtin_amdgcn_readlane(up_to, 63);
-            for (int32_t first = 64; first < a.batch; first += 64) {
-                int32_t keys, sum;
-                scan(a, first, keys, sum);
-                total += __builtin_amdgcn_readlane(sum, 63);
-            }
-            total *= a.kv_heads;
-        }
-        workers = total < a.splits ? total : a.splits;
-        quotient = workers ? total / workers : 0;
-        rest = total - quotient * workers;
-    }
-    // worker w's first group, w G / W
-    __device__ __forceinline__ int32_t first_of(int32_t w) const { return w * quotient + w * rest / workers; }
-    // the worker that has group x
-    __device__ __forceinline__ int32_t worker_of(int32_t x) const
-    {
-        int32_t w = (int32_t)((float)x * ((float)workers / (float)total));
-        w = w < workers ? w : workers - 1;
-        while (first_of(w) > x)
-            --w;
-        while (first_of(w + 1) <= x)
-            ++w;
-        return w;
-    }
-    // Sets b, count, groups and begin: to the entry that holds group x, or to `entry`.
-    __device__ __forceinline__ void find(const Args &a, int32_t x, int32_t entry = -1)
-    {
-        if (!a.lengths) {
-            count = (int32_t)a.keys;
-            groups = groups_of(count);
-            b = entry >= 0 ? entry : x / (groups * a.kv_heads);
-            begin = b * groups * a.kv_heads;
-            return;
-        }
-        int32_t before = 0; // groups of a key head each, of the entries in front
-        for (int32_t first = 0;; first += 64) {
-            if (first)
-                scan(a, first, mine, up_to);
-            const int32_t lane = (int32_t)threadIdx.x & 63;
-            const uint64_t found = __ballot(entry >= 0 ? first + lane == entry : (before + up_to) * a.kv_heads > x);
-            if (found || first + 64 >= a.batch) {
-                const int at = found ? __builtin_ctzll(found) : 63;
-                b = first + at;
-                count = __builtin_amdgcn_readlane(mine, at);
-                groups = groups_of(count);
-                begin = (before + __builtin_amdgcn_readlane(up_to, at) - groups) * a.kv_heads;
-                return;
-            }
-            before += __builtin_amdgcn_readlane(up_to, 63);
-        }
-    }
-};
+constexpr int kWorkers = 256;
 
 template <typename IO_, int DP_> struct TokenShape {
     typedef IO_ IO;

@@ -151,13 +151,34 @@ template <typename IO_, int DP_, int ROWS_, bool V_LDS_, int PER_> struct BackSh
     static constexpr int DP = DP_, ROWS = ROWS_, PER = PER_, kWaves = 4;
     static constexpr bool V_LDS = V_LDS_;
     static constexpr int kOwn = 32 * kWaves; // keys or rows of a workgroup
+    static_assert(kOwn == kGroup, "");
     // keys' kernel: Q, dO, lse, delta of ROWS rows; queries' kernel: K, V of 64 keys
     static constexpr uint32_t kRowsTile = kTileBytes<DP, ROWS>, kKeyStage = 2 * kRowsTile + 2 * ROWS * 4u;
     static constexpr uint32_t kKeysTile = kTileBytes<DP, 64>, kRowStage = 2 * kKeysTile, kCover = 2 * kRowStage; // and behind two of those what covers keys
     static constexpr size_t kKeyLds = 2 * (size_t)kKeyStage + (V_LDS ? 2 * (size_t)kKeysTile : 0), kRowLds = kCover + 2 * 64 * 4;
 };
 
-// dK and dV of 32 keys a wavefront.
+// How many workgroups share the walk over the rows of each of `groups` groups of keys, `most` in all: what makes their last round on the device a full
+// one, counted in tiles of rows.  A part costs three to begin with, and where there are several, their way to the workspace and back is that of about
+// 32 for 512 parts.  (188 groups of 128 keys, 16,384 rows of 128 channels, 512 workgroups at once: 535 us with 2 parts, 465 with 5.)
+__host__ __device__ __forceinline__ int32_t parts_of(int64_t groups, int32_t tiles, int32_t at_once, int32_t most)
+{
+    int32_t best = 1;
+    int64_t least = INT64_MAX;
+    for (int32_t n = 1; n <= 8; ++n) {
+        const int64_t all = groups * n;
+        if (n > 1 && (all > most || 4 * n > tiles))
+            break;
+        const int64_t cost = (all + at_once - 1) / at_once * ((tiles + n - 1) / n + 3) + (n > 1 ? all / 16 : 0);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
+}
+
+// dK and dV of 32 keys a wavefront, of a group of 128 a workgroup, from all rows or, where there are few groups (a.splits), from a part of them.
 template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(const Args a)
 {
     using IO = typename SH::IO;
@@ -170,11 +191,32 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     const int32_t item = work_item(a);
     if (item >= a.work)
         return;
-    const int32_t per_head = a.key_tiles * a.splits;
-    const int32_t bh = item / per_head, rest = item - bh * per_head;
-    const int32_t key_tile = rest / a.splits, split = rest - key_tile * a.splits;
-    const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
-    const int32_t count = keys_of(a, b);
+    const int32_t tiles = (int32_t)((a.rows + ROWS - 1) / ROWS);
+    int32_t b, kvh, key_tile, count, t0 = 0, t1 = tiles;
+    bool whole = true;
+    if (a.splits) {
+        Deal deal(a);
+        const int32_t parts = parts_of(deal.total, tiles, a.at_once, a.splits), g = item / parts, per = (tiles + parts - 1) / parts;
+        if (g >= deal.total)
+            return;
+        deal.find(a, g);
+        b = deal.b;
+        count = deal.count;
+        kvh = (g - deal.begin) / deal.groups;
+        key_tile = g - deal.begin - kvh * deal.groups;
+        t0 = (item - g * parts) * per;
+        t1 = t0 + per < tiles ? t0 + per : tiles;
+        whole = parts == 1;
+    } else {
+        const int32_t bh = item / a.key_tiles;
+        key_tile = item - bh * a.key_tiles;
+        b = bh / a.kv_heads;
+        kvh = bh - b * a.kv_heads;
+        count = keys_of(a, b);
+        if ((int64_t)key_tile * SH::kOwn >= count) // no valid key in the workgroup: zeros
+            t1 = 0;
+    }
+    const int32_t bh = b * a.kv_heads + kvh;
     const int64_t key0 = (int64_t)key_tile * SH::kOwn + wave * 32, key = key0 + col; // this wavefront's and this lane's
 
     // ---- keys and values as second operands: lane l has key l mod 32, channels 16 s + 8 (l / 32) ..
@@ -203,11 +245,6 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     const uint64_t d_base = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
     const RowLoads<DP, ROWS, SH::kWaves> q_loads(wave, lane, a.q, q_base, a.even_q && ROWS % a.group == 0, a),
         d_loads(wave, lane, a.dout, d_base, a.even_dout && ROWS % a.group == 0, a);
-    const int32_t tiles = (int32_t)((a.rows + ROWS - 1) / ROWS);
-    int32_t t0 = split * a.tiles_per_split, t1 = t0 + a.tiles_per_split;
-    t1 = t1 < tiles ? t1 : tiles;
-    if ((int64_t)key_tile * SH::kOwn >= count) // no valid key in the workgroup: nothing to add
-        t1 = t0;
     const bool works = key0 < count; // (a wavefront without keys loads for the others)
     const float up = gradient_scale<IO>(a, bh), c = a.c;
 
@@ -305,7 +342,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     if (key >= a.keys)
         return;
     const float by = a.scale / up;
-    const int64_t line = ((int64_t)b * a.keys + key) * a.kv_heads + kvh, all = (int64_t)a.batch * a.keys * a.kv_heads;
+    const int64_t line = ((int64_t)b * a.keys + key) * a.kv_heads + kvh;
+    float *const to = a.partial + ((int64_t)item * 2 * kGroup + (wave * 32 + (int)col)) * a.dim;
 #pragma unroll
     for (int part = 0; part < ND; ++part)
 #pragma unroll
@@ -319,7 +357,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
                 x[j] = valid ? dk[part][4 * g + j] * by : 0.0f;
                 y[j] = valid ? dv[part][4 * g + j] : 0.0f;
             }
-            if (a.splits == 1) {
+            if (whole) {
                 u32x2 u, z;
                 u[0] = MM::two(x[0], x[1]);
                 u[1] = MM::two(x[2], x[3]);
@@ -328,11 +366,42 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
                 *reinterpret_cast<u32x2 *>(a.dk + (line * a.dim + channel) * 2) = u;
                 *reinterpret_cast<u32x2 *>(a.dv + (line * a.dim + channel) * 2) = z;
             } else {
-                float *const to = a.partial + ((int64_t)split * all + line) * a.dim + channel;
-                *reinterpret_cast<f32x4 *>(to) = x;
-                *reinterpret_cast<f32x4 *>(to + (int64_t)a.splits * all * a.dim) = y;
+                *reinterpret_cast<f32x4 *>(to + channel) = x;
+                *reinterpret_cast<f32x4 *>(to + kGroup * a.dim + channel) = y;
             }
         }
+}
+
+// The sum of the parts of a group of keys, and zeros for a group without keys: block (quarter, dK or dV, group, key head), four elements a lane and pass.
+template <typename IO> __global__ __launch_bounds__(256) void sum_keys_kernel(const Args a, int32_t row_tiles)
+{
+    const int32_t quarter = (int32_t)blockIdx.x & 3, which = (int32_t)blockIdx.x >> 2 & 1, item = (int32_t)blockIdx.x >> 3;
+    const int32_t bh = item / a.key_tiles, key_tile = item - bh * a.key_tiles;
+    const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
+    Deal deal(a);
+    deal.find(a, 0, b);
+    int32_t parts = 0;
+    if (key_tile < deal.groups) {
+        parts = parts_of(deal.total, row_tiles, a.at_once, a.splits);
+        if (parts == 1) // written as it should be
+            return;
+    }
+    const int64_t first = (int64_t)(deal.begin + kvh * deal.groups + key_tile) * parts;
+    const int32_t quads = a.dim / 4, keys = kGroup / 4, key0 = quarter * keys;
+    for (int32_t i = (int32_t)threadIdx.x; i < keys * quads; i += 256) {
+        const int32_t row = i / quads, key = key_tile * kGroup + key0 + row;
+        if (key >= a.keys)
+            break;
+        const float *const from = a.partial + ((first * 2 + which) * kGroup + key0) * a.dim + 4 * i;
+        f32x4 v = {};
+        for (int32_t n = 0; n < parts; ++n)
+            v += *reinterpret_cast<const f32x4 *>(from + (int64_t)n * 2 * kGroup * a.dim);
+        u32x2 o;
+        o[0] = Matrix<IO>::two(v[0], v[1]);
+        o[1] = Matrix<IO>::two(v[2], v[3]);
+        const int64_t line = ((int64_t)b * a.keys + key) * a.kv_heads + kvh;
+        *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + (line * a.dim + 4 * (i - row * quads)) * 2) = o;
+    }
 }
 
 // dQ of 32 rows a wavefront.
@@ -503,11 +572,12 @@ typedef void (*Kernel)(Args);
 struct BackVariant {
     Kernel keys, queries;
     int own, rows; // keys or rows of a workgroup; rows of a stage of the keys' kernel
+    int at_once;   // workgroups of the keys' kernel that the device holds
     size_t keys_lds, queries_lds;
 };
 template <class SH> static BackVariant back_variant()
 {
-    return BackVariant{keys_kernel<SH>, queries_kernel<SH>, SH::kOwn, SH::ROWS, SH::kKeyLds, SH::kRowLds};
+    return BackVariant{keys_kernel<SH>, queries_kernel<SH>, SH::kOwn, SH::ROWS, 256 * SH::PER, SH::kKeyLds, SH::kRowLds};
 }
 template <typename IO> static BackVariant pick(int32_t dim)
 {
@@ -549,11 +619,22 @@ static BackPlan back_plan(const Args &a, grkan_dtype_t io)
     p.keys.padded = p.queries.padded = padded;
     p.keys.key_tiles = (int32_t)((a.keys + p.v.own - 1) / p.v.own);
     p.queries.row_tiles = (int32_t)((a.rows + p.v.own - 1) / p.v.own);
-    split(heads * p.keys.key_tiles, (a.rows + p.v.rows - 1) / p.v.rows, p.keys);
+    // Groups of keys that do not fill the device: their walks are shared.  How many of the groups have keys, and so how many share one, the kernel
+    // knows, or the host where there are no lengths.
+    const int64_t groups = heads * p.keys.key_tiles;
+    const int32_t tiles = (int32_t)((a.rows + p.v.rows - 1) / p.v.rows), most = 2 * p.v.at_once;
+    p.keys.at_once = p.v.at_once;
+    p.keys.splits = 0;
+    if (groups > 0 && groups <= p.v.at_once && tiles >= 8) {
+        if (a.lengths)
+            p.keys.splits = 8 * groups < most ? (int32_t)(8 * groups) : most;
+        else if (const int32_t parts = parts_of(groups, tiles, p.v.at_once, most); parts > 1)
+            p.keys.splits = (int32_t)groups * parts;
+    }
     split(heads * p.queries.row_tiles, (a.keys + kRowTile - 1) / kRowTile, p.queries);
     p.stats = (size_t)heads * (size_t)padded * 2 + (((size_t)heads * (size_t)(padded / kRowTile) + 3) & ~(size_t)3);
     // (one after the other: they share the memory)
-    const size_t of_keys = p.keys.splits > 1 ? 2 * (size_t)p.keys.splits * (size_t)heads * (size_t)a.keys * (size_t)a.dim : 0;
+    const size_t of_keys = 2 * (size_t)p.keys.splits * kGroup * (size_t)a.dim;
     const size_t of_rows = p.queries.splits > 1 ? (size_t)p.queries.splits * (size_t)heads * (size_t)a.rows * (size_t)a.dim : 0;
     p.partial = of_keys > of_rows ? of_keys : of_rows;
     return p;
@@ -570,10 +651,9 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
     const int64_t heads = (int64_t)p.keys.batch * p.keys.kv_heads;
     const int64_t rows_grid = heads * (p.keys.padded / kRowTile);
     Args k = p.keys, q = p.queries;
-    const int64_t key_work = heads * k.key_tiles * k.splits, row_work = heads * q.row_tiles * q.splits;
-    const int64_t key_elements = (int64_t)k.batch * k.keys * k.kv_heads * k.dim, row_elements = heads * k.rows * k.dim;
-    const int64_t key_blocks = (key_elements / 8 + 255) / 256, row_blocks = (row_elements / 8 + 255) / 256;
-    if (rows_grid > INT32_MAX || key_work > INT32_MAX / 2 || row_work > INT32_MAX / 2 || (k.splits > 1 && key_blocks > INT32_MAX) ||
+    const int64_t groups = heads * k.key_tiles, key_work = k.splits ? k.splits : groups, row_work = heads * q.row_tiles * q.splits;
+    const int64_t row_elements = heads * k.rows * k.dim, row_blocks = (row_elements / 8 + 255) / 256;
+    if (rows_grid > INT32_MAX || key_work > INT32_MAX / 2 || row_work > INT32_MAX / 2 ||
         (q.splits > 1 && row_blocks > INT32_MAX))
         return GRKAN_ERR_UNSUPPORTED;
     if (!allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) || !allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))
@@ -581,14 +661,12 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
     if (rows_grid > 0)
         rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
     if (key_work > 0) {
-        const unsigned grid = spread(k, key_work, (int64_t)k.key_tiles * k.splits);
+        const unsigned grid = spread(k, key_work, k.splits ? key_work : k.key_tiles);
         void *args[] = {&k};
         if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3(grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
             return GRKAN_ERR_LAUNCH;
-        if (k.splits > 1) {
-            sum_kernel<IO><<<dim3((unsigned)key_blocks), 256, 0, stream>>>(k.partial, k.splits, key_elements, k.dk);
-            sum_kernel<IO><<<dim3((unsigned)key_blocks), 256, 0, stream>>>(k.partial + (int64_t)k.splits * key_elements, k.splits, key_elements, k.dv);
-        }
+        if (k.splits)
+            sum_keys_kernel<IO><<<dim3((unsigned)(8 * groups)), 256, 0, stream>>>(k, (int32_t)((k.rows + p.v.rows - 1) / p.v.rows));
     }
     if (row_work > 0) {
         const unsigned grid = spread(q, row_work, (int64_t)q.row_tiles * q.splits);

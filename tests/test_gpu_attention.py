@@ -415,3 +415,51 @@ def test_on_another_stream_and_in_a_graph():
             again = cross_attention(*eager, lengths)
             assert torch.equal(out, again)
             assert all(torch.equal(a, b) for a, b in zip(grads, torch.autograd.grad(again, eager, dout)))
+
+
+# walks that are shared: over the keys of few rows, over the rows of few keys; more than 64 batch entries; whole groups without a valid key
+SHARED = [(100, 1, 200, 4, 2, 64), (70, 40, 300, 2, 2, 64), (130, 3, 33, 2, 1, 128), (2, 900, 700, 8, 2, 128), (3, 2100, 400, 1, 1, 64),
+          (1, 20, 12000, 2, 1, 64), (1, 600, 9000, 1, 1, 32), (66, 300, 140, 3, 1, 96), (1, 5000, 120, 2, 1, 72)]
+
+
+@pytest.mark.parametrize("masks", ["none", "lengths", "mask"])
+@pytest.mark.parametrize("shape", SHARED)
+def test_shared_walks(shape, masks):
+    test_forward_and_backward(shape, masks, "f16" if shape[-1] == 96 else "bf16")
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 3000, 4, 2, 64), (80, 2, 40, 2, 2, 128), (2, 900, 300, 4, 2, 128), (2, 40, 5000, 2, 2, 64)])
+def test_no_key_at_all(shape):
+    """Lengths of zero, or a mask of nothing, in every batch entry: zeros everywhere."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, shape, "bf16", "none")
+    bad = torch.full_like(k, math.nan)
+    leaves = [t.detach().requires_grad_() for t in (q, bad, bad)]
+    for how in ({"key_lengths": torch.zeros(shape[0], dtype=torch.int32, device="cuda:0")},
+                {"key_mask": torch.zeros(shape[0], shape[2], dtype=torch.bool, device="cuda:0")}):
+        out = cross_attention(*leaves, **how)
+        assert (out == 0).all()
+        for g in torch.autograd.grad(out, leaves, torch.ones_like(out)):
+            assert (g == 0).all()
+
+
+@pytest.mark.parametrize("group", [3, 5, 6])
+def test_odd_groups_in_strided_layouts(group):
+    """Tiles of rows that end inside a query, in tensors with the heads before the tokens, the upstream gradient's layout another still."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    shape = (2, 211, 330, 2 * group, 2, 64)
+    q, k, v, lengths, _, valid = _operands(torch, shape, "bf16", "lengths", seed=group)
+    apart = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k, v)]
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(group)
+    dout = _rand(torch, gen, "bf16", 2, 211, 2 * group, 3, 64)[:, :, :, 1]
+    leaves = [t.detach().requires_grad_() for t in apart]
+    out = cross_attention(*leaves, key_lengths=lengths)
+    got = (out.detach(),) + torch.autograd.grad(out, leaves, dout)
+    _assert_within(got, _formulas(torch, q, k, v, valid, 0.125, "bf16", dout), group)
