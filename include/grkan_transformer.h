@@ -30,7 +30,7 @@ extern "C" {
  *   y            [rows, D], contiguous: of io or, with scale, in 8 bits
  *   scale        NULL, or float32 [rows]: then y is float8 (e4m3, OCP: largest value 448) and stands for
  *                y * scale, scale = (largest magnitude of the row) / 448; a row of zeros has scale 0.  A row with
- *                a NaN or an infinity has NaN as its scale.
+ *                a NaN or an infinity, or whose squares' sum is past float32, has NaN as its scale.
  *
  * All arithmetic is float32; y is made of the rounded h (what the backward pass sees) and rounded once.
  * 1 <= D <= 16384, else GRKAN_ERR_UNSUPPORTED.  Pointers aligned to their elements.
@@ -73,6 +73,7 @@ grkan_status_t grkan_rms_norm_bwd(const void *h, const void *dy, const void *dh,
  *              position_token_stride
  * frequencies: DEVICE float64 [pairs], radians per step of position; axis: DEVICE int32 [pairs], each below `axes` (checked by
  * the caller: the kernel reads what it says, clamped to 0 .. axes - 1).
+ * dim even, 4096 at most, heads 65536 at most, and 2^31 blocks of work at most, else GRKAN_ERR_UNSUPPORTED.
  * The angle is formed and reduced to one turn in float64, so that it is as exact at position 1,000,000 as at 1; sine and
  * cosine in float32, once for each token and pair.
  */
@@ -109,7 +110,8 @@ grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t count, const 
  *         backward pass: log2 of the sum of exp(scale q k^T) over the valid keys; an infinity where there is none
  * io: GRKAN_BF16 or GRKAN_F16; scores, their statistics and all sums are float32, the probabilities are rounded to io for
  * the product with v.
- * dim a multiple of 8 up to 128; scale finite and positive; else GRKAN_ERR_UNSUPPORTED.
+ * dim a multiple of 8 up to 128; scale finite and positive; queries x heads / kv_heads, keys and batch x kv_heads in 31 bits; token strides of
+ * k and v that are not negative and below 2^24: else GRKAN_ERR_UNSUPPORTED.
  *
  * Backward: P is recomputed from lse.  dout strided as q is; dq as out, dk and dv [batch, keys, kv_heads, dim], contiguous,
  * 16-byte aligned, overwritten (with zeros for keys that are not valid).

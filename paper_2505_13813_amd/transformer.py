@@ -145,6 +145,7 @@ class KATCrossBlock(nn.Module):
     The last addition is left to the norm behind it, which has the sum in registers anyway: a block takes (branch, stream) and
     returns (branch, stream), the value being their sum; stream None means that branch is the value.
 
+    Parameters and inputs are bfloat16 or float16, or float32 under autocast to one of the two, which keeps the stream in float32.
     `rotary_pairs`: rotated channel pairs of each head for each axis of the positions; none: no rotation.  `context_dim`: channels of
     the encoder's states (default: dim)."""
 
@@ -178,7 +179,7 @@ class KATCrossBlock(nn.Module):
 
     def forward(self, branch, context=None, stream=None, positions=None, context_positions=None, key_lengths=None,
                 key_mask=None, keys_values=None):
-        y, x = (self.norm1(branch), branch) if stream is None else self.norm1(branch, stream)
+        y, x = (self.norm1(branch), branch) if stream is None else self.norm1(branch.to(stream.dtype), stream)
         q = self.to_q(y).unflatten(-1, (self.heads, self.head_dim))
         if keys_values is not None:
             k, v = keys_values
@@ -189,7 +190,7 @@ class KATCrossBlock(nn.Module):
             if self.rotary is not None:
                 q, k = self.rotary(q, positions, k, context_positions)
         out = cross_attention(q, k, v, key_lengths, key_mask)
-        y, x = self.norm2(self.proj(out.flatten(-2)), x)
+        y, x = self.norm2(self.proj(out.flatten(-2)).to(x.dtype), x)
         return self.mlp(y), x
 
 
@@ -211,4 +212,4 @@ class KATCrossDecoder(nn.Module):
         for i, block in enumerate(self.blocks):
             x, stream = block(x, context, stream, positions, context_positions, key_lengths, key_mask,
                               None if cache is None else cache[i])
-        return self.norm(x) if stream is None else self.norm(x, stream)[0]
+        return self.norm(x) if stream is None else self.norm(x.to(stream.dtype), stream)[0]
