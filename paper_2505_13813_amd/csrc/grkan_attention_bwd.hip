@@ -81,28 +81,36 @@ template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const 
     const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
     const uint64_t out = reinterpret_cast<uint64_t>(a.out) + 2u * (uint64_t)((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim);
     const uint64_t dout = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
-    float largest = 0.0f;
+    const uint32_t row0 = (uint32_t)tile * kRowTile + (threadIdx.x >> 4);
+    u32x4 o[4], d[4];
+    float lse[4], largest = 0.0f;
+    // (all loads in front, without a branch: they wait for one another otherwise)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t row = (uint32_t)tile * kRowTile + 16u * k + (threadIdx.x >> 4);
-        const bool there = (int64_t)row < a.rows;
-        float sum = 0.0f;
-        if (there && 8u * lane16 < (uint32_t)a.dim) {
-            const u32x4 o = gload16(out + 2u * (uint64_t)row_offset(row, (uint32_t)a.group, heads_dim, a.dim) + 16u * lane16, 0);
-            const u32x4 d = gload16(dout + (uint64_t)row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head) + 16u * lane16, 0);
+        const uint32_t row = row0 + 16u * k;
+        const bool there = (int64_t)row < a.rows, loaded = there && 8u * lane16 < (uint32_t)a.dim;
+        const uint64_t zeros = reinterpret_cast<uint64_t>(kZeros);
+        o[k] = gload16(loaded ? out + 2u * (uint64_t)row_offset(row, (uint32_t)a.group, heads_dim, a.dim) + 16u * lane16 : zeros, 0);
+        d[k] = gload16(loaded ? dout + (uint64_t)row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head) + 16u * lane16 : zeros, 0);
+        const float *const from = there ? a.lse + ((int64_t)bh * a.rows + row) : reinterpret_cast<const float *>(kZeros);
+        lse[k] = *from;
+    }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = MM::first(d[j]), y = MM::second(d[j]);
-                sum += x * MM::first(o[j]) + y * MM::second(o[j]);
-                largest = fmaxf(largest, fmaxf(fabsf(x), fabsf(y)));
-            }
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t row = row0 + 16u * k;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = MM::first(d[k][j]), y = MM::second(d[k][j]);
+            sum += x * MM::first(o[k][j]) + y * MM::second(o[k][j]);
+            largest = fmaxf(largest, fmaxf(fabsf(x), fabsf(y)));
         }
 #pragma unroll
         for (int s = 8; s > 0; s /= 2)
             sum += __shfl_xor(sum, s);
         if (lane16 == 0) {
             const int64_t at = (int64_t)bh * a.padded + row;
-            a.row_lse[at] = there ? a.lse[(int64_t)bh * a.rows + row] : __builtin_inff();
+            a.row_lse[at] = (int64_t)row < a.rows ? lse[k] : __builtin_inff();
             a.row_delta[at] = sum;
         }
     }
