@@ -461,7 +461,7 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
     const RowOperand<DP> row_operand(lane);
     const ColumnOperand<DP> column_operand(lane);
     const uint64_t k_base = a.k.at + (uint64_t)(b * a.k.batch + kvh * a.k.head), v_base = a.v.at + (uint64_t)(b * a.v.batch + kvh * a.v.head);
-    ValidKeys valid(a, b, count);
+    ValidKeys valid(a, b, count, t1);
     arrived(q);
     arrived(o);
     arrived(lse);
