@@ -10,7 +10,7 @@
 //
 // What bounds them.  Many rows: 4 dim products and some 1.3 vector operations and an exponential for each score, and little of the two runs
 // at once: a loop of these alone, without memory, takes 510 ns for 32 rows, 64 keys and 64 channels with three wavefronts on a SIMD, its products alone
-// 245; here it is 700 (4 x 2048 x 2048 of 16 heads: 100 us = 690 TFLOP/s; with 128 channels 165 us = 830; 2 x 4096 queries, 4,001 and 1,808 keys of 16
+// 245; here it is 655 with four (16 x 2048 x 2048 of 12 heads: 252 us = 820 TFLOP/s; 4 x 2048 x 2048 of 16 heads of 128 165 us = 830; 2 x 4096 queries, 4,001 and 1,808 keys of 16
 // heads of 128: 219 us = 890).  Few rows: memory (16 single tokens of 32 heads, 2,268 to 8,191 keys of eight, 0.29 GB: 62 us = 4.6 TB/s, and 5 to join).
 //
 // The maximum of a row is raised only where a score passes it by more than 2^8 in the exponent: the probabilities are then at most 256,
@@ -173,7 +173,9 @@ template <typename IO_, int DP_> struct Shape {
     static constexpr size_t kLds = kCover + 2 * KT * 4;
 };
 
-template <class SH> __global__ __launch_bounds__(256, 2) void forward_kernel(const Args a)
+// Up to 64 channels four workgroups fit a compute unit (128 registers; us with three, of 129, and with four: 16 x 2048 x 2048 of 12 heads of 64
+// 266 to 289 / 252, 4 x 2048 x 2048 of 16 115 to 124 / 110, 64 x 197 x 360 of 12 38 / 37, and 32 x 256 x 785 of 12, which is one round of three, 36 / 37).
+template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void forward_kernel(const Args a)
 {
     constexpr int DP = SH::DP, KT = SH::KT;
     extern __shared__ __align__(256) char smem[];
