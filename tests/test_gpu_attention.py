@@ -463,3 +463,27 @@ def test_odd_groups_in_strided_layouts(group):
     out = cross_attention(*leaves, key_lengths=lengths)
     got = (out.detach(),) + torch.autograd.grad(out, leaves, dout)
     _assert_within(got, _formulas(torch, q, k, v, valid, 0.125, "bf16", dout), group)
+
+
+def test_queries_past_32_bits():
+    """4.6 GB of queries, outputs and their gradients: the last queries' as the formulas have them, and as in a call of their own."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    queries, heads, dim, keys, last = 560000, 32, 128, 40, 100
+    assert queries * heads * dim * 2 > 2 ** 32
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(11)
+    q = torch.empty(1, queries, heads, dim, dtype=torch.bfloat16, device="cuda:0")
+    q.normal_(generator=gen)
+    k, v = (_rand(torch, gen, "bf16", 1, keys, 4, dim) for _ in range(2))
+    leaves = [q.requires_grad_(), k, v]
+    out = cross_attention(*leaves)
+    dout = torch.ones_like(q)
+    dout[:, -last:].normal_(generator=gen)
+    dq, = torch.autograd.grad(out, q, dout)
+    valid = torch.ones(1, keys, dtype=torch.bool, device="cuda:0")
+    with torch.no_grad():
+        wanted = _formulas(torch, q[:, -last:], k, v, valid, dim ** -0.5, "bf16", dout[:, -last:])[:2]
+        _assert_within([out[:, -last:].contiguous(), dq[:, -last:].contiguous()], wanted, "last")

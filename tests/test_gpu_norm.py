@@ -254,3 +254,35 @@ def test_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, rms_norm(x * (k + 1), w, r)))
+
+
+def test_rows_past_32_bits():
+    """Rows 0.5 GB apart, 5 GB in all, and a contiguous tensor of 4.6 GB: as the same rows dense, or alone."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import rms_norm
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(12)
+    w = torch.rand(1000, device="cuda:0", generator=gen).bfloat16()
+    far = torch.empty(10 * (2 ** 28 + 3), dtype=torch.bfloat16, device="cuda:0").as_strided((10, 1000), (2 ** 28 + 3, 1))
+    far.copy_(torch.randn(10, 1000, device="cuda:0", generator=gen))
+    near = far.contiguous()
+    dy = torch.randn(10, 1000, device="cuda:0", generator=gen).bfloat16()
+    found = []
+    for x in (far, near):
+        x = x.detach().requires_grad_()
+        y = rms_norm(x, w)
+        found.append((y, *torch.autograd.grad(y, x, dy)))
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+    del far
+    rows, dim = 1150000, 2000
+    assert rows * dim * 2 > 2 ** 32
+    x = torch.empty(rows, dim, dtype=torch.bfloat16, device="cuda:0").normal_(generator=gen)
+    w = torch.rand(dim, device="cuda:0", generator=gen)
+    x.requires_grad_()
+    y = rms_norm(x, w)
+    dx, = torch.autograd.grad(y, x, x.detach())
+    end = x.detach()[-9:].clone().requires_grad_()
+    alone = rms_norm(end, w)
+    assert torch.equal(y[-9:], alone) and torch.equal(dx[-9:], torch.autograd.grad(alone, end, end.detach())[0])

@@ -172,3 +172,24 @@ def test_axis_out_of_range_reads_the_last_one():
     p = torch.randint(0, 9, (5, 2), device="cuda:0")
     far = torch.tensor([0, 1, 2, 7, -1, 1, 100000, 0], dtype=torch.int32, device="cuda:0")
     assert torch.equal(rotary(x, p, f, far), rotary(x, p, f, far.clamp(0, 1)))
+
+
+def test_tokens_past_32_bits():
+    """Tokens 0.5 GB apart, and a contiguous tensor of 4.6 GB: as the same tokens dense, or alone."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import rotary, rotary_frequencies
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(13)
+    f, axis = rotary_frequencies((32,), device="cuda:0")
+    far = torch.empty(10 * 2 ** 28 + 128, dtype=torch.bfloat16, device="cuda:0").as_strided((1, 10, 2, 64), (0, 2 ** 28, 64, 1))
+    far.copy_(torch.randn(1, 10, 2, 64, device="cuda:0", generator=gen))
+    at = torch.arange(10, device="cuda:0")[:, None] * 100003
+    assert torch.equal(rotary(far, at, f, axis), rotary(far.contiguous(), at, f, axis))
+    del far
+    tokens = 280000
+    x = torch.empty(1, tokens, 128, 64, dtype=torch.bfloat16, device="cuda:0").normal_(generator=gen)
+    assert x.numel() * 2 > 2 ** 32
+    at = torch.arange(tokens, device="cuda:0", dtype=torch.int32)[:, None]
+    assert torch.equal(rotary(x, at, f, axis)[:, -5:], rotary(x[:, -5:], at[-5:], f, axis))
