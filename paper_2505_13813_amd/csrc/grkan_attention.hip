@@ -4,8 +4,8 @@
 //   * With rows enough (queries x heads that share a key head), a workgroup of four wavefronts has 32 each; 64 keys and their
 //     values at a time come to LDS by LDS-direct loads, two tiles deep, and serve all four.
 //     Where the workgroups would not fill the chip, the keys are split over several, and a second launch joins them.
-//   * With 32 rows or fewer (single tokens) the keys are what there is to read: the four wavefronts have the same rows and
-//     tiles of 32 keys of their own, in LDS of their own, without a barrier, and join what they found at the end.  All the keys are dealt
+//   * With 32 rows or fewer (single tokens), or few tiles of 32, the keys are what there is to read: the four wavefronts have the same rows and
+//     tiles of 32 keys of their own, in LDS of their own, without a barrier, and join what they found at the end.  Where single tokens' keys are long, they are dealt
 //     out evenly to a workgroup on each compute unit, and a second launch joins the parts.
 //
 // What bounds them.  Many rows: 4 dim products and some 1.3 vector operations and an exponential for each score, and little of the two runs
@@ -364,7 +364,7 @@ template <typename IO_, int DP_> struct TokenShape {
     static_assert(((DP + 4) * 32 * kWaves + 64 * kWaves) * sizeof(float) <= kLds, ""); // what the wavefronts join
 };
 
-// With a.splits workers; 0: each has one key head by itself and writes the output.
+// With a.splits workers (32 rows at most); 0: each has 32 rows of one key head by itself and writes the output.
 template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void tokens_kernel(const Args a)
 {
     constexpr int DP = SH::DP, KT = SH::KT, ND = DP / 32;
@@ -381,10 +381,10 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
     const uint32_t stages = lds0 + (uint32_t)wave * 2u * SH::kStage, covers = lds0 + SH::kCover + (uint32_t)wave * 2u * KT * 4u;
     const float c = a.c;
 
-    // groups [g0, g1) of a key head; the part's place in `out`
-    auto part = [&](int32_t b, int32_t kvh, int32_t count, int32_t g0, int32_t g1) {
+    // rows row0 .. row0 + 31 and groups [g0, g1) of a key head
+    auto part = [&](int32_t b, int32_t kvh, uint32_t row0, int32_t count, int32_t g0, int32_t g1) {
         Rows<typename SH::IO, DP, KT> rows;
-        rows.load(a, b, kvh, row, h);
+        rows.load(a, b, kvh, row0 + row, h);
         rows.clear();
         constexpr int kTiles = kGroup / KT;
         const int32_t tiles = (count + KT - 1) / KT, t0 = g0 * kTiles + wave, t1 = g1 * kTiles < tiles ? g1 * kTiles : tiles;
@@ -456,8 +456,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
         }
         const int64_t bh = (int64_t)b * a.kv_heads + kvh, slot = bh + worker;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum, l2 = log2_sum(top, sum, c);
-        if ((int64_t)row < a.rows) { // wavefront w writes channels 32 w .., 32 (w + kWaves) ..
-            char *const out = shared ? reinterpret_cast<char *>(a.partial + (slot * a.rows + row) * a.dim) : out_row(a, b, kvh, row);
+        if ((int64_t)row0 + row < a.rows) { // wavefront w writes channels 32 w .., 32 (w + kWaves) ..
+            char *const out = shared ? reinterpret_cast<char *>(a.partial + (slot * a.rows + row) * a.dim) : out_row(a, b, kvh, row0 + row);
 #pragma unroll 1
             for (int d = wave; d < ND; d += SH::kWaves) {
                 f32x16 all;
@@ -481,7 +481,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
                 if (shared)
                     a.partial[((int64_t)a.batch * a.kv_heads + a.splits) * a.rows * a.dim + slot * a.rows + row] = l2;
                 else if (a.lse)
-                    a.lse[bh * a.rows + row] = lse_of(l2);
+                    a.lse[bh * a.rows + row0 + row] = lse_of(l2);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -489,8 +489,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
     };
 
     if (!shared) {
-        const int32_t b = worker / a.kv_heads, count = keys_of(a, b);
-        part(b, worker - b * a.kv_heads, count, 0, Deal::groups_of(count));
+        const int32_t bh = worker / a.row_tiles, b = bh / a.kv_heads, count = keys_of(a, b);
+        part(b, bh - b * a.kv_heads, 32u * (uint32_t)(worker - bh * a.row_tiles), count, 0, Deal::groups_of(count));
         return;
     }
     Deal deal(a);
@@ -502,7 +502,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
     while (x < end) {
         const int32_t kvh = (x - deal.begin) / deal.groups, g0 = x - deal.begin - kvh * deal.groups;
         const int32_t g1 = end - x < deal.groups - g0 ? g0 + end - x : deal.groups;
-        part(deal.b, kvh, deal.count, g0, g1);
+        part(deal.b, kvh, 0, deal.count, g0, g1);
         x += g1 - g0;
         if (x < end && x == deal.begin + deal.groups * a.kv_heads) { // the next entry with keys
             deal.begin = x;
@@ -634,23 +634,33 @@ struct Variant {
     size_t lds;
 };
 
-template <typename IO, int DP> static Variant pick(int64_t rows)
+template <typename IO, int DP> static Variant pick(bool few)
 {
-    if (rows <= 32)
+    if (few)
         return Variant{tokens_kernel<TokenShape<IO, DP>>, join_tokens_kernel<IO>, true, 32, kGroup, 64 * TokenShape<IO, DP>::kWaves, TokenShape<IO, DP>::kLds};
     return Variant{forward_kernel<Shape<IO, DP>>, join_kernel<IO>, false, Shape<IO, DP>::kRows, Shape<IO, DP>::KT, 256, Shape<IO, DP>::kLds};
 }
-template <typename IO> static Variant pick(int32_t dim, int64_t rows)
+template <typename IO> static Variant pick(int32_t dim, bool few)
 {
-    return dim <= 32 ? pick<IO, 32>(rows) : dim <= 64 ? pick<IO, 64>(rows) : dim <= 96 ? pick<IO, 96>(rows) : pick<IO, 128>(rows);
+    return dim <= 32 ? pick<IO, 32>(few) : dim <= 64 ? pick<IO, 64>(few) : dim <= 96 ? pick<IO, 96>(few) : pick<IO, 128>(few);
 }
 
 // The kernel, and how the keys are split.
 static Variant plan(Args &a, grkan_dtype_t io)
 {
-    const Variant v = io == GRKAN_BF16 ? pick<__bf16>(a.dim, a.rows) : pick<_Float16>(a.dim, a.rows);
-    const int64_t heads = (int64_t)a.batch * a.kv_heads, tiles = (a.keys + v.keys - 1) / v.keys;
-    if (v.few) {
+    const int64_t heads = (int64_t)a.batch * a.kv_heads;
+    // 32 rows or fewer, or 32 to a workgroup: there the four wavefronts share the keys, which takes less time where no compute unit has more than one
+    // workgroup and the walk is neither over at once nor long enough to be split over several (us with four times 32 rows / with 32, of one
+    // image's 197 tokens or so and twelve heads: 64 channels 40 keys 5.8 / 5.9, 200 8.3 / 7.0, 577 14.8 / 10.3, 1,500 13.9 / 18.2; 128 channels 7.5 / 8.2,
+    // 11.5 / 9.5, 17.3 / 15.8, 17.6 / 30.4; 264 workgroups 577 keys 15.6 / 12.7 and 20.7 / 31.0).
+    const bool few = a.rows <= 32 || (heads * ((a.rows + 31) / 32) <= kWorkers && a.keys > 128 && a.keys <= 768);
+    const Variant v = io == GRKAN_BF16 ? pick<__bf16>(a.dim, few) : pick<_Float16>(a.dim, few);
+    const int64_t tiles = (a.keys + v.keys - 1) / v.keys;
+    if (few) {
+        a.row_tiles = (int32_t)((a.rows + 31) / 32);
+        a.splits = 0;
+        if (a.row_tiles > 1)
+            return v;
         // A worker on every compute unit, with 256 keys at least; none where a key head each does as well: 1,024 of them, or all short
         // (the second launch takes as long as 1,024 keys one behind the other).
         const int64_t most = heads * tiles / 2;
@@ -721,7 +731,7 @@ extern "C" grkan_status_t grkan_attention_fwd(const grkan_attention_t *at, void 
     const size_t need = attention::forward_bytes(a, v);
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return GRKAN_ERR_WORKSPACE;
-    const int64_t heads = (int64_t)a.batch * a.kv_heads, work = v.few ? (a.splits > 0 ? a.splits : heads) : heads * a.row_tiles * a.splits;
+    const int64_t heads = (int64_t)a.batch * a.kv_heads, work = v.few ? (a.splits > 0 ? a.splits : heads * a.row_tiles) : heads * a.row_tiles * a.splits;
     const int64_t join = !need ? 0 : v.few ? heads : (heads * a.rows * (a.dim / 8) + 255) / 256;
     if (work > INT32_MAX / 2 || join > INT32_MAX)
         return GRKAN_ERR_UNSUPPORTED;
