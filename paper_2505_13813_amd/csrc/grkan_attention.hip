@@ -17,6 +17,7 @@
 // which neither 16-bit type minds, and the accumulators are scaled in few of the tiles instead of in most.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <unordered_set>
@@ -645,15 +646,56 @@ template <typename IO> static Variant pick(int32_t dim, bool few)
     return dim <= 32 ? pick<IO, 32>(few) : dim <= 64 ? pick<IO, 64>(few) : dim <= 96 ? pick<IO, 96>(few) : pick<IO, 128>(few);
 }
 
+// Whether the four wavefronts of a workgroup share the keys of 32 rows, instead of having 32 rows each.  Measured, in us (four times 32 rows / 32):
+//   * where no compute unit, or with 64 channels only every other, has more than one workgroup, and the walk is neither over at once nor worth a split over several.  96 heads of 64 channels, one
+//     row: 64 keys 5.2 / 5.8, 200 8.1 / 6.4, 400 10.4 / 8.8, 1,600 14 / 17; twelve with 128 rows: 577 keys 14.8 / 10.3, 1,500 13.9 / 18.2.
+//     With 128 channels: 200 keys 10.4 / 10.2, 800 17 / 20; twelve with 128 rows: 577 keys 17.3 / 15.8.
+//   * single tokens on long keys of uneven lengths, which are dealt out evenly.  300 heads, 5,000 keys at most, 64 channels 78 / 55, 128 channels 134 / 108; 768 heads
+//     of 128 272 / 236; 96 heads 25 / 24 and 32 / 37.
+static bool shares_keys(const Args &a, int64_t heads)
+{
+    const int64_t work = heads * ((a.rows + 31) / 32);
+    if (a.keys > 128 && (a.dim <= 64 ? work <= kWorkers + kWorkers / 2 && a.keys <= 896 : work <= kWorkers && a.keys <= 640))
+        return true;
+    return a.rows <= 32 && a.lengths && a.keys > 2048 && heads >= 128;
+}
+
+// Over how many workgroups the keys of each of `base` are split, four tiles each at least: what takes the least time, counted in tiles of one
+// that has a compute unit for itself.  Two there take 1.1 times as long as one, more as much longer as they are, up to `together`, and the
+// others behind them; a split's beginning takes two tiles, the second launch six, or four of more than 64 channels, and the parts' way through
+// memory, `rows` each, one for 6 MB, or 8 (`tile`: how much longer than in the forward pass a tile takes).  (us without and with: three batch entries with 700 queries, 5,000 keys, sixteen heads of 64, which are 288
+// workgroups, 107 / 76; 300 heads of 128, one query, 5,000 keys 159 / 146.)
+int64_t splits_of(int64_t base, int64_t tiles, int64_t rows, int64_t dim, double together, double tile)
+{
+    const double second = (dim <= 64 ? 6.0 : 4.0) / tile, bytes = (dim <= 64 ? 6e6 : 8e6) * tile;
+    int64_t best = 1;
+    double least = 0;
+    auto look = [&](int64_t n) {
+        if (n < 1 || (n > 1 && (base < 1 || 4 * n > tiles)))
+            return;
+        const double all = (double)base * (double)n, each = std::ceil(all / 256.0), rounds = std::floor(each / together), rest = each - rounds * together;
+        const double share = rounds * 0.55 * together + (rest > 0 ? std::max(1.0, 0.55 * rest) : 0.0);
+        const double cost = (double)((tiles + n - 1) / n + 2) * share + (n > 1 ? second + all * (double)(rows * dim) * 8.0 / bytes : 0.0);
+        if (n == 1 || cost < least) {
+            best = n;
+            least = cost;
+        }
+    };
+    for (int64_t n = 1; n <= 8; ++n)
+        look(n);
+    if (base > 0 && base < 64)
+        for (int64_t most : {256, 512}) {
+            const int64_t n = most / base;
+            look(n < tiles / 4 ? n : tiles / 4);
+        }
+    return best;
+}
+
 // The kernel, and how the keys are split.
 static Variant plan(Args &a, grkan_dtype_t io)
 {
     const int64_t heads = (int64_t)a.batch * a.kv_heads;
-    // 32 rows or fewer, or 32 to a workgroup: there the four wavefronts share the keys, which takes less time where no compute unit has more than one
-    // workgroup and the walk is neither over at once nor long enough to be split over several (us with four times 32 rows / with 32, of one
-    // image's 197 tokens or so and twelve heads: 64 channels 40 keys 5.8 / 5.9, 200 8.3 / 7.0, 577 14.8 / 10.3, 1,500 13.9 / 18.2; 128 channels 7.5 / 8.2,
-    // 11.5 / 9.5, 17.3 / 15.8, 17.6 / 30.4; 264 workgroups 577 keys 15.6 / 12.7 and 20.7 / 31.0).
-    const bool few = a.rows <= 32 || (heads * ((a.rows + 31) / 32) <= kWorkers && a.keys > 128 && a.keys <= 768);
+    const bool few = shares_keys(a, heads);
     const Variant v = io == GRKAN_BF16 ? pick<__bf16>(a.dim, few) : pick<_Float16>(a.dim, few);
     const int64_t tiles = (a.keys + v.keys - 1) / v.keys;
     if (few) {
@@ -668,11 +710,7 @@ static Variant plan(Args &a, grkan_dtype_t io)
         return v;
     }
     a.row_tiles = (int32_t)((a.rows + v.rows - 1) / v.rows);
-    // as many as give each compute unit two workgroups, each with four tiles at least
-    const int64_t base = heads * a.row_tiles;
-    int64_t splits = base > 0 && base < 384 ? 512 / base : 1;
-    splits = splits < tiles / 4 ? splits : tiles / 4;
-    splits = splits > 1 ? splits : 1;
+    const int64_t splits = splits_of(heads * a.row_tiles, tiles, a.rows < v.rows ? a.rows : v.rows, a.dim, a.dim <= 64 ? 4 : 2, 1.0);
     a.tiles_per_split = (int32_t)((tiles + splits - 1) / splits);
     if (a.tiles_per_split < 1)
         a.tiles_per_split = 1;

@@ -603,19 +603,6 @@ template <typename IO> static BackVariant pick(int32_t dim)
     return back_variant<BackShape<IO, 128, 32, true, 2>>();
 }
 
-// How many workgroups share the walk of one: enough to give each compute unit two, four tiles each at least.
-static void split(int64_t base, int64_t tiles, Args &a)
-{
-    int64_t splits = base > 0 && base < 384 ? 512 / base : 1;
-    splits = splits < tiles / 4 ? splits : tiles / 4;
-    splits = splits > 1 ? splits : 1;
-    const int64_t per = (tiles + splits - 1) / splits;
-    a.tiles_per_split = (int32_t)(per > 1 ? per : 1);
-    a.splits = (int32_t)((tiles + a.tiles_per_split - 1) / a.tiles_per_split);
-    if (a.splits < 1)
-        a.splits = 1;
-}
-
 struct BackPlan {
     BackVariant v;
     Args keys, queries;
@@ -644,7 +631,13 @@ static BackPlan back_plan(const Args &a, grkan_dtype_t io)
         else if (const int32_t parts = parts_of(groups, tiles, p.v.at_once, most); parts > 1)
             p.keys.splits = (int32_t)groups * parts;
     }
-    split(heads * p.queries.row_tiles, (a.keys + kRowTile - 1) / kRowTile, p.queries);
+    const int64_t row_work = heads * p.queries.row_tiles, key_tiles = (a.keys + kRowTile - 1) / kRowTile;
+    const int64_t splits = splits_of(row_work, key_tiles, a.rows < p.v.own ? a.rows : p.v.own, a.dim, a.dim <= 64 ? 3 : 2, 1.6);
+    const int64_t per = (key_tiles + splits - 1) / splits;
+    p.queries.tiles_per_split = (int32_t)(per > 1 ? per : 1);
+    p.queries.splits = (int32_t)((key_tiles + p.queries.tiles_per_split - 1) / p.queries.tiles_per_split);
+    if (p.queries.splits < 1)
+        p.queries.splits = 1;
     p.stats = (size_t)heads * (size_t)padded * 2 + (((size_t)heads * (size_t)(padded / kRowTile) + 3) & ~(size_t)3);
     // (one after the other: they share the memory)
     const size_t of_keys = 2 * (size_t)p.keys.splits * kGroup * (size_t)a.dim;

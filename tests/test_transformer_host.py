@@ -212,3 +212,16 @@ def test_the_modules_keep_their_frequencies():
     for bad in (dict(heads=5), dict(heads=6, kv_heads=4)):
         with pytest.raises(ValueError):
             KATCrossBlock(192, **bad)
+
+
+def test_attention_workspaces_of_every_small_size(lib):
+    """The plan is made for every combination of few and many queries, keys, heads and channels; what is asked for can be had."""
+    for queries in (0, 1, 5, 32, 33, 129, 4096):
+        for keys in (0, 1, 64, 129, 300, 700, 1000, 9000, 100000):
+            for batch, kv_heads in ((1, 1), (1, 12), (30, 10), (300, 8)):
+                for dim in (8, 64, 128):
+                    for lengths in (None, 16):
+                        a = _attention(batch=batch, queries=queries, keys=keys, heads=kv_heads, kv_heads=kv_heads, dim=dim, key_lengths=lengths)
+                        assert lib.grkan_attention_workspace_bytes(ctypes.byref(a), 0) < 1 << 30
+                        need = lib.grkan_attention_workspace_bytes(ctypes.byref(a), 1)
+                        assert need < (1 << 30) + 16 * batch * queries * kv_heads
