@@ -39,6 +39,7 @@ struct Args {
     float c; // scale x log2(e)
     float scale;
     char *out;              // dq in the backward pass
+    uint64_t forward_out;   // the backward pass' second input
     char *dk, *dv;
     float *lse;             // [batch, kv_heads, rows]
     float *partial;         // [splits][batch, kv_heads][rows][dim], then the splits' lse [splits][batch, kv_heads][rows]

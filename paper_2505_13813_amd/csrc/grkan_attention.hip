@@ -552,12 +552,16 @@ bool allow_lds(const void *kernel, size_t bytes)
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64)
         return false;
-    std::lock_guard<std::mutex> lock(mu);
-    if (done[dev].count(kernel))
-        return true;
-    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+    try { // (no exception leaves the C interface)
+        std::lock_guard<std::mutex> lock(mu);
+        if (done[dev].count(kernel))
+            return true;
+        if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+            return false;
+        done[dev].insert(kernel);
+    } catch (...) {
         return false;
-    done[dev].insert(kernel);
+    }
     return true;
 }
 
@@ -591,7 +595,7 @@ grkan_status_t fill(const grkan_attention_t *at, grkan_dtype_t io, Args *to)
     if (io != GRKAN_BF16 && io != GRKAN_F16)
         return GRKAN_ERR_DTYPE;
     const int64_t group = at->heads / at->kv_heads;
-    if (at->dim % 8 != 0 || at->dim > 128 || !(at->scale > 0) || !std::isfinite(at->scale))
+    if (at->dim % 8 != 0 || at->dim > 128 || !(at->scale > 0) || !std::isfinite(at->scale * 1.4426950408889634f))
         return GRKAN_ERR_UNSUPPORTED;
     // rows and tiles are counted in 31 bits, offsets in a tile of 64 tokens too
     const int64_t most = (int64_t)1 << 31;

@@ -5,12 +5,12 @@
 // Seven products as they stand (the scores and D twice), in two kernels, so that every gradient is summed by whoever owns it: no
 // atomics, the same bits each time.  One has keys, walks the rows and keeps dK and dV; the other has rows, walks the keys and
 // keeps dQ.  In both, as in the forward pass, the product that is contracted next is left in the registers as the operand of the next.
-// A third, small one makes delta in front of them.
+// delta is made by the queries' kernel, or in front of both by a small one.
 //
 // Bound by the products and the vector operations between them (two fused multiply-adds, an exponential and a rounding for each score), of which little
 // runs at once: the matrix units are busy for 42 % (keys) and 53 % (queries) of the time with 128 channels, 25 and 33 % with 64.  2 x 4096 queries, 4,001 and 1,808
 // keys, 16 heads of 128 that read four, float16: keys' kernel 459 us = 850 TFLOP/s, queries' 297 us = 985, where a large library product
-// reaches 1,500; rows 15, sums 24.  32 x 256 queries, 785 keys, 12 heads of 64: 80, 50 and 8.
+// reaches 1,500; rows 15, sums 24.  32 x 256 queries, 785 keys, 12 heads of 64, bfloat16: 80 and 51.
 //
 // float16: S' of a small upstream gradient would be below its range.  The products take 2^e S', with e such that the largest |dO| of
 // the key head becomes 1/4 to 1/2 (2^e S' then stays below 65,504 for values of up to 1,000), and the sums are scaled back in float32.
@@ -74,7 +74,10 @@ __device__ __forceinline__ void load_words_to_lds(uint64_t base, uint32_t lane_o
     asm volatile("s_nop 4\n\tglobal_load_lds_dword %1, %2" : : "{m0}"(lds_at), "v"(lane_off), "s"(base) : "memory");
 }
 
-// delta, and copies of lse, of 64 rows for each workgroup: sixteen lanes a row, eight channels each.
+// float16: delta, and copies of lse, of 64 rows for each workgroup: sixteen lanes a row, eight channels each.  (bfloat16, which is not scaled, needs no launch in
+// front: the queries' kernel has the rows of dO in its registers, reads those of O once, and leaves both for the keys' kernel behind it.  32 x 256 queries of
+// 12 heads of 64, 785 keys and a mask, forward and all gradients: 158 us in the place of 164.)
+template <typename IO> constexpr bool kRowsFirst = !__is_same(IO, __bf16);
 template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const Args a)
 {
     using MM = Matrix<IO>;
@@ -84,7 +87,7 @@ template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const 
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
     const uint32_t lane16 = threadIdx.x & 15u;
     const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
-    const uint64_t out = reinterpret_cast<uint64_t>(a.out) + 2u * (uint64_t)((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim);
+    const uint64_t out = a.forward_out + 2u * (uint64_t)((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim);
     const uint64_t dout = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
     const uint32_t row0 = (uint32_t)tile * kRowTile + (threadIdx.x >> 4);
     u32x4 o[4], d[4];
@@ -452,8 +455,32 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
         }
     }
     const float up = gradient_scale<IO>(a, bh), c = a.c;
-    float lse = there ? a.row_lse[(int64_t)bh * a.padded + row] : __builtin_inff();
-    float delta = there ? a.row_delta[(int64_t)bh * a.padded + row] * up : 0.0f;
+    float lse = there ? a.lse[(int64_t)bh * a.rows + row] : __builtin_inff();
+    float delta = 0.0f;
+    if constexpr (kRowsFirst<IO>) {
+        delta = there ? a.row_delta[(int64_t)bh * a.padded + row] * up : 0.0f;
+    } else {
+        // the rows' statistics, for the keys' kernel too
+        const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
+        const uint64_t at = a.forward_out + 2u * (uint64_t)((int64_t)b * (a.rows / a.group) * heads_dim + (int64_t)kvh * a.group * a.dim +
+                                                            row_offset(row, (uint32_t)a.group, heads_dim, a.dim));
+        u32x4 y[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const uint32_t channel = 16u * s + 8u * h;
+            y[s] = gload16(there && channel < (uint32_t)a.dim ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                delta += MM::first(o[s][j]) * MM::first(y[s][j]) + MM::second(o[s][j]) * MM::second(y[s][j]);
+        delta = halves_sum(delta);
+        if (split == 0 && h == 0 && row < (uint32_t)a.padded) {
+            a.row_lse[(int64_t)bh * a.padded + row] = lse;
+            a.row_delta[(int64_t)bh * a.padded + row] = delta;
+        }
+    }
     f32x16 dq[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -664,15 +691,9 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
         return GRKAN_ERR_UNSUPPORTED;
     if (!allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) || !allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))
         return GRKAN_ERR_LAUNCH;
-    if (rows_grid > 0)
-        rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
-    if (key_work > 0) {
-        const unsigned grid = spread(k, key_work, k.splits ? key_work : k.key_tiles);
-        void *args[] = {&k};
-        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3(grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
-            return GRKAN_ERR_LAUNCH;
-        if (k.splits)
-            sum_keys_kernel<IO><<<dim3((unsigned)(8 * groups)), 256, 0, stream>>>(k, (int32_t)((k.rows + p.v.rows - 1) / p.v.rows));
+    if constexpr (kRowsFirst<IO>) {
+        if (rows_grid > 0)
+            rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
     }
     if (row_work > 0) {
         const unsigned grid = spread(q, row_work, (int64_t)q.row_tiles * q.splits);
@@ -681,6 +702,14 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
             return GRKAN_ERR_LAUNCH;
         if (q.splits > 1)
             sum_kernel<IO><<<dim3((unsigned)row_blocks), 256, 0, stream>>>(q.partial, q.splits, row_elements, q.out);
+    }
+    if (key_work > 0) {
+        const unsigned grid = spread(k, key_work, k.splits ? key_work : k.key_tiles);
+        void *args[] = {&k};
+        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3(grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
+            return GRKAN_ERR_LAUNCH;
+        if (k.splits)
+            sum_keys_kernel<IO><<<dim3((unsigned)(8 * groups)), 256, 0, stream>>>(k, (int32_t)((k.rows + p.v.rows - 1) / p.v.rows));
     }
     return hipGetLastError() == hipSuccess ? GRKAN_OK : GRKAN_ERR_LAUNCH;
 }
@@ -725,7 +754,7 @@ extern "C" grkan_status_t grkan_attention_bwd(const grkan_attention_t *at, const
         to->dk = static_cast<char *>(dk);
         to->dv = static_cast<char *>(dv);
     }
-    p.keys.out = static_cast<char *>(const_cast<void *>(out)); // (read by the rows' kernel)
+    p.keys.forward_out = p.queries.forward_out = address(out);
     p.queries.out = static_cast<char *>(dq);
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
     return io == GRKAN_BF16 ? attention::backward<__bf16>(p, stream) : attention::backward<_Float16>(p, stream);
