@@ -371,10 +371,11 @@ std::optional<variable_list> rotary(const Tensor &q, const Tensor &positions, co
 
 // ------------------------------------------------------------------------------------------------ cross attention
 
-// t as the kernels read it: dense channels, strides and address in whole 16 bytes; a copy where it is not.
-Tensor in_vectors(const Tensor &t)
+// t as the kernels read it: dense channels, strides and address in whole 16 bytes, tokens less than `apart` elements apart; a copy where it
+// is not.
+Tensor in_vectors(const Tensor &t, int64_t apart = std::numeric_limits<int64_t>::max())
 {
-    bool fine = t.stride(3) == 1 && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0;
+    bool fine = t.stride(3) == 1 && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && (t.size(1) <= 1 || t.stride(1) < apart);
     for (int d = 0; d < 3; ++d)
         fine = fine && (t.stride(d) % 8 == 0 || t.size(d) == 1);
     return fine ? t : t.contiguous();
@@ -400,8 +401,9 @@ struct Attended {
         TORCH_CHECK_VALUE(scale > 0 && std::isfinite(scale), "scale must be finite and positive");
         io = *io_of(q_);
         q = in_vectors(q_);
-        k = in_vectors(k_);
-        v = in_vectors(v_);
+        constexpr int64_t kApart = 16777212; // (the kernels' limit)
+        k = in_vectors(k_, kApart);
+        v = in_vectors(v_, kApart);
         a.q = q.data_ptr();
         a.k = k.data_ptr();
         a.v = v.data_ptr();

@@ -487,3 +487,22 @@ def test_queries_past_32_bits():
     with torch.no_grad():
         wanted = _formulas(torch, q[:, -last:], k, v, valid, dim ** -0.5, "bf16", dout[:, -last:])[:2]
         _assert_within([out[:, -last:].contiguous(), dq[:, -last:].contiguous()], wanted, "last")
+
+
+def test_keys_further_apart_than_the_kernels_offsets():
+    """Tokens of 2^24 elements each (copied): as the dense ones."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(14)
+    far = torch.empty(6 * 2 ** 24, dtype=torch.bfloat16, device="cuda:0").as_strided((1, 5, 2, 64), (0, 2 ** 24, 64, 1))
+    far.copy_(_rand(torch, gen, "bf16", 1, 5, 2, 64))
+    q = _rand(torch, gen, "bf16", 1, 40, 2, 64)
+    found = []
+    for k in (far, far.contiguous()):
+        leaves = [t.detach().requires_grad_() for t in (q, k, k)]
+        out = cross_attention(*leaves)
+        found.append((out, *torch.autograd.grad(out, leaves, q)))
+    assert all(torch.equal(a, b) for a, b in zip(*found))
