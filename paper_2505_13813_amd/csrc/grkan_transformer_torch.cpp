@@ -378,7 +378,8 @@ Tensor in_vectors(const Tensor &t, int64_t apart = std::numeric_limits<int64_t>:
     bool fine = t.stride(3) == 1 && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && (t.size(1) <= 1 || t.stride(1) < apart);
     for (int d = 0; d < 3; ++d)
         fine = fine && (t.stride(d) % 8 == 0 || t.size(d) == 1);
-    return fine ? t : t.contiguous();
+    // (a copy of its own: contiguous() returns a contiguous tensor as it is, at whatever address)
+    return fine ? t : t.clone(at::MemoryFormat::Contiguous);
 }
 
 struct Attended {
