@@ -212,6 +212,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
             write_cover(lds0 + SH::kCover + (at ? KT * 4u : 0u), word, lane);
     };
     arrived(rows.q);
+    uint64_t some = 0; // valid keys
     // (a wavefront without rows loads for the others; two loops, as one with a condition in it would copy the sums in every pass)
     auto walk = [&](auto works) {
         uint32_t at = 0;
@@ -230,6 +231,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
                 rows.take(k_operand.moved(lds0 + at), v_operand.moved(lds0 + at + 2 * SH::kTile), word,
                           lds0 + SH::kCover + (at ? KT * 4u : 0u), a.c, h);
             at ^= SH::kTile;
+            some |= word;
             word = next;
         }
     };
@@ -238,6 +240,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         return;
     }
     walk(std::true_type{});
+    if (some == 0) // (a query may hold NaN, and masked keys' scores are 0 NaN then)
+        rows.clear();
     if ((int64_t)row >= a.rows)
         return;
 
@@ -397,7 +401,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
         constexpr int kAhead = 2 * TileLoads<DP, KT, 1>::kMine, kStep = SH::kWaves;
         arrived(rows.q);
         uint32_t at = SH::kStage;
-        uint64_t word = 0;
+        uint64_t word = 0, some = 0; // valid keys: of a tile, of any
 #pragma unroll 1
         for (int32_t t = t0 - kStep; t < t1; t += kStep) {
             const bool more = t + kStep < t1;
@@ -419,9 +423,12 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void 
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
             }
             at ^= SH::kStage;
+            some |= word;
             word = next;
         }
 
+        if (some == 0) // (a query may hold NaN, and masked keys' scores are 0 NaN then)
+            rows.clear();
         // the wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order
         constexpr int kPitch = DP + 4; // of a row's channels
         float *const joined = reinterpret_cast<float *>(smem);         // [wave][32 rows][channel]

@@ -520,7 +520,7 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
         const auto columns = column_operand.moved(lds0 + at);
         at ^= SH::kRowStage;
         word = next;
-        if (t < t0 || !works)
+        if (t < t0 || !works || now == 0) // (queries and dO may be NaN where no key is valid)
             continue;
 #pragma unroll
         for (int kb = 0; kb < KT / 32; ++kb) {

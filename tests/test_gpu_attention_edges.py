@@ -1,6 +1,8 @@
 """GPU tests of cross attention at the edges of what it takes."""
+import math
+
 import pytest
-from test_gpu_attention import _rand
+from test_gpu_attention import _operands, _rand, _type
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +36,38 @@ def test_contiguous_operands_off_16_bytes(which, elements):
         out = cross_attention(*leaves)
         found.append((out.detach(), *torch.autograd.grad(out, leaves, given["dout"])))
     assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(3, 1, 3000, 4, 2, 64), (4, 40, 700, 2, 2, 128), (2, 900, 300, 4, 2, 128), (3, 20, 100, 2, 2, 64),
+                                   (2, 300, 5000, 2, 2, 64)])
+def test_no_key_in_an_entry_whatever_its_queries_hold(shape, dtype):
+    """NaN and infinities in the queries and upstream gradients of an entry whose mask leaves nothing (padding): zeros there, and the
+    other entries' bits as with zeros in their place."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, *_ = _operands(torch, shape, dtype, "none")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(22)
+    dout = _rand(torch, gen, dtype, *q.shape)
+    mask = torch.rand(shape[0], shape[2], generator=gen, device="cuda:0") < 0.7
+    mask[1] = False
+    bad = torch.tensor([math.nan, math.inf, -math.inf, 1.0], device="cuda:0").to(_type(torch, dtype))
+    found = []
+    for poison in (False, True):
+        leaves = [t.detach().clone() for t in (q, k, v)]
+        up = dout.clone()
+        for t in (leaves[0], up):
+            t[1] = bad[torch.randint(0, 4, t[1].shape, generator=gen, device="cuda:0")] if poison else 0.0
+        if poison:
+            leaves[1][1], leaves[2][1] = math.nan, math.inf
+        for t in leaves:
+            t.requires_grad_()
+        out = cross_attention(*leaves, key_mask=mask)
+        found.append((out.detach(), *torch.autograd.grad(out, leaves, up)))
+        assert torch.equal(out, cross_attention(*(t.detach() for t in leaves), key_mask=mask))
+    for name, a, b in zip(("out", "dq", "dk", "dv"), *found):
+        assert (b[1] == 0).all(), name
+        assert torch.equal(a, b), name
