@@ -73,7 +73,9 @@ grkan_status_t grkan_rms_norm_bwd(const void *h, const void *dy, const void *dh,
  *              position_token_stride
  * frequencies: DEVICE float64 [pairs], radians per step of position; axis: DEVICE int32 [pairs], each below `axes` (checked by
  * the caller: the kernel reads what it says, clamped to 0 .. axes - 1).
- * dim even, 4096 at most, heads 65536 at most, and 2^31 blocks of work at most, else GRKAN_ERR_UNSUPPORTED.
+ * dim even, 4096 at most; heads x c x max(heads, c) below 2^32, with c = dim / 16 (float32: dim / 8), or 2, 4, 8 times that where
+ * `pairs` or dim / 2 is not a multiple of 8 (float32: 4); workgroups of up to 512 / (heads x c) tokens, one at least, below 2^24, as a
+ * launch has less than 2^32 threads: else GRKAN_ERR_UNSUPPORTED.
  * The angle is formed and reduced to one turn in float64, so that it is as exact at position 1,000,000 as at 1; sine and
  * cosine in float32, once for each token and pair.
  */
@@ -111,7 +113,8 @@ grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t count, const 
  * io: GRKAN_BF16 or GRKAN_F16; scores, their statistics and all sums are float32, the probabilities are rounded to io for
  * the product with v.
  * dim a multiple of 8 up to 128; scale finite and positive; queries x heads / kv_heads, keys and batch x kv_heads in 31 bits; token strides of
- * k and v that are not negative and below 2^24: else GRKAN_ERR_UNSUPPORTED.
+ * k and v that are not negative and below 2^24; batch x kv_heads x tiles of 64 rows (queries x heads / kv_heads) or 128 keys up to
+ * 14,000,000, as a launch has less than 2^32 threads: else GRKAN_ERR_UNSUPPORTED.
  *
  * Backward: P is recomputed from lse.  dout strided as q is; dq as out, dk and dv [batch, keys, kv_heads, dim], contiguous,
  * 16-byte aligned, overwritten (with zeros for keys that are not valid).

@@ -419,7 +419,8 @@ __device__ __forceinline__ int32_t work_item(const Args &a)
 grkan_status_t fill(const grkan_attention_t *a, grkan_dtype_t io, Args *to); // checks and arguments (grkan_attention.hip)
 bool allow_lds(const void *kernel, size_t bytes);
 bool in_offsets(int64_t token_stride, int64_t head_stride, int64_t heads);    // of a tile, in elements of 2 bytes
-unsigned spread(Args &a, int64_t work, int64_t per_head); // sets work and run; the grid
+constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1;  // of 256 threads: a launch has less than 2^32
+int64_t spread(Args &a, int64_t work, int64_t per_head); // sets work (kMostBlocks at most) and run; the grid, which may be more
 int64_t splits_of(int64_t base, int64_t tiles, int64_t rows, int64_t dim, double together, double tile); // of a walk over the keys
 
 } // namespace attention

@@ -572,13 +572,13 @@ bool allow_lds(const void *kernel, size_t bytes)
     return true;
 }
 
-unsigned spread(Args &a, int64_t work, int64_t per_head)
+int64_t spread(Args &a, int64_t work, int64_t per_head)
 {
     int64_t run = work / 64 < per_head ? work / 64 : per_head;
     run = run > 1 ? run : 1;
     a.work = (int32_t)work;
     a.run = (int32_t)run;
-    return (unsigned)((work + 8 * run - 1) / (8 * run) * 8 * run);
+    return (work + 8 * run - 1) / (8 * run) * 8 * run;
 }
 
 static bool fine_operand(const void *p, int64_t batch, int64_t token, int64_t head)
@@ -782,17 +782,19 @@ extern "C" grkan_status_t grkan_attention_fwd(const grkan_attention_t *at, void 
         return GRKAN_ERR_WORKSPACE;
     const int64_t heads = (int64_t)a.batch * a.kv_heads, work = v.few ? (a.splits > 0 ? a.splits : heads * a.row_tiles) : heads * a.row_tiles * a.splits;
     const int64_t join = !need ? 0 : v.few ? heads : (heads * a.rows * (a.dim / 8) + 255) / 256;
-    if (work > INT32_MAX / 2 || join > INT32_MAX)
+    if (work > attention::kMostBlocks || join > attention::kMostBlocks)
+        return GRKAN_ERR_UNSUPPORTED;
+    const int64_t grid = v.few ? work : attention::spread(a, work, (int64_t)a.row_tiles * a.splits);
+    if (grid > attention::kMostBlocks)
         return GRKAN_ERR_UNSUPPORTED;
     a.out = static_cast<char *>(out);
     a.lse = lse;
     a.partial = static_cast<float *>(workspace);
-    const unsigned grid = v.few ? (unsigned)work : attention::spread(a, work, (int64_t)a.row_tiles * a.splits);
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3(grid), dim3((unsigned)v.threads), args, v.lds, stream) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3((unsigned)v.threads), args, v.lds, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     if (join > 0 && hipLaunchKernel(reinterpret_cast<const void *>(v.join), dim3((unsigned)join), dim3(256), args, 0, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;

@@ -686,8 +686,11 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
     Args k = p.keys, q = p.queries;
     const int64_t groups = heads * k.key_tiles, key_work = k.splits ? k.splits : groups, row_work = heads * q.row_tiles * q.splits;
     const int64_t row_elements = heads * k.rows * k.dim, row_blocks = (row_elements / 8 + 255) / 256;
-    if (rows_grid > INT32_MAX || key_work > INT32_MAX / 2 || row_work > INT32_MAX / 2 ||
-        (q.splits > 1 && row_blocks > INT32_MAX))
+    if (rows_grid > kMostBlocks || key_work > kMostBlocks || row_work > kMostBlocks || (q.splits > 1 && row_blocks > kMostBlocks))
+        return GRKAN_ERR_UNSUPPORTED;
+    const int64_t row_grid = row_work > 0 ? spread(q, row_work, (int64_t)q.row_tiles * q.splits) : 0;
+    const int64_t key_grid = key_work > 0 ? spread(k, key_work, k.splits ? key_work : k.key_tiles) : 0;
+    if (row_grid > kMostBlocks || key_grid > kMostBlocks)
         return GRKAN_ERR_UNSUPPORTED;
     if (!allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) || !allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))
         return GRKAN_ERR_LAUNCH;
@@ -696,17 +699,15 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
             rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
     }
     if (row_work > 0) {
-        const unsigned grid = spread(q, row_work, (int64_t)q.row_tiles * q.splits);
         void *args[] = {&q};
-        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.queries), dim3(grid), dim3(256), args, p.v.queries_lds, stream) != hipSuccess)
+        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.queries), dim3((unsigned)row_grid), dim3(256), args, p.v.queries_lds, stream) != hipSuccess)
             return GRKAN_ERR_LAUNCH;
         if (q.splits > 1)
             sum_kernel<IO><<<dim3((unsigned)row_blocks), 256, 0, stream>>>(q.partial, q.splits, row_elements, q.out);
     }
     if (key_work > 0) {
-        const unsigned grid = spread(k, key_work, k.splits ? key_work : k.key_tiles);
         void *args[] = {&k};
-        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3(grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
+        if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3((unsigned)key_grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
             return GRKAN_ERR_LAUNCH;
         if (k.splits)
             sum_keys_kernel<IO><<<dim3((unsigned)(8 * groups)), 256, 0, stream>>>(k, (int32_t)((k.rows + p.v.rows - 1) / p.v.rows));

@@ -16,7 +16,8 @@ namespace rotary {
 
 using namespace vec;
 
-constexpr int kThreads = 256, kMostAngles = 4096; // angles of a workgroup in LDS: 32 KB
+constexpr int kThreads = 256, kMostAngles = 4096;       // angles of a workgroup in LDS: 32 KB
+constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1; // a launch has less than 2^32 threads
 
 struct Tensor {
     const char *x;
@@ -221,7 +222,7 @@ extern "C" grkan_status_t grkan_rotary(const grkan_rotary_t *tensors, int32_t co
         if (i == 0)
             a.first_blocks = blocks;
     }
-    if (blocks > INT32_MAX)
+    if (blocks > rotary::kMostBlocks)
         return GRKAN_ERR_UNSUPPORTED;
     if (blocks == 0)
         return GRKAN_OK;

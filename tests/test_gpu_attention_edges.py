@@ -71,3 +71,23 @@ def test_no_key_in_an_entry_whatever_its_queries_hold(shape, dtype):
     for name, a, b in zip(("out", "dq", "dk", "dv"), *found):
         assert (b[1] == 0).all(), name
         assert torch.equal(a, b), name
+
+
+def test_as_many_workgroups_as_a_launch_takes():
+    """14,000,000 entries of one query and one key give their values; 2^24 are refused, and nothing is left behind for the next call."""
+    import torch
+
+    import paper_2505_13813_amd as grkan
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    for entries, taken in ((14000000, True), (2 ** 24, False)):
+        v = torch.arange(entries, device="cuda:0").remainder(251).to(torch.bfloat16)[:, None, None, None].repeat(1, 1, 1, 8)
+        leaves = [t.requires_grad_() for t in (torch.ones_like(v), torch.ones_like(v), v)]
+        if taken:
+            out = cross_attention(*leaves)
+            dq, dk, dv = torch.autograd.grad(out, leaves, v.detach())
+            assert torch.equal(out, v) and torch.equal(dv, v) and (dq == 0).all() and (dk == 0).all()
+        else:
+            with pytest.raises(grkan.GrkanError):
+                cross_attention(*leaves)
+            assert float(v.detach()[:3].float().sum()) == 24.0

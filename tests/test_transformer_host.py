@@ -225,3 +225,17 @@ def test_attention_workspaces_of_every_small_size(lib):
                         assert lib.grkan_attention_workspace_bytes(ctypes.byref(a), 0) < 1 << 30
                         need = lib.grkan_attention_workspace_bytes(ctypes.byref(a), 1)
                         assert need < (1 << 30) + 16 * batch * queries * kv_heads
+
+
+def test_more_workgroups_than_a_launch_takes(lib):
+    """A launch has less than 2^32 threads: sizes that need more are refused as unsupported, not left to the launch."""
+    many = 1 << 24
+    for queries in (1, 200):
+        a = _attention(batch=many, queries=queries, heads=1, kv_heads=1)
+        assert lib.grkan_attention_fwd(ctypes.byref(a), 16, None, 16, 1 << 60, BF16, None) == UNSUPPORTED
+        for io in (BF16, F16):
+            assert lib.grkan_attention_bwd(ctypes.byref(a), 16, 16, 16, 64, 64, 64, 16, 16, 16, 16, 1 << 60, io, None) == UNSUPPORTED
+    # 12 x 40 items of two channels to a token, a token to a workgroup
+    t = binding.RotaryOperand(x=16, out=16, positions=16, batch=1, tokens=many, heads=12, batch_stride=0, token_stride=960, head_stride=80,
+                              position_batch_stride=0, position_token_stride=1, positions_dtype=0)
+    assert lib.grkan_rotary(ctypes.byref(t), 1, 16, 16, 13, 1, 80, 0, 0, BF16, None) == UNSUPPORTED
