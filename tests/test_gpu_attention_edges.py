@@ -2,7 +2,7 @@
 import math
 
 import pytest
-from test_gpu_attention import _operands, _rand, _type
+from test_gpu_attention import _assert_within, _formulas, _operands, _rand, _type
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,31 @@ def test_as_many_workgroups_as_a_launch_takes():
             with pytest.raises(grkan.GrkanError):
                 cross_attention(*leaves)
             assert float(v.detach()[:3].float().sum()) == 24.0
+
+
+@pytest.mark.parametrize("shape", [(1, 60, 1500, 2, 2, 64), (2, 45, 4001, 6, 2, 128), (1, 300, 700, 1, 1, 32), (1, 33, 2000, 3, 1, 96)])
+def test_float16_gradients_of_rows_of_different_sizes(shape):
+    """Upstream gradients of 2^6 to 2^-8 of the same size otherwise, row by row: a query's gradient is as exact as if all were of its size
+    (its own bound times its factor, and half a step of float16 below 2^-14 for the result); the keys' within their bounds."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    q, k, v, _, _, valid = _operands(torch, shape, "f16", "none")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(23)
+    each = _rand(torch, gen, "f16", *q.shape).clamp(-4.0, 4.0)
+    by = torch.exp2((6 - torch.arange(shape[1], device="cuda:0") % 15).double())[None, :, None, None]
+    dout = (each.double() * by).half()
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    out = cross_attention(*leaves)
+    dq, dk, dv = torch.autograd.grad(out, leaves, dout)
+    scale = shape[-1] ** -0.5
+    # (a row's largest is 1 at least, where the bound allows for 4 everywhere)
+    assert each.abs().amax(-1).min() >= 1 and each.abs().max() <= 4
+    exact, bound = _formulas(torch, q, k, v, valid, scale, "f16", each)[1]
+    off = ((dq.double() - by * exact).abs() - by * bound - 2.0 ** -25) / by
+    assert bool((off <= 0).all()), (shape, float(off.max()), off.amax((0, 2, 3))[:15].tolist())
+    wanted = _formulas(torch, q, k, v, valid, scale, "f16", dout)
+    _assert_within([out.detach()], wanted[:1], shape)
+    _assert_within([dk, dv], wanted[2:], shape)
