@@ -43,8 +43,9 @@ struct Args {
     char *dk, *dv;
     float *lse;             // [batch, kv_heads, rows]
     float *partial;         // [splits][batch, kv_heads][rows][dim], then the splits' lse [splits][batch, kv_heads][rows]
-    // backward: of each row, padded to whole tiles of 64, its lse and sum over channels of dout out; the largest |dout| of each 64
-    float *row_lse, *row_delta, *row_most;
+    // backward: of each row, padded to whole tiles of 64, its lse and sum over channels of dout out; float16: of each 64 rows the largest |dout| and
+    // the largest |sum|, of each 32 keys the largest sum over channels of v^2
+    float *row_lse, *row_delta, *row_most, *value_most;
     int32_t padded;         // rows with the padding
     int32_t even_q, even_dout; // places of a tile's rows in q and dout in 32 bits
     int32_t splits, tiles_per_split; // (splits: the workers, where the groups of keys are dealt out; the most parts, in the keys' gradients)

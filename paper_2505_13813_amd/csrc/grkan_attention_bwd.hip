@@ -13,9 +13,12 @@
 // reaches 1,500; rows 15, sums 24.  32 x 256 queries, 785 keys, 12 heads of 64, bfloat16: 80 and 51.
 //
 // float16: S' of a small upstream gradient would be below its range.  The products take 2^e S', with e such that the largest |dO| becomes 1/4 to
-// 1/2 (2^e S' then stays below 65,504 for values of up to 1,000), and the sums are scaled back in float32.  For dQ it is the largest of the row, which
+// 1/2, and the sums are scaled back in float32.  For dQ it is the largest of the row, which
 // no other row has a part in: with one e for all, a row 2^-12 as large as the largest was off by 6 % (4,001 keys of 128 channels; 0.03 % so).  For dK, a sum
-// over rows, it is the largest of the key head.
+// over rows, it is the largest of the key head.  |S'| is at most |D| + |delta|, and |D| at most sqrt(dim) max |dO| times the value's length: where that
+// passes half of the type's range (values from some 250 on in all of 128 channels), e is lowered, for dK by the key's own value, for dQ by the key
+// head's longest one, which the keys' kernel leaves.  (Without that, values of 20,000 and a third of a row's probability made S' infinite.
+// 32 x 256 queries, 785 keys, 12 heads of 64 with a mask, float16, forward and backward: 168 us without, 170 so.)
 #include <hip/hip_runtime.h>
 
 #include "grkan_attention.h"
@@ -76,6 +79,26 @@ __device__ __forceinline__ void load_words_to_lds(uint64_t base, uint32_t lane_o
     asm volatile("s_nop 4\n\tglobal_load_lds_dword %1, %2" : : "{m0}"(lds_at), "v"(lane_off), "s"(base) : "memory");
 }
 
+// The largest of a wavefront's numbers (none negative), as bits, in all lanes.  (In registers: the keys' kernel has three of these in front of a walk
+// that may be short.  4 x 64 queries, 16,000 keys, eight heads of 128 that read two, float16: 150 us with shuffles through LDS and more loads, 145 so.)
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t bits)
+{
+    auto with = [&](uint32_t o) { bits = o > bits ? o : bits; };
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)bits, 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2 of four
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)bits, 0x4e, 0xf, 0xf, true));  // 2 3 0 1
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)bits, 0x141, 0xf, 0xf, true)); // eight mirrored
+    with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)bits, 0x140, 0xf, 0xf, true)); // sixteen mirrored
+    const auto rows = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    bits = rows[0] > rows[1] ? rows[0] : rows[1];
+    const auto halves = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    return halves[0] > halves[1] ? halves[0] : halves[1];
+}
+__device__ __forceinline__ uint32_t greater(uint32_t bits, float v)
+{
+    const uint32_t o = __builtin_bit_cast(uint32_t, v);
+    return o > bits ? o : bits;
+}
+
 // float16: delta, and copies of lse, of 64 rows for each workgroup: sixteen lanes a row, eight channels each.  (bfloat16, which is not scaled, needs no launch in
 // front: the queries' kernel has the rows of dO in its registers, reads those of O once, and leaves both for the keys' kernel behind it.  32 x 256 queries of
 // 12 heads of 64, 785 keys and a mask, forward and all gradients: 158 us in the place of 164.)
@@ -83,7 +106,7 @@ template <typename IO> constexpr bool kRowsFirst = !__is_same(IO, __bf16);
 template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const Args a)
 {
     using MM = Matrix<IO>;
-    __shared__ uint32_t most[4];
+    __shared__ uint32_t most[4][2];
     const int32_t tiles = a.padded / kRowTile;
     const int32_t bh = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - bh * tiles;
     const int32_t b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
@@ -93,7 +116,7 @@ template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const 
     const uint64_t dout = a.dout.at + (uint64_t)(b * a.dout.batch + (int64_t)kvh * a.group * a.dout.head);
     const uint32_t row0 = (uint32_t)tile * kRowTile + (threadIdx.x >> 4);
     u32x4 o[4], d[4];
-    float lse[4], largest = 0.0f;
+    float lse[4], largest = 0.0f, sums = 0.0f;
     // (all loads in front, without a branch: they wait for one another otherwise)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -118,25 +141,24 @@ template <typename IO> __global__ __launch_bounds__(256) void rows_kernel(const 
 #pragma unroll
         for (int s = 8; s > 0; s /= 2)
             sum += __shfl_xor(sum, s);
+        sums = fmaxf(sums, fabsf(sum));
         if (lane16 == 0) {
             const int64_t at = (int64_t)bh * a.padded + row;
             a.row_lse[at] = (int64_t)row < a.rows ? lse[k] : __builtin_inff();
             a.row_delta[at] = sum;
         }
     }
-    uint32_t bits = __builtin_bit_cast(uint32_t, largest);
-#pragma unroll
-    for (int s = 32; s > 0; s /= 2) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)bits, s);
-        bits = o > bits ? o : bits;
+    const uint32_t bits[2] = {most_of_lanes(__builtin_bit_cast(uint32_t, largest)), most_of_lanes(__builtin_bit_cast(uint32_t, sums))};
+    if ((threadIdx.x & 63) == 0) {
+        most[threadIdx.x >> 6][0] = bits[0];
+        most[threadIdx.x >> 6][1] = bits[1];
     }
-    if ((threadIdx.x & 63) == 0)
-        most[threadIdx.x >> 6] = bits;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w)
-            bits = most[w] > bits ? most[w] : bits;
-        a.row_most[(int64_t)bh * tiles + tile] = __builtin_bit_cast(float, bits);
+    if (threadIdx.x < 2) {
+        uint32_t all = 0;
+        for (int w = 0; w < 4; ++w)
+            all = most[w][threadIdx.x] > all ? most[w][threadIdx.x] : all;
+        a.row_most[2 * ((int64_t)bh * tiles + tile) + threadIdx.x] = __builtin_bit_cast(float, all);
     }
 }
 
@@ -148,25 +170,13 @@ __device__ __forceinline__ float scale_of(uint32_t bits)
     return bits == 0 || e > 17 ? 1.0f : __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
 }
 
-// of a key head (1 for bfloat16)
-template <typename IO> __device__ __forceinline__ float gradient_scale(const Args &a, int32_t bh)
+// 2^e lowered, where what it multiplies may pass 32,768 otherwise: sqrt(dim) / 2 for each unit of a value's length (squared: length2), and `up` sums
+// (where they are not finite: not)
+__device__ __forceinline__ float lowered(float up, float length2, float sums, int32_t dim)
 {
-    if constexpr (sizeof(IO) == 2 && __is_same(IO, __bf16)) {
-        return 1.0f;
-    } else {
-        const int32_t tiles = a.padded / kRowTile;
-        uint32_t bits = 0;
-        for (int32_t i = (int32_t)threadIdx.x & 63; i < tiles; i += 64) {
-            const uint32_t o = __builtin_bit_cast(uint32_t, a.row_most[(int64_t)bh * tiles + i]);
-            bits = o > bits ? o : bits;
-        }
-#pragma unroll
-        for (int s = 32; s > 0; s /= 2) {
-            const uint32_t o = (uint32_t)__shfl_xor((int)bits, s);
-            bits = o > bits ? o : bits;
-        }
-        return scale_of(bits);
-    }
+    const float most = 0.5f * sqrtf(length2 * (float)dim) + up * sums;
+    const int e = (int)(__builtin_bit_cast(uint32_t, most) >> 23) - 127 - 15; // 2^(e + 15) .. 2^(e + 16)
+    return e < 0 || e > 100 ? up : up * __builtin_bit_cast(float, (uint32_t)(127 - (e + 1)) << 23);
 }
 
 // ROWS: of a stage of the keys' kernel.  V_LDS: that kernel reads V from LDS at every use; its registers hold K and the sums alone.
@@ -270,7 +280,35 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void keys_kernel(
     const RowLoads<DP, ROWS, SH::kWaves> q_loads(wave, lane, a.q, q_base, a.even_q && ROWS % a.group == 0, a),
         d_loads(wave, lane, a.dout, d_base, a.even_dout && ROWS % a.group == 0, a);
     const bool works = key0 < count; // (a wavefront without keys loads for the others)
-    const float up = gradient_scale<IO>(a, bh), c = a.c;
+    const float c = a.c;
+    float up = 1.0f; // of the key
+    if constexpr (kRowsFirst<IO>) {
+        u32x4 value[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const uint32_t channel = 16u * s + 8u * h;
+            const bool there = valid && channel < (uint32_t)a.dim;
+            value[s] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        }
+        const int32_t row_tiles = a.padded / kRowTile;
+        uint32_t largest = 0, sums = 0;
+        for (int32_t i = lane; i < row_tiles; i += 64) {
+            const f32x2 both = reinterpret_cast<const f32x2 *>(a.row_most)[(int64_t)bh * row_tiles + i];
+            largest = greater(largest, both[0]);
+            sums = greater(sums, both[1]);
+        }
+        float length2 = 0.0f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                length2 += MM::first(value[s][j]) * MM::first(value[s][j]) + MM::second(value[s][j]) * MM::second(value[s][j]);
+        length2 = halves_sum(length2);
+        up = lowered(scale_of(most_of_lanes(largest)), length2, __builtin_bit_cast(float, most_of_lanes(sums)), a.dim);
+        const uint32_t longest = most_of_lanes(__builtin_bit_cast(uint32_t, length2) & 0x7fffffffu);
+        if (lane == 0) // (the same by all that share the group)
+            a.value_most[((int64_t)bh * a.key_tiles + key_tile) * SH::kWaves + wave] = __builtin_bit_cast(float, longest);
+    }
 
     auto issue = [&](int32_t t, uint32_t stage) {
         const uint32_t row0 = (uint32_t)t * ROWS;
@@ -472,6 +510,15 @@ template <class SH> __global__ __launch_bounds__(256, 2) void queries_kernel(con
             for (int j = 0; j < 4; ++j)
                 largest = fmaxf(largest, fmaxf(fabsf(MM::first(o[s][j])), fabsf(MM::second(o[s][j]))));
         up = scale_of(__builtin_bit_cast(uint32_t, halves_max(largest)));
+        const int32_t groups = Deal::groups_of(keys_of(a, b));
+        uint32_t longest = 0;
+        for (int32_t i = lane; i < groups; i += 64) {
+            const f32x4 values = reinterpret_cast<const f32x4 *>(a.value_most)[(int64_t)bh * a.key_tiles + i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                longest = greater(longest, values[j]);
+        }
+        up = lowered(up, __builtin_bit_cast(float, most_of_lanes(longest)), there ? fabsf(a.row_delta[(int64_t)bh * a.padded + row]) : 0.0f, a.dim);
     }
     float lse = there ? a.lse[(int64_t)bh * a.rows + row] : __builtin_inff();
     float delta = 0.0f;
@@ -651,7 +698,7 @@ template <typename IO> static BackVariant pick(int32_t dim)
 struct BackPlan {
     BackVariant v;
     Args keys, queries;
-    size_t stats, partial; // elements of the workspace
+    size_t value_most, stats, partial; // elements of the workspace: up to the values' lengths, up to the parts, of the parts
 };
 
 static BackPlan back_plan(const Args &a, grkan_dtype_t io)
@@ -662,7 +709,7 @@ static BackPlan back_plan(const Args &a, grkan_dtype_t io)
     const int64_t heads = (int64_t)a.batch * a.kv_heads;
     const int32_t padded = (int32_t)((a.rows + kRowTile - 1) / kRowTile) * kRowTile;
     p.keys.padded = p.queries.padded = padded;
-    p.keys.key_tiles = (int32_t)((a.keys + p.v.own - 1) / p.v.own);
+    p.keys.key_tiles = p.queries.key_tiles = (int32_t)((a.keys + p.v.own - 1) / p.v.own);
     p.queries.row_tiles = (int32_t)((a.rows + p.v.own - 1) / p.v.own);
     // Groups of keys that do not fill the device: their walks are shared.  How many of the groups have keys, and so how many share one, the kernel
     // knows, or the host where there are no lengths.
@@ -683,7 +730,9 @@ static BackPlan back_plan(const Args &a, grkan_dtype_t io)
     p.queries.splits = (int32_t)((key_tiles + p.queries.tiles_per_split - 1) / p.queries.tiles_per_split);
     if (p.queries.splits < 1)
         p.queries.splits = 1;
-    p.stats = (size_t)heads * (size_t)padded * 2 + (((size_t)heads * (size_t)(padded / kRowTile) + 3) & ~(size_t)3);
+    static_assert(kGroup == 4 * 32, ""); // (a group's lengths are read at once)
+    p.value_most = (2 * (size_t)heads * (size_t)padded + 2 * (size_t)heads * (size_t)(padded / kRowTile) + 3) & ~(size_t)3;
+    p.stats = p.value_most + 4 * (size_t)heads * (size_t)p.keys.key_tiles;
     // (one after the other: they share the memory)
     const size_t of_keys = 2 * (size_t)p.keys.splits * kGroup * (size_t)a.dim;
     const size_t of_rows = p.queries.splits > 1 ? (size_t)p.queries.splits * (size_t)heads * (size_t)a.rows * (size_t)a.dim : 0;
@@ -716,20 +765,29 @@ template <typename IO> static grkan_status_t backward(const BackPlan &p, hipStre
         if (rows_grid > 0)
             rows_kernel<IO><<<dim3((unsigned)rows_grid), 256, 0, stream>>>(k);
     }
-    if (row_work > 0) {
+    auto queries = [&] {
+        if (row_work == 0)
+            return true;
         void *args[] = {&q};
         if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.queries), dim3((unsigned)row_grid), dim3(256), args, p.v.queries_lds, stream) != hipSuccess)
-            return GRKAN_ERR_LAUNCH;
+            return false;
         if (q.splits > 1)
             sum_kernel<IO><<<dim3((unsigned)row_blocks), 256, 0, stream>>>(q.partial, q.splits, row_elements, q.out);
-    }
-    if (key_work > 0) {
+        return true;
+    };
+    auto keys = [&] {
+        if (key_work == 0)
+            return true;
         void *args[] = {&k};
         if (hipLaunchKernel(reinterpret_cast<const void *>(p.v.keys), dim3((unsigned)key_grid), dim3(256), args, p.v.keys_lds, stream) != hipSuccess)
-            return GRKAN_ERR_LAUNCH;
+            return false;
         if (k.splits)
             sum_keys_kernel<IO><<<dim3((unsigned)(8 * groups)), 256, 0, stream>>>(k, (int32_t)((k.rows + p.v.rows - 1) / p.v.rows));
-    }
+        return true;
+    };
+    // each needs what the other leaves: the lengths of the values, or the rows' statistics
+    if (kRowsFirst<IO> ? !keys() || !queries() : !queries() || !keys())
+        return GRKAN_ERR_LAUNCH;
     return hipGetLastError() == hipSuccess ? GRKAN_OK : GRKAN_ERR_LAUNCH;
 }
 
@@ -769,6 +827,7 @@ extern "C" grkan_status_t grkan_attention_bwd(const grkan_attention_t *at, const
         to->row_lse = static_cast<float *>(workspace);
         to->row_delta = to->row_lse + padded;
         to->row_most = to->row_delta + padded;
+        to->value_most = to->row_lse + p.value_most;
         to->partial = to->row_lse + p.stats;
         to->dk = static_cast<char *>(dk);
         to->dv = static_cast<char *>(dv);

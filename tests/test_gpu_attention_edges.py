@@ -119,3 +119,44 @@ def test_float16_gradients_of_rows_of_different_sizes(shape):
     wanted = _formulas(torch, q, k, v, valid, scale, "f16", dout)
     _assert_within([out.detach()], wanted[:1], shape)
     _assert_within([dk, dv], wanted[2:], shape)
+
+
+@pytest.mark.parametrize("shape", [(2, 40, 3, 2, 1, 128), (1, 40, 200, 1, 1, 128), (2, 200, 130, 2, 2, 64), (1, 33, 40, 3, 3, 24)])
+@pytest.mark.parametrize("size", [300.0, 3000.0, 20000.0])
+@pytest.mark.parametrize("masked", [False, True])
+def test_float16_gradients_with_large_values(masked, size, shape):
+    """Values of thousands whose channels agree in sign, and a small loss: its gradients are in float16's range, and what they are summed
+    of stays in it as well.  Beside the bound: the terms' steps of 2^-24 are those of at most
+    4 max |dO| max(1, 2 sqrt(dim) max |v_j| / 32768) times a number below 1."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import cross_attention
+
+    batch, queries, keys, heads, kv, dim = shape
+    q, k, _, _, _, valid = _operands(torch, shape, "f16", "none")
+    q = q / 4
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(24)
+
+    def spread(*shape):
+        return 0.5 + torch.rand(*shape, generator=gen, device="cuda:0")
+
+    sign = torch.where(torch.arange(keys, device="cuda:0") % 2 == 0, 1.0, -1.0)[None, :, None, None]
+    v = (size * sign * spread(batch, keys, kv, dim)).half()
+    dout = (0.02 / size * spread(*q.shape)).half()
+    mask = None
+    if masked:  # every third key, NaN and infinities there
+        mask = torch.arange(keys, device="cuda:0").remainder(3)[None].repeat(batch, 1) != 2
+        valid, k, v = mask, k.clone(), v.clone()
+        k[:, 2::3], v[:, 2::3] = math.nan, math.inf
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    out = cross_attention(*leaves, key_mask=mask)
+    got = (out.detach(),) + torch.autograd.grad(out, leaves, dout)
+    assert all(bool(t.isfinite().all()) for t in got), [int((~t.isfinite()).sum()) for t in got]
+    scale = dim ** -0.5
+    wanted = _formulas(torch, q, k, v, valid, scale, "f16", dout)
+    step = 2.0 ** -25 * 4 * float(dout.max()) * max(1.0, 2 * dim ** 0.5 * float(v[valid].double().norm(dim=-1).max()) / 32768) * scale
+    group = heads // kv
+    more = [0.0, step * torch.where(valid[..., None, None], k, 0).double().abs().sum(1, keepdim=True).repeat_interleave(group, 2),
+            step * q.double().abs().sum(1, keepdim=True).unflatten(2, (kv, group)).sum(3), 0.0]
+    _assert_within(got, [(exact, bound + m) for (exact, bound), m in zip(wanted, more)], (shape, size))
