@@ -363,6 +363,7 @@ std::optional<variable_list> rotary(const Tensor &q, const Tensor &positions, co
     const Tensor kt = of_optional(k), kp = of_optional(k_positions);
     if (!takes({&q, &positions, &frequencies, &axis, &kt, &kp}))
         return std::nullopt;
+    TORCH_CHECK(!recorded({&positions, &frequencies, &kp}), "positions and frequencies have no gradient: detach them, or call without one (torch.no_grad())");
     TORCH_CHECK_VALUE(!kt.defined() == !kp.defined(), "k and its positions come together");
     if (recorded({&q, &kt}))
         return Rotary::apply(q, positions, frequencies, axis, k, k_positions, interleaved);

@@ -89,7 +89,7 @@ def rotary(q, positions, frequencies, axis, k=None, k_positions=None, interleave
     q (and k) [batch, tokens, heads, dim], any strides with dense channels; positions (of q, and of k where no k_positions
     are given) [tokens, axes] or [batch, tokens, axes], int32, int64 or float32.  A pair is channels (j, pairs + j) or, interleaved,
     (2 j, 2 j + 1); channels behind the pairs are copied.  Entries of `axis` are below `axes`.  Returns q, or (q, k) from one
-    launch, contiguous.  Differentiable (once) with respect to q and k."""
+    launch, contiguous.  Differentiable (once) with respect to q and k; positions or frequencies that want a gradient are refused."""
     if k is not None and k_positions is None:
         k_positions = positions
     out = _taken(binding.load_native().rotary(q, positions, frequencies, axis, k, k_positions, bool(interleaved)), "rotary")

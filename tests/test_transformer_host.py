@@ -239,3 +239,20 @@ def test_more_workgroups_than_a_launch_takes(lib):
     t = binding.RotaryOperand(x=16, out=16, positions=16, batch=1, tokens=many, heads=12, batch_stride=0, token_stride=960, head_stride=80,
                               position_batch_stride=0, position_token_stride=1, positions_dtype=0)
     assert lib.grkan_rotary(ctypes.byref(t), 1, 16, 16, 13, 1, 80, 0, 0, BF16, None) == UNSUPPORTED
+
+
+def test_positions_and_frequencies_have_no_gradient():
+    """What has none is refused where it would be wanted, and taken where it is not (and then refused for lying on the CPU)."""
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    q = torch.zeros(1, 4, 2, 64)
+    p, (f, axis) = T.grid_positions(4).float(), T.rotary_frequencies((8,))
+    for x in (q, q.clone().requires_grad_()):
+        for bad in ((x, p, f.clone().requires_grad_(), axis), (x, p.clone().requires_grad_(), f, axis),
+                    (x, p, f, axis, q, p.clone().requires_grad_())):
+            with pytest.raises(RuntimeError, match="no gradient"):
+                T.rotary(*bad)
+            with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+                T.rotary(*bad)
