@@ -196,12 +196,12 @@ class KATCrossBlock(nn.Module):
 
 class KATCrossDecoder(nn.Module):
     """KATCrossBlocks one behind the other, and a norm: queries [batch, tokens, dim] to an encoder's states
-    [batch, keys, context_dim]."""
+    [batch, keys, context_dim].  `eps` is that of every norm."""
 
-    def __init__(self, depth: int, dim: int, heads: int, **block):
+    def __init__(self, depth: int, dim: int, heads: int, *, eps: float = 1e-6, **block):
         super().__init__()
-        self.blocks = nn.ModuleList(KATCrossBlock(dim, heads, **block) for _ in range(depth))
-        self.norm = RMSNorm(dim)
+        self.blocks = nn.ModuleList(KATCrossBlock(dim, heads, eps=eps, **block) for _ in range(depth))
+        self.norm = RMSNorm(dim, eps)
 
     def cached(self, context, positions=None):
         """What forward(cache=...) takes: the keys and values of every block."""

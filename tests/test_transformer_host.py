@@ -256,3 +256,11 @@ def test_positions_and_frequencies_have_no_gradient():
                 T.rotary(*bad)
             with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
                 T.rotary(*bad)
+
+
+def test_the_decoder_has_one_eps():
+    from paper_2505_13813_amd.transformer import KATCrossDecoder
+
+    for given, eps in (({}, 1e-6), ({"eps": 1e-3}, 1e-3)):
+        m = KATCrossDecoder(2, 64, 2, groups=4, **given)
+        assert [n.eps for b in m.blocks for n in (b.norm1, b.norm2)] + [m.norm.eps] == [eps] * 5
