@@ -146,7 +146,8 @@ class KATCrossBlock(nn.Module):
     returns (branch, stream), the value being their sum; stream None means that branch is the value.
 
     Parameters and inputs are bfloat16 or float16, or float32 under autocast to one of the two, which keeps the stream in float32.
-    `rotary_pairs`: rotated channel pairs of each head for each axis of the positions; none: no rotation.  `context_dim`: channels of
+    `rotary_pairs`: rotated channel pairs of each head for each axis of the positions; none: no rotation.  With rotation the tokens'
+    positions are given and, with a context, the context's own.  `context_dim`: channels of
     the encoder's states (default: dim)."""
 
     def __init__(self, dim: int, heads: int, kv_heads: Optional[int] = None, context_dim: Optional[int] = None,
@@ -164,6 +165,11 @@ class KATCrossBlock(nn.Module):
         self.norm2 = RMSNorm(dim, eps)
         self.mlp = KATMlp(dim, hidden, groups)
 
+    def _positions(self, **given):
+        for name, positions in given.items():
+            if self.rotary is not None and positions is None:
+                raise ValueError("a block with rotation needs %s" % name)
+
     def keys_values(self, context):
         """(k, v) [batch, keys, kv_heads, head_dim] of the encoder's states, not rotated yet."""
         kv = self.to_kv(context).unflatten(-1, (2, self.kv_heads, self.head_dim))
@@ -172,6 +178,7 @@ class KATCrossBlock(nn.Module):
     def cached(self, context, positions=None):
         """(k, v) as forward(keys_values=...) takes them: made once where single tokens attend to the same states again and
         again."""
+        self._positions(positions=positions)
         k, v = self.keys_values(context)
         if self.rotary is not None:
             k = self.rotary(k, positions)
@@ -179,6 +186,10 @@ class KATCrossBlock(nn.Module):
 
     def forward(self, branch, context=None, stream=None, positions=None, context_positions=None, key_lengths=None,
                 key_mask=None, keys_values=None):
+        if keys_values is None:
+            self._positions(positions=positions, context_positions=context_positions)
+        else:
+            self._positions(positions=positions)
         y, x = (self.norm1(branch), branch) if stream is None else self.norm1(branch.to(stream.dtype), stream)
         q = self.to_q(y).unflatten(-1, (self.heads, self.head_dim))
         if keys_values is not None:

@@ -264,3 +264,20 @@ def test_the_decoder_has_one_eps():
     for given, eps in (({}, 1e-6), ({"eps": 1e-3}, 1e-3)):
         m = KATCrossDecoder(2, 64, 2, groups=4, **given)
         assert [n.eps for b in m.blocks for n in (b.norm1, b.norm2)] + [m.norm.eps] == [eps] * 5
+
+
+def test_a_block_with_rotation_wants_all_positions():
+    """An encoder's states are never turned by the queries' positions."""
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    m = T.KATCrossDecoder(1, 64, 2, groups=4, rotary_pairs=(8,))
+    x, at = torch.zeros(1, 4, 64), T.grid_positions(4)
+    for call in (lambda: m(x, x, at), lambda: m.blocks[0](x, x, None, at)):
+        with pytest.raises(ValueError, match="context_positions"):
+            call()
+    cache = [(x, x)]
+    for call in (lambda: m(x, x, None, at), lambda: m(x, cache=cache), lambda: m.cached(x), lambda: m.blocks[0].cached(x)):
+        with pytest.raises(ValueError, match=r"\bpositions\b"):
+            call()
