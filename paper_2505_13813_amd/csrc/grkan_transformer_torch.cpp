@@ -102,6 +102,19 @@ template <typename Compute> variable_list gradients(const variable_list &operand
     return found;
 }
 
+// The arguments of an entry, by name: what is no tensor is a TypeError, and not one of the calls that are not taken.
+struct Operands : Arguments {
+    Tensor tensor(pybind11::handle h, const char *name)
+    {
+        TORCH_CHECK_TYPE(THPVariable_Check(h.ptr()), name, " must be a tensor, got ", h.is_none() ? "None" : Py_TYPE(h.ptr())->tp_name);
+        return Arguments::tensor(h);
+    }
+    OptionalTensor optional(pybind11::handle h, const char *name)
+    {
+        return h.is_none() ? std::nullopt : OptionalTensor(tensor(h, name));
+    }
+};
+
 // ------------------------------------------------------------------------------------------------ norm
 
 // t [..., D] as rows a constant number of elements apart; a copy where it is none.
@@ -535,27 +548,28 @@ void define_transformer(pybind11::module_ &mod)
 {
     using pybind11::handle;
     mod.def("rms_norm", [](handle x_, handle weight_, handle residual_, double eps) {
-        Arguments args;
-        const Tensor x = args.tensor(x_), weight = args.tensor(weight_);
-        const OptionalTensor residual = args.optional(residual_);
+        Operands args;
+        const Tensor x = args.tensor(x_, "x"), weight = args.tensor(weight_, "weight");
+        const OptionalTensor residual = args.optional(residual_, "residual");
         return args.call([&] { return rms_norm(x, weight, residual, eps); });
     });
     mod.def("rms_norm_8bit", [](handle x_, handle weight_, handle residual_, double eps) {
-        Arguments args;
-        const Tensor x = args.tensor(x_), weight = args.tensor(weight_);
-        const OptionalTensor residual = args.optional(residual_);
+        Operands args;
+        const Tensor x = args.tensor(x_, "x"), weight = args.tensor(weight_, "weight");
+        const OptionalTensor residual = args.optional(residual_, "residual");
         return args.call([&] { return rms_norm_8bit(x, weight, residual, eps); });
     });
     mod.def("rotary", [](handle q_, handle positions_, handle frequencies_, handle axis_, handle k_, handle k_positions_, bool interleaved) {
-        Arguments args;
-        const Tensor q = args.tensor(q_), positions = args.tensor(positions_), frequencies = args.tensor(frequencies_), axis = args.tensor(axis_);
-        const OptionalTensor k = args.optional(k_), k_positions = args.optional(k_positions_);
+        Operands args;
+        const Tensor q = args.tensor(q_, "q"), positions = args.tensor(positions_, "positions");
+        const Tensor frequencies = args.tensor(frequencies_, "frequencies"), axis = args.tensor(axis_, "axis");
+        const OptionalTensor k = args.optional(k_, "k"), k_positions = args.optional(k_positions_, "k_positions");
         return args.call([&] { return rotary(q, positions, frequencies, axis, k, k_positions, interleaved); });
     });
     mod.def("cross_attention", [](handle q_, handle k_, handle v_, handle lengths_, handle mask_, std::optional<double> scale) {
-        Arguments args;
-        const Tensor q = args.tensor(q_), k = args.tensor(k_), v = args.tensor(v_);
-        const OptionalTensor lengths = args.optional(lengths_), mask = args.optional(mask_);
+        Operands args;
+        const Tensor q = args.tensor(q_, "q"), k = args.tensor(k_, "k"), v = args.tensor(v_, "v");
+        const OptionalTensor lengths = args.optional(lengths_, "key_lengths"), mask = args.optional(mask_, "key_mask");
         return args.call([&] { return cross_attention(q, k, v, lengths, mask, scale); });
     });
 }

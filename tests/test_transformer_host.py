@@ -281,3 +281,20 @@ def test_a_block_with_rotation_wants_all_positions():
     for call in (lambda: m(x, x, None, at), lambda: m(x, cache=cache), lambda: m.cached(x), lambda: m.blocks[0].cached(x)):
         with pytest.raises(ValueError, match=r"\bpositions\b"):
             call()
+
+
+def test_missing_operands_are_named():
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    x, w, q = torch.zeros(4, 64), torch.ones(64), torch.zeros(1, 4, 2, 64)
+    p, (f, axis) = T.grid_positions(4), T.rotary_frequencies((8,))
+    for call, name in ((lambda: T.rms_norm(None, w), "x"), (lambda: T.rms_norm(x, None), "weight"), (lambda: T.rms_norm(x, w, 1.0), "residual"),
+                       (lambda: T.rms_norm_8bit(x, w.tolist()), "weight"), (lambda: T.rotary(None, p, f, axis), "q"),
+                       (lambda: T.rotary(q, None, f, axis), "positions"), (lambda: T.rotary(q, p, None, axis), "frequencies"),
+                       (lambda: T.rotary(q, p, f, [0] * 8), "axis"), (lambda: T.rotary(q, p, f, axis, q, [[0]]), "k_positions"),
+                       (lambda: T.cross_attention(q, None, q), "k"), (lambda: T.cross_attention(q, q, None), "v"),
+                       (lambda: T.cross_attention(q, q, q, [4]), "key_lengths"), (lambda: T.cross_attention(q, q, q, None, [True]), "key_mask")):
+        with pytest.raises(TypeError, match=r"^%s must be a tensor" % name):
+            call()
