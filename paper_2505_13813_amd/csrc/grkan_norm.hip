@@ -151,7 +151,8 @@ template <class SH, typename W, bool RESIDUAL, bool EIGHT> __global__ __launch_b
         // stay in range.)
         float unit = 1.0f, factor = 0.0f, remainder = 0.0f;
         if constexpr (EIGHT) {
-            unit = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) & 0x7f800000u);
+            // (s is infinite for a row of zeros, where eps is 0)
+            unit = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, fminf(s, 0x1p126f)) & 0x7f800000u);
             // magnitudes as whole numbers: a NaN is the largest
             uint32_t most = 0;
 #pragma unroll
@@ -166,7 +167,8 @@ template <class SH, typename W, bool RESIDUAL, bool EIGHT> __global__ __launch_b
                     }
                 }
             }
-            const float largest = __builtin_bit_cast(float, row_max<SH>(most, shared, slot)), amax = largest * (s / unit);
+            const float largest = __builtin_bit_cast(float, row_max<SH>(most, shared, slot));
+            const float amax = largest == 0.0f && s == __builtin_inff() ? 0.0f : largest * (s / unit);
             const float scale = amax < __builtin_inff() ? amax / kMost8 : __builtin_nanf("");
             if (scale != scale) {
                 factor = scale;

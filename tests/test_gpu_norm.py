@@ -128,6 +128,26 @@ def test_8_bits_of_special_rows():
         assert scale[row] > 0 and ((found - y).abs() <= 2.0 ** -4 * y.abs() + 2.0 ** -9 * scale[row].double()).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [5, 768, 5000])
+def test_8_bits_of_zeros_without_eps(D, dtype):
+    """With eps 0, too, a row of zeros has scale 0 and zeros; the others as with an eps that does not matter (float32 sums of a row, and one
+    rounding)."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import rms_norm_8bit
+
+    x, _, w = _operands(torch, 6, D, dtype)
+    x[::2] = 0.0
+    q, scale = rms_norm_8bit(x, w, eps=0.0)
+    assert (scale[::2] == 0).all() and (q[::2].float() == 0).all()
+    h, w64 = x[1::2].double(), w.double()
+    y = h / h.square().mean(-1, keepdim=True).sqrt() * w64
+    exact = y.abs().amax(-1) / 448
+    assert ((scale[1::2].double() - exact).abs() <= (SUM + 2.0 ** -22) * exact).all()
+    assert torch.equal(q[1::2].float(), rms_norm_8bit(x, w, eps=1e-30)[0][1::2].float())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_and_alignment(dtype):
     """Rows apart, rows off 16-byte boundaries, and layouts that are copied: the same bits as from contiguous tensors."""
