@@ -8,9 +8,10 @@
 // delta is made by the queries' kernel, or in front of both by a small one.
 //
 // Bound by the products and the vector operations between them (two fused multiply-adds, an exponential and a rounding for each score), of which little
-// runs at once: the matrix units are busy for 42 % (keys) and 53 % (queries) of the time with 128 channels, 25 and 33 % with 64.  2 x 4096 queries, 4,001 and 1,808
-// keys, 16 heads of 128 that read four, float16: keys' kernel 459 us = 850 TFLOP/s, queries' 297 us = 985, where a large library product
-// reaches 1,500; rows 15, sums 24.  32 x 256 queries, 785 keys, 12 heads of 64, bfloat16: 80 and 51.
+// runs at once, and waiting for the next stage: the matrix units are busy for 42 % (keys) and 53 % (queries) of the time with 128 channels, 26 and 30 % with 64, and the
+// wavefronts wait for 51, 41, 39 and 34 %.  2 x 4096 queries, 4,001 and 1,808 keys, 16 heads of 128 that read four, float16: keys' kernel 459 - 472 us = 830 - 850
+// TFLOP/s, queries' 297 - 307 us = 950 - 985, where a large library product reaches 1,500; rows 15, sums 24.  32 x 256 queries, 785 keys, 12 heads of 64,
+// bfloat16: 80 - 84 and 51 - 55.
 //
 // float16: S' of a small upstream gradient would be below its range.  The products take 2^e S', with e such that the largest |dO| becomes 1/4 to
 // 1/2, and the sums are scaled back in float32.  For dQ it is the largest of the row, which

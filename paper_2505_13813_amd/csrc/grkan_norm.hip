@@ -7,7 +7,9 @@
 // stays in registers from the sum of squares to the store: one wavefront has a row of up to 2,048 elements (1,024 in float32), four
 // wavefronts one of up to 8,192 (4,096), sixteen a longer one.  A row whose length is no multiple of the vector ends in a vector that
 // repeats elements of the one before: they are stored twice with the same value and counted once.  (25,216 x 768 in bfloat16 with a
-// residual: forward 28.5 us = 5.4 TB/s, where a large copy reaches 5.5; 16,384 x 4096 to 8 bits 82 us = 5.7 TB/s.)
+// residual: forward 28.5 us = 5.4 TB/s, where a large copy reaches 5.5; 16,384 x 4096 to 8 bits 82 us = 5.7 TB/s.
+// float32, 4,096 x 8192 with a residual, sixteen wavefronts: forward 94 us = 5.7 TB/s, backward, which spills two registers there, 112 = 4.8; 8,192 x 4096 with
+// four, which does not spill, 88 and 115.)
 //
 // The weights' gradient is a sum over rows: a lane has the same columns in every row it visits and keeps their sums in registers; each
 // workgroup leaves one row of sums in the workspace, and a second launch adds those in a fixed order.  (25,216 x 768: 28 to 32 us for
