@@ -143,6 +143,105 @@ grkan_status_t grkan_attention_bwd(const grkan_attention_t *attention, const voi
                                    void *dk, void *dv, void *workspace, size_t workspace_bytes, grkan_dtype_t io,
                                    void *hip_stream);
 
+/*
+ * Causal attention over sequences that lie packed one behind the other: a token attends to the tokens of its own sequence up to itself.
+ * With head h of the queries reading head h div (heads / kv_heads) of the keys and values, and j up to i in the same sequence:
+ *
+ *     P_ij = exp(scale q_i k_j) / (sum over j of exp(scale q_i k_j))         out_i = sum over j of P_ij v_j
+ *
+ *   q  [tokens, heads, dim] of io; k, v [tokens, kv_heads, dim]; strides of token and head, each a multiple of 8 elements, and 16-byte aligned
+ *      pointers (else GRKAN_ERR_ALIGN)
+ *   offsets  DEVICE int32 (int64 with offsets_64) [sequences + 1], not falling: sequence s has tokens offsets[s] up to, not with, offsets[s + 1].
+ *      Sequences may be empty; tokens in front of the first and behind the last belong to none: zeros come out, and their gradients are zeros.  What lies
+ *      past 0 .. tokens is clamped to it; where offsets fall, what comes out for the tokens between is unspecified.
+ *      NULL: `sequences` of the same length, tokens / sequences (else GRKAN_ERR_SHAPE).
+ *   out [tokens, heads, dim] of io, contiguous, 16-byte aligned
+ *   lse NULL, or float32 [kv_heads, tokens, heads / kv_heads] (grkan_causal_attention_lse_count() elements), for the backward pass: log2 of the sum of
+ *      exp(scale q k^T); an infinity for tokens of no sequence
+ * No sequence has any influence on another one, and no later token on an earlier one's output, NaN and infinities included.
+ * io, precision, dim and scale as for cross attention.  tokens x heads / kv_heads and sequences below 2^30, heads / kv_heads below 2^20; token strides that are
+ * not negative and below 2^24, head strides of q that are not negative and below 2^29 / (heads / kv_heads); kv_heads x (tokens x heads / kv_heads / 32 + sequences + 2) below 2^24: else GRKAN_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    const void *offsets;
+    int64_t tokens;
+    int32_t sequences, heads, kv_heads, dim, offsets_64;
+    int64_t q_token_stride, q_head_stride;
+    int64_t k_token_stride, k_head_stride;
+    int64_t v_token_stride, v_head_stride;
+    float scale;
+} grkan_causal_attention_t;
+size_t grkan_causal_attention_lse_count(const grkan_causal_attention_t *attention);
+grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *attention, void *out, float *lse, grkan_dtype_t io, void *hip_stream);
+
+/*
+ * Its backward pass: P is recomputed from lse.  out as the forward pass left it; dout [tokens, heads, dim] strided as q is; dq as out, dk and dv
+ * [tokens, kv_heads, dim], contiguous, 16-byte aligned, overwritten.  What a sequence's tokens hold reaches its own gradients alone (a NaN or an
+ * infinity in one token may reach those of all its sequence).
+ * workspace: grkan_causal_attention_bwd_workspace_bytes() bytes of scratch (host-only query; 0 for arguments that are refused), 16-byte aligned, untouched until the
+ * enqueued work has finished.
+ */
+size_t grkan_causal_attention_bwd_workspace_bytes(const grkan_causal_attention_t *attention);
+grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *attention, const void *out, const float *lse, const void *dout,
+                                          int64_t dout_token_stride, int64_t dout_head_stride, void *dq, void *dk, void *dv, void *workspace,
+                                          size_t workspace_bytes, grkan_dtype_t io, void *hip_stream);
+
+/*
+ * A cache of keys and values in pages: position p of sequence s lies in row p mod page_size of page table[s][p / page_size].
+ *
+ *   k_pages, v_pages  [pages, page_size, kv_heads, dim] of io; strides of page, token and head, each a multiple of 8 elements, and 16-byte aligned pointers
+ *                     (else GRKAN_ERR_ALIGN)
+ *   table    DEVICE int32 [sequences, table_entries], rows table_stride apart.  An entry that is no page (below 0, or from `pages` on) holds nothing:
+ *            what is written there goes nowhere, and its positions are not attended to.  Entries behind a sequence's length are not read.
+ *   lengths  DEVICE int32 (int64 with lengths_64) [sequences]: how many positions each sequence has, the new tokens among them (clamped to 0 .. page_size x
+ *            table_entries for attention)
+ * io: GRKAN_BF16 or GRKAN_F16; dim a multiple of 8 up to 128; pages below 2^31, page_size x table_entries below 2^30, token strides that are not negative and below
+ * 2^24: else GRKAN_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    void *k_pages, *v_pages;
+    const int32_t *table;
+    const void *lengths;
+    int64_t pages;
+    int32_t page_size, sequences, table_entries, kv_heads, dim, lengths_64;
+    int64_t table_stride;
+    int64_t k_page_stride, k_token_stride, k_head_stride;
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+} grkan_paged_cache_t;
+
+/*
+ * Keys and values of new tokens into the pages: k, v [tokens, kv_heads, dim] of io with strides of token and head (as those of the pages), the sequences' tokens
+ * packed one behind the other as for causal attention (offsets as there; NULL: tokens / sequences of each).  The last of sequence s goes to position
+ * lengths[s] - 1, the others in front of it.  Tokens of no sequence are left out, and so are those of a sequence that has more tokens than length, where their
+ * positions would be below 0, and all of one whose length is more than its row of the table has place for.
+ * Where two tokens have the same place (a page in two sequences' rows), which one it holds afterwards is unspecified.
+ * tokens below 2^30, kv_heads x dim below 2^24: else GRKAN_ERR_UNSUPPORTED.
+ */
+grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, const void *k, const void *v, const void *offsets, int32_t offsets_64, int64_t tokens,
+                                 int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, grkan_dtype_t io,
+                                 void *hip_stream);
+
+/*
+ * Attention of the newest tokens over the cache: q [sequences, tokens, heads, dim] of io, token i of sequence s being that of position lengths[s] - tokens + i,
+ * which sees the positions up to its own (the new tokens' keys and values have been written).  Strides as k's above, of sequence, token and head.
+ * out [sequences, tokens, heads, dim] of io, contiguous, 16-byte aligned; zeros for a token that sees nothing (below position 0, or no page).  What the
+ * pages hold elsewhere has no influence, NaN and infinities included, and neither has a later token on an earlier one.  Precision and scale as for cross attention.
+ * tokens x heads / kv_heads below 2^30 and kv_heads x tiles of 32 of them too, sequences x that up to 2^24 - 1: else GRKAN_ERR_UNSUPPORTED.
+ * workspace: grkan_paged_attention_workspace_bytes() bytes of scratch (host-only query; 0: none is needed and it may be NULL), 16-byte aligned, untouched until the
+ * enqueued work has finished.
+ */
+typedef struct {
+    const void *q;
+    int64_t tokens;
+    int32_t heads;
+    int64_t sequence_stride, token_stride, head_stride;
+    float scale;
+} grkan_paged_queries_t;
+size_t grkan_paged_attention_workspace_bytes(const grkan_paged_cache_t *cache, const grkan_paged_queries_t *queries);
+grkan_status_t grkan_paged_attention(const grkan_paged_cache_t *cache, const grkan_paged_queries_t *queries, void *out, void *workspace,
+                                     size_t workspace_bytes, grkan_dtype_t io, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -112,6 +112,69 @@ class Attention(ctypes.Structure):
                    q.shape[3], int(wide), *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *mask, scale)
 
 
+class CausalAttention(ctypes.Structure):
+    """grkan_causal_attention_t"""
+
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p),
+        ("tokens", ctypes.c_int64),
+        ("sequences", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("offsets_64", ctypes.c_int32),
+        ("q_token_stride", ctypes.c_int64),
+        ("q_head_stride", ctypes.c_int64),
+        ("k_token_stride", ctypes.c_int64),
+        ("k_head_stride", ctypes.c_int64),
+        ("v_token_stride", ctypes.c_int64),
+        ("v_head_stride", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class PagedCacheOperand(ctypes.Structure):
+    """grkan_paged_cache_t"""
+
+    _fields_ = [
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+        ("pages", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("sequences", ctypes.c_int32),
+        ("table_entries", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("lengths_64", ctypes.c_int32),
+        ("table_stride", ctypes.c_int64),
+        ("k_page_stride", ctypes.c_int64),
+        ("k_token_stride", ctypes.c_int64),
+        ("k_head_stride", ctypes.c_int64),
+        ("v_page_stride", ctypes.c_int64),
+        ("v_token_stride", ctypes.c_int64),
+        ("v_head_stride", ctypes.c_int64),
+    ]
+
+
+class PagedQueries(ctypes.Structure):
+    """grkan_paged_queries_t"""
+
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("tokens", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+        ("sequence_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+    ]
+
+
 def load_library():
     """Load libgrkan.so (built in-tree by paper_2505_13813_amd/build.py)."""
     global _lib
@@ -204,6 +267,21 @@ def load_library():
     lib.grkan_attention_fwd.restype = ctypes.c_int
     lib.grkan_attention_bwd.argtypes = [ctypes.POINTER(Attention), vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, sz, ctypes.c_int, vp]
     lib.grkan_attention_bwd.restype = ctypes.c_int
+    causal, cache, queries = (ctypes.POINTER(c) for c in (CausalAttention, PagedCacheOperand, PagedQueries))
+    lib.grkan_causal_attention_lse_count.argtypes = [causal]
+    lib.grkan_causal_attention_lse_count.restype = sz
+    lib.grkan_causal_attention_fwd.argtypes = [causal, vp, vp, ctypes.c_int, vp]
+    lib.grkan_causal_attention_fwd.restype = ctypes.c_int
+    lib.grkan_causal_attention_bwd_workspace_bytes.argtypes = [causal]
+    lib.grkan_causal_attention_bwd_workspace_bytes.restype = sz
+    lib.grkan_causal_attention_bwd.argtypes = [causal, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, ctypes.c_int, vp]
+    lib.grkan_causal_attention_bwd.restype = ctypes.c_int
+    lib.grkan_paged_write.argtypes = [cache, vp, vp, vp, i32, i64, i64, i64, i64, i64, ctypes.c_int, vp]
+    lib.grkan_paged_write.restype = ctypes.c_int
+    lib.grkan_paged_attention_workspace_bytes.argtypes = [cache, queries]
+    lib.grkan_paged_attention_workspace_bytes.restype = sz
+    lib.grkan_paged_attention.argtypes = [cache, queries, vp, vp, sz, ctypes.c_int, vp]
+    lib.grkan_paged_attention.restype = ctypes.c_int
     lib.grkan_alg1_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, vp]
     lib.grkan_alg1_bwd.restype = ctypes.c_int
     _lib = lib

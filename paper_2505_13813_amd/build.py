@@ -12,9 +12,11 @@ LIB = PKG / "libgrkan.so"
 SOURCES = [CSRC / "grkan_kernels.hip", CSRC / "grkan_plan.cpp", CSRC / "grkan_alg1_baseline.hip",
            CSRC / "grkan_linear.hip", CSRC / "grkan_linear_grad.hip", CSRC / "grkan_hidden.hip",
            CSRC / "grkan_product.hip", CSRC / "grkan_block.hip", CSRC / "grkan_norm.hip", CSRC / "grkan_rotary.hip",
-           CSRC / "grkan_attention.hip", CSRC / "grkan_attention_bwd.hip"]
+           CSRC / "grkan_attention.hip", CSRC / "grkan_attention_bwd.hip", CSRC / "grkan_causal.hip",
+           CSRC / "grkan_causal_bwd.hip", CSRC / "grkan_paged.hip"]
 HEADERS = [CSRC / "grkan_walk.h", CSRC / "grkan_plan.h", CSRC / "grkan_elem.h", CSRC / "grkan_tile.h", CSRC / "grkan_stage2.h",
-           CSRC / "grkan_vector.h", CSRC / "grkan_attention.h",
+           CSRC / "grkan_vector.h", CSRC / "grkan_attention.h", CSRC / "grkan_attention_rows.h",
+           CSRC / "grkan_attention_back.h", CSRC / "grkan_packed.h",
            PKG.parent / "include" / "grkan.h",
            PKG.parent / "include" / "grkan_alg1.h", PKG.parent / "include" / "grkan_transformer.h"]
 

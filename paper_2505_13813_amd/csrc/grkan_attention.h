@@ -124,6 +124,14 @@ template <int N> __device__ __forceinline__ void arrived(u32x4 (&r)[N])
 }
 __device__ __forceinline__ void arrived(float &r) { asm volatile("" : "+v"(r)); }
 
+// The lane's number, computed where it is asked for: for loops that have no register to keep it in.
+__device__ __forceinline__ uint32_t lane_here()
+{
+    uint32_t lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    return lane;
+}
+
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // Tiles of ROWS tokens (keys) by WAVES wavefronts, a KB at a time.  Where one wavefront loads a tile by itself, in a loop: that kernel is over in
@@ -188,6 +196,15 @@ template <int N> struct Addresses {
             asm volatile("" : "+v"(r.at[i]));
         }
         return r;
+    }
+    // the same in place: for loops that have no registers for both
+    __device__ __forceinline__ void move(uint32_t by)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            at[i] += by;
+            asm volatile("" : "+v"(at[i]));
+        }
     }
 };
 
@@ -324,7 +341,10 @@ __device__ __forceinline__ f32x16 read_cover(uint32_t at, int block, uint32_t h)
 // workers gives all the same to do, whatever the batch entries' lengths are.
 // (Everything in 32 bits: the host lets no more than 2^30 groups come here.)
 constexpr int kGroup = 128;
-struct Deal {
+// How many walks over an entry's keys there are: its key heads.
+__device__ __forceinline__ int32_t units_of(const Args &a) { return a.kv_heads; }
+
+template <class A> struct DealOf {
     int32_t total, workers; // G, and W: as many as the host asked for, but none without a group
     int32_t quotient, rest; // of G by W
     // batch entry b, its keys, the groups of one of its key heads, and the group that its first one begins with
@@ -334,7 +354,7 @@ struct Deal {
     __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + kGroup - 1) / kGroup; }
 
     // keys of entry first + lane (0 behind the last), and the running sum of the groups
-    __device__ __forceinline__ static void scan(const Args &a, int32_t first, int32_t &keys, int32_t &sum)
+    __device__ __forceinline__ static void scan(const A &a, int32_t first, int32_t &keys, int32_t &sum)
     {
         const int32_t lane = (int32_t)threadIdx.x & 63, entry = first + lane;
         keys = entry < a.batch ? keys_of(a, entry) : 0;
@@ -346,10 +366,10 @@ struct Deal {
         }
     }
 
-    __device__ __forceinline__ explicit Deal(const Args &a)
+    __device__ __forceinline__ explicit DealOf(const A &a)
     {
         if (!a.lengths) {
-            total = groups_of((int32_t)a.keys) * a.kv_heads * a.batch;
+            total = groups_of((int32_t)a.keys) * units_of(a) * a.batch;
         } else {
             scan(a, 0, mine, up_to);
             total = __builtin_amdgcn_readlane(up_to, 63);
@@ -358,7 +378,7 @@ struct Deal {
                 scan(a, first, keys, sum);
                 total += __builtin_amdgcn_readlane(sum, 63);
             }
-            total *= a.kv_heads;
+            total *= units_of(a);
         }
         workers = total < a.splits ? total : a.splits;
         quotient = workers ? total / workers : 0;
@@ -378,13 +398,13 @@ struct Deal {
         return w;
     }
     // Sets b, count, groups and begin: to the entry that holds group x, or to `entry`.
-    __device__ __forceinline__ void find(const Args &a, int32_t x, int32_t entry = -1)
+    __device__ __forceinline__ void find(const A &a, int32_t x, int32_t entry = -1)
     {
         if (!a.lengths) {
             count = (int32_t)a.keys;
             groups = groups_of(count);
-            b = entry >= 0 ? entry : x / (groups * a.kv_heads);
-            begin = b * groups * a.kv_heads;
+            b = entry >= 0 ? entry : x / (groups * units_of(a));
+            begin = b * groups * units_of(a);
             return;
         }
         int32_t before = 0; // groups of a key head each, of the entries in front
@@ -393,19 +413,20 @@ struct Deal {
             if (first)
                 scan(a, first, keys, sum);
             const int32_t lane = (int32_t)threadIdx.x & 63;
-            const uint64_t found = __ballot(entry >= 0 ? first + lane == entry : (before + sum) * a.kv_heads > x);
+            const uint64_t found = __ballot(entry >= 0 ? first + lane == entry : (before + sum) * units_of(a) > x);
             if (found || first + 64 >= a.batch) {
                 const int at = found ? __builtin_ctzll(found) : 63;
                 b = first + at;
                 count = __builtin_amdgcn_readlane(keys, at);
                 groups = groups_of(count);
-                begin = (before + __builtin_amdgcn_readlane(sum, at) - groups) * a.kv_heads;
+                begin = (before + __builtin_amdgcn_readlane(sum, at) - groups) * units_of(a);
                 return;
             }
             before += __builtin_amdgcn_readlane(sum, 63);
         }
     }
 };
+typedef DealOf<Args> Deal;
 
 // Workgroups go round-robin over the 8 XCDs.  Runs of work items go to one XCD, whose L2 fetches their keys and values once; runs
 // are short enough (host: spread) that every XCD has several of them, of long and of short batch entries.

@@ -1,0 +1,296 @@
+// Causal attention over packed sequences on gfx950 (MI355X), forward: row r of a sequence (a token's query of one head) sees the sequence's keys up to its
+// own token's,
+//
+//     out_r = sum_{j <= r} exp(scale q_r k_j - m_r) v_j / sum_{j <= r} exp(scale q_r k_j - m_r)
+//
+// in one pass with the running maximum and sum, as cross attention does it (grkan_attention.hip), from the same parts: the queries of the heads that
+// share a key head are one list of rows, and the probabilities go from the products of the scores to those of the values in registers.
+// Products and masks stop at the diagonal: a workgroup ends at its last row's key, a wavefront leaves out tiles behind its own, and only the tiles that the
+// diagonal crosses take comparisons.  The longest walks are launched first.
+//
+// A later token has no influence on an earlier one, NaN and infinities included: in the tiles on the diagonal its weight is zero, but zero times NaN is
+// NaN.  Rows whose sums are not finite at the end are gone through a second time with those tiles row by row (Rows::add_each).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "grkan_attention_rows.h"
+#include "grkan_packed.h"
+
+namespace grkan {
+namespace attention {
+
+// Zeros, and an lse that gives no probability, for 32 rows that belong to no sequence.
+template <int DP> __device__ __forceinline__ void clear_rows(const Packed &a, const Segment &s, int32_t kvh, uint32_t row0, int32_t rows, int lane)
+{
+    const uint32_t row = row0 + ((uint32_t)lane & 31u), h = (uint32_t)lane >> 5;
+    if ((int32_t)row >= rows)
+        return;
+    char *const out = a.out + packed_at(a, s, kvh, row);
+    for (int32_t channel = 8 * (int32_t)h; channel < a.dim; channel += 16)
+        *reinterpret_cast<u32x4 *>(out + 2 * channel) = u32x4{};
+    if (h == 0 && a.lse)
+        a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = __builtin_inff();
+}
+
+// ------------------------------------------------------------------------------------------------ 32 rows a wavefront, 128 a workgroup
+
+template <typename IO_, int DP_> struct CausalShape {
+    typedef IO_ IO;
+    static constexpr int DP = DP_, KT = 64, kWaves = 4, kRows = 32 * kWaves;
+    static constexpr uint32_t kTile = kTileBytes<DP, KT>;
+    static constexpr uint32_t kFlag = 4 * kTile; // behind K and V, two of each
+    static constexpr size_t kLds = kFlag + 16;
+};
+
+template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void causal_kernel(const Packed a)
+{
+    constexpr int DP = SH::DP, KT = SH::KT;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
+
+    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
+    const Segment s = segment_of<SH::kRows>(a, a.slots - 1 - turn, a.group);
+    const int32_t all = s.count * a.group; // rows of the segment
+    const int64_t begin = (int64_t)s.tile * SH::kRows;
+    if (begin >= all)
+        return;
+    const uint32_t row0 = (uint32_t)begin + (uint32_t)wave * 32u, row = row0 + col;
+    if (s.none) {
+        clear_rows<DP>(a, s, kvh, row0, all, lane);
+        return;
+    }
+    Rows<typename SH::IO, DP, KT> rows;
+    const uint32_t query = row / group;
+    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
+              (int32_t)row < all, a.dim, h);
+
+    // keys: of the workgroup up to its last row's, of the wavefront all below `from`, none from `to` on
+    const int32_t end = (int32_t)((uint32_t)begin + SH::kRows - 1 < (uint32_t)all ? (uint32_t)begin + SH::kRows - 1 : (uint32_t)all - 1) / a.group + 1;
+    const int32_t from = (int32_t)(row0 / group) + 1, to = (int32_t)((row0 + 31u) / group) + 1;
+    const int32_t tiles = (end + KT - 1) / KT;
+    const LastTwiceLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+    auto issue = [&](int32_t t, uint32_t at) {
+        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, a.dim, end - t * KT, lds0 + at);
+        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, a.dim, end - t * KT, lds0 + at + 2 * SH::kTile);
+    };
+    if (a.dim < DP) {
+#pragma unroll 1
+        for (uint32_t at = 0; at < 2 * SH::kTile; at += SH::kTile) {
+            k_loads.clear(lane, lds0 + at);
+            v_loads.clear(lane, lds0 + at + 2 * SH::kTile);
+        }
+    }
+    arrived(rows.q);
+    const bool works = (int32_t)row0 < all; // (a wavefront without rows loads for the others)
+    // (two loops: one with a condition in it would copy the sums)
+    auto walk = [&](auto each) {
+        rows.clear();
+        RowOperand<DP> k_from(lane);
+        ColumnOperand<DP> v_from(lane);
+        k_from.move(lds0);
+        v_from.move(lds0 + 2 * SH::kTile);
+        uint32_t at = 0;
+        issue(0, 0);
+#pragma unroll 1
+        for (int32_t t = 0; t < tiles; ++t) {
+            wait_loads<0>();
+            barrier(); // all wavefronts' loads of this tile are there, and all are done with the tile before
+            if (t + 1 < tiles)
+                issue(t + 1, at ^ SH::kTile);
+            at ^= SH::kTile;
+            if (t > 0) { // (K and V are moved alike)
+                k_from.move(at ? 0u - SH::kTile : SH::kTile);
+                v_from.move(at ? 0u - SH::kTile : SH::kTile);
+            }
+            if (!works || t * KT >= to)
+                continue;
+            f32x16 x[KT / 32];
+            rows.scores(k_from, x);
+            const bool crossed = t * KT + KT > from;
+            if (crossed)
+                rows.cut(x, (int32_t)query - t * KT, h);
+            uint32_t p[KT / 32][8];
+            rows.probabilities(x, a.c, p);
+            if constexpr (decltype(each)::value) {
+                if (crossed) {
+                    rows.add_each(p, v_from, (int32_t)query - t * KT, col, h);
+                    continue;
+                }
+            }
+            rows.add(p, v_from);
+        }
+    };
+    walk(std::false_type{});
+    // (by all wavefronts, which load for one another)
+    uint32_t *const flag = reinterpret_cast<uint32_t *>(smem + SH::kFlag);
+    if (lane == 0)
+        flag[wave] = works && rows.not_finite();
+    wait_loads<0>();
+    barrier();
+    if (__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0)
+        walk(std::true_type{});
+    if ((int32_t)row >= all)
+        return;
+    const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    char *const out = a.out + packed_at(a, s, kvh, row);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+        store_channels<typename SH::IO>(rows.acc[d], d, inv, a, out, false, h);
+    if (h == 0 && a.lse)
+        a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = lse_of(log2_sum(rows.top, sum, a.c));
+}
+
+// ------------------------------------------------------------------------------------------------ 32 rows, their keys shared by four wavefronts
+
+template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void causal_few_kernel(const Packed a)
+{
+    constexpr int DP = SH::DP, KT = SH::KT;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
+
+    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
+    const Segment s = segment_of<32>(a, a.slots - 1 - turn, a.group);
+    const int32_t all = s.count * a.group;
+    const int64_t begin = (int64_t)s.tile * 32;
+    if (begin >= all)
+        return;
+    const uint32_t row0 = (uint32_t)begin, row = row0 + col;
+    if (s.none) {
+        if (wave == 0)
+            clear_rows<DP>(a, s, kvh, row0, all, lane);
+        return;
+    }
+    Rows<typename SH::IO, DP, KT> rows;
+    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
+              (int32_t)row < all, a.dim, h);
+    const int32_t end = (int32_t)(row0 + 31u < (uint32_t)all ? row0 + 31u : (uint32_t)all - 1) / a.group + 1;
+    const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+    const Later later{(int32_t)(row / group), (int32_t)(row0 / group)};
+    for (bool each = false;; each = true) {
+        rows.clear();
+        walk_alone<SH>(
+            rows, wave, (end + KT - 1) / KT, lds0, wave, lane, a.c, a.dim,
+            [&](int32_t t) { return end - t * KT >= KT ? rows.kAll : ((uint64_t)1 << (end - t * KT)) - 1u; },
+            [&](int32_t t, uint64_t word, bool whole, uint32_t to) {
+                k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, word, whole, to);
+                v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, word, whole, to + SH::kTile);
+            },
+            later, each);
+        if (each || !rows.not_finite())
+            break;
+    }
+    join_wavefronts<SH>(rows, smem, wave, lane, (int32_t)row < all, a, a.out + packed_at(a, s, kvh, row),
+                        a.lse + (a.lse ? (int64_t)kvh * a.rows + packed_row(a, s, row) : 0), false);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+static bool fine_operand(const void *p, int64_t token, int64_t head) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (token | head) % 8 == 0; }
+
+grkan_status_t fill(const grkan_causal_attention_t *at, grkan_dtype_t io, Packed *to)
+{
+    if (!at)
+        return GRKAN_ERR_NULL;
+    if (at->tokens < 0 || at->sequences < 0 || at->heads < 1 || at->kv_heads < 1 || at->heads % at->kv_heads != 0 || at->dim < 1)
+        return GRKAN_ERR_SHAPE;
+    if (!at->offsets && (at->sequences == 0 ? at->tokens != 0 : at->tokens % at->sequences != 0))
+        return GRKAN_ERR_SHAPE;
+    if (io != GRKAN_BF16 && io != GRKAN_F16)
+        return GRKAN_ERR_DTYPE;
+    const int64_t group = at->heads / at->kv_heads;
+    if (at->dim % 8 != 0 || at->dim > 128 || !(at->scale > 0) || !std::isfinite(at->scale * 1.4426950408889634f))
+        return GRKAN_ERR_UNSUPPORTED;
+    // rows, and tiles with them, are counted in 31 bits; offsets in a tile of 64 tokens too
+    const int64_t most = (int64_t)1 << 30;
+    if (group >= 1 << 20 || at->tokens >= most || at->tokens * group >= most || at->sequences >= most)
+        return GRKAN_ERR_UNSUPPORTED;
+    if (!in_offsets(at->q_token_stride, at->q_head_stride, group) || !in_offsets(at->k_token_stride, 0, 1) || !in_offsets(at->v_token_stride, 0, 1))
+        return GRKAN_ERR_UNSUPPORTED;
+    if (at->tokens > 0 && (!at->q || !at->k || !at->v))
+        return GRKAN_ERR_NULL;
+    if (!fine_operand(at->q, at->q_token_stride, at->q_head_stride) || !fine_operand(at->k, at->k_token_stride, at->k_head_stride) ||
+        !fine_operand(at->v, at->v_token_stride, at->v_head_stride) || reinterpret_cast<uintptr_t>(at->offsets) % (at->offsets_64 ? 8 : 4) != 0)
+        return GRKAN_ERR_ALIGN;
+    Packed a = {};
+    a.q = Operand{reinterpret_cast<uint64_t>(at->q), 0, at->q_token_stride * 2, at->q_head_stride * 2};
+    a.k = Operand{reinterpret_cast<uint64_t>(at->k), 0, at->k_token_stride * 2, at->k_head_stride * 2};
+    a.v = Operand{reinterpret_cast<uint64_t>(at->v), 0, at->v_token_stride * 2, at->v_head_stride * 2};
+    a.rows = at->tokens * group;
+    a.keys = at->tokens;
+    a.batch = 1;
+    a.kv_heads = at->kv_heads;
+    a.group = (int32_t)group;
+    a.dim = at->dim;
+    a.scale = at->scale;
+    a.c = at->scale * 1.4426950408889634f;
+    a.offsets = at->offsets;
+    a.offsets_64 = at->offsets_64;
+    a.sequences = at->sequences;
+    a.tokens = (int32_t)at->tokens;
+    a.each = at->sequences > 0 ? (int32_t)(at->tokens / at->sequences) : 0;
+    *to = a;
+    return GRKAN_OK;
+}
+
+typedef void (*Kernel)(Packed);
+struct CausalVariant {
+    Kernel kernel;
+    size_t lds;
+};
+template <typename IO, int DP> static CausalVariant pick(bool few)
+{
+    if (few)
+        return CausalVariant{causal_few_kernel<TokenShape<IO, DP>>, TokenShape<IO, DP>::kLds};
+    return CausalVariant{causal_kernel<CausalShape<IO, DP>>, CausalShape<IO, DP>::kLds};
+}
+template <typename IO> static CausalVariant pick(int32_t dim, bool few)
+{
+    return dim <= 32 ? pick<IO, 32>(few) : dim <= 64 ? pick<IO, 64>(few) : dim <= 96 ? pick<IO, 96>(few) : pick<IO, 128>(few);
+}
+
+} // namespace attention
+} // namespace grkan
+
+using namespace grkan;
+
+extern "C" size_t grkan_causal_attention_lse_count(const grkan_causal_attention_t *at)
+{
+    return !at || at->tokens < 0 || at->heads < 0 ? 0 : (size_t)at->tokens * (size_t)at->heads;
+}
+
+extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *at, void *out, float *lse, grkan_dtype_t io, void *hip_stream)
+{
+    attention::Packed a;
+    const grkan_status_t bad = attention::fill(at, io, &a);
+    if (bad != GRKAN_OK)
+        return bad;
+    if (a.tokens == 0)
+        return GRKAN_OK;
+    if (!out)
+        return GRKAN_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(out) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
+        return GRKAN_ERR_ALIGN;
+    const bool few = attention::slots_of<128>(a, a.group) * a.kv_heads < 512;
+    const int64_t slots = few ? attention::slots_of<32>(a, a.group) : attention::slots_of<128>(a, a.group), grid = slots * a.kv_heads;
+    if (grid > attention::kMostBlocks)
+        return GRKAN_ERR_UNSUPPORTED;
+    a.slots = (int32_t)slots;
+    a.out = static_cast<char *>(out);
+    a.lse = lse;
+    const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a.dim, few) : attention::pick<_Float16>(a.dim, few);
+    if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
+        return GRKAN_ERR_LAUNCH;
+    void *args[] = {&a};
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3(256), args, v.lds, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+        return GRKAN_ERR_LAUNCH;
+    return GRKAN_OK;
+}

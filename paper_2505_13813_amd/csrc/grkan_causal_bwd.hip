@@ -1,0 +1,655 @@
+// Causal attention over packed sequences on gfx950 (MI355X), backward.  With P recomputed from the rows' lse, D = dO V^T and delta = the row's sum of dO O,
+//
+//     dV_j = sum_{i >= j} P_ij dO_i      S'_ij = P_ij (D_ij - delta_i)      dQ_i = scale sum_{j <= i} S'_ij K_j      dK_j = scale sum_{i >= j} S'_ij Q_i
+//
+// in two kernels as cross attention has them (grkan_attention_bwd.hip): one owns keys and walks the rows that see them, one owns rows and walks the keys that
+// they see; no atomics, the same bits each time.  Tiles that the diagonal crosses take comparisons, the others none, and what lies behind it is left out.
+//
+// A key sees the more rows the earlier it is, so the walks of a long sequence's first keys are cut into slabs of rows, each a workgroup's, whose sums a second launch
+// adds up; the queries' kernel starts its longest walks first.
+//
+// float16: scaled as there; the largest upstream gradient is that of the key's own sequence, from the key's tile on.
+#include <hip/hip_runtime.h>
+
+#include "grkan_attention_back.h"
+#include "grkan_packed.h"
+
+namespace grkan {
+namespace attention {
+
+// float16: of 64 rows of a segment delta, and the largest |dO| and |delta|: sixteen lanes a row, eight channels each.
+template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel(const Packed a)
+{
+    using MM = Matrix<IO>;
+    __shared__ uint32_t most[4][2];
+    const int32_t slot = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - slot * a.kv_heads;
+    const Segment s = segment_of<kRowTile>(a, slot, a.group);
+    const int32_t all = s.count * a.group;
+    if (s.none || (int64_t)s.tile * kRowTile >= all)
+        return;
+    const uint32_t lane16 = threadIdx.x & 15u;
+    const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
+    const uint64_t out = a.forward_out + (uint64_t)packed_at(a, s, kvh, 0);
+    const uint64_t dout = a.dout.at + (uint64_t)((int64_t)s.first * a.dout.token + (int64_t)kvh * a.group * a.dout.head);
+    const uint32_t row0 = (uint32_t)s.tile * kRowTile + (threadIdx.x >> 4);
+    u32x4 o[4], d[4];
+    float largest = 0.0f, sums = 0.0f;
+    // (all loads in front, without a branch: they wait for one another otherwise)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t row = row0 + 16u * k;
+        const bool there = (int32_t)row < all, loaded = there && 8u * lane16 < (uint32_t)a.dim;
+        const uint64_t zeros = reinterpret_cast<uint64_t>(kZeros);
+        o[k] = gload16(loaded ? out + 2u * (uint64_t)row_offset(row, (uint32_t)a.group, heads_dim, a.dim) + 16u * lane16 : zeros, 0);
+        d[k] = gload16(loaded ? dout + (uint64_t)row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head) + 16u * lane16 : zeros, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t row = row0 + 16u * k;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float x = MM::first(d[k][j]), y = MM::second(d[k][j]);
+            sum += x * MM::first(o[k][j]) + y * MM::second(o[k][j]);
+            largest = fmaxf(largest, fmaxf(fabsf(x), fabsf(y)));
+        }
+#pragma unroll
+        for (int i = 8; i > 0; i /= 2)
+            sum += __shfl_xor(sum, i);
+        sums = fmaxf(sums, fabsf(sum));
+        if (lane16 == 0 && (int32_t)row < all)
+            a.row_delta[(int64_t)kvh * a.rows + packed_row(a, s, row)] = sum;
+    }
+    const uint32_t bits[2] = {most_of_lanes(__builtin_bit_cast(uint32_t, largest)), most_of_lanes(__builtin_bit_cast(uint32_t, sums))};
+    if ((threadIdx.x & 63) == 0) {
+        most[threadIdx.x >> 6][0] = bits[0];
+        most[threadIdx.x >> 6][1] = bits[1];
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        uint32_t found = 0;
+        for (int w = 0; w < 4; ++w)
+            found = most[w][threadIdx.x] > found ? most[w][threadIdx.x] : found;
+        a.row_most[2 * ((int64_t)kvh * a.row_tiles + slot) + threadIdx.x] = __builtin_bit_cast(float, found);
+    }
+}
+
+// The rows that tile `tile` of a segment's keys is seen by: tiles [first, tiles) of `size` rows, in `parts` slabs of `per`.
+struct Walk {
+    int32_t first, tiles, parts, per;
+    __device__ __forceinline__ Walk(const Packed &a, const Segment &s, int32_t own, int32_t size)
+    {
+        const int32_t all = s.count * a.group;
+        first = (int32_t)((int64_t)s.tile * own * a.group / size);
+        tiles = (all + size - 1) / size;
+        const int32_t n = tiles - first;
+        parts = (n + a.slab - 1) / a.slab;
+        parts = parts < 1 ? 1 : parts < a.parts ? parts : a.parts;
+        per = (n + parts - 1) / parts;
+    }
+};
+
+// dK and dV of 32 keys a wavefront, of 128 a workgroup, from all the rows that see them or a slab of those.
+template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_kernel(const Packed a)
+{
+    using IO = typename SH::IO;
+    using MM = Matrix<IO>;
+    constexpr int DP = SH::DP, ROWS = SH::ROWS, ND = DP / 32, NS = DP / 16;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
+    // block ((part, slot), key head)
+    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
+    const int32_t part = turn / a.key_tiles, slot = turn - part * a.key_tiles;
+    const Segment s = segment_of<SH::kOwn>(a, slot, 1);
+    const int64_t begin = (int64_t)s.tile * SH::kOwn;
+    if (begin >= s.count)
+        return;
+    const Walk walk(a, s, SH::kOwn, ROWS);
+    if (part >= (s.none ? 1 : walk.parts))
+        return;
+    const int32_t all = s.count * a.group, count = s.count;
+    const int32_t t0 = walk.first + part * walk.per, t1 = s.none ? t0 : t0 + walk.per < walk.tiles ? t0 + walk.per : walk.tiles;
+    const int32_t key0 = (int32_t)begin + wave * 32, key = key0 + (int32_t)col; // this wavefront's and this lane's
+    const bool valid = key < count, works = key0 < count;
+
+    // ---- keys and values as second operands: lane l has key l mod 32, channels 16 s + 8 (l / 32) ..
+    u32x4 k[NS], v[SH::V_LDS ? 1 : NS];
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+#pragma unroll
+    for (int st = 0; st < NS; ++st) {
+        const uint32_t channel = 16u * st + 8u * h;
+        const bool there = valid && channel < (uint32_t)a.dim;
+        k[st] = gload16(there ? k_base + (uint64_t)key * (uint64_t)a.k.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        if constexpr (!SH::V_LDS)
+            v[st] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+    }
+    f32x16 dk[ND], dv[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        dk[d] = f32x16{};
+        dv[d] = f32x16{};
+    }
+
+    const uint64_t q_base = a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head);
+    const uint64_t d_base = a.dout.at + (uint64_t)((int64_t)s.first * a.dout.token + (int64_t)kvh * a.group * a.dout.head);
+    const RowsTwiceLoads<DP, ROWS, SH::kWaves> q_loads(wave, lane, a.q, a), d_loads(wave, lane, a.dout, a);
+    const float c = a.c;
+    float up = 1.0f; // of the key
+    if constexpr (kRowsFirst<IO>) {
+        u32x4 value[NS];
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+            const uint32_t channel = 16u * st + 8u * h;
+            const bool there = valid && channel < (uint32_t)a.dim;
+            value[st] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        }
+        const int32_t base = slot_of<kRowTile>(s.first, a.group, s.index);
+        const int32_t row_tiles = s.none ? 0 : (all + kRowTile - 1) / kRowTile;
+        uint32_t largest = 0, sums = 0;
+        for (int32_t i = (int32_t)(begin * a.group / kRowTile) + lane; i < row_tiles; i += 64) {
+            const f32x2 both = reinterpret_cast<const f32x2 *>(a.row_most)[(int64_t)kvh * a.row_tiles + base + i];
+            largest = greater(largest, both[0]);
+            sums = greater(sums, both[1]);
+        }
+        float length2 = 0.0f;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                length2 += MM::first(value[st][j]) * MM::first(value[st][j]) + MM::second(value[st][j]) * MM::second(value[st][j]);
+        length2 = halves_sum(length2);
+        up = lowered(scale_of(most_of_lanes(largest)), length2, __builtin_bit_cast(float, most_of_lanes(sums)), a.dim);
+        const uint32_t longest = most_of_lanes(__builtin_bit_cast(uint32_t, length2) & 0x7fffffffu);
+        if (lane == 0 && part == 0)
+            a.value_most[((int64_t)kvh * a.key_tiles + slot) * SH::kWaves + wave] = __builtin_bit_cast(float, longest);
+    }
+
+    auto issue = [&](int32_t t, uint32_t stage) {
+        q_loads.issue(a.q, q_base, t, all, a, stage);
+        d_loads.issue(a.dout, d_base, t, all, a, stage + SH::kRowsTile);
+        if (wave < 2) {
+            const float *const from = (wave ? a.row_delta : a.lse) + (int64_t)kvh * a.rows + packed_row(a, s, (int64_t)t * ROWS);
+            const int32_t l = (int32_t)lane_here(), left = all - t * ROWS;
+            if (l < ROWS)
+                load_words_to_lds(uniform_u64(reinterpret_cast<uint64_t>(from)), (uint32_t)(l < left ? l : left - 1) * 4u,
+                                  stage + 2 * SH::kRowsTile + (uint32_t)wave * ROWS * 4u);
+        }
+    };
+
+    const uint32_t stages = lds0 + (SH::V_LDS ? 2 * SH::kKeysTile : 0u);
+    // (moved from stage to stage in place: there are no registers for copies)
+    RowOperand<DP> rows(lane), v_rows(lane);
+    ColumnOperand<DP> columns(lane);
+    rows.move(stages + SH::kKeyStage);
+    columns.move(stages + SH::kKeyStage);
+    v_rows.move(lds0 + (uint32_t)wave * row_at<DP>(32u));
+    uint32_t at = SH::kKeyStage;
+    if constexpr (SH::V_LDS) {
+        if (t0 < t1) {
+            const TileLoads<DP, 64, SH::kWaves> v_loads(wave, lane, a.v.token, a.dim);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int32_t first = (int32_t)begin + 64 * half;
+                v_loads.issue(v_base + (uint64_t)first * (uint64_t)a.v.token, a.v.token, __ballot(first + lane < count), false, lds0 + (uint32_t)half * SH::kKeysTile);
+            }
+        }
+    }
+    if (a.dim < DP) {
+#pragma unroll 1
+        for (uint32_t stage = stages; stage < stages + 2 * SH::kKeyStage; stage += SH::kKeyStage) {
+            q_loads.clear(lane, stage);
+            d_loads.clear(lane, stage + SH::kRowsTile);
+        }
+    }
+    arrived(k);
+    if constexpr (!SH::V_LDS)
+        arrived(v);
+    const int32_t first_row = key0 * a.group, last_row = (key0 + 31) * a.group; // that see the wavefront's first key, and its last
+#pragma unroll 1
+    for (int32_t t = t0 - 1; t < t1; ++t) {
+        if (t >= t0) {
+            wait_loads<0>();
+            barrier();
+        }
+        if (t + 1 < t1)
+            issue(t + 1, stages + (at ^ SH::kKeyStage));
+        const uint32_t by = at ? SH::kKeyStage : 0u - SH::kKeyStage, stage = stages + at;
+        at ^= SH::kKeyStage;
+        if (t >= t0) {
+            rows.move(by);
+            columns.move(by);
+        }
+        if (t < t0 || !works || (t + 1) * ROWS <= first_row)
+            continue;
+        const uint32_t stats = stage + 2 * SH::kRowsTile + 16u * (lane_here() >> 5);
+        const bool crossed = t * ROWS < last_row || (t + 1) * ROWS > all;
+#pragma unroll
+        for (int rb = 0; rb < ROWS / 32; ++rb) {
+            f32x16 p = {}, d = {};
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+                p = MM::multiply(RowOperand<DP>::read(rows, rb, st), k[st], p);
+            u32x4 w[2];
+#pragma unroll
+            for (int quad = 0; quad < 4; ++quad) {
+                const f32x4 lse = __builtin_bit_cast(f32x4, lds_read16(stats + (32u * rb + 8u * quad) * 4u));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    p[4 * quad + j] = __builtin_amdgcn_exp2f(fmaf(p[4 * quad + j], c, -lse[j]));
+            }
+            if (crossed) { // rows of the tile that see the key: from `from` on, and before the segment's end
+                const int32_t l = (int32_t)lane_here(), row0 = t * ROWS + 32 * rb + 4 * (l >> 5);
+                const int32_t from = (key0 + (l & 31)) * a.group - row0;
+                const uint32_t span = (uint32_t)(all - row0 - from);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    p[i] = (uint32_t)(8 * (i / 4) + i % 4 - from) < span ? p[i] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                w[i / 4][i % 4] = MM::two(p[2 * i], p[2 * i + 1]);
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                u32x4 value;
+                if constexpr (SH::V_LDS)
+                    value = RowOperand<DP>::read(v_rows, 0, st);
+                else
+                    value = v[st];
+                d = MM::multiply(RowOperand<DP>::read(rows, rb, st, SH::kRowsTile), value, d);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+                    dv[n] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, n, SH::kRowsTile), w[half], dv[n]);
+#pragma unroll
+            for (int quad = 0; quad < 4; ++quad) {
+                const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(stats + (ROWS + 32u * rb + 8u * quad) * 4u));
+                float y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    y[j] = p[4 * quad + j] * fmaf(d[4 * quad + j], up, -delta[j] * up);
+                w[quad / 2][2 * (quad % 2)] = MM::two(y[0], y[1]);
+                w[quad / 2][2 * (quad % 2) + 1] = MM::two(y[2], y[3]);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+                    dk[n] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, n), w[half], dk[n]);
+        }
+    }
+
+    const int32_t l = (int32_t)lane_here(), mine = key0 + (l & 31);
+    if (mine >= count)
+        return;
+    const float by = a.scale / up;
+    const int64_t line = ((int64_t)s.first + mine) * a.kv_heads + kvh;
+    const bool whole = s.none || walk.parts == 1;
+    // parts: [slab][dK, dV][tokens, kv_heads, dim]
+    const int64_t lines = (int64_t)a.tokens * a.kv_heads;
+    float *const to = a.partial + (2 * part * lines + line) * a.dim;
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int channel = 32 * n + 8 * g + 4 * (l >> 5);
+            if (channel >= a.dim)
+                continue;
+            f32x4 x, y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = dk[n][4 * g + j] * by;
+                y[j] = dv[n][4 * g + j];
+            }
+            if (whole) {
+                u32x2 u, z;
+                u[0] = MM::two(x[0], x[1]);
+                u[1] = MM::two(x[2], x[3]);
+                z[0] = MM::two(y[0], y[1]);
+                z[1] = MM::two(y[2], y[3]);
+                *reinterpret_cast<u32x2 *>(a.dk + (line * a.dim + channel) * 2) = u;
+                *reinterpret_cast<u32x2 *>(a.dv + (line * a.dim + channel) * 2) = z;
+            } else {
+                *reinterpret_cast<f32x4 *>(to + channel) = x;
+                *reinterpret_cast<f32x4 *>(to + lines * a.dim + channel) = y;
+            }
+        }
+}
+
+// The sum of the slabs' parts of a tile of keys, in their order: block (quarter, dK or dV, slot, key head), four elements a lane and pass.
+template <typename IO> __global__ __launch_bounds__(256) void causal_sum_kernel(const Packed a, int32_t size)
+{
+    const int32_t quarter = (int32_t)blockIdx.x & 3, which = (int32_t)blockIdx.x >> 2 & 1, item = (int32_t)blockIdx.x >> 3;
+    const int32_t slot = item / a.kv_heads, kvh = item - slot * a.kv_heads;
+    const Segment s = segment_of<kGroup>(a, slot, 1);
+    const int64_t begin = (int64_t)s.tile * kGroup;
+    if (s.none || begin >= s.count)
+        return;
+    const Walk walk(a, s, kGroup, size);
+    if (walk.parts == 1) // written as it should be
+        return;
+    const int32_t quads = a.dim / 4, keys = kGroup / 4, key0 = (int32_t)begin + quarter * keys;
+    const int64_t lines = (int64_t)a.tokens * a.kv_heads;
+    for (int32_t i = (int32_t)threadIdx.x; i < keys * quads; i += 256) {
+        const int32_t row = i / quads, key = key0 + row;
+        if (key >= s.count)
+            break;
+        const int64_t line = ((int64_t)s.first + key) * a.kv_heads + kvh;
+        const int32_t channel = 4 * (i - row * quads);
+        const float *const from = a.partial + (which * lines + line) * a.dim + channel;
+        f32x4 v = {};
+        for (int32_t n = 0; n < walk.parts; ++n)
+            v += *reinterpret_cast<const f32x4 *>(from + 2 * n * lines * a.dim);
+        u32x2 o;
+        o[0] = Matrix<IO>::two(v[0], v[1]);
+        o[1] = Matrix<IO>::two(v[2], v[3]);
+        *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + (line * a.dim + channel) * 2) = o;
+    }
+}
+
+// dQ of 32 rows a wavefront.
+template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_kernel(const Packed a)
+{
+    using IO = typename SH::IO;
+    using MM = Matrix<IO>;
+    constexpr int DP = SH::DP, ND = DP / 32, NS = DP / 16, KT = 64;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
+    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
+    const Segment s = segment_of<SH::kOwn>(a, a.slots - 1 - turn, a.group);
+    const int32_t all = s.count * a.group;
+    const int64_t begin = (int64_t)s.tile * SH::kOwn;
+    if (begin >= all)
+        return;
+    const uint32_t row0 = (uint32_t)begin + (uint32_t)wave * 32u, row = row0 + col;
+    const bool there = (int32_t)row < all, works = (int32_t)row0 < all && !s.none;
+    u32x4 q[NS], o[NS];
+    {
+        const uint64_t q_at = a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head));
+        const uint64_t o_at =
+            a.dout.at + (uint64_t)((int64_t)s.first * a.dout.token + (int64_t)kvh * a.group * a.dout.head + row_offset(row, group, a.dout.token, a.dout.head));
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+            const uint32_t channel = 16u * st + 8u * h;
+            const bool loaded = there && channel < (uint32_t)a.dim;
+            q[st] = gload16(loaded ? q_at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            o[st] = gload16(loaded ? o_at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        }
+    }
+    // keys: of the workgroup up to its last row's, of the wavefront all below `from`, none from `to` on
+    const int32_t last = (int32_t)((uint32_t)begin + SH::kOwn - 1 < (uint32_t)all ? (uint32_t)begin + SH::kOwn - 1 : (uint32_t)all - 1) / a.group;
+    const int32_t end = s.none ? 0 : last + 1;
+    const int32_t from = (int32_t)(row0 / group) + 1, to = (int32_t)((row0 + 31u) / group) + 1, query = (int32_t)(row / group);
+    const float c = a.c;
+    const int64_t place = packed_row(a, s, row);
+    float up = 1.0f; // of the row
+    float lse = there ? a.lse[(int64_t)kvh * a.rows + place] : __builtin_inff();
+    float delta = 0.0f;
+    if constexpr (kRowsFirst<IO>) {
+        float largest = 0.0f;
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                largest = fmaxf(largest, fmaxf(fabsf(MM::first(o[st][j])), fabsf(MM::second(o[st][j]))));
+        up = scale_of(__builtin_bit_cast(uint32_t, halves_max(largest)));
+        const int32_t base = slot_of<SH::kOwn>(s.first, 1, s.index), groups = (end + SH::kOwn - 1) / SH::kOwn;
+        uint32_t longest = 0;
+        for (int32_t i = lane; i < groups; i += 64) {
+            const f32x4 values = reinterpret_cast<const f32x4 *>(a.value_most)[(int64_t)kvh * a.key_tiles + base + i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                longest = greater(longest, values[j]);
+        }
+        delta = there && !s.none ? a.row_delta[(int64_t)kvh * a.rows + place] : 0.0f;
+        up = lowered(up, __builtin_bit_cast(float, most_of_lanes(longest)), fabsf(delta), a.dim);
+        delta *= up;
+    } else {
+        // for the keys' kernel too
+        const uint64_t at = a.forward_out + (uint64_t)packed_at(a, s, kvh, row);
+        u32x4 y[NS];
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+            const uint32_t channel = 16u * st + 8u * h;
+            y[st] = gload16(there && channel < (uint32_t)a.dim ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+        }
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                delta += MM::first(o[st][j]) * MM::first(y[st][j]) + MM::second(o[st][j]) * MM::second(y[st][j]);
+        delta = halves_sum(delta);
+        if (h == 0 && there)
+            a.row_delta[(int64_t)kvh * a.rows + place] = delta;
+    }
+    f32x16 dq[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+        dq[d] = f32x16{};
+
+    const int32_t tiles = (end + KT - 1) / KT;
+    const LastTwiceLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
+    const RowOperand<DP> row_operand(lane);
+    const ColumnOperand<DP> column_operand(lane);
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+    if (a.dim < DP) {
+#pragma unroll 1
+        for (uint32_t at = 0; at < 2 * SH::kRowStage; at += SH::kRowStage) {
+            k_loads.clear(lane, lds0 + at);
+            v_loads.clear(lane, lds0 + at + SH::kKeysTile);
+        }
+    }
+    arrived(q);
+    arrived(o);
+    arrived(lse);
+    arrived(delta);
+    uint32_t at = SH::kRowStage;
+#pragma unroll 1
+    for (int32_t t = -1; t < tiles; ++t) {
+        if (t >= 0) {
+            wait_loads<0>();
+            barrier();
+        }
+        if (t + 1 < tiles) {
+            const uint32_t next = lds0 + (at ^ SH::kRowStage);
+            const int32_t left = end - (t + 1) * KT;
+            k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, a.dim, left, next);
+            v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, a.dim, left, next + SH::kKeysTile);
+        }
+        const auto rows = row_operand.moved(lds0 + at);
+        const auto columns = column_operand.moved(lds0 + at);
+        at ^= SH::kRowStage;
+        if (t < 0 || !works || t * KT >= to)
+            continue;
+        const bool crossed = t * KT + KT > from;
+#pragma unroll
+        for (int kb = 0; kb < KT / 32; ++kb) {
+            fence_schedule(); // (the two halves mixed take more registers than there are)
+            f32x16 x = {}, d = {};
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+                x = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], x);
+#pragma unroll
+            for (int st = 0; st < NS; ++st)
+                d = MM::multiply(RowOperand<DP>::read(rows, kb, st, SH::kKeysTile), o[st], d);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse)) * fmaf(d[i], up, -delta);
+            if (crossed) {
+                const int32_t seen = query - t * KT - 32 * kb - 4 * (int32_t)h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    x[i] = 8 * (i / 4) + i % 4 <= seen ? x[i] : 0.0f;
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                u32x4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = MM::two(x[8 * half + 2 * j], x[8 * half + 2 * j + 1]);
+#pragma unroll
+                for (int n = 0; n < ND; ++n)
+                    dq[n] = MM::multiply(ColumnOperand<DP>::read(columns, kb, half, n), w, dq[n]);
+            }
+        }
+    }
+
+    if (!there)
+        return;
+    const float by = a.scale / up;
+    char *const out = a.out + packed_at(a, s, kvh, row);
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int channel = 32 * n + 8 * g + 4 * (int)h;
+            if (channel >= a.dim)
+                continue;
+            u32x2 w;
+            w[0] = MM::two(dq[n][4 * g] * by, dq[n][4 * g + 1] * by);
+            w[1] = MM::two(dq[n][4 * g + 2] * by, dq[n][4 * g + 3] * by);
+            *reinterpret_cast<u32x2 *>(out + channel * 2) = w;
+        }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+typedef void (*Kernel)(Packed);
+struct CausalBack {
+    Kernel rows, keys, queries;
+    void (*sum)(Packed, int32_t);
+    int size;    // rows of a stage of the keys' kernel
+    int at_once; // workgroups of it that the device holds
+    size_t keys_lds, queries_lds;
+};
+template <class SH> static CausalBack variant()
+{
+    return CausalBack{causal_rows_kernel<typename SH::IO>, causal_keys_kernel<SH>, causal_queries_kernel<SH>, causal_sum_kernel<typename SH::IO>, SH::ROWS,
+                      256 * SH::PER, SH::kKeyLds, SH::kRowLds};
+}
+template <typename IO> static CausalBack pick(int32_t dim)
+{
+    if (dim <= 32)
+        return variant<BackShape<IO, 32, 64, false, 2>>();
+    if (dim <= 64)
+        return variant<BackShape<IO, 64, 32, true, 3>>();
+    if (dim <= 96)
+        return variant<BackShape<IO, 96, 64, false, 2>>();
+    return variant<BackShape<IO, 128, 32, true, 2>>();
+}
+
+struct CausalPlan {
+    CausalBack v;
+    Packed a;
+    size_t row_most, value_most, stats, partial; // elements of the workspace: in front of the largest of the rows, of the values' lengths and of the parts; of the parts
+};
+
+static CausalPlan plan(const Packed &given, grkan_dtype_t io)
+{
+    CausalPlan p;
+    p.v = io == GRKAN_BF16 ? pick<__bf16>(given.dim) : pick<_Float16>(given.dim);
+    Packed &a = p.a;
+    a = given;
+    a.row_tiles = (int32_t)slots_of<kRowTile>(a, a.group);
+    a.key_tiles = (int32_t)slots_of<kGroup>(a, 1);
+    a.slots = (int32_t)slots_of<kGroup>(a, a.group);
+    // Slabs: as if the sequences were all of one length, which the host does not know; where one is longer its parts are the more.
+    const int64_t each = a.sequences > 0 ? ((int64_t)a.tokens + a.sequences - 1) / a.sequences : 0;
+    const int64_t walk = (each * a.group + p.v.size - 1) / p.v.size, longest = (a.rows + p.v.size - 1) / p.v.size; // tiles of rows: of a first key, at most
+    const int64_t share = (int64_t)a.kv_heads * ((a.tokens + kGroup - 1) / kGroup) * walk / 2 / p.v.at_once;        // of all, of each workgroup at once
+    const int64_t slab = share * 3 / 5 > 32 ? share * 3 / 5 : 32;
+    // (of a GB at most: where that is less than the parts wanted, there are tiles of keys enough)
+    const int64_t part = 2 * (int64_t)a.tokens * a.kv_heads * a.dim, held = ((int64_t)1 << 28) / (part > 0 ? part : 1), most = held < 16 ? held : 16;
+    const int64_t parts = (longest + slab - 1) / slab;
+    a.slab = (int32_t)slab;
+    a.parts = (int32_t)(parts < most ? parts : most);
+    if (a.parts < 1)
+        a.parts = 1;
+    p.row_most = ((size_t)a.kv_heads * (size_t)a.rows + 3) & ~(size_t)3;
+    p.value_most = p.row_most + ((2 * (size_t)a.kv_heads * (size_t)a.row_tiles + 3) & ~(size_t)3);
+    p.stats = p.value_most + 4 * (size_t)a.kv_heads * (size_t)a.key_tiles;
+    p.partial = a.parts > 1 ? (size_t)a.parts * (size_t)part : 0;
+    return p;
+}
+
+} // namespace attention
+} // namespace grkan
+
+using namespace grkan;
+
+extern "C" size_t grkan_causal_attention_bwd_workspace_bytes(const grkan_causal_attention_t *at)
+{
+    attention::Packed a;
+    if (attention::fill(at, GRKAN_BF16, &a) != GRKAN_OK)
+        return 0;
+    const attention::CausalPlan p = attention::plan(a, GRKAN_BF16);
+    return (p.stats + p.partial) * sizeof(float);
+}
+
+extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *at, const void *out, const float *lse, const void *dout,
+                                                     int64_t dout_token_stride, int64_t dout_head_stride, void *dq, void *dk, void *dv, void *workspace,
+                                                     size_t workspace_bytes, grkan_dtype_t io, void *hip_stream)
+{
+    attention::Packed given;
+    const grkan_status_t bad = attention::fill(at, io, &given);
+    if (bad != GRKAN_OK)
+        return bad;
+    if (given.tokens == 0)
+        return GRKAN_OK;
+    if (!out || !lse || !dout || !dq || !dk || !dv)
+        return GRKAN_ERR_NULL;
+    auto address = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
+    if ((address(out) | address(dout) | address(dq) | address(dk) | address(dv)) % 16 != 0 || address(lse) % 4 != 0 ||
+        (dout_token_stride | dout_head_stride) % 8 != 0)
+        return GRKAN_ERR_ALIGN;
+    if (!attention::in_offsets(dout_token_stride, dout_head_stride, given.group))
+        return GRKAN_ERR_UNSUPPORTED;
+    attention::CausalPlan p = attention::plan(given, io);
+    const size_t need = (p.stats + p.partial) * sizeof(float);
+    if (!workspace || workspace_bytes < need || address(workspace) % 16 != 0)
+        return GRKAN_ERR_WORKSPACE;
+    attention::Packed &a = p.a;
+    const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts, sum_grid = 8 * heads * a.key_tiles;
+    const int64_t queries_grid = heads * a.slots;
+    if (rows_grid > attention::kMostBlocks || keys_grid > attention::kMostBlocks || queries_grid > attention::kMostBlocks ||
+        (a.parts > 1 && sum_grid > attention::kMostBlocks))
+        return GRKAN_ERR_UNSUPPORTED;
+    a.dout = attention::Operand{address(dout), 0, dout_token_stride * 2, dout_head_stride * 2};
+    a.lse = const_cast<float *>(lse);
+    a.row_delta = static_cast<float *>(workspace);
+    a.row_most = a.row_delta + p.row_most;
+    a.value_most = a.row_delta + p.value_most;
+    a.partial = a.row_delta + p.stats;
+    a.dk = static_cast<char *>(dk);
+    a.dv = static_cast<char *>(dv);
+    a.forward_out = address(out);
+    a.out = static_cast<char *>(dq);
+    if (!attention::allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) ||
+        !attention::allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))
+        return GRKAN_ERR_LAUNCH;
+    hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
+    auto launch = [&](attention::Kernel kernel, int64_t grid, size_t lds) {
+        void *args[] = {&a};
+        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)grid), dim3(256), args, lds, stream) == hipSuccess;
+    };
+    auto keys = [&] {
+        if (!launch(p.v.keys, keys_grid, p.v.keys_lds))
+            return false;
+        if (a.parts == 1)
+            return true;
+        int32_t size = p.v.size;
+        void *args[] = {&a, &size};
+        return hipLaunchKernel(reinterpret_cast<const void *>(p.v.sum), dim3((unsigned)sum_grid), dim3(256), args, 0, stream) == hipSuccess;
+    };
+    // each needs what the other leaves: the lengths of the values, or the rows' statistics
+    if (io == GRKAN_F16)
+        return launch(p.v.rows, rows_grid, 0) && keys() && launch(p.v.queries, queries_grid, p.v.queries_lds) ? GRKAN_OK : GRKAN_ERR_LAUNCH;
+    return launch(p.v.queries, queries_grid, p.v.queries_lds) && keys() ? GRKAN_OK : GRKAN_ERR_LAUNCH;
+}

@@ -10,6 +10,7 @@
 #include "../../include/grkan_transformer.h"
 #include "grkan_torch.h"
 
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 
 namespace {
@@ -385,6 +386,13 @@ std::optional<variable_list> rotary(const Tensor &q, const Tensor &positions, co
 
 // ------------------------------------------------------------------------------------------------ cross attention
 
+double scale_or_default(const std::optional<double> &scale, const Tensor &q)
+{
+    return scale ? *scale : q.dim() > 0 && q.size(-1) > 0 ? 1.0 / std::sqrt((double)q.size(-1)) : 1.0;
+}
+
+constexpr int64_t kApart = 16777212; // elements between tokens, at most: the kernels' limit
+
 // t as the kernels read it: dense channels, strides and address in whole 16 bytes, tokens less than `apart` elements apart; a copy where it
 // is not.
 Tensor in_vectors(const Tensor &t, int64_t apart = std::numeric_limits<int64_t>::max())
@@ -416,7 +424,6 @@ struct Attended {
         TORCH_CHECK_VALUE(scale > 0 && std::isfinite(scale), "scale must be finite and positive");
         io = *io_of(q_);
         q = in_vectors(q_);
-        constexpr int64_t kApart = 16777212; // (the kernels' limit)
         k = in_vectors(k_, kApart);
         v = in_vectors(v_, kApart);
         a.q = q.data_ptr();
@@ -536,10 +543,289 @@ std::optional<Tensor> cross_attention(const Tensor &q, const Tensor &k, const Te
     const Tensor n = of_optional(lengths), m = of_optional(mask);
     if (!takes({&q, &k, &v, &n, &m}))
         return std::nullopt;
-    const double by = scale ? *scale : q.dim() > 0 && q.size(-1) > 0 ? 1.0 / std::sqrt((double)q.size(-1)) : 1.0;
+    const double by = scale_or_default(scale, q);
     if (recorded({&q, &k, &v}))
         return CrossAttention::apply(q, k, v, lengths, mask, by);
     return attention_forward(q, k, v, n, m, by, false)[0];
+}
+
+// ------------------------------------------------------------------------------------------------ causal attention
+
+// [tokens, heads, dim] of a packed operand, or of [batch, tokens, heads, dim], as the kernels read it; a copy where it is not.
+Tensor in_rows(const Tensor &given, int64_t group)
+{
+    const Tensor t = given.dim() == 4 ? given.flatten(0, 1) : given;
+    bool fine = t.stride(2) == 1 && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0;
+    for (int d = 0; d < 2; ++d)
+        fine = fine && (t.size(d) <= 1 || t.stride(d) % 8 == 0);
+    fine = fine && (t.size(0) <= 1 || (t.stride(0) >= 0 && t.stride(0) < kApart));
+    fine = fine && (t.size(1) <= 1 || (t.stride(1) >= 0 && t.stride(1) < ((int64_t)1 << 29) / group));
+    return fine ? t : t.clone(at::MemoryFormat::Contiguous);
+}
+
+void check_sixteen_bits(const Tensor &t, const char *name)
+{
+    check_gpu(t, name);
+    TORCH_CHECK_TYPE(t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf, name, " must be bfloat16 or float16, got ", t.scalar_type());
+}
+
+void check_dim(int64_t dim) { TORCH_CHECK_VALUE(dim >= 8 && dim <= 128 && dim % 8 == 0, "dim must be a multiple of 8, 128 at most, got ", dim); }
+
+void check_scale(double scale)
+{
+    TORCH_CHECK_VALUE(scale > 0 && std::isfinite(scale) && std::isfinite((float)(scale * 1.4426950408889634)), "scale must be finite and positive");
+}
+
+// offsets [sequences + 1], contiguous
+Tensor check_offsets(const Tensor &offsets, const Tensor &of, const char *name)
+{
+    TORCH_CHECK_TYPE(offsets.scalar_type() == at::kInt || offsets.scalar_type() == at::kLong, "offsets must be int32 or int64, got ", offsets.scalar_type());
+    TORCH_CHECK_VALUE(offsets.device() == of.device() && offsets.dim() == 1 && offsets.size(0) >= 1 && offsets.size(0) <= INT32_MAX,
+                      "offsets must be a [sequences + 1] tensor on the device of ", name);
+    return offsets.contiguous();
+}
+
+struct Causal {
+    Tensor q, k, v, offsets; // what the pointers point into
+    grkan_causal_attention_t a = {};
+    grkan_dtype_t io;
+    int64_t group;
+
+    Causal(const Tensor &q_, const Tensor &k_, const Tensor &v_, const Tensor &offsets_, double scale)
+    {
+        check_sixteen_bits(q_, "q");
+        check_like(k_, q_, "k", "q");
+        check_like(v_, q_, "v", "q");
+        const int64_t n = q_.dim();
+        TORCH_CHECK_VALUE((n == 3 || n == 4) && k_.dim() == n && k_.sizes() == v_.sizes() && k_.size(n - 1) == q_.size(n - 1) &&
+                              k_.sizes().slice(0, n - 2) == q_.sizes().slice(0, n - 2),
+                          "q must be [tokens, heads, dim] or [batch, tokens, heads, dim], k and v the same with kv_heads");
+        TORCH_CHECK_VALUE(n == 3 || !offsets_.defined(), "offsets go with packed tokens, [tokens, heads, dim]");
+        const int64_t heads = q_.size(n - 2), kv = k_.size(n - 2), dim = q_.size(n - 1);
+        TORCH_CHECK_VALUE(heads >= 1 && kv >= 1 && heads <= INT32_MAX && heads % kv == 0, "the heads of q must be a multiple of those of k and v");
+        check_dim(dim);
+        check_scale(scale);
+        io = *io_of(q_);
+        group = heads / kv;
+        q = in_rows(q_, group);
+        k = in_rows(k_, 1);
+        v = in_rows(v_, 1);
+        a.q = q.data_ptr();
+        a.k = k.data_ptr();
+        a.v = v.data_ptr();
+        a.tokens = q.size(0);
+        a.heads = (int32_t)heads;
+        a.kv_heads = (int32_t)kv;
+        a.dim = (int32_t)dim;
+        if (offsets_.defined()) {
+            offsets = check_offsets(offsets_, q_, "q");
+            a.offsets = offsets.data_ptr();
+            a.offsets_64 = offsets.scalar_type() == at::kLong;
+            a.sequences = (int32_t)offsets.size(0) - 1;
+        } else {
+            TORCH_CHECK_VALUE(n == 3 || q_.size(0) <= INT32_MAX, "there are too many sequences");
+            a.sequences = n == 4 && a.tokens > 0 ? (int32_t)q_.size(0) : 1;
+        }
+        // (the stride of a dimension of one element is never used)
+        auto strides = [](const Tensor &t, int64_t &token, int64_t &head) {
+            token = t.size(0) > 1 ? t.stride(0) : 0;
+            head = t.size(1) > 1 ? t.stride(1) : 0;
+        };
+        strides(q, a.q_token_stride, a.q_head_stride);
+        strides(k, a.k_token_stride, a.k_head_stride);
+        strides(v, a.v_token_stride, a.v_head_stride);
+        a.scale = (float)scale;
+    }
+};
+
+// {out, lse}; lse only where a backward pass may follow
+variable_list causal_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, double scale, bool with_lse)
+{
+    check_gpu(q, "q");
+    const c10::DeviceGuard guard(q.device());
+    const Causal d(q, k, v, offsets, scale);
+    const Tensor out = at::empty(q.sizes(), q.options());
+    Tensor lse;
+    if (with_lse)
+        lse = at::empty({(int64_t)grkan_causal_attention_lse_count(&d.a)}, q.options().dtype(at::kFloat));
+    check(grkan_causal_attention_fwd(&d.a, out.data_ptr(), with_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, d.io, stream_of(q)),
+          "grkan_causal_attention_fwd");
+    return {out, lse};
+}
+
+variable_list causal_backward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, double scale, const Tensor &out, const Tensor &lse,
+                              const Tensor &dout_)
+{
+    check_gpu(q, "q");
+    const c10::DeviceGuard guard(q.device());
+    const Causal d(q, k, v, offsets, scale);
+    check_like(out, q, "the saved output", "q");
+    check_like(dout_, q, "the gradient of the output", "q");
+    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.is_contiguous() && dout_.sizes() == q.sizes() && lse.scalar_type() == at::kFloat &&
+                          lse.device() == q.device() && lse.is_contiguous() && lse.numel() == (int64_t)grkan_causal_attention_lse_count(&d.a),
+                      "what the forward pass saved must match q");
+    const Tensor dout = in_rows(dout_, d.group);
+    const Tensor ws = at::empty({(int64_t)grkan_causal_attention_bwd_workspace_bytes(&d.a)}, q.options().dtype(at::kByte));
+    const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(v.sizes(), v.options());
+    check(grkan_causal_attention_bwd(&d.a, out.data_ptr(), static_cast<const float *>(lse.data_ptr()), dout.data_ptr(),
+                                     dout.size(0) > 1 ? dout.stride(0) : 0, dout.size(1) > 1 ? dout.stride(1) : 0, dq.data_ptr(), dk.data_ptr(),
+                                     dv.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), d.io, stream_of(q)),
+          "grkan_causal_attention_bwd");
+    return {dq, dk, dv};
+}
+
+struct CausalAttention : public torch::autograd::Function<CausalAttention> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &q, const Tensor &k, const Tensor &v, const OptionalTensor &offsets, double scale)
+    {
+        ctx->set_materialize_grads(false);
+        ctx->saved_data["scale"] = scale;
+        const variable_list out = causal_forward(q, k, v, of_optional(offsets), scale, true);
+        ctx->save_for_backward({q, k, v, of_optional(offsets), out[0], out[1]});
+        return out[0];
+    }
+
+    static variable_list backward(AutogradContext *ctx, const variable_list &grads)
+    {
+        const auto s = ctx->get_saved_variables();
+        variable_list out(5);
+        if (!grads[0].defined())
+            return out;
+        const double scale = ctx->saved_data["scale"].toDouble();
+        const variable_list found =
+            gradients({s[0], s[1], s[2], grads[0]}, [&] { return causal_backward(s[0], s[1], s[2], s[3], scale, s[4], s[5], grads[0]); });
+        for (int i = 0; i < 3; ++i)
+            out[i] = found[i];
+        return out;
+    }
+};
+
+std::optional<Tensor> causal_attention(const Tensor &q, const Tensor &k, const Tensor &v, const OptionalTensor &offsets, const std::optional<double> &scale)
+{
+    const Tensor n = of_optional(offsets);
+    if (!takes({&q, &k, &v, &n}))
+        return std::nullopt;
+    const double by = scale_or_default(scale, q);
+    if (recorded({&q, &k, &v}))
+        return CausalAttention::apply(q, k, v, offsets, by);
+    return causal_forward(q, k, v, n, by, false)[0];
+}
+
+// ------------------------------------------------------------------------------------------------ pages
+
+struct Cache {
+    Tensor table, lengths; // what the pointers point into
+    grkan_paged_cache_t c = {};
+    grkan_dtype_t io;
+
+    Cache(const Tensor &k, const Tensor &v, const Tensor &table_, const Tensor &lengths_)
+    {
+        check_sixteen_bits(k, "k_pages");
+        check_like(v, k, "v_pages", "k_pages");
+        TORCH_CHECK_VALUE(k.dim() == 4 && k.sizes() == v.sizes() && k.size(1) >= 1 && k.size(2) >= 1 && k.size(1) <= INT32_MAX && k.size(2) <= INT32_MAX,
+                          "k_pages and v_pages must be [pages, page_size, kv_heads, dim]");
+        check_dim(k.size(3));
+        for (const Tensor *t : {&k, &v}) {
+            bool fine = t->stride(3) == 1 && reinterpret_cast<uintptr_t>(t->data_ptr()) % 16 == 0;
+            for (int d = 0; d < 3; ++d)
+                fine = fine && (t->size(d) <= 1 || t->stride(d) % 8 == 0);
+            TORCH_CHECK_VALUE(fine && (t->size(1) <= 1 || (t->stride(1) >= 0 && t->stride(1) < kApart)),
+                              "the pages must have dense channels, strides and an address in whole 16 bytes, and tokens less than 2^24 elements apart");
+        }
+        TORCH_CHECK_TYPE(table_.scalar_type() == at::kInt, "table must be int32, got ", table_.scalar_type());
+        TORCH_CHECK_TYPE(lengths_.scalar_type() == at::kInt || lengths_.scalar_type() == at::kLong, "lengths must be int32 or int64, got ",
+                         lengths_.scalar_type());
+        TORCH_CHECK_VALUE(table_.device() == k.device() && table_.dim() == 2 && table_.size(0) <= INT32_MAX && table_.size(1) <= INT32_MAX,
+                          "table must be [sequences, entries] on the device of the pages");
+        TORCH_CHECK_VALUE(lengths_.device() == k.device() && lengths_.dim() == 1 && lengths_.size(0) == table_.size(0),
+                          "lengths must be [sequences] on the device of the pages");
+        table = table_.size(1) <= 1 || table_.stride(1) == 1 ? table_ : table_.contiguous();
+        lengths = lengths_.contiguous();
+        io = *io_of(k);
+        c.k_pages = k.data_ptr();
+        c.v_pages = v.data_ptr();
+        c.table = static_cast<const int32_t *>(table.data_ptr());
+        c.lengths = lengths.data_ptr();
+        c.lengths_64 = lengths.scalar_type() == at::kLong;
+        c.pages = k.size(0);
+        c.page_size = (int32_t)k.size(1);
+        c.sequences = (int32_t)table.size(0);
+        c.table_entries = (int32_t)table.size(1);
+        c.kv_heads = (int32_t)k.size(2);
+        c.dim = (int32_t)k.size(3);
+        c.table_stride = table.size(0) > 1 ? table.stride(0) : 0;
+        auto strides = [](const Tensor &t, int64_t &page, int64_t &token, int64_t &head) {
+            page = t.size(0) > 1 ? t.stride(0) : 0;
+            token = t.size(1) > 1 ? t.stride(1) : 0;
+            head = t.size(2) > 1 ? t.stride(2) : 0;
+        };
+        strides(k, c.k_page_stride, c.k_token_stride, c.k_head_stride);
+        strides(v, c.v_page_stride, c.v_token_stride, c.v_head_stride);
+    }
+};
+
+std::optional<bool> paged_write(const Tensor &k, const Tensor &v, const Tensor &k_pages, const Tensor &v_pages, const Tensor &table, const Tensor &lengths,
+                                const OptionalTensor &offsets_)
+{
+    Tensor offsets = of_optional(offsets_);
+    if (!takes({&k, &v, &k_pages, &v_pages, &table, &lengths, &offsets}))
+        return std::nullopt;
+    TORCH_CHECK(!recorded({&k, &v, &k_pages, &v_pages}), "the cache has no gradient: call paged_write without one (torch.no_grad())");
+    check_gpu(k_pages, "k_pages");
+    const c10::DeviceGuard guard(k_pages.device());
+    const Cache d(k_pages, v_pages, table, lengths);
+    at::assert_no_internal_overlap(k_pages);
+    at::assert_no_internal_overlap(v_pages);
+    check_like(k, k_pages, "k", "k_pages");
+    check_like(v, k_pages, "v", "k_pages");
+    const int64_t n = k.dim();
+    TORCH_CHECK_VALUE((n == 3 || n == 4) && k.sizes() == v.sizes() && k.size(n - 2) == k_pages.size(2) && k.size(n - 1) == k_pages.size(3),
+                      "k and v must be [tokens, kv_heads, dim] with offsets, or [sequences, tokens, kv_heads, dim], of the pages' heads and dim");
+    TORCH_CHECK_VALUE(n == 3 ? offsets.defined() : !offsets.defined() && k.size(0) == table.size(0),
+                      "packed tokens, [tokens, kv_heads, dim], come with offsets; [sequences, tokens, kv_heads, dim] without, one for each row of the table");
+    if (offsets.defined()) {
+        offsets = check_offsets(offsets, k_pages, "the pages");
+        TORCH_CHECK_VALUE(offsets.size(0) == table.size(0) + 1, "offsets must be [sequences + 1], sequences being the rows of the table");
+    }
+    const Tensor kr = in_rows(k, 1), vr = in_rows(v, 1);
+    check(grkan_paged_write(&d.c, kr.data_ptr(), vr.data_ptr(), data_of(offsets), offsets.defined() && offsets.scalar_type() == at::kLong, kr.size(0),
+                            kr.size(0) > 1 ? kr.stride(0) : 0, kr.size(1) > 1 ? kr.stride(1) : 0, vr.size(0) > 1 ? vr.stride(0) : 0,
+                            vr.size(1) > 1 ? vr.stride(1) : 0, d.io, stream_of(k_pages)),
+          "grkan_paged_write");
+    for (const Tensor *t : {&k_pages, &v_pages})
+        if (!t->is_inference())
+            t->unsafeGetTensorImpl()->bump_version();
+    return true;
+}
+
+std::optional<Tensor> paged_attention(const Tensor &q_, const Tensor &k_pages, const Tensor &v_pages, const Tensor &table, const Tensor &lengths,
+                                      const std::optional<double> &scale)
+{
+    if (!takes({&q_, &k_pages, &v_pages, &table, &lengths}))
+        return std::nullopt;
+    TORCH_CHECK(!recorded({&q_, &k_pages, &v_pages}), "attention over the cache has no gradient: call it without one (torch.no_grad())");
+    check_sixteen_bits(q_, "q");
+    const c10::DeviceGuard guard(q_.device());
+    check_like(k_pages, q_, "k_pages", "q");
+    const Cache d(k_pages, v_pages, table, lengths);
+    TORCH_CHECK_VALUE(q_.dim() == 4 && q_.size(0) == table.size(0) && q_.size(3) == k_pages.size(3),
+                      "q must be [sequences, tokens, heads, dim], with a sequence for each row of the table and the pages' dim");
+    TORCH_CHECK_VALUE(q_.size(2) >= 1 && q_.size(2) <= INT32_MAX && q_.size(2) % k_pages.size(2) == 0, "the heads of q must be a multiple of those of the pages");
+    const double by = scale_or_default(scale, q_);
+    check_scale(by);
+    const Tensor q = in_vectors(q_);
+    grkan_paged_queries_t a = {};
+    a.q = q.data_ptr();
+    a.tokens = q.size(1);
+    a.heads = (int32_t)q.size(2);
+    a.sequence_stride = q.size(0) > 1 ? q.stride(0) : 0;
+    a.token_stride = q.size(1) > 1 ? q.stride(1) : 0;
+    a.head_stride = q.size(2) > 1 ? q.stride(2) : 0;
+    a.scale = (float)by;
+    const Tensor out = at::empty(q.sizes(), q.options());
+    const size_t need = grkan_paged_attention_workspace_bytes(&d.c, &a);
+    const Tensor ws = need ? at::empty({(int64_t)need}, q.options().dtype(at::kByte)) : Tensor();
+    check(grkan_paged_attention(&d.c, &a, out.data_ptr(), data_of(ws), need, d.io, stream_of(q)), "grkan_paged_attention");
+    return out;
 }
 
 } // namespace
@@ -571,5 +857,25 @@ void define_transformer(pybind11::module_ &mod)
         const Tensor q = args.tensor(q_, "q"), k = args.tensor(k_, "k"), v = args.tensor(v_, "v");
         const OptionalTensor lengths = args.optional(lengths_, "key_lengths"), mask = args.optional(mask_, "key_mask");
         return args.call([&] { return cross_attention(q, k, v, lengths, mask, scale); });
+    });
+    mod.def("causal_attention", [](handle q_, handle k_, handle v_, handle offsets_, std::optional<double> scale) {
+        Operands args;
+        const Tensor q = args.tensor(q_, "q"), k = args.tensor(k_, "k"), v = args.tensor(v_, "v");
+        const OptionalTensor offsets = args.optional(offsets_, "offsets");
+        return args.call([&] { return causal_attention(q, k, v, offsets, scale); });
+    });
+    mod.def("paged_write", [](handle k_, handle v_, handle k_pages_, handle v_pages_, handle table_, handle lengths_, handle offsets_) {
+        Operands args;
+        const Tensor k = args.tensor(k_, "k"), v = args.tensor(v_, "v");
+        const Tensor k_pages = args.tensor(k_pages_, "k_pages"), v_pages = args.tensor(v_pages_, "v_pages");
+        const Tensor table = args.tensor(table_, "table"), lengths = args.tensor(lengths_, "lengths");
+        const OptionalTensor offsets = args.optional(offsets_, "offsets");
+        return args.call([&] { return paged_write(k, v, k_pages, v_pages, table, lengths, offsets); });
+    });
+    mod.def("paged_attention", [](handle q_, handle k_pages_, handle v_pages_, handle table_, handle lengths_, std::optional<double> scale) {
+        Operands args;
+        const Tensor q = args.tensor(q_, "q"), k_pages = args.tensor(k_pages_, "k_pages"), v_pages = args.tensor(v_pages_, "v_pages");
+        const Tensor table = args.tensor(table_, "table"), lengths = args.tensor(lengths_, "lengths");
+        return args.call([&] { return paged_attention(q, k_pages, v_pages, table, lengths, scale); });
     });
 }

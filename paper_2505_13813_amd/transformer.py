@@ -107,6 +107,41 @@ def cross_attention(q, k, v, key_lengths=None, key_mask=None, scale: Optional[fl
     return _taken(binding.load_native().cross_attention(q, k, v, key_lengths, key_mask, scale), "cross_attention")
 
 
+@_outside_graphs
+def causal_attention(q, k, v, offsets=None, scale: Optional[float] = None):
+    """softmax(scale q k^T) v over the tokens of the same sequence up to the token itself, head h reading key head h // (heads / kv_heads).
+
+    q [tokens, heads, dim], k, v [tokens, kv_heads, dim]: sequences packed one behind the other, sequence s being tokens offsets[s] up to, not with,
+    offsets[s + 1] (int [sequences + 1], not falling; one sequence where there are none).  Tokens in front of the first and behind the last belong to no sequence:
+    zeros, and zeros as their gradients.  Or q [batch, tokens, heads, dim], k and v alike, without offsets: a sequence each.
+    bfloat16 or float16, dim a multiple of 8 up to 128, any strides with dense channels; scale: dim ** -0.5.
+    No sequence has any influence on another, and no later token on an earlier one's output, NaN and infinities included.  Differentiable (once) with
+    respect to q, k and v."""
+    return _taken(binding.load_native().causal_attention(q, k, v, offsets, scale), "causal_attention")
+
+
+@_outside_graphs
+def paged_write(k, v, k_pages, v_pages, table, lengths, offsets=None) -> None:
+    """Keys and values of new tokens into a cache in pages, in place.  Position p of sequence s lies in row p % page_size of page table[s, p // page_size].
+
+    k_pages, v_pages [pages, page_size, kv_heads, dim] bfloat16 or float16, whose strides and address are whole 16 bytes, channels dense (they may be a view
+    of [pages, kv_heads, page_size, dim]); table int32 [sequences, entries]; lengths int [sequences]: with the new tokens.  k, v [tokens, kv_heads, dim] packed, with
+    offsets as in causal_attention, or [sequences, tokens, kv_heads, dim].  A sequence's last new token goes to position lengths[s] - 1, the
+    others in front of it.  Tokens of no sequence go nowhere, and neither do those whose entry is no page (below 0, or too large), whose position would be below 0, or
+    whose sequence is longer than its row of the table has place for.  No gradient."""
+    _taken(binding.load_native().paged_write(k, v, k_pages, v_pages, table, lengths, offsets), "paged_write")
+
+
+@_outside_graphs
+def paged_attention(q, k_pages, v_pages, table, lengths, scale: Optional[float] = None):
+    """Attention of the newest tokens over a cache in pages (paged_write): q [sequences, tokens, heads, dim], token i of sequence s being that of position
+    lengths[s] - tokens + i, sees the positions up to its own, its keys and values having been written.  One token, or a few.
+
+    A token that sees nothing (an empty sequence, an entry that is no page) gets zeros.  What the pages hold elsewhere, NaN and infinities included, has no
+    influence.  Split over the cache's length where that pays, and joined.  scale: dim ** -0.5.  No gradient."""
+    return _taken(binding.load_native().paged_attention(q, k_pages, v_pages, table, lengths, scale), "paged_attention")
+
+
 class RMSNorm(nn.Module):
     """rms_norm with its weight: forward(x) gives y, forward(x, residual) gives (y, x + residual)."""
 

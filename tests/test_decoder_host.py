@@ -1,0 +1,193 @@
+"""Causal attention and the cache in pages without a GPU: the C interface's structures and refusals (each before anything is launched), workspaces, and the refusal
+of tensors on the CPU."""
+import ctypes
+import math
+import re
+from pathlib import Path
+
+import pytest
+
+from paper_2505_13813_amd import binding
+
+ROOT = Path(__file__).resolve().parent.parent
+OK, NULL, SHAPE, ALIGN, WORKSPACE, DTYPE, UNSUPPORTED = 0, 1, 2, 4, 5, 6, 8
+F32, BF16, F16 = binding.GRKAN_F32, binding.GRKAN_BF16, binding.GRKAN_F16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return binding.load_library()
+
+
+@pytest.mark.parametrize("name,struct", [("grkan_causal_attention_t", binding.CausalAttention), ("grkan_paged_cache_t", binding.PagedCacheOperand),
+                                         ("grkan_paged_queries_t", binding.PagedQueries)])
+def test_structures_match_the_header(name, struct):
+    text = re.sub(r"/\*.*?\*/", "", (ROOT / "include" / "grkan_transformer.h").read_text(), flags=re.S)
+    body = re.search(r"typedef struct \{([^}]*)\} %s;" % name, text).group(1)
+    kinds = {"void": ctypes.c_void_p, "int32_t": ctypes.c_int32, "int64_t": ctypes.c_int64, "float": ctypes.c_float}
+    fields = []
+    for line in body.split(";"):
+        if line.strip():
+            kind, names = re.match(r"\s*(?:const )?(\w+)\s+(.*)", line, flags=re.S).groups()
+            fields += [(n.strip(" *\n"), ctypes.c_void_p if "*" in n else kinds[kind]) for n in names.split(",")]
+    assert fields == list(struct._fields_)
+
+
+def _causal(**fields):
+    given = dict(q=16, k=16, v=16, offsets=16, tokens=40, sequences=3, heads=4, kv_heads=2, dim=64, q_token_stride=256, q_head_stride=64, k_token_stride=128,
+                 k_head_stride=64, v_token_stride=128, v_head_stride=64, scale=0.125)
+    given.update(fields)
+    return binding.CausalAttention(**given)
+
+
+BAD_CAUSAL = [({"q": None}, NULL), ({"k": None}, NULL), ({"v": None}, NULL), ({"tokens": -1}, SHAPE), ({"sequences": -1}, SHAPE), ({"heads": 0}, SHAPE),
+              ({"heads": 5}, SHAPE), ({"kv_heads": 0}, SHAPE), ({"dim": 0}, SHAPE), ({"offsets": None}, SHAPE), ({"offsets": None, "sequences": 0}, SHAPE),
+              ({"dim": 60}, UNSUPPORTED), ({"dim": 136}, UNSUPPORTED), ({"scale": 0.0}, UNSUPPORTED), ({"scale": -1.0}, UNSUPPORTED),
+              ({"scale": math.inf}, UNSUPPORTED), ({"scale": math.nan}, UNSUPPORTED), ({"scale": 3e38}, UNSUPPORTED), ({"tokens": 1 << 30}, UNSUPPORTED),
+              ({"tokens": 1 << 29, "heads": 8}, UNSUPPORTED), ({"heads": 2 << 20, "tokens": 1}, UNSUPPORTED), ({"k_token_stride": -128}, UNSUPPORTED),
+              ({"q_token_stride": 1 << 25}, UNSUPPORTED), ({"v_token_stride": 1 << 25}, UNSUPPORTED), ({"q_head_stride": -64}, UNSUPPORTED),
+              ({"q_head_stride": 1 << 30}, UNSUPPORTED), ({"sequences": 1 << 30}, UNSUPPORTED), ({"q": 24}, ALIGN), ({"k": 24}, ALIGN), ({"v": 24}, ALIGN),
+              ({"q_token_stride": 257}, ALIGN), ({"k_head_stride": 60}, ALIGN), ({"offsets": 18}, ALIGN), ({"offsets": 20, "offsets_64": 1}, ALIGN)]
+
+
+@pytest.mark.parametrize("fields,status", BAD_CAUSAL)
+def test_causal_refusals(lib, fields, status):
+    a = _causal(**fields)
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, BF16, None) == status
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 40, BF16, None) == status
+    assert lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a)) == 0
+
+
+def test_causal_refusals_of_outputs(lib):
+    a = _causal()
+    assert lib.grkan_causal_attention_fwd(None, 16, None, BF16, None) == NULL
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), None, None, BF16, None) == NULL
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 24, None, BF16, None) == ALIGN
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, 18, BF16, None) == ALIGN
+    for io in (F32, 9):
+        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, io, None) == DTYPE
+    need = lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a))
+
+    def bwd(out=16, lse=16, dout=16, strides=(256, 64), dq=16, dk=16, dv=16, ws=16, size=need):
+        return lib.grkan_causal_attention_bwd(ctypes.byref(a), out, lse, dout, *strides, dq, dk, dv, ws, size, BF16, None)
+
+    for name in ("out", "lse", "dout", "dq", "dk", "dv"):
+        assert bwd(**{name: None}) == NULL, name
+        assert bwd(**{name: 18}) == ALIGN, name
+    assert bwd(strides=(257, 64)) == ALIGN and bwd(strides=(1 << 25, 64)) == UNSUPPORTED and bwd(strides=(-256, 64)) == UNSUPPORTED
+    assert need > 0 and bwd(size=need - 1) == WORKSPACE and bwd(ws=None) == WORKSPACE and bwd(ws=24) == WORKSPACE
+    none = _causal(tokens=0, q=None, k=None, v=None)
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(none), None, None, BF16, None) == OK
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(none), None, None, None, 0, 0, None, None, None, None, 0, BF16, None) == OK
+    assert lib.grkan_causal_attention_lse_count(ctypes.byref(a)) == 40 * 4
+
+
+def test_causal_workspaces(lib):
+    """The plan is made for every combination of few and many tokens, sequences and heads; what is asked for can be had."""
+    for tokens in (1, 127, 5000, 70000, 1 << 20):
+        for sequences in (1, 3, 200, 40000):
+            for heads, kv in ((1, 1), (12, 12), (32, 4), (40, 1)):
+                for dim in (8, 64, 128):
+                    a = _causal(tokens=tokens, sequences=sequences, heads=heads, kv_heads=kv, dim=dim)
+                    need = lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a))
+                    assert 0 < need < (1 << 30) + 64 * (tokens + sequences) * heads
+
+
+def test_more_workgroups_than_a_launch_takes(lib):
+    a = _causal(tokens=1 << 24, heads=64, kv_heads=64, sequences=1 << 24)
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, BF16, None) == UNSUPPORTED
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 60, BF16, None) == UNSUPPORTED
+
+
+def _cache(**fields):
+    given = dict(k_pages=16, v_pages=16, table=16, lengths=16, pages=100, page_size=16, sequences=3, table_entries=20, kv_heads=2, dim=64, lengths_64=0, table_stride=20,
+                 k_page_stride=2048, k_token_stride=128, k_head_stride=64, v_page_stride=2048, v_token_stride=128, v_head_stride=64)
+    given.update(fields)
+    return binding.PagedCacheOperand(**given)
+
+
+def _queries(**fields):
+    given = dict(q=16, tokens=1, heads=4, sequence_stride=256, token_stride=256, head_stride=64, scale=0.125)
+    given.update(fields)
+    return binding.PagedQueries(**given)
+
+
+BAD_CACHE = [({"k_pages": None}, NULL), ({"v_pages": None}, NULL), ({"table": None}, NULL), ({"lengths": None}, NULL), ({"pages": -1}, SHAPE), ({"page_size": 0}, SHAPE),
+             ({"sequences": -1}, SHAPE), ({"table_entries": -1}, SHAPE), ({"kv_heads": 0}, SHAPE), ({"dim": 0}, SHAPE), ({"dim": 60}, UNSUPPORTED), ({"dim": 136}, UNSUPPORTED),
+             ({"pages": 1 << 31}, UNSUPPORTED), ({"page_size": 1 << 20, "table_entries": 1 << 10}, UNSUPPORTED), ({"k_token_stride": -128}, UNSUPPORTED),
+             ({"v_token_stride": 1 << 25}, UNSUPPORTED), ({"k_pages": 24}, ALIGN), ({"v_pages": 24}, ALIGN), ({"table": 18}, ALIGN), ({"lengths": 18}, ALIGN),
+             ({"lengths": 20, "lengths_64": 1}, ALIGN), ({"k_page_stride": 2047}, ALIGN), ({"v_head_stride": 60}, ALIGN)]
+
+
+@pytest.mark.parametrize("fields,status", BAD_CACHE)
+def test_cache_refusals(lib, fields, status):
+    c, q = _cache(**fields), _queries()
+    assert lib.grkan_paged_attention(ctypes.byref(c), ctypes.byref(q), 16, 16, 1 << 40, BF16, None) == status
+    assert lib.grkan_paged_write(ctypes.byref(c), 16, 16, 16, 0, 5, 128, 64, 128, 64, BF16, None) == status
+    assert lib.grkan_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(q)) == 0
+
+
+@pytest.mark.parametrize("fields,status", [({"q": None}, NULL), ({"tokens": -1}, SHAPE), ({"heads": 0}, SHAPE), ({"heads": 3}, SHAPE), ({"tokens": 1 << 30}, UNSUPPORTED),
+                                           ({"tokens": 1 << 29, "heads": 8}, UNSUPPORTED), ({"scale": 0.0}, UNSUPPORTED), ({"scale": math.nan}, UNSUPPORTED),
+                                           ({"q": 24}, ALIGN), ({"token_stride": 60}, ALIGN)])
+def test_queries_refusals(lib, fields, status):
+    c, q = _cache(), _queries(**fields)
+    assert lib.grkan_paged_attention(ctypes.byref(c), ctypes.byref(q), 16, 16, 1 << 40, BF16, None) == status
+    assert lib.grkan_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(q)) == 0
+
+
+def test_other_refusals_of_pages(lib):
+    c, q = _cache(), _queries()
+
+    def attend(cache=c, queries=q, out=16, ws=16, size=1 << 40, io=BF16):
+        return lib.grkan_paged_attention(ctypes.byref(cache) if cache else None, ctypes.byref(queries) if queries else None, out, ws, size, io, None)
+
+    assert attend(cache=None) == NULL and attend(queries=None) == NULL and attend(out=None) == NULL and attend(out=24) == ALIGN
+    for io in (F32, 9):
+        assert attend(io=io) == DTYPE
+        assert lib.grkan_paged_write(ctypes.byref(c), 16, 16, 16, 0, 5, 128, 64, 128, 64, io, None) == DTYPE
+    long = _cache(table_entries=1000)
+    need = lib.grkan_paged_attention_workspace_bytes(ctypes.byref(long), ctypes.byref(q))
+    assert need > 0 and attend(long, size=need - 1) == WORKSPACE and attend(long, ws=None, size=need) == WORKSPACE and attend(long, ws=24, size=need) == WORKSPACE
+    assert attend(_cache(sequences=0), out=None) == OK and attend(queries=_queries(tokens=0, q=None), out=None) == OK
+    many = _cache(sequences=1 << 24)
+    assert attend(many) == UNSUPPORTED
+
+    def write(cache=c, k=16, v=16, offsets=16, wide=0, tokens=5, strides=(128, 64, 128, 64)):
+        return lib.grkan_paged_write(ctypes.byref(cache) if cache else None, k, v, offsets, wide, tokens, *strides, BF16, None)
+
+    assert write(cache=None) == NULL and write(k=None) == NULL and write(v=None) == NULL
+    assert write(tokens=-1) == SHAPE and write(offsets=None, tokens=5) == SHAPE and write(cache=_cache(sequences=0), offsets=None) == SHAPE
+    assert write(k=24) == ALIGN and write(v=24) == ALIGN and write(offsets=18) == ALIGN and write(offsets=20, wide=1) == ALIGN and write(strides=(60, 64, 128, 64)) == ALIGN
+    assert write(tokens=1 << 30) == UNSUPPORTED and write(cache=_cache(kv_heads=1 << 21)) == UNSUPPORTED
+    assert write(tokens=0, k=None, v=None) == OK and write(cache=_cache(pages=0, k_pages=None, v_pages=None)) == OK
+
+
+def test_paged_workspaces(lib):
+    for sequences in (1, 7, 300, 5000):
+        for entries in (1, 30, 10000):
+            for kv, heads in ((1, 1), (8, 32), (12, 12)):
+                for tokens in (1, 5, 100):
+                    for dim in (8, 64, 128):
+                        c = _cache(sequences=sequences, table_entries=entries, kv_heads=kv, dim=dim)
+                        need = lib.grkan_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(_queries(heads=heads, tokens=tokens)))
+                        assert need <= 4 * 32 * 129 * (1024 + 256)
+
+
+def test_tensors_on_the_cpu_and_missing_ones_are_refused():
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    q, pool = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 16, 2, 64, dtype=torch.bfloat16)
+    table, lengths, offsets = torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, dtype=torch.int32), torch.zeros(5, dtype=torch.int32)
+    for call in (lambda: T.causal_attention(q, q, q), lambda: T.causal_attention(q, q, q, offsets), lambda: T.paged_attention(q[:, None], pool, pool, table, lengths),
+                 lambda: T.paged_write(q, q, pool, pool, table, lengths, offsets)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    for call, name in ((lambda: T.causal_attention(None, q, q), "q"), (lambda: T.causal_attention(q, q, q, [0, 4]), "offsets"),
+                       (lambda: T.paged_attention(q, pool, None, table, lengths), "v_pages"), (lambda: T.paged_attention(q, pool, pool, None, lengths), "table"),
+                       (lambda: T.paged_attention(q, pool, pool, table, 4), "lengths"), (lambda: T.paged_write(q, None, pool, pool, table, lengths), "v"),
+                       (lambda: T.paged_write(q, q, None, pool, table, lengths), "k_pages")):
+        with pytest.raises(TypeError, match=r"^%s must be a tensor" % name):
+            call()

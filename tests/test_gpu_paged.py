@@ -1,0 +1,409 @@
+"""GPU tests of the cache in pages: what new tokens leave in it, bit by bit, and the attention of the newest tokens over it against the formulas in 64 bits
+(bounds: attention_bounds.py)."""
+import math
+
+import pytest
+from attention_bounds import assert_within, formulas
+
+pytestmark = pytest.mark.gpu
+
+# lengths with the new tokens, new tokens of each, tokens of a page, heads, key heads, dim
+CASES = [([1], 1, 16, 1, 1, 8), ([500], 1, 16, 12, 12, 64), ([40, 0, 1, 129], 1, 32, 8, 2, 128), ([700, 31, 2000], 1, 1, 4, 4, 64),
+         ([33, 64, 95, 96], 1, 24, 6, 2, 80), ([3000], 1, 128, 32, 8, 128), ([5, 3, 0, 700], 5, 8, 12, 4, 96), ([9000, 40], 1, 64, 2, 1, 64),
+         ([100, 2, 64], 16, 20, 8, 2, 32), ([130] * 90, 1, 16, 2, 2, 64), ([2500, 1], 40, 7, 3, 1, 72), ([4097, 333, 0, 0, 8000], 2, 256, 8, 1, 128),
+         ([60, 61], 33, 1000, 2, 2, 40), ([300] * 300, 1, 64, 4, 4, 24), ([20000], 3, 5, 4, 1, 104), ([6000, 3500], 1, 2, 2, 2, 64)]
+
+
+def _type(torch, dtype):
+    return {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+
+
+def _rand(torch, gen, dtype, *shape, std=1.0):
+    return (torch.randn(*shape, device="cuda:0", generator=gen) * std).to(_type(torch, dtype))
+
+
+def _cache(torch, lengths, page, kv, dim, dtype, seed=0, spare=3, heads_first=False, poison=True):
+    """(k_pages, v_pages, table, keys, values): keys and values [length, kv, dim] of each sequence, in pages in an order of chance.  With `poison`, NaN and
+    infinities in all places that hold nothing; entries behind the sequences are no pages."""
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(1000 * seed + page + dim)
+    counts = [-(-n // page) for n in lengths]
+    pages, wide = sum(counts) + spare, max(counts + [0]) + 2
+    order = torch.randperm(pages, generator=gen, device="cuda:0").tolist()
+    bad = torch.tensor([math.nan, math.inf, -math.inf], device="cuda:0").to(_type(torch, dtype))
+    found = []
+    for _ in range(2):
+        t = bad[torch.randint(0, 3, (pages, page, kv, dim), generator=gen, device="cuda:0")] if poison else _rand(torch, gen, dtype, pages, page, kv, dim)
+        found.append(t.transpose(1, 2).contiguous().transpose(1, 2) if heads_first else t)
+    table, each = torch.full((len(lengths), wide), 2 ** 31 - 1, dtype=torch.int32), ([], [])
+    for s, n in enumerate(lengths):
+        mine = [order.pop() for _ in range(counts[s])]
+        table[s, :counts[s]] = torch.tensor(mine, dtype=torch.int32)
+        position = torch.arange(n, device="cuda:0")
+        at = torch.tensor(mine, dtype=torch.int64, device="cuda:0")[position // page] if n else position
+        for t, held in zip(found, each):
+            held.append(_rand(torch, gen, dtype, n, kv, dim, std=1.3))
+            t[at, position % page] = held[-1]
+    return *found, table.cuda(), *each
+
+
+def _assert_attends(torch, got, q, lengths, keys, values, dtype, label):
+    n, dim = q.shape[1], q.shape[3]
+    for s, length in enumerate(lengths):
+        first = max(0, n - length)  # tokens in front of it have no position
+        assert (got[s, :first] == 0).all(), (label, s)
+        if length == 0:
+            continue
+        position = length - n + torch.arange(first, n, device="cuda:0")
+        ok = torch.arange(length, device="cuda:0") <= position[:, None]
+        assert_within([got[s, first:]], formulas(torch, q[s, first:], keys[s], values[s], ok, dim ** -0.5, dtype), (label, s))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "%s+%s %s %s %sx%s %s" % (len(c[0]), sum(c[0]), *c[1:]))
+def test_attention(case, dtype):
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention
+
+    print(case, dtype, flush=True)
+    lengths, n, page, heads, kv, dim = case
+    k_pages, v_pages, table, keys, values = _cache(torch, lengths, page, kv, dim, dtype, heads_first=dim == 64)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(5)
+    q = _rand(torch, gen, dtype, len(lengths), n, heads, dim, std=1.5)
+    given = torch.tensor(lengths, device="cuda:0", dtype=torch.int64 if n == 1 else torch.int32)
+    got = paged_attention(q, k_pages, v_pages, table, given)
+    assert got.is_contiguous() and got.dtype == q.dtype and got.shape == q.shape
+    _assert_attends(torch, got, q, lengths, keys, values, dtype, case)
+    assert torch.equal(got, paged_attention(q, k_pages, v_pages, table, given))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", [([7, 0, 1, 40], [0, 0, 0, 0], 16, 2, 64), ([5, 3, 2], [11, 0, 30], 8, 1, 40), ([1] * 70, [3 * i for i in range(70)], 16, 8, 128),
+                                  ([1000, 1, 0, 0, 130], [17, 100, 3, 0, 1], 20, 4, 96), ([2000], [5], 1, 2, 8), ([3] * 300, [0] * 300, 64, 3, 72)])
+def test_write(case, dtype):
+    """Packed tokens with NaN and infinities among them: their places hold them bit by bit, all others what they held; tokens of no sequence go nowhere."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_write
+
+    new, before, page, kv, dim = case
+    print(case, dtype, flush=True)
+    lengths = [a + b for a, b in zip(new, before)]
+    k_pages, v_pages, table, *_ = _cache(torch, lengths, page, kv, dim, dtype, 1, poison=False)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(6)
+    front, behind = 3, 5
+    both = _rand(torch, gen, dtype, front + sum(new) + behind, 2, kv, dim)
+    both[torch.rand(both.shape, generator=gen, device="cuda:0") < 0.01] = math.nan
+    k, v = both[:, 0], both[:, 1]
+    offsets = [front]
+    for n in new:
+        offsets.append(offsets[-1] + n)
+    want = [k_pages.clone(), v_pages.clone()]
+    for s, n in enumerate(new):
+        position = before[s] + torch.arange(n, device="cuda:0")
+        for to, t in zip(want, (k, v)):
+            to[table[s].long()[position // page], position % page] = t[offsets[s]:offsets[s + 1]]
+    versions = k_pages._version, v_pages._version
+    assert paged_write(k, v, k_pages, v_pages, table, torch.tensor(lengths, device="cuda:0"), torch.tensor(offsets, device="cuda:0", dtype=torch.int32)) is None
+    for got, w in zip((k_pages, v_pages), want):
+        assert torch.equal(got.view(torch.int16), w.view(torch.int16))
+    assert k_pages._version > versions[0] and v_pages._version > versions[1]
+
+
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_write_of_as_many_tokens_each(heads_first):
+    """[sequences, tokens, kv_heads, dim] without offsets, strided and misaligned, into pages of either layout: the bits of the packed call."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_write
+
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(7)
+    for tokens, page in ((1, 16), (9, 5)):
+        lengths = [tokens, tokens + 40, tokens + 7]
+        start = _cache(torch, lengths, page, 2, 64, "bf16", 2, heads_first=heads_first, poison=False)
+        k, v = (_rand(torch, gen, "bf16", 3, tokens, 2, 64) for _ in range(2))
+        given, found = torch.tensor(lengths, device="cuda:0", dtype=torch.int32), []
+        offsets = torch.arange(4, device="cuda:0") * tokens
+        off = [torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda:0")[1:].view(t.shape).copy_(t) for t in (k, v)]
+        turned = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (k, v)]
+        for call in ((k.flatten(0, 1), v.flatten(0, 1), offsets), (k, v, None), (*off, None), (*turned, None)):
+            pages = [t.clone(memory_format=torch.preserve_format) for t in start[:2]]
+            assert pages[0].stride() == start[0].stride()
+            paged_write(call[0], call[1], *pages, start[2], given, call[2])
+            found.append(pages)
+        assert all(torch.equal(a, b) for pages in found[1:] for a, b in zip(found[0], pages))
+        assert not torch.equal(found[0][0], start[0])
+
+
+@pytest.mark.parametrize("page", [8, 32])
+def test_entries_that_are_no_pages(page):
+    """Entries below 0 and past the pages: nothing is written there, their positions are not attended to, and a token that has no others gets zeros."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention, paged_write
+
+    lengths = [3 * page + 3, 2 * page, page // 2, 40 * page]
+    k_pages, v_pages, table, keys, values = _cache(torch, lengths, page, 2, 64, "bf16", 3)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(8)
+    q = _rand(torch, gen, "bf16", 4, 2, 4, 64)
+    table[0, 1], table[1, :2], table[2, 0], table[3, 7] = -1, 2 ** 31 - 1, -2 ** 31, k_pages.shape[0]
+    got = paged_attention(q, k_pages, v_pages, table, torch.tensor(lengths, device="cuda:0"))
+    for s, gone in ((0, [1]), (1, [0, 1]), (2, [0]), (3, [7])):
+        n = lengths[s]
+        at = torch.arange(n, device="cuda:0")
+        kept = torch.ones(n, dtype=torch.bool, device="cuda:0")
+        for p in gone:
+            kept &= at // page != p
+        ok = (at <= n - 2 + torch.arange(2, device="cuda:0")[:, None]) & kept
+        clean = [torch.where(kept[:, None, None], t[s], 0) for t in (keys, values)]
+        assert_within([got[s]], formulas(torch, q[s], *clean, ok, 0.125, "bf16"), s)
+    assert (got[1] == 0).all() and (got[2] == 0).all()
+    before = [k_pages.clone(), v_pages.clone()]
+    new = _rand(torch, gen, "bf16", 4, page + 1, 2, 64)
+    paged_write(new, new, k_pages, v_pages, table, torch.tensor(lengths, device="cuda:0"))
+    for got, w in zip((k_pages, v_pages), before):
+        for s, n in enumerate(lengths):
+            for i in range(page + 1):
+                p = n - page - 1 + i
+                if p >= 0 and 0 <= int(table[s, p // page]) < w.shape[0]:
+                    w[int(table[s, p // page]), p % page] = new[s, i]
+        assert torch.equal(got.view(torch.int16), w.view(torch.int16))
+
+
+def test_lengths_outside_the_table():
+    """A length below 0 is no length, one past the table's places ends there for attention and writes nothing."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention, paged_write
+
+    page, places = 16, 5 * 16
+    k_pages, v_pages, table, keys, values = _cache(torch, [places, places, places], page, 1, 64, "f16", 4, poison=False)
+    table = table[:, :5].contiguous()
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(9)
+    q = _rand(torch, gen, "f16", 3, 1, 2, 64)
+    given = torch.tensor([places, places + 1, -3], device="cuda:0")
+    got = paged_attention(q, k_pages, v_pages, table, given)
+    _assert_attends(torch, got, q, [places, places, 0], keys, values, "f16", "lengths")
+    huge = torch.tensor([places, 2 ** 40, -2 ** 40], device="cuda:0")
+    assert torch.equal(got, paged_attention(q, k_pages, v_pages, table, huge))
+    before = k_pages.clone()
+    new = _rand(torch, gen, "f16", 3, 2, 1, 64)
+    for lengths in (given, huge):
+        paged_write(new, new, k_pages, v_pages, table, lengths)
+    before[table[0, 4].long(), 14:] = new[0]
+    assert torch.equal(k_pages, before)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_later_tokens_have_no_influence(page, dtype):
+    """NaN and infinities in the newest token's keys and values: the tokens before it get the same bits."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention
+
+    for lengths, n, heads, kv, dim in (([70, 300], 4, 4, 2, 64), ([3000, 50], 3, 8, 8, 128), ([200, 9], 20, 4, 1, 96)):
+        k_pages, v_pages, table, *_ = _cache(torch, lengths, page, kv, dim, dtype, 5)
+        gen = torch.Generator(device="cuda:0")
+        gen.manual_seed(10)
+        q = _rand(torch, gen, dtype, 2, n, heads, dim)
+        given = torch.tensor(lengths, device="cuda:0")
+        want = paged_attention(q, k_pages, v_pages, table, given)
+        for s, length in enumerate(lengths):
+            at = table[s, (length - 1) // page].long(), (length - 1) % page
+            k2, v2 = k_pages.clone(), v_pages.clone()
+            k2[at], v2[at] = math.nan, math.inf
+            got = paged_attention(q, k2, v2, table, given)
+            assert torch.equal(got[1 - s], want[1 - s]) and torch.equal(got[s, :-1], want[s, :-1])
+            assert bool((~got[s, -1].isfinite()).all())
+
+
+def test_layouts_of_queries():
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention
+
+    k_pages, v_pages, table, *_ = _cache(torch, [50, 400], 16, 2, 64, "bf16", 6)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(11)
+    q = _rand(torch, gen, "bf16", 2, 3, 4, 64)
+    given = torch.tensor([50, 400], device="cuda:0")
+    want = paged_attention(q, k_pages, v_pages, table, given)
+    off = torch.empty(q.numel() + 1, dtype=q.dtype, device="cuda:0")[1:].view(q.shape).copy_(q)
+    wide = torch.zeros(2, 3, 4, 96, dtype=q.dtype, device="cuda:0")[..., 16:80].copy_(q)
+    for other in (q.permute(2, 0, 3, 1).contiguous().permute(1, 3, 0, 2), off, wide, q.transpose(1, 2).contiguous().transpose(1, 2)):
+        assert torch.equal(paged_attention(other, k_pages, v_pages, table, given), want)
+    turned = table.t().contiguous().t()
+    every_other = torch.stack([given, given], 1)[:, 0]
+    assert torch.equal(paged_attention(q, k_pages, v_pages, turned, every_other), want)
+    sliced = torch.cat([table, table], 1)[:, :table.shape[1]]
+    assert torch.equal(paged_attention(q, k_pages, v_pages, sliced, given), want)
+    assert torch.equal(paged_attention(q, k_pages, v_pages, table, given, scale=0.125), want)
+
+
+def test_a_page_of_two_sequences():
+    """Pages in two rows of the table, as of prompts that begin alike."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention
+
+    lengths = [100, 90]
+    k_pages, v_pages, table, keys, values = _cache(torch, lengths, 16, 2, 64, "bf16", 7)
+    table[1, :4] = table[0, :4]
+    for t in (keys, values):
+        t[1] = torch.cat([t[0][:64], t[1][64:]])
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(12)
+    q = _rand(torch, gen, "bf16", 2, 1, 4, 64)
+    _assert_attends(torch, paged_attention(q, k_pages, v_pages, table, torch.tensor(lengths, device="cuda:0")), q, lengths, keys, values, "bf16", "shared")
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_pages_past_32_bits(page):
+    """A pool of 5 GiB whose last pages are used."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention, paged_write
+
+    pages = (5 << 30) // (2 * page * 128)
+    pool = torch.zeros(pages, page, 1, 128, dtype=torch.bfloat16, device="cuda:0")
+    n = 300
+    table = (pages - 1 - torch.arange(-(-n // page), device="cuda:0", dtype=torch.int32))[None].contiguous()
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(13)
+    k = _rand(torch, gen, "bf16", 1, n, 1, 128)
+    q = _rand(torch, gen, "bf16", 1, 2, 2, 128)
+    lengths = torch.tensor([n], device="cuda:0")
+    paged_write(k, k, pool, pool, table, lengths)
+    assert torch.equal(pool[-(n // page):].flip(0).reshape(-1, 1, 128), k[0, :n // page * page])
+    assert int(pool[:4].count_nonzero()) == 0
+    _assert_attends(torch, paged_attention(q, pool, pool, table, lengths), q, [n], [k[0]], [k[0]], "bf16", "far")
+
+
+def test_refusals():
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention, paged_write
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype, device="cuda:0")
+
+    pool, table, lengths = t(4, 16, 2, 64), t(3, 2, dtype=torch.int32), t(3, dtype=torch.int32)
+    q, k = t(3, 1, 4, 64), t(3, 1, 2, 64)
+    odd = t(4, 16, 2, 65)[..., :64]
+    off = t(4 * 16 * 2 * 64 + 1)[1:].view(4, 16, 2, 64)
+    for bad in ((q, pool, t(4, 16, 2, 32), table, lengths), (q, pool, t(5, 16, 2, 64), table, lengths), (q[:2], pool, pool, table, lengths), (q[0], pool, pool, table, lengths),
+                (t(3, 1, 3, 64), pool, pool, table, lengths), (t(3, 1, 4, 32), pool, pool, table, lengths), (q, pool, pool, table[0], lengths),
+                (q, pool, pool, table, lengths[:2]), (q, pool, pool, table.cpu(), lengths), (q, pool, pool, table, lengths.cpu()), (q, odd, odd, table, lengths),
+                (q, off, off, table, lengths), (q.cpu(), pool, pool, table, lengths), (q, pool.cpu(), pool, table, lengths), (q, pool[:, :0], pool[:, :0], table, lengths)):
+        with pytest.raises(ValueError):
+            paged_attention(*bad)
+    for bad in ((q.half(), pool, pool, table, lengths), (q.float(), pool.float(), pool.float(), table, lengths), (q, pool, pool, table.long(), lengths),
+                (q, pool, pool, table, lengths.float()), (q, pool, None, table, lengths), (q, pool, pool, [[0]], lengths)):
+        with pytest.raises(TypeError):
+            paged_attention(*bad)
+    for scale in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(ValueError):
+            paged_attention(q, pool, pool, table, lengths, scale)
+    offsets = torch.tensor([0, 1, 2, 3], device="cuda:0")
+    for bad in ((k[0], k[0], pool, pool, table, lengths), (k[:, 0], k[:, 0], pool, pool, table, lengths, offsets[:3]), (k, k, pool, pool, table, lengths, offsets),
+                (k[:2], k[:2], pool, pool, table, lengths), (t(3, 1, 1, 64), t(3, 1, 1, 64), pool, pool, table, lengths), (k, t(3, 2, 2, 64), pool, pool, table, lengths),
+                (k, k, odd, odd, table, lengths), (k, k, off, off, table, lengths), (k.cpu(), k, pool, pool, table, lengths)):
+        with pytest.raises(ValueError):
+            paged_write(*bad)
+    with pytest.raises(TypeError):
+        paged_write(k.half(), k.half(), pool, pool, table, lengths)
+    with pytest.raises(RuntimeError):
+        paged_write(k, k, pool[:1].expand(4, 16, 2, 64), pool, table, lengths)
+    for call in (lambda x: paged_attention(x, pool, pool, table, lengths), lambda x: paged_write(x[:, :, :2], k, pool, pool, table, lengths)):
+        with pytest.raises(RuntimeError, match="no gradient"):
+            call(q.clone().requires_grad_())
+        with torch.no_grad():
+            call(q.clone().requires_grad_())
+    assert paged_attention(q[:0], pool, pool, table[:0], lengths[:0]).shape == (0, 1, 4, 64)
+    assert (paged_attention(q, pool[:0], pool[:0], table, lengths + 5) == 0).all()
+    assert (paged_attention(q, pool, pool, table[:, :0], lengths + 5) == 0).all()
+    paged_write(k[:, :0], k[:, :0], pool, pool, table, lengths)
+
+
+def test_on_another_stream_and_in_graphs():
+    """Token by token on a stream of its own and from a captured step that is replayed as the sequences grow, with eager calls on other caches between; two
+    graphs that share the allocator's pool."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention, paged_write
+
+    page, steps = 16, 40
+    start = [2990, 5, 1000]
+    k_pages, v_pages, table, keys, values = _cache(torch, [n + steps for n in start], page, 2, 64, "bf16", 8, poison=False)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(14)
+    q, k, v = (_rand(torch, gen, "bf16", 3, steps, h, 64) for h in (4, 2, 2))
+    eager = []
+    pages = [k_pages.clone(), v_pages.clone()]
+    lengths = torch.tensor(start, device="cuda:0", dtype=torch.int32)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in range(steps):
+            lengths += 1
+            paged_write(k[:, i:i + 1], v[:, i:i + 1], *pages, table, lengths)
+            eager.append(paged_attention(q[:, i:i + 1], *pages, table, lengths))
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for s, n in enumerate(start):
+        keys[s], values[s] = torch.cat([keys[s][:n], k[s]]), torch.cat([values[s][:n], v[s]])
+    last = paged_attention(q[:, -5:], *pages, table, lengths)
+    _assert_attends(torch, last, q[:, -5:].contiguous(), [n + steps for n in start], keys, values, "bf16", "grown")
+    held = [torch.zeros_like(t[:, :1]).contiguous() for t in (q, k, v)]
+    lengths = torch.tensor(start, device="cuda:0", dtype=torch.int32)
+    pages = [k_pages.clone(), v_pages.clone()]
+    graphs, results = [], []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=graphs[0].pool() if graphs else None):
+            lengths += 1
+            paged_write(held[1], held[2], *pages, table, lengths)
+            results.append(paged_attention(held[0], *pages, table, lengths))
+        graphs.append(graph)
+    lengths.copy_(torch.tensor(start, device="cuda:0"))
+    other = _cache(torch, [700, 800], 8, 2, 64, "bf16", 9)
+    want = paged_attention(q[:2, :1], *other[:3], torch.tensor([700, 800], device="cuda:0"))
+    for i in range(steps):
+        for to, t in zip(held, (q, k, v)):
+            to.copy_(t[:, i:i + 1])
+        graphs[i % 2].replay()
+        got = results[i % 2].clone()
+        assert torch.equal(paged_attention(q[:2, :1], *other[:3], torch.tensor([700, 800], device="cuda:0")), want)
+        torch.cuda.synchronize()
+        assert torch.equal(got, eager[i]), i
+
+
+def test_as_a_prompt_and_then_tokens():
+    """A prompt's attention, its keys and values into pages, and the newest tokens over the pages: near what the prompt with them gets at once."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import causal_attention, paged_attention, paged_write
+
+    for dtype in ("bf16", "f16"):
+        lengths, n = [130, 7, 511], 6
+        gen = torch.Generator(device="cuda:0")
+        gen.manual_seed(15)
+        q, k, v = (_rand(torch, gen, dtype, sum(lengths), h, 128) for h in (8, 2, 2))
+        offsets = torch.tensor([0, 130, 137, 648], device="cuda:0")
+        whole = causal_attention(q, k, v, offsets)
+        k_pages, v_pages, table, *_ = _cache(torch, lengths, 16, 2, 128, dtype, 10)
+        given = torch.tensor(lengths, device="cuda:0")
+        paged_write(k, v, k_pages, v_pages, table, given, offsets)
+        newest = torch.stack([q[end - n:end] for end in (130, 137, 648)])
+        got = paged_attention(newest, k_pages, v_pages, table, given)
+        _assert_attends(torch, got, newest, lengths, [k[:130], k[130:137], k[137:]], [v[:130], v[130:137], v[137:]], dtype, "then")
+        want = torch.stack([whole[end - n:end] for end in (130, 137, 648)])
+        # each within u (|out| + P |v|) of the exact one; P |v| is below the largest value
+        assert float((got.double() - want.double()).abs().max()) <= 4 * {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype] * float(v.abs().max())
