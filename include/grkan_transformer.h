@@ -193,7 +193,7 @@ grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *attent
  *   k_pages, v_pages  [pages, page_size, kv_heads, dim] of io; strides of page, token and head, each a multiple of 8 elements, and 16-byte aligned pointers
  *                     (else GRKAN_ERR_ALIGN)
  *   table    DEVICE int32 [sequences, table_entries], rows table_stride apart.  An entry that is no page (below 0, or from `pages` on) holds nothing:
- *            what is written there goes nowhere, and its positions are not attended to.  Entries behind a sequence's length are not read.
+ *            what is written there goes nowhere, and its positions are not attended to.  What entries behind a sequence's length hold has no influence.
  *   lengths  DEVICE int32 (int64 with lengths_64) [sequences]: how many positions each sequence has, the new tokens among them (clamped to 0 .. page_size x
  *            table_entries for attention)
  * io: GRKAN_BF16 or GRKAN_F16; dim a multiple of 8 up to 128; pages below 2^31, page_size x table_entries below 2^30, token strides that are not negative and below

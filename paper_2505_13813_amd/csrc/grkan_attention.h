@@ -60,6 +60,10 @@ template <> struct Matrix<__bf16> {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f32x4 multiply16(const u32x4 &a, const u32x4 &b, const f32x4 &c) // 16 x 16 x 32
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ uint32_t two(float a, float b) { return pack(a, b); }
     static __device__ __forceinline__ float first(uint32_t w) { return low(w); }
     static __device__ __forceinline__ float second(uint32_t w) { return high(w); }
@@ -68,6 +72,10 @@ template <> struct Matrix<_Float16> {
     static __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4 multiply16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
     static __device__ __forceinline__ uint32_t two(float a, float b)
     {
@@ -263,6 +271,20 @@ __device__ __forceinline__ float halves_sum(float v)
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
+// The same of the four lanes l mod 16, l mod 16 + 16, ..
+__device__ __forceinline__ float quarters_max(float v)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    return halves_max(fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])));
+}
+__device__ __forceinline__ float quarters_sum(float v)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    return halves_sum(__builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
 __device__ __forceinline__ int32_t keys_of(const Args &a, int32_t b)
 {
     if (!a.lengths)
@@ -344,14 +366,15 @@ constexpr int kGroup = 128;
 // How many walks over an entry's keys there are: its key heads.
 __device__ __forceinline__ int32_t units_of(const Args &a) { return a.kv_heads; }
 
-template <class A> struct DealOf {
+// GROUP: keys of a group.
+template <class A, int GROUP = kGroup> struct DealOf {
     int32_t total, workers; // G, and W: as many as the host asked for, but none without a group
     int32_t quotient, rest; // of G by W
     // batch entry b, its keys, the groups of one of its key heads, and the group that its first one begins with
     int32_t b, count, groups, begin;
     int32_t mine, up_to; // of entry `lane`: its keys; the groups up to and with it, of one key head each
 
-    __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + kGroup - 1) / kGroup; }
+    __device__ __forceinline__ static int32_t groups_of(int32_t keys) { return (keys + GROUP - 1) / GROUP; }
 
     // keys of entry first + lane (0 behind the last), and the running sum of the groups
     __device__ __forceinline__ static void scan(const A &a, int32_t first, int32_t &keys, int32_t &sum)

@@ -3,10 +3,14 @@
 // Position p of sequence s lies in row p mod page_size of page table[s][p / page_size].  Of the `queries` newest tokens of a sequence of `length`, token i sees
 // the positions up to length - queries + i: out_i = sum_p softmax_p(scale q_i k_p) v_p.
 //
-// The keys and values are read once, which bounds it: there are few rows for each.  As cross attention's kernel for single tokens (grkan_attention.hip), from the same
-// parts: the four wavefronts of a workgroup take tiles of 32 keys each, without a barrier, and join what they found; the keys of all sequences and heads are dealt
-// out evenly, in groups of 128, to a workgroup on each compute unit, and a second launch joins the parts.  Where the pages are whole tiles a tile has one address;
-// elsewhere every lane has its key's.  The table's entries come to LDS in front of the walk, so that no load waits for another one within it.
+// The keys and values are read once, and that bounds it, as there are few rows for each: 32 sequences of 1 to 8,191 positions, 32 heads of 128 on 8, 592 MB, in 111 us =
+// 5.4 TB/s, where reading alone gets 6.0.  A wavefront has tiles of 32 keys and their values by itself, without a barrier.  While it computes it loads little, and
+// so the others must: eight wavefronts on a compute unit with 128 channels, a buffer each, do better than four with two (142 us; with everything in the cache, where only
+// the way through a tile counts, 126, and 56 so: the products have sixteen rows in place of 32, two wavefronts fill one another's waits).  The wavefronts side by side
+// have the heads that lie side by side in memory (116 us with whole heads one behind the other).  Short walks are joined in their workgroup; long ones are dealt
+// out evenly to all wavefronts, whatever the lengths are, and a second launch joins the parts.
+// Where the pages are whole tiles a tile has one address; elsewhere every lane has its key's (pages of 16: 115 us).  The table's entries come to LDS in front of the
+// walk, so that no load waits for another one within it.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -23,168 +27,482 @@ struct Paged : Args { // keys: that a row of the table has place for; rows: quer
     int64_t pages;
     int32_t page, entries; // tokens of a page; of a row of the table
     int32_t queries;
-    int32_t unit_rows; // of a part: 32, or all where they are fewer
+    int32_t tile_rows; // of a walk: 16 or 32
+    int32_t unit_rows; // of a part: as many, or all where they are fewer
+    int32_t bundle;     // walks that are dealt out together: 8, 4, 2 or 1
+    int32_t join_lanes; // in the second launch: lanes of a row's piece
 };
 
-// Walks over a sequence's keys: each key head and tile of 32 rows.
-__device__ __forceinline__ int32_t units_of(const Paged &a) { return a.kv_heads * a.row_tiles; }
+// Walks over a sequence's keys: each key head and tile of rows.  Where they are dealt out, `bundle` of them go together, a wavefront each.
+__device__ __forceinline__ int32_t walks_of(const Paged &a) { return a.kv_heads * a.row_tiles; }
+__device__ __forceinline__ int32_t units_of(const Paged &a) { return walks_of(a) / a.bundle; }
 
-constexpr int kWorkers = 256;
-constexpr int kEntries = 2048; // of the table in LDS at once
+// Places for parts: worker w's of unit u is in u + w (no two are in the same: from one part to the next, one of the two rises).
+__device__ __forceinline__ int64_t slots_of(const Paged &a) { return ((int64_t)a.batch * units_of(a) + a.splits) * a.bundle; }
 
-template <typename IO_, int DP_> struct PagedShape : TokenShape<IO_, DP_> {
-    using Base = TokenShape<IO_, DP_>;
-    static constexpr uint32_t kTable = (uint32_t)Base::kLds;
-    static constexpr size_t kLds = Base::kLds + kEntries * 4;
+constexpr int kTileKeys = 32;
+constexpr int kEntries = 256; // of the table in LDS at once, for each wavefront
+constexpr int kWaves = 8;     // of a workgroup
+
+// BLOCKS: of sixteen rows.
+template <typename IO_, int DP_, int BLOCKS_> struct PagedShape {
+    typedef IO_ IO;
+    static constexpr int DP = DP_, BLOCKS = BLOCKS_, kRows = 16 * BLOCKS;
+    static constexpr uint32_t kTile = kTileBytes<DP, kTileKeys>, kTable = 2 * kTile * kWaves;
+    static constexpr size_t kLds = kTable + kWaves * kEntries * 4;
+    static constexpr int kPitch = DP + 4; // of a row's channels, where the wavefronts join theirs
+    static_assert((size_t)kWaves * kRows * (kPitch + 2) * sizeof(float) <= kLds, "");
+    static constexpr int kPerUnit = BLOCKS == 1 && 2 * kLds <= 160 * 1024 ? 2 : 1; // workgroups of a compute unit
 };
 
-template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void paged_kernel(const Paged a)
+// A row's way over the pages: which keys of a tile there are, and its loads.  table: of positions from `first` x page on, in LDS, -1 where there is no page.
+template <class SH> struct Pages {
+    static constexpr int KT = kTileKeys, DP = SH::DP;
+    using Loads = TileLoads<DP, KT, 1>;
+    const Paged &a;
+    const int32_t *table;
+    const Loads &k_loads, &v_loads;
+    uint64_t k_head, v_head;
+    int lane;
+    int32_t first, end; // the table's first entry; keys
+    int32_t page, place; // where whole tiles are in a page: of the tile; else of key t KT + lane mod 32
+
+    __device__ __forceinline__ bool even() const { return a.page % KT == 0; }
+
+    __device__ __forceinline__ uint64_t word(int32_t t)
+    {
+        const int32_t left = end - t * KT;
+        const uint64_t below = left >= KT ? 0xffffffffu : ((uint64_t)1 << left) - 1u;
+        if (even()) {
+            const int32_t entry = t * KT / a.page;
+            page = __builtin_amdgcn_readfirstlane(table[entry - first]);
+            place = t * KT - entry * a.page;
+            return page >= 0 ? below : 0;
+        }
+        const int32_t key = t * KT + (lane & 31), entry = key / a.page;
+        place = key - entry * a.page;
+        page = key < end ? table[entry - first] : -1;
+        return below & __ballot(page >= 0);
+    }
+    // keys or values (o, loads, head) of the tile that word() was asked for last
+    __device__ __forceinline__ void load(const Operand &o, const Loads &loads, uint64_t head, uint64_t word, uint32_t to) const
+    {
+        if (even()) {
+            loads.issue(head + (page < 0 ? 0 : (uint64_t)page) * (uint64_t)o.batch + (uint64_t)place * (uint64_t)o.token, o.token, word, word == 0xffffffffu && a.dim == DP,
+                        to);
+            return;
+        }
+#pragma unroll 1
+        for (int turn = 0; turn < Loads::kTurns; ++turn)
+#pragma unroll
+            for (int q = 0; q < Loads::kEach; ++q) {
+                const uint32_t e = (uint32_t)q * 64u + (uint32_t)lane, r0 = e / Loads::kChunks, piece = (e % Loads::kChunks) ^ swizzle<DP>(r0);
+                const int32_t r = (int32_t)(r0 + Loads::kTokens * (uint32_t)turn);
+                const int64_t p = __shfl(page, r), i = __shfl(place, r);
+                const bool there = p >= 0 && (word >> r & 1u) && piece * 8u < (uint32_t)a.dim;
+                load_to_lds_at(there ? head + (uint64_t)(p * o.batch + i * o.token) + piece * 16u : reinterpret_cast<uint64_t>(kZeros),
+                               to + (uint32_t)(turn * Loads::kEach + q) * kBlock<DP>);
+            }
+    }
+    __device__ __forceinline__ void load_keys(uint64_t word, uint32_t to) const { load(a.k, k_loads, k_head, word, to); }
+    __device__ __forceinline__ void load_values(uint64_t word, uint32_t to) const { load(a.v, v_loads, v_head, word, to); }
+};
+
+__device__ __forceinline__ int32_t page_or_none(const Paged &a, int32_t page) { return page >= 0 && page < a.pages ? page : -1; }
+
+// Sixteen rows for each block, in 16 x 16 x 32 instructions: S^T = K Q^T leaves a lane, of row l mod 16 and with g = l / 16, keys 4 g .. and 16 + 4 g .. of a tile
+// of 32, which in this order are the second operand of V^T P^T; V^T comes by transposing reads, two for each.
+template <class SH> struct PagedRows {
+    using IO = typename SH::IO;
+    using MM = Matrix<IO>;
+    static constexpr int DP = SH::DP, BLOCKS = SH::BLOCKS, NS = DP / 32, ND = DP / 16;
+
+    u32x4 q[BLOCKS][NS];   // lane l: row l mod 16, channels 32 s + 8 (l / 16) ..
+    f32x4 acc[BLOCKS][ND]; // channels 16 d + 4 (l / 16) ..
+    float top[BLOCKS], sum[BLOCKS];
+    int32_t last[BLOCKS]; // the last key that the lane's row sees
+    int32_t first, seen;  // the least of the rows' last ones; keys that any sees
+
+    __device__ __forceinline__ void load(const Paged &a, int32_t b, int32_t kvh, uint32_t row0, int32_t count, int lane)
+    {
+        const uint32_t group = (uint32_t)a.group, g = (uint32_t)lane >> 4;
+        const uint32_t end = row0 + SH::kRows < (uint32_t)a.rows ? row0 + SH::kRows : (uint32_t)a.rows;
+        const int32_t before = count - a.queries;
+        first = before + (int32_t)(row0 / group);
+        seen = before + (int32_t)((end - 1) / group) + 1;
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            const uint32_t row = row0 + 16u * n + ((uint32_t)lane & 15u);
+            last[n] = before + (int32_t)(row / group);
+            const uint64_t at = a.q.at + (uint64_t)(b * a.q.batch + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head));
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const uint32_t channel = 32u * s + 8u * g;
+                q[n][s] = gload16((int64_t)row < a.rows && channel < (uint32_t)a.dim ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                acc[n][d] = f32x4{};
+            top[n] = -__builtin_inff();
+            sum[n] = 0.0f;
+        }
+    }
+
+    // The scores of tile t; word: which of its keys there are.
+    __device__ __forceinline__ void scores(uint32_t keys_at, int32_t t, uint64_t word, int lane, f32x4 (&x)[BLOCKS][2]) const
+    {
+        const uint32_t i = (uint32_t)lane & 15u, g = (uint32_t)lane >> 4;
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n)
+            x[n][0] = x[n][1] = f32x4{};
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const u32x4 k = lds_read16(keys_at + row_at<DP>(i) + (((uint32_t)(4 * s) + g) ^ swizzle<DP>(i)) * 16u + row_at<DP>(16u * half));
+#pragma unroll
+                for (int n = 0; n < BLOCKS; ++n)
+                    x[n][half] = MM::multiply16(k, q[n][s], x[n][half]);
+            }
+        if (word != 0xffffffffu || t * kTileKeys + kTileKeys - 1 > first) {
+            const uint32_t mine = (uint32_t)word >> (4u * g);
+            const int32_t key = t * kTileKeys + 4 * (int32_t)g;
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[n][j / 4][j % 4] = (mine >> (16 * (j / 4) + j % 4) & 1u) && key + 16 * (j / 4) + j % 4 <= last[n] ? x[n][j / 4][j % 4] : -__builtin_inff();
+        }
+    }
+    __device__ __forceinline__ void probabilities(const f32x4 (&x)[BLOCKS][2], float c, u32x4 (&p)[BLOCKS])
+    {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            float most = x[n][0][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j)
+                most = fmaxf(most, x[n][j / 4][j % 4]);
+            most = quarters_max(most);
+            if (__ballot(most > top[n] + fminf(8.0f / c, 1e38f)) != 0) {
+                const float next = fmaxf(top[n], most);
+                const float by = next > -__builtin_inff() ? __builtin_amdgcn_exp2f((top[n] - next) * c) : 1.0f;
+                sum[n] *= by;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    acc[n][d] *= by;
+                top[n] = next;
+            }
+            const float less = top[n] > -__builtin_inff() ? top[n] * c : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float y = __builtin_amdgcn_exp2f(fmaf(x[n][j / 4][j % 4], c, -less)), z = __builtin_amdgcn_exp2f(fmaf(x[n][j / 4][j % 4 + 1], c, -less));
+                sum[n] += y + z;
+                p[n][j / 2] = MM::two(y, z);
+            }
+        }
+    }
+    // channels 16 d .. of the values, as first operand
+    static __device__ __forceinline__ u32x4 values(uint32_t values_at, int d, int lane)
+    {
+        const uint32_t r = (uint32_t)lane >> 2, piece = 2u * d + (((uint32_t)lane & 3u) >> 1);
+        const uint32_t at = values_at + row_at<DP>(r) + (piece ^ swizzle<DP>(r)) * 16u + ((uint32_t)lane & 1u) * 8u;
+        const u32x2 y = __builtin_bit_cast(u32x2, lds_read_transposed(at)), z = __builtin_bit_cast(u32x2, lds_read_transposed(at + row_at<DP>(16u)));
+        u32x4 v;
+        v[0] = y[0];
+        v[1] = y[1];
+        v[2] = z[0];
+        v[3] = z[1];
+        return v;
+    }
+    __device__ __forceinline__ void add(const u32x4 (&p)[BLOCKS], uint32_t values_at, int lane)
+    {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const u32x4 v = values(values_at, d, lane);
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n)
+                acc[n][d] = MM::multiply16(v, p[n], acc[n][d]);
+        }
+    }
+    // A row at a time, with zeros in place of the values behind its last key (Rows::add_each).
+    __device__ __forceinline__ void add_each(const u32x4 (&p)[BLOCKS], uint32_t values_at, int32_t t, int lane)
+    {
+#pragma unroll 1
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int n = 0; n < BLOCKS; ++n) {
+                const int32_t mine = __builtin_amdgcn_readlane(last[n], r) - t * kTileKeys - 4 * (lane >> 4);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    u32x4 v = values(values_at, d, lane);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int32_t key = 16 * (j / 2) + 2 * (j % 2);
+                        v[j] = key > mine ? 0u : key + 1 > mine ? v[j] & 0xffffu : v[j];
+                    }
+                    const f32x4 all = MM::multiply16(v, p[n], acc[n][d]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[n][d][i] = (lane & 15) == r ? all[i] : acc[n][d][i];
+                }
+            }
+    }
+    __device__ __forceinline__ bool not_finite() const
+    {
+        float x = 0.0f;
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x = fmaf(acc[n][d][i], 0.0f, x);
+        return __ballot(x != x) != 0;
+    }
+
+    // A wavefront's way through tiles t0, t0 + STEP, .. below t1 without a barrier.  Keys and values have a buffer each, and each is loaded anew as soon as it has been read:
+    // the next keys are on their way while this tile's probabilities are made, and the other wavefronts' loads while it computes.  Returns whether there was a key.
+    template <int STEP> __device__ __forceinline__ bool walk(Pages<SH> &pages, int32_t t0, int32_t t1, uint32_t keys_at, int lane, float c, bool each)
+    {
+        constexpr int kLoads = TileLoads<DP, kTileKeys, 1>::kMine;
+        const uint32_t values_at = keys_at + SH::kTile;
+        if (t0 >= t1)
+            return false;
+        uint64_t word = pages.word(t0), some = word;
+        pages.load_keys(word, keys_at);
+        pages.load_values(word, values_at);
+#pragma unroll 1
+        for (int32_t t = t0; t < t1; t += STEP) {
+            const bool more = t + STEP < t1;
+            wait_loads<kLoads>();
+            f32x4 x[BLOCKS][2];
+            scores(keys_at, t, word, lane, x);
+            const bool some_later = t * kTileKeys + kTileKeys - 1 > first;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the keys' buffer is loaded into next)
+            if (more) {
+                word = pages.word(t + STEP);
+                some |= word;
+                pages.load_keys(word, keys_at);
+            }
+            u32x4 p[BLOCKS];
+            probabilities(x, c, p);
+            if (more)
+                wait_loads<kLoads>();
+            else
+                wait_loads<0>();
+            if (some_later && each)
+                add_each(p, values_at, t, lane);
+            else
+                add(p, values_at, lane);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (more)
+                pages.load_values(word, values_at);
+        }
+        return some != 0;
+    }
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n)
+            arrived(q[n]);
+    }
+};
+
+// A walk to a workgroup, whose wavefronts share the keys and join what they found.
+template <class SH> __global__ __launch_bounds__(64 * kWaves, 2 * SH::kPerUnit) void paged_kernel(const Paged a)
 {
-    constexpr int DP = SH::DP, KT = SH::KT;
+    constexpr int DP = SH::DP, KT = kTileKeys, kAll = kWaves * kEntries;
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
     int32_t *const table = reinterpret_cast<int32_t *>(smem + SH::kTable);
-    const bool shared = a.splits > 0;
-    const int32_t worker = (int32_t)blockIdx.x;
-    const bool even = a.page % KT == 0; // a tile is in one page
-
+    const int32_t units = walks_of(a), b = (int32_t)blockIdx.x / units, unit = (int32_t)blockIdx.x - b * units;
+    const int32_t row_tile = unit / a.kv_heads, kvh = unit - row_tile * a.kv_heads;
+    const uint32_t row0 = (uint32_t)SH::kRows * (uint32_t)row_tile;
+    const int32_t *const entries_of = a.table + (int64_t)b * a.table_stride;
+    // (the first entries do not wait for the length)
+    const int32_t early = tid < a.entries ? page_or_none(a, entries_of[tid]) : -1;
     const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
-
-    // groups [g0, g1) of walk `unit` of a sequence
-    auto part = [&](int32_t b, int32_t unit, int32_t count, int32_t g0, int32_t g1) {
-        const int32_t row_tile = unit / a.kv_heads, kvh = unit - row_tile * a.kv_heads;
-        const uint32_t row0 = 32u * (uint32_t)row_tile, row = row0 + col, group = (uint32_t)a.group;
-        const uint32_t rows_end = row0 + 32u < (uint32_t)a.rows ? row0 + 32u : (uint32_t)a.rows;
-        Rows<typename SH::IO, DP, KT> rows;
-        rows.load(a, b, kvh, row, h);
-        // of the rows the last keys: the lane's, the first row's, and the last row's, behind which there are no keys for the tile of rows
-        const int32_t before = count - a.queries;
-        const Later later{before + (int32_t)(row / group), before + (int32_t)(row0 / group)};
-        const int32_t seen = before + (int32_t)((rows_end - 1) / group) + 1, end = g1 * kGroup < seen ? g1 * kGroup : seen;
-        const int32_t chunk = (kEntries - 1) / kGroup * kGroup; // keys, with page >= 1
-        const uint64_t k_head = a.k.at + (uint64_t)(kvh * a.k.head), v_head = a.v.at + (uint64_t)(kvh * a.v.head);
-        bool each = false;
-        for (;;) {
-            rows.clear();
-            bool some = false;
+    PagedRows<SH> rows;
+    rows.load(a, b, kvh, row0, keys_of(a, b), lane);
+    constexpr int kChunk = (kAll - 1) / KT * KT; // keys, with pages of one
+    Pages<SH> pages{a, table, k_loads, v_loads, a.k.at + (uint64_t)(kvh * a.k.head), a.v.at + (uint64_t)(kvh * a.v.head), lane, 0, 0, -1, 0};
+    table[tid] = early;
+    rows.arrive();
+    for (bool each = false;; each = true) {
+        rows.clear();
+        bool some = false;
 #pragma unroll 1
-            for (int64_t key0 = (int64_t)g0 * kGroup; key0 < end; key0 += (int64_t)chunk * a.page) {
-                const int64_t behind = key0 + (int64_t)chunk * a.page;
-                const int32_t key1 = behind < end ? (int32_t)behind : end, first = (int32_t)key0 / a.page, last = (key1 - 1) / a.page;
-                const int32_t *const from = a.table + (int64_t)b * a.table_stride;
+        for (int64_t key0 = 0; key0 < rows.seen; key0 += (int64_t)kChunk * a.page) {
+            const int64_t behind = key0 + (int64_t)kChunk * a.page;
+            pages.end = behind < rows.seen ? (int32_t)behind : rows.seen;
+            pages.first = (int32_t)key0 / a.page;
+            const int32_t entries = (pages.end - 1) / a.page - pages.first + 1;
+            if (key0 > 0 || each) {
                 barrier(); // (all are done with the entries before)
-                for (int32_t i = first + tid; i <= last; i += 256) {
-                    const int32_t page = from[i];
-                    table[i - first] = page >= 0 && page < a.pages ? page : -1;
-                }
-                wait_loads<0>();
-                barrier();
-                int32_t page = -1, place = 0; // even: of the tile; else of key t KT + lane mod 32
-                some |= walk_alone<SH>(
-                    rows, (int32_t)(key0 / KT) + wave, (key1 + KT - 1) / KT, lds0, wave, lane, a.c, a.dim,
-                    [&](int32_t t) -> uint64_t {
-                        const int32_t left = key1 - t * KT;
-                        const uint64_t below = left >= KT ? rows.kAll : ((uint64_t)1 << left) - 1u;
-                        if (even) {
-                            const int32_t entry = t * KT / a.page;
-                            page = __builtin_amdgcn_readfirstlane(table[entry - first]);
-                            place = t * KT - entry * a.page;
-                            return page >= 0 ? below : 0;
-                        }
-                        const int32_t key = t * KT + (int32_t)col, entry = key / a.page;
-                        place = key - entry * a.page;
-                        page = key < key1 ? table[entry - first] : -1;
-                        return below & __ballot(page >= 0);
-                    },
-                    [&](int32_t t, uint64_t word, bool whole, uint32_t to) {
-                        if (even) {
-                            k_loads.issue(k_head + (uint64_t)(page < 0 ? 0 : page) * (uint64_t)a.k.batch + (uint64_t)place * (uint64_t)a.k.token, a.k.token, word, whole, to);
-                            v_loads.issue(v_head + (uint64_t)(page < 0 ? 0 : page) * (uint64_t)a.v.batch + (uint64_t)place * (uint64_t)a.v.token, a.v.token, word, whole,
-                                          to + SH::kTile);
-                            return;
-                        }
-                        using Loads = TileLoads<DP, KT, 1>;
-#pragma unroll 1
-                        for (int turn = 0; turn < Loads::kTurns; ++turn)
-#pragma unroll
-                            for (int q = 0; q < Loads::kEach; ++q) {
-                                const uint32_t e = (uint32_t)q * 64u + (uint32_t)lane, r0 = e / Loads::kChunks, piece = (e % Loads::kChunks) ^ swizzle<DP>(r0);
-                                const int32_t r = (int32_t)(r0 + Loads::kTokens * (uint32_t)turn);
-                                const int64_t p = __shfl(page, r), i = __shfl(place, r);
-                                const bool there = p >= 0 && (word >> r & 1u) && piece * 8u < (uint32_t)a.dim;
-                                const uint64_t zeros = reinterpret_cast<uint64_t>(kZeros);
-                                const uint32_t at = to + (uint32_t)(turn * Loads::kEach + q) * kBlock<DP>;
-                                load_to_lds_at(there ? k_head + (uint64_t)(p * a.k.batch + i * a.k.token) + piece * 16u : zeros, at);
-                                load_to_lds_at(there ? v_head + (uint64_t)(p * a.v.batch + i * a.v.token) + piece * 16u : zeros, at + SH::kTile);
-                            }
-                    },
-                    later, each);
+                for (int32_t i = tid; i < entries; i += 64 * kWaves)
+                    table[i] = page_or_none(a, entries_of[pages.first + i]);
+            } else {
+                for (int32_t i = tid + 64 * kWaves; i < entries; i += 64 * kWaves)
+                    table[i] = page_or_none(a, entries_of[i]);
             }
-            if (!some) // (a query may hold NaN, and masked keys' scores are 0 NaN then)
-                rows.clear();
-            // (all wavefronts, for the barriers)
-            if (each || __syncthreads_or(rows.not_finite()) == 0)
-                break;
-            each = true;
+            wait_loads<0>();
+            barrier();
+            some |= rows.template walk<kWaves>(pages, (int32_t)(key0 / KT) + wave, (pages.end + KT - 1) / KT, lds0 + (uint32_t)wave * 2u * SH::kTile, lane, a.c, each);
         }
-        const int64_t unit_at = (int64_t)b * units_of(a) + unit, slot = unit_at + worker;
-        char *const out = shared ? reinterpret_cast<char *>(a.partial + (slot * a.unit_rows + col) * a.dim) : out_row(a, b, kvh, row);
-        float *const lse = a.partial + (shared ? ((int64_t)a.batch * units_of(a) + a.splits) * a.unit_rows * a.dim + slot * a.unit_rows + col : 0);
-        join_wavefronts<SH>(rows, smem, wave, lane, (int64_t)row < a.rows, a, out, lse, shared);
-    };
-
-    if (!shared) {
-        const int32_t units = units_of(a), b = worker / units, count = keys_of(a, b);
-        part(b, worker - b * units, count, 0, DealOf<Paged>::groups_of(count));
-        return;
+        if (!some) // (a query may hold NaN, and the scores of keys that are not there are 0 NaN then)
+            rows.clear();
+        // (all wavefronts, for the barriers; and this one is in front of what is joined, which lies where the tiles were)
+        const bool again = __syncthreads_or(rows.not_finite()) != 0;
+        if (each || !again)
+            break;
     }
-    DealOf<Paged> deal(a);
+    // sums relative to a common maximum, added in wavefront order
+    constexpr int kPitch = SH::kPitch, kRows = SH::kRows;
+    float *const joined = reinterpret_cast<float *>(smem);     // [wave][row][channel]
+    float *const stats = joined + kWaves * kRows * kPitch;     // [wave][2][row]
+#pragma unroll
+    for (int n = 0; n < SH::BLOCKS; ++n) {
+        const int row = 16 * n + (lane & 15);
+        const float sum = quarters_sum(rows.sum[n]);
+        if (lane < 16) {
+            stats[wave * 2 * kRows + row] = rows.top[n];
+            stats[wave * 2 * kRows + kRows + row] = sum;
+        }
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+            *reinterpret_cast<f32x4 *>(joined + (wave * kRows + row) * kPitch + 16 * d + 4 * (lane >> 4)) = rows.acc[n][d];
+    }
+    __syncthreads();
+    for (int i = tid; i < kRows * (DP / 4); i += 64 * kWaves) {
+        const int row = i / (DP / 4), channel = 4 * (i - row * (DP / 4));
+        if ((int64_t)row0 + row >= a.rows || channel >= a.dim)
+            continue;
+        float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            top = fmaxf(top, stats[w * 2 * kRows + row]);
+        f32x4 o = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float m = stats[w * 2 * kRows + row], by = m > -__builtin_inff() ? __builtin_amdgcn_exp2f((m - top) * a.c) : 0.0f;
+            sum += stats[w * 2 * kRows + kRows + row] * by;
+            o += *reinterpret_cast<const f32x4 *>(joined + (w * kRows + row) * kPitch + channel) * by;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        u32x2 w;
+        w[0] = Matrix<typename SH::IO>::two(o[0] * inv, o[1] * inv);
+        w[1] = Matrix<typename SH::IO>::two(o[2] * inv, o[3] * inv);
+        *reinterpret_cast<u32x2 *>(out_row(a, b, kvh, row0 + (uint32_t)row) + 2 * channel) = w;
+    }
+}
+
+// The walks dealt out evenly to the wavefronts, in groups of 32 keys.  Each goes its way by itself, without a barrier, from walk to walk, and leaves
+// what it found of each for the second launch: while one begins or ends a walk, the others' loads keep the memory busy.  `bundle` wavefronts side by side have the
+// same keys of as many heads, which lie side by side in memory, and count as one worker (a.splits of those).
+typedef DealOf<Paged, kTileKeys> WaveDeal;
+template <class SH> __global__ __launch_bounds__(64 * kWaves, 2 * SH::kPerUnit) void paged_waves_kernel(const Paged a)
+{
+    constexpr int DP = SH::DP, KT = kTileKeys;
+    extern __shared__ __align__(256) char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int32_t *const table = reinterpret_cast<int32_t *>(smem + SH::kTable) + wave * kEntries;
+    // (the wavefronts of a workgroup are far from one another: the rest of the division is on all compute units)
+    const int32_t turn = wave / a.bundle, mine = wave - turn * a.bundle, worker = turn * (int32_t)gridDim.x + (int32_t)blockIdx.x;
+    WaveDeal deal(a);
     if (worker >= deal.workers)
         return;
+    const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
+    constexpr int kChunk = (kEntries - 1) / KT * KT; // keys, with pages of one
     int32_t x = deal.first_of(worker);
     const int32_t end = deal.first_of(worker + 1);
     deal.find(a, x);
+#pragma unroll 1
     while (x < end) {
-        const int32_t unit = (x - deal.begin) / deal.groups, g0 = x - deal.begin - unit * deal.groups;
+        const int32_t unit = (x - deal.begin) / deal.groups, g0 = x - deal.begin - unit * deal.groups, b = deal.b;
         const int32_t g1 = end - x < deal.groups - g0 ? g0 + end - x : deal.groups;
-        part(deal.b, unit, deal.count, g0, g1);
+        const int32_t walk = unit * a.bundle + mine, row_tile = walk / a.kv_heads, kvh = walk - row_tile * a.kv_heads;
+        const uint32_t row0 = (uint32_t)SH::kRows * (uint32_t)row_tile;
+        PagedRows<SH> rows;
+        rows.load(a, b, kvh, row0, deal.count, lane);
+        const int32_t stop = g1 * KT < rows.seen ? g1 * KT : rows.seen;
+        const int32_t *const entries_of = a.table + (int64_t)b * a.table_stride;
+        Pages<SH> pages{a, table, k_loads, v_loads, a.k.at + (uint64_t)(kvh * a.k.head), a.v.at + (uint64_t)(kvh * a.v.head), lane, 0, 0, -1, 0};
+#pragma unroll 1
+        for (bool each = false;; each = true) {
+            rows.clear();
+            bool some = false;
+#pragma unroll 1
+            for (int64_t key0 = (int64_t)g0 * KT; key0 < stop; key0 += (int64_t)kChunk * a.page) {
+                const int64_t behind = key0 + (int64_t)kChunk * a.page;
+                pages.end = behind < stop ? (int32_t)behind : stop;
+                pages.first = (int32_t)key0 / a.page;
+                const int32_t entries = (pages.end - 1) / a.page - pages.first + 1;
+                for (int32_t i = lane; i < entries; i += 64)
+                    table[i] = page_or_none(a, entries_of[pages.first + i]);
+                rows.arrive();
+                wait_loads<0>();
+                some |= rows.template walk<1>(pages, (int32_t)(key0 / KT), (pages.end + KT - 1) / KT, lds0 + (uint32_t)wave * 2u * SH::kTile, lane, a.c, each);
+            }
+            if (!some) // (a query may hold NaN, and the scores of keys that are not there are 0 NaN then)
+                rows.clear();
+            if (each || !rows.not_finite())
+                break;
+        }
+        const int64_t slot = ((int64_t)b * units_of(a) + unit + worker) * a.bundle + mine;
+#pragma unroll
+        for (int n = 0; n < SH::BLOCKS; ++n) {
+            const float sum = quarters_sum(rows.sum[n]), inv = sum == 0.0f ? 0.0f : 1.0f / sum, l2 = log2_sum(rows.top[n], sum, a.c);
+            const int32_t row = 16 * n + (lane & 15);
+            if ((int64_t)row0 + row >= a.rows)
+                continue;
+            float *const out = a.partial + (slot * a.unit_rows + row) * a.dim;
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                if (const int channel = 16 * d + 4 * (lane >> 4); channel < a.dim)
+                    *reinterpret_cast<f32x4 *>(out + channel) = rows.acc[n][d] * inv;
+            if (lane < 16)
+                a.partial[slots_of(a) * a.unit_rows * a.dim + slot * a.unit_rows + row] = l2;
+        }
         x += g1 - g0;
         if (x < end && x == deal.begin + deal.groups * units_of(a)) { // the next sequence with keys
             deal.begin = x;
             do {
                 deal.count = keys_of(a, ++deal.b);
-                deal.groups = DealOf<Paged>::groups_of(deal.count);
+                deal.groups = WaveDeal::groups_of(deal.count);
             } while (deal.groups == 0);
         }
     }
 }
 
-// out of the workers' parts: a workgroup for each walk, dim / 8 lanes a row, or sixteen times as many at most where the rows leave lanes over
+// out of the workers' parts: a.join_lanes lanes for eight channels of a row
 template <typename IO> __global__ __launch_bounds__(256) void join_paged_kernel(const Paged a)
 {
-    const int32_t units = units_of(a), b = (int32_t)blockIdx.x / units, unit = (int32_t)blockIdx.x - b * units;
-    const int32_t row_tile = unit / a.kv_heads, kvh = unit - row_tile * a.kv_heads;
-    DealOf<Paged> deal(a);
+    const uint32_t pieces = (uint32_t)a.dim / 8u, lanes = (uint32_t)a.join_lanes, all = (uint32_t)a.unit_rows * pieces, each = 256u / lanes;
+    const int32_t turns = (int32_t)((all + each - 1) / each), place = (int32_t)blockIdx.x / turns, turn = (int32_t)blockIdx.x - place * turns;
+    const int32_t walks = walks_of(a), b = place / walks, walk = place - b * walks, unit = walk / a.bundle, mine = walk - unit * a.bundle;
+    const int32_t row_tile = walk / a.kv_heads, kvh = walk - row_tile * a.kv_heads;
+    WaveDeal deal(a);
     deal.find(a, -1, b);
     const int32_t x0 = deal.begin + unit * deal.groups;
     const int32_t w0 = deal.groups ? deal.worker_of(x0) : 0, parts = deal.groups ? deal.worker_of(x0 + deal.groups - 1) - w0 + 1 : 0;
-    const uint32_t pieces = (uint32_t)a.dim / 8u, row0 = 32u * (uint32_t)row_tile;
-    const uint32_t rows = (uint32_t)a.rows - row0 < 32u ? (uint32_t)a.rows - row0 : 32u;
-    const float *const stats = a.partial + ((int64_t)a.batch * units + a.splits) * a.unit_rows * a.dim;
-    const uint32_t items = rows * pieces;
-    uint32_t lanes = 1;
-    while (lanes < 16 && items * lanes * 2 <= 256)
-        lanes *= 2;
-    const uint32_t sub = threadIdx.x & (lanes - 1);
-    for (uint32_t i = threadIdx.x / lanes; i < items; i += 256 / lanes) {
-        const uint32_t row = i / pieces, piece = i - row * pieces;
-        auto line = [&](int32_t p) { return ((int64_t)blockIdx.x + w0 + p) * a.unit_rows + row; };
-        join_parts<IO>(
-            parts, (int32_t)sub, (int32_t)lanes, [&](int32_t p) { return a.partial + line(p) * a.dim + 8u * piece; }, [&](int32_t p) { return stats[line(p)]; },
-            out_row(a, b, kvh, row0 + row) + 16u * piece);
-    }
+    const uint32_t sub = threadIdx.x & (lanes - 1), item = (uint32_t)turn * each + threadIdx.x / lanes, row = item / pieces, piece = item - row * pieces;
+    const uint32_t row_at = (uint32_t)(a.tile_rows * row_tile) + row;
+    if (item >= all || (int64_t)row_at >= a.rows)
+        return;
+    const float *const stats = a.partial + slots_of(a) * a.unit_rows * a.dim;
+    const int64_t first = (int64_t)b * units_of(a) + unit + w0;
+    auto line = [&](int32_t p) { return ((first + p) * a.bundle + mine) * a.unit_rows + row; };
+    join_parts<IO>(
+        parts, (int32_t)sub, (int32_t)lanes, [&](int32_t p) { return a.partial + line(p) * a.dim + 8u * piece; }, [&](int32_t p) { return stats[line(p)]; },
+        out_row(a, b, kvh, row_at) + 16u * piece);
 }
 
 // ------------------------------------------------------------------------------------------------ into the pages
@@ -308,7 +626,7 @@ static grkan_status_t fill(const grkan_paged_cache_t *c, const grkan_paged_queri
     if (!(q->scale > 0) || !std::isfinite(q->scale * 1.4426950408889634f))
         return GRKAN_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)1 << 30;
-    if (q->tokens >= most || rows >= most || (rows + 31) / 32 * c->kv_heads >= most)
+    if (q->tokens >= most || rows >= most || (rows + 15) / 16 * c->kv_heads >= most)
         return GRKAN_ERR_UNSUPPORTED;
     if (c->sequences > 0 && rows > 0 && !q->q)
         return GRKAN_ERR_NULL;
@@ -334,32 +652,49 @@ static grkan_status_t fill(const grkan_paged_cache_t *c, const grkan_paged_queri
     a.page = c->page_size;
     a.entries = c->table_entries;
     a.queries = (int32_t)q->tokens;
-    a.row_tiles = (int32_t)((rows + 31) / 32);
-    a.unit_rows = rows < 32 ? (int32_t)rows : 32;
-    // A worker on every compute unit, with 256 keys at least; none where a walk each does as well: 1,024 of them, or all short.
-    const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, groups = (a.keys + kGroup - 1) / kGroup, parts = walks * groups / 2;
-    a.splits = walks >= 1024 || groups <= 8 || parts <= walks || walks * groups >= most ? 0 : (int32_t)(parts < kWorkers ? parts : kWorkers);
+    a.tile_rows = rows <= 16 ? 16 : 32;
+    a.row_tiles = (int32_t)((rows + a.tile_rows - 1) / a.tile_rows);
+    a.unit_rows = rows < a.tile_rows ? (int32_t)rows : a.tile_rows;
+    // As many wavefronts as the device holds, or one for each tile of 32 keys; none where a workgroup for each walk does as well: 1,024 of them, or all short (the second
+    // launch takes 4 us, and eight wavefronts on 1,000 keys no more than that in excess.  us without and with, one walk to each of twelve heads of 64 channels: 500 keys
+    // 8.5 / 8.2 + 4.4, 1,000 12.2 / 8.3 + 4.7; 32 walks of 128 channels, 1,000 keys 18.0 / 10.5 + 5.0; 192 of 64, 1,000 keys 12.4 / 11.9 + 4.6).
+    const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, groups = (a.keys + 31) / 32;
+    a.bundle = 1;
+    a.splits = 0;
+    if (walks < 1024 && groups > (a.dim <= 64 ? 32 : 24) && walks * groups < most) {
+        while (a.bundle < kWaves && a.kv_heads * a.row_tiles % (2 * a.bundle) == 0)
+            a.bundle *= 2;
+        const int64_t waves = a.dim > 64 ? 2048 : 4096, blocks = ((walks * groups < waves ? walks * groups : waves) + kWaves - 1) / kWaves;
+        a.splits = (int32_t)(blocks * kWaves / a.bundle);
+        const int32_t each = (int32_t)((int64_t)a.splits * a.bundle / walks) + 1; // parts of a walk
+        a.join_lanes = 1;
+        while (a.join_lanes < 64 && a.join_lanes * 4 < each)
+            a.join_lanes *= 2;
+    }
     *to = a;
     return GRKAN_OK;
 }
 
 static size_t workspace_of(const Paged &a)
 {
-    return a.splits > 0 ? ((size_t)a.batch * (size_t)a.kv_heads * (size_t)a.row_tiles + (size_t)a.splits) * (size_t)a.unit_rows * (size_t)(a.dim + 1) * sizeof(float) : 0;
+    return a.splits > 0 ? ((size_t)a.batch * (size_t)a.kv_heads * (size_t)a.row_tiles + (size_t)a.splits * (size_t)a.bundle) * (size_t)a.unit_rows * (size_t)(a.dim + 1) * sizeof(float)
+                        : 0;
 }
 
 typedef void (*Kernel)(Paged);
 struct PagedVariant {
-    Kernel kernel, join;
+    Kernel kernel, waves, join;
     size_t lds;
 };
-template <typename IO, int DP> static PagedVariant variant()
+template <typename IO, int DP, int BLOCKS> static PagedVariant variant()
 {
-    return PagedVariant{paged_kernel<PagedShape<IO, DP>>, join_paged_kernel<IO>, PagedShape<IO, DP>::kLds};
+    using SH = PagedShape<IO, DP, BLOCKS>;
+    return PagedVariant{paged_kernel<SH>, paged_waves_kernel<SH>, join_paged_kernel<IO>, SH::kLds};
 }
-template <typename IO> static PagedVariant pick(int32_t dim)
+template <typename IO, int DP> static PagedVariant variant(int32_t rows) { return rows <= 16 ? variant<IO, DP, 1>() : variant<IO, DP, 2>(); }
+template <typename IO> static PagedVariant pick(int32_t dim, int32_t rows)
 {
-    return dim <= 32 ? variant<IO, 32>() : dim <= 64 ? variant<IO, 64>() : dim <= 96 ? variant<IO, 96>() : variant<IO, 128>();
+    return dim <= 32 ? variant<IO, 32>(rows) : dim <= 64 ? variant<IO, 64>(rows) : dim <= 96 ? variant<IO, 96>(rows) : variant<IO, 128>(rows);
 }
 
 } // namespace attention
@@ -389,19 +724,21 @@ extern "C" grkan_status_t grkan_paged_attention(const grkan_paged_cache_t *cache
     const size_t need = attention::workspace_of(a);
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
         return GRKAN_ERR_WORKSPACE;
-    const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, work = a.splits > 0 ? a.splits : walks;
-    if (work > attention::kMostBlocks || (need && walks > attention::kMostBlocks))
+    const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, work = a.splits > 0 ? (int64_t)a.splits * a.bundle / attention::kWaves : walks;
+    const int64_t each = need ? 256 / a.join_lanes : 1, join = need ? walks * ((a.unit_rows * (a.dim / 8) + each - 1) / each) : 0;
+    if (work > attention::kMostBlocks || join > attention::kMostBlocks)
         return GRKAN_ERR_UNSUPPORTED;
     a.out = static_cast<char *>(out);
     a.partial = static_cast<float *>(workspace);
-    const attention::PagedVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a.dim) : attention::pick<_Float16>(a.dim);
-    if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
+    const attention::PagedVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a.dim, a.tile_rows) : attention::pick<_Float16>(a.dim, a.tile_rows);
+    const void *const kernel = reinterpret_cast<const void *>(need ? v.waves : v.kernel);
+    if (!attention::allow_lds(kernel, v.lds))
         return GRKAN_ERR_LAUNCH;
     hipStream_t const stream = static_cast<hipStream_t>(hip_stream);
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)work), dim3(256), args, v.lds, stream) != hipSuccess)
+    if (hipLaunchKernel(kernel, dim3((unsigned)work), dim3(64 * attention::kWaves), args, v.lds, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
-    if (need && hipLaunchKernel(reinterpret_cast<const void *>(v.join), dim3((unsigned)walks), dim3(256), args, 0, stream) != hipSuccess)
+    if (need && hipLaunchKernel(reinterpret_cast<const void *>(v.join), dim3((unsigned)join), dim3(256), args, 0, stream) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     return GRKAN_OK;
 }
