@@ -33,40 +33,39 @@ template <int DP> __device__ __forceinline__ void clear_rows(const Packed &a, co
         a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = __builtin_inff();
 }
 
-// ------------------------------------------------------------------------------------------------ 32 rows a wavefront, 128 a workgroup
+// ------------------------------------------------------------------------------------------------ 32 rows a wavefront, tiles of 64 keys for all
 
-template <typename IO_, int DP_> struct CausalShape {
+// PARTS: wavefronts that share the keys of a tile, of 32 rows each; the others have rows of their own.
+template <typename IO_, int DP_, int PARTS_> struct CausalShape {
     typedef IO_ IO;
-    static constexpr int DP = DP_, KT = 64, kWaves = 4, kRows = 32 * kWaves;
+    static constexpr int DP = DP_, PARTS = PARTS_, KT = 64, kKeys = KT / PARTS, kWaves = 4, kRows = 32 * kWaves / PARTS;
     static constexpr uint32_t kTile = kTileBytes<DP, KT>;
     static constexpr uint32_t kFlag = 4 * kTile; // behind K and V, two of each
     static constexpr size_t kLds = kFlag + 16;
+    static_assert(PARTS == 1 || (DP / 8 * 64 * 16 + 2 * 64 * 4) * (kWaves / 2) <= kFlag, ""); // what the wavefronts join
 };
 
 template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void causal_kernel(const Packed a)
 {
-    constexpr int DP = SH::DP, KT = SH::KT;
+    constexpr int DP = SH::DP, KT = SH::KT, KEYS = SH::kKeys, ND = DP / 32;
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
+    const int rows_of = wave / SH::PARTS, part = wave % SH::PARTS;
 
     const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
-    const Segment s = segment_of<SH::kRows>(a, a.slots - 1 - turn, a.group);
+    const Segment s = segment_of<SH::kRows>(a, turn, a.group, true);
     const int32_t all = s.count * a.group; // rows of the segment
     const int64_t begin = (int64_t)s.tile * SH::kRows;
     if (begin >= all)
         return;
-    const uint32_t row0 = (uint32_t)begin + (uint32_t)wave * 32u, row = row0 + col;
+    const uint32_t row0 = (uint32_t)begin + (uint32_t)rows_of * 32u, row = row0 + col;
     if (s.none) {
-        clear_rows<DP>(a, s, kvh, row0, all, lane);
+        if (part == 0)
+            clear_rows<DP>(a, s, kvh, row0, all, lane);
         return;
     }
-    Rows<typename SH::IO, DP, KT> rows;
-    const uint32_t query = row / group;
-    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
-              (int32_t)row < all, a.dim, h);
-
     // keys: of the workgroup up to its last row's, of the wavefront all below `from`, none from `to` on
     const int32_t end = (int32_t)((uint32_t)begin + SH::kRows - 1 < (uint32_t)all ? (uint32_t)begin + SH::kRows - 1 : (uint32_t)all - 1) / a.group + 1;
     const int32_t from = (int32_t)(row0 / group) + 1, to = (int32_t)((row0 + 31u) / group) + 1;
@@ -85,6 +84,11 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
             v_loads.clear(lane, lds0 + at + 2 * SH::kTile);
         }
     }
+    issue(0, 0);
+    Rows<typename SH::IO, DP, KEYS> rows;
+    const uint32_t query = row / group;
+    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
+              (int32_t)row < all, a.dim, h);
     arrived(rows.q);
     const bool works = (int32_t)row0 < all; // (a wavefront without rows loads for the others)
     // (two loops: one with a condition in it would copy the sums)
@@ -92,10 +96,9 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         rows.clear();
         RowOperand<DP> k_from(lane);
         ColumnOperand<DP> v_from(lane);
-        k_from.move(lds0);
-        v_from.move(lds0 + 2 * SH::kTile);
+        k_from.move(lds0 + row_at<DP>((uint32_t)(KEYS * part)));
+        v_from.move(lds0 + row_at<DP>((uint32_t)(KEYS * part)) + 2 * SH::kTile);
         uint32_t at = 0;
-        issue(0, 0);
 #pragma unroll 1
         for (int32_t t = 0; t < tiles; ++t) {
             wait_loads<0>();
@@ -107,18 +110,19 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
                 k_from.move(at ? 0u - SH::kTile : SH::kTile);
                 v_from.move(at ? 0u - SH::kTile : SH::kTile);
             }
-            if (!works || t * KT >= to)
+            const int32_t key0 = t * KT + KEYS * part; // the wavefront's first
+            if (!works || key0 >= to)
                 continue;
-            f32x16 x[KT / 32];
+            f32x16 x[KEYS / 32];
             rows.scores(k_from, x);
-            const bool crossed = t * KT + KT > from;
+            const bool crossed = key0 + KEYS > from;
             if (crossed)
-                rows.cut(x, (int32_t)query - t * KT, h);
-            uint32_t p[KT / 32][8];
+                rows.cut(x, (int32_t)query - key0, h);
+            uint32_t p[KEYS / 32][8];
             rows.probabilities(x, a.c, p);
             if constexpr (decltype(each)::value) {
                 if (crossed) {
-                    rows.add_each(p, v_from, (int32_t)query - t * KT, col, h);
+                    rows.add_each(p, v_from, (int32_t)query - key0, col, h);
                     continue;
                 }
             }
@@ -132,64 +136,56 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         flag[wave] = works && rows.not_finite();
     wait_loads<0>();
     barrier();
-    if (__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0)
+    if (__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0) {
+        issue(0, 0);
         walk(std::true_type{});
+        barrier();
+    }
+    if constexpr (SH::PARTS > 1) { // the first adds the second's, relative to a common maximum
+        static_assert(SH::PARTS == 2, "");
+        f32x4 *const sums = reinterpret_cast<f32x4 *>(smem) + rows_of * ND * 4 * 64 + lane;
+        float *const stats = reinterpret_cast<float *>(smem + SH::kWaves / 2 * ND * 4 * 64 * 16) + rows_of * 2 * 64 + lane;
+        if (part == 1) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 o;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        o[j] = rows.acc[d][4 * g + j];
+                    sums[(4 * d + g) * 64] = o;
+                }
+            stats[0] = rows.top;
+            stats[64] = rows.sum;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier();
+        if (part == 1)
+            return;
+        const float other = stats[0], top = fmaxf(rows.top, other), low = top > -__builtin_inff() ? top : 0.0f;
+        const float mine = __builtin_amdgcn_exp2f((rows.top - low) * a.c), its = __builtin_amdgcn_exp2f((other - low) * a.c);
+        rows.top = top;
+        rows.sum = rows.sum * mine + stats[64] * its;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 o = sums[(4 * d + g) * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    rows.acc[d][4 * g + j] = rows.acc[d][4 * g + j] * mine + o[j] * its;
+            }
+    }
     if ((int32_t)row >= all)
         return;
     const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     char *const out = a.out + packed_at(a, s, kvh, row);
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
+    for (int d = 0; d < ND; ++d)
         store_channels<typename SH::IO>(rows.acc[d], d, inv, a, out, false, h);
     if (h == 0 && a.lse)
         a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = lse_of(log2_sum(rows.top, sum, a.c));
-}
-
-// ------------------------------------------------------------------------------------------------ 32 rows, their keys shared by four wavefronts
-
-template <class SH> __global__ __launch_bounds__(256, SH::DP > 64 ? 1 : 2) void causal_few_kernel(const Packed a)
-{
-    constexpr int DP = SH::DP, KT = SH::KT;
-    extern __shared__ __align__(256) char smem[];
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
-
-    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
-    const Segment s = segment_of<32>(a, a.slots - 1 - turn, a.group);
-    const int32_t all = s.count * a.group;
-    const int64_t begin = (int64_t)s.tile * 32;
-    if (begin >= all)
-        return;
-    const uint32_t row0 = (uint32_t)begin, row = row0 + col;
-    if (s.none) {
-        if (wave == 0)
-            clear_rows<DP>(a, s, kvh, row0, all, lane);
-        return;
-    }
-    Rows<typename SH::IO, DP, KT> rows;
-    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
-              (int32_t)row < all, a.dim, h);
-    const int32_t end = (int32_t)(row0 + 31u < (uint32_t)all ? row0 + 31u : (uint32_t)all - 1) / a.group + 1;
-    const TileLoads<DP, KT, 1> k_loads(0, lane, a.k.token, a.dim), v_loads(0, lane, a.v.token, a.dim);
-    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
-    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
-    const Later later{(int32_t)(row / group), (int32_t)(row0 / group)};
-    for (bool each = false;; each = true) {
-        rows.clear();
-        walk_alone<SH>(
-            rows, wave, (end + KT - 1) / KT, lds0, wave, lane, a.c, a.dim,
-            [&](int32_t t) { return end - t * KT >= KT ? rows.kAll : ((uint64_t)1 << (end - t * KT)) - 1u; },
-            [&](int32_t t, uint64_t word, bool whole, uint32_t to) {
-                k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, word, whole, to);
-                v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, word, whole, to + SH::kTile);
-            },
-            later, each);
-        if (each || !rows.not_finite())
-            break;
-    }
-    join_wavefronts<SH>(rows, smem, wave, lane, (int32_t)row < all, a, a.out + packed_at(a, s, kvh, row),
-                        a.lse + (a.lse ? (int64_t)kvh * a.rows + packed_row(a, s, row) : 0), false);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -245,16 +241,25 @@ typedef void (*Kernel)(Packed);
 struct CausalVariant {
     Kernel kernel;
     size_t lds;
+    int64_t slots;
 };
-template <typename IO, int DP> static CausalVariant pick(bool few)
+template <class SH> static CausalVariant shared(const Packed &a) { return CausalVariant{causal_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group)}; }
+template <typename IO, int DP> static CausalVariant pick(const Packed &a)
 {
-    if (few)
-        return CausalVariant{causal_few_kernel<TokenShape<IO, DP>>, TokenShape<IO, DP>::kLds};
-    return CausalVariant{causal_kernel<CausalShape<IO, DP>>, CausalShape<IO, DP>::kLds};
+    return few_rows(a) ? shared<CausalShape<IO, DP, 2>>(a) : shared<CausalShape<IO, DP, 1>>(a);
 }
-template <typename IO> static CausalVariant pick(int32_t dim, bool few)
+template <typename IO> static CausalVariant pick(const Packed &a)
 {
-    return dim <= 32 ? pick<IO, 32>(few) : dim <= 64 ? pick<IO, 64>(few) : dim <= 96 ? pick<IO, 96>(few) : pick<IO, 128>(few);
+    return a.dim <= 32 ? pick<IO, 32>(a) : a.dim <= 64 ? pick<IO, 64>(a) : a.dim <= 96 ? pick<IO, 96>(a) : pick<IO, 128>(a);
+}
+
+// Two wavefronts on the tiles of 64 keys of the same rows where tiles of 128 rows do not fill the device (four workgroups of a compute unit, with 128 channels two): the
+// longest walk is then what counts, and it is half as long.  us with 128 rows to a workgroup and with 64: twelve heads of 64 channels, 24 sequences of 60 to 1,000 tokens
+// 25.5 / 21.7, eight of 120 to 2,000 39.4 / 30.0, one of 4,096 74 / 55, 40 of 60 to 1,000 36.6 / 39.3, 60 of 12 to 200 13.4 / 14.7, 16 of 240 to 4,000 130 / 161; 32 heads of 128 on
+// eight, one of 1,000 33.1 / 28.6, of 2,000 62.6 / 64.4, eight of 60 to 1,000 38.2 / 50.7; 16 of 96 on four, eight of 120 to 2,000 56.8 / 44.8.
+bool few_rows(const Packed &a)
+{
+    return slots_of<128>(a, a.group) * a.kv_heads <= (a.dim <= 64 ? 1024 : a.dim <= 96 ? 2048 : 448);
 }
 
 } // namespace attention
@@ -279,14 +284,13 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
         return GRKAN_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(out) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
         return GRKAN_ERR_ALIGN;
-    const bool few = attention::slots_of<128>(a, a.group) * a.kv_heads < 512;
-    const int64_t slots = few ? attention::slots_of<32>(a, a.group) : attention::slots_of<128>(a, a.group), grid = slots * a.kv_heads;
+    const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a) : attention::pick<_Float16>(a);
+    const int64_t grid = v.slots * a.kv_heads;
     if (grid > attention::kMostBlocks)
         return GRKAN_ERR_UNSUPPORTED;
-    a.slots = (int32_t)slots;
+    a.slots = (int32_t)v.slots;
     a.out = static_cast<char *>(out);
     a.lse = lse;
-    const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a.dim, few) : attention::pick<_Float16>(a.dim, few);
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};

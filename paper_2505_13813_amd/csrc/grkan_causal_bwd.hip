@@ -11,6 +11,8 @@
 // float16: scaled as there; the largest upstream gradient is that of the key's own sequence, from the key's tile on.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "grkan_attention_back.h"
 #include "grkan_packed.h"
 
@@ -23,7 +25,7 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
     using MM = Matrix<IO>;
     __shared__ uint32_t most[4][2];
     const int32_t slot = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - slot * a.kv_heads;
-    const Segment s = segment_of<kRowTile>(a, slot, a.group);
+    const Segment s = segment_of<kRowTile>(a, slot, a.group, true);
     const int32_t all = s.count * a.group;
     if (s.none || (int64_t)s.tile * kRowTile >= all)
         return;
@@ -70,26 +72,70 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
         uint32_t found = 0;
         for (int w = 0; w < 4; ++w)
             found = most[w][threadIdx.x] > found ? most[w][threadIdx.x] : found;
-        a.row_most[2 * ((int64_t)kvh * a.row_tiles + slot) + threadIdx.x] = __builtin_bit_cast(float, found);
+        a.row_most[2 * ((int64_t)kvh * a.row_tiles + place_of<kRowTile>(s.first, a.group, s.index) + s.tile) + threadIdx.x] = __builtin_bit_cast(float, found);
     }
 }
 
-// The rows that tile `tile` of a segment's keys is seen by: tiles [first, tiles) of `size` rows, in `parts` slabs of `per`.
+// PARTS: wavefronts that share the rows of a stage, for the same 32 keys, or the keys of a tile, for the same 32 rows; the others have keys or rows of their own.
+template <typename IO, int DP, int ROWS, bool V_LDS, int PER, int PARTS_> struct CausalBackShape : BackShape<IO, DP, ROWS, V_LDS, PER> {
+    using Base = BackShape<IO, DP, ROWS, V_LDS, PER>;
+    static constexpr int PARTS = PARTS_, kOwn = 32 * Base::kWaves / PARTS;
+    static constexpr uint32_t kValues = V_LDS ? kOwn / 64 * Base::kKeysTile : 0; // in front of the stages
+    static constexpr size_t kKeyLds = 2 * (size_t)Base::kKeyStage + kValues;
+    static_assert(PARTS == 1 || (ROWS == 64 && (size_t)2 * 2 * (DP / 8) * 64 * 16 <= kKeyLds), ""); // what the wavefronts join
+};
+
+// The rows that tile `tile` of a segment's keys is seen by: tiles [first, tiles) of `size` rows, in `parts` slabs of `per`, the first of what remains.
 struct Walk {
     int32_t first, tiles, parts, per;
+    __device__ __forceinline__ int32_t begin(int32_t part) const { return part == 0 ? first : tiles - (parts - part) * per; }
     __device__ __forceinline__ Walk(const Packed &a, const Segment &s, int32_t own, int32_t size)
     {
         const int32_t all = s.count * a.group;
         first = (int32_t)((int64_t)s.tile * own * a.group / size);
         tiles = (all + size - 1) / size;
-        const int32_t n = tiles - first;
-        parts = (n + a.slab - 1) / a.slab;
-        parts = parts < 1 ? 1 : parts < a.parts ? parts : a.parts;
-        per = (n + parts - 1) / parts;
+        const int32_t n = tiles - first, most = (n + a.parts - 1) / a.parts;
+        per = a.slab > most ? a.slab : most;
+        parts = n > per ? (n + per - 1) / per : 1;
     }
 };
 
-// dK and dV of 32 keys a wavefront, of 128 a workgroup, from all the rows that see them or a slab of those.
+// Sums of two wavefronts of the same keys or rows: the second leaves its own in LDS (and is done: false), the first adds them.
+template <int N, typename Sums> __device__ __forceinline__ bool add_second(char *smem, int own, int shared, int lane, Sums &&sums)
+{
+    f32x4 *const place = reinterpret_cast<f32x4 *>(smem) + own * N * 4 * 64 + lane;
+    wait_loads<0>();
+    barrier(); // (all are done with what lay there)
+    if (shared == 1) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = sums(n)[4 * g + j];
+                place[(4 * n + g) * 64] = o;
+            }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    if (shared == 1)
+        return false;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 o = place[(4 * n + g) * 64];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sums(n)[4 * g + j] += o[j];
+        }
+    return true;
+}
+
+// dK and dV of 32 keys a wavefront, from all the rows that see them or a slab of those.  Whole slabs are launched first, what remains of a
+// walk last.
 template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_kernel(const Packed a)
 {
     using IO = typename SH::IO;
@@ -101,8 +147,9 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
     const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5;
     // block ((part, slot), key head)
     const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
-    const int32_t part = turn / a.key_tiles, slot = turn - part * a.key_tiles;
-    const Segment s = segment_of<SH::kOwn>(a, slot, 1);
+    const int32_t back = turn / a.key_tiles, part = a.parts - 1 - back, slot = turn - back * a.key_tiles;
+    const int own = wave / SH::PARTS, shared = wave % SH::PARTS;
+    const Segment s = segment_of<SH::kOwn>(a, slot, 1, false);
     const int64_t begin = (int64_t)s.tile * SH::kOwn;
     if (begin >= s.count)
         return;
@@ -110,8 +157,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
     if (part >= (s.none ? 1 : walk.parts))
         return;
     const int32_t all = s.count * a.group, count = s.count;
-    const int32_t t0 = walk.first + part * walk.per, t1 = s.none ? t0 : t0 + walk.per < walk.tiles ? t0 + walk.per : walk.tiles;
-    const int32_t key0 = (int32_t)begin + wave * 32, key = key0 + (int32_t)col; // this wavefront's and this lane's
+    const int32_t t0 = walk.begin(part), t1 = s.none ? t0 : part + 1 < walk.parts ? walk.begin(part + 1) : walk.tiles;
+    const int32_t key0 = (int32_t)begin + own * 32, key = key0 + (int32_t)col; // this wavefront's and this lane's
     const bool valid = key < count, works = key0 < count;
 
     // ---- keys and values as second operands: lane l has key l mod 32, channels 16 s + 8 (l / 32) ..
@@ -146,7 +193,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
             const bool there = valid && channel < (uint32_t)a.dim;
             value[st] = gload16(there ? v_base + (uint64_t)key * (uint64_t)a.v.token + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
-        const int32_t base = slot_of<kRowTile>(s.first, a.group, s.index);
+        const int32_t base = place_of<kRowTile>(s.first, a.group, s.index);
         const int32_t row_tiles = s.none ? 0 : (all + kRowTile - 1) / kRowTile;
         uint32_t largest = 0, sums = 0;
         for (int32_t i = (int32_t)(begin * a.group / kRowTile) + lane; i < row_tiles; i += 64) {
@@ -163,8 +210,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         length2 = halves_sum(length2);
         up = lowered(scale_of(most_of_lanes(largest)), length2, __builtin_bit_cast(float, most_of_lanes(sums)), a.dim);
         const uint32_t longest = most_of_lanes(__builtin_bit_cast(uint32_t, length2) & 0x7fffffffu);
-        if (lane == 0 && part == 0)
-            a.value_most[((int64_t)kvh * a.key_tiles + slot) * SH::kWaves + wave] = __builtin_bit_cast(float, longest);
+        if (lane == 0 && part == 0 && shared == 0)
+            a.value_most[((int64_t)kvh * a.value_tiles + place_of<kGroup>(s.first, 1, s.index)) * (kGroup / 32) + key0 / 32] = __builtin_bit_cast(float, longest);
     }
 
     auto issue = [&](int32_t t, uint32_t stage) {
@@ -179,19 +226,19 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         }
     };
 
-    const uint32_t stages = lds0 + (SH::V_LDS ? 2 * SH::kKeysTile : 0u);
+    const uint32_t stages = lds0 + SH::kValues;
     // (moved from stage to stage in place: there are no registers for copies)
     RowOperand<DP> rows(lane), v_rows(lane);
     ColumnOperand<DP> columns(lane);
-    rows.move(stages + SH::kKeyStage);
-    columns.move(stages + SH::kKeyStage);
-    v_rows.move(lds0 + (uint32_t)wave * row_at<DP>(32u));
+    rows.move(stages + SH::kKeyStage + row_at<DP>((uint32_t)(32 * shared)));
+    columns.move(stages + SH::kKeyStage + row_at<DP>((uint32_t)(32 * shared)));
+    v_rows.move(lds0 + (uint32_t)own * row_at<DP>(32u));
     uint32_t at = SH::kKeyStage;
     if constexpr (SH::V_LDS) {
         if (t0 < t1) {
             const TileLoads<DP, 64, SH::kWaves> v_loads(wave, lane, a.v.token, a.dim);
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
+            for (int half = 0; half < SH::kOwn / 64; ++half) {
                 const int32_t first = (int32_t)begin + 64 * half;
                 v_loads.issue(v_base + (uint64_t)first * (uint64_t)a.v.token, a.v.token, __ballot(first + lane < count), false, lds0 + (uint32_t)half * SH::kKeysTile);
             }
@@ -224,10 +271,10 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         }
         if (t < t0 || !works || (t + 1) * ROWS <= first_row)
             continue;
-        const uint32_t stats = stage + 2 * SH::kRowsTile + 16u * (lane_here() >> 5);
+        const uint32_t stats = stage + 2 * SH::kRowsTile + 128u * (uint32_t)shared + 16u * (lane_here() >> 5);
         const bool crossed = t * ROWS < last_row || (t + 1) * ROWS > all;
 #pragma unroll
-        for (int rb = 0; rb < ROWS / 32; ++rb) {
+        for (int rb = 0; rb < ROWS / 32 / SH::PARTS; ++rb) {
             f32x16 p = {}, d = {};
 #pragma unroll
             for (int st = 0; st < NS; ++st)
@@ -241,7 +288,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
                     p[4 * quad + j] = __builtin_amdgcn_exp2f(fmaf(p[4 * quad + j], c, -lse[j]));
             }
             if (crossed) { // rows of the tile that see the key: from `from` on, and before the segment's end
-                const int32_t l = (int32_t)lane_here(), row0 = t * ROWS + 32 * rb + 4 * (l >> 5);
+                const int32_t l = (int32_t)lane_here(), row0 = t * ROWS + 32 * (rb + shared) + 4 * (l >> 5);
                 const int32_t from = (key0 + (l & 31)) * a.group - row0;
                 const uint32_t span = (uint32_t)(all - row0 - from);
 #pragma unroll
@@ -283,6 +330,9 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         }
     }
 
+    if constexpr (SH::PARTS > 1) // the first adds what the second has
+        if (!add_second<2 * ND>(smem, own, shared, lane, [&](int n) -> f32x16 & { return n < ND ? dk[n] : dv[n - ND]; }))
+            return;
     const int32_t l = (int32_t)lane_here(), mine = key0 + (l & 31);
     if (mine >= count)
         return;
@@ -320,55 +370,91 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         }
 }
 
-// The sum of the slabs' parts of a tile of keys, in their order: block (quarter, dK or dV, slot, key head), four elements a lane and pass.
-template <typename IO> __global__ __launch_bounds__(256) void causal_sum_kernel(const Packed a, int32_t size)
+// The sum of the slabs' parts of a tile of keys, in their order: block (half of the keys, dK or dV, slot, key head), four times four elements a lane and pass.
+template <typename IO, int OWN> __global__ __launch_bounds__(256) void causal_sum_kernel(const Packed a, int32_t size)
 {
-    const int32_t quarter = (int32_t)blockIdx.x & 3, which = (int32_t)blockIdx.x >> 2 & 1, item = (int32_t)blockIdx.x >> 3;
+    const int32_t half = (int32_t)blockIdx.x & 1, which = (int32_t)blockIdx.x >> 1 & 1, item = (int32_t)blockIdx.x >> 2;
     const int32_t slot = item / a.kv_heads, kvh = item - slot * a.kv_heads;
-    const Segment s = segment_of<kGroup>(a, slot, 1);
-    const int64_t begin = (int64_t)s.tile * kGroup;
+    const Segment s = segment_of<OWN>(a, slot, 1, false);
+    const int64_t begin = (int64_t)s.tile * OWN;
     if (s.none || begin >= s.count)
         return;
-    const Walk walk(a, s, kGroup, size);
+    const Walk walk(a, s, OWN, size);
     if (walk.parts == 1) // written as it should be
         return;
-    const int32_t quads = a.dim / 4, keys = kGroup / 4, key0 = (int32_t)begin + quarter * keys;
+    const int32_t quads = a.dim / 4, key0 = (int32_t)begin + half * (OWN / 2), left = s.count - key0, keys = left < OWN / 2 ? left : OWN / 2;
     const int64_t lines = (int64_t)a.tokens * a.kv_heads;
-    for (int32_t i = (int32_t)threadIdx.x; i < keys * quads; i += 256) {
-        const int32_t row = i / quads, key = key0 + row;
-        if (key >= s.count)
-            break;
-        const int64_t line = ((int64_t)s.first + key) * a.kv_heads + kvh;
-        const int32_t channel = 4 * (i - row * quads);
-        const float *const from = a.partial + (which * lines + line) * a.dim + channel;
-        f32x4 v = {};
-        for (int32_t n = 0; n < walk.parts; ++n)
-            v += *reinterpret_cast<const f32x4 *>(from + 2 * n * lines * a.dim);
-        u32x2 o;
-        o[0] = Matrix<IO>::two(v[0], v[1]);
-        o[1] = Matrix<IO>::two(v[2], v[3]);
-        *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + (line * a.dim + channel) * 2) = o;
+    for (int32_t i0 = (int32_t)threadIdx.x; i0 < keys * quads; i0 += 4 * 256) {
+        f32x4 v[4] = {};
+        int64_t place[4]; // of the four elements, in [tokens, kv_heads, dim]
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int32_t i = i0 + 256 * n < keys * quads ? i0 + 256 * n : i0, row = i / quads;
+            place[n] = (((int64_t)s.first + key0 + row) * a.kv_heads + kvh) * a.dim + 4 * (i - row * quads);
+        }
+        for (int32_t p = 0; p < walk.parts; ++p) {
+            const float *const from = a.partial + (2 * p + which) * lines * a.dim;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                v[n] += *reinterpret_cast<const f32x4 *>(from + place[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if (i0 + 256 * n >= keys * quads)
+                break;
+            u32x2 o;
+            o[0] = Matrix<IO>::two(v[n][0], v[n][1]);
+            o[1] = Matrix<IO>::two(v[n][2], v[n][3]);
+            *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + place[n] * 2) = o;
+        }
     }
 }
 
 // dQ of 32 rows a wavefront.
-template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_kernel(const Packed a)
+template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_queries_kernel(const Packed a)
 {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
-    constexpr int DP = SH::DP, ND = DP / 32, NS = DP / 16, KT = 64;
+    constexpr int DP = SH::DP, ND = DP / 32, NS = DP / 16, KT = 64, KEYS = KT / PARTS, kOwn = 32 * SH::kWaves / PARTS;
+    static_assert(PARTS == 1 || (size_t)2 * (DP / 8) * 64 * 16 <= SH::kRowLds, ""); // what the wavefronts join
     extern __shared__ __align__(256) char smem[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
     const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
-    const Segment s = segment_of<SH::kOwn>(a, a.slots - 1 - turn, a.group);
+    const Segment s = segment_of<kOwn>(a, turn, a.group, true);
+    const int own = wave / PARTS, shared = wave % PARTS;
     const int32_t all = s.count * a.group;
-    const int64_t begin = (int64_t)s.tile * SH::kOwn;
+    const int64_t begin = (int64_t)s.tile * kOwn;
     if (begin >= all)
         return;
-    const uint32_t row0 = (uint32_t)begin + (uint32_t)wave * 32u, row = row0 + col;
+    const uint32_t row0 = (uint32_t)begin + (uint32_t)own * 32u, row = row0 + col;
     const bool there = (int32_t)row < all, works = (int32_t)row0 < all && !s.none;
+    // keys: of the workgroup up to its last row's, of the wavefront all below `from`, none from `to` on
+    const int32_t last = (int32_t)((uint32_t)begin + kOwn - 1 < (uint32_t)all ? (uint32_t)begin + kOwn - 1 : (uint32_t)all - 1) / a.group;
+    const int32_t end = s.none ? 0 : last + 1;
+    const int32_t from = (int32_t)(row0 / group) + 1, to = (int32_t)((row0 + 31u) / group) + 1, query = (int32_t)(row / group);
+    const int32_t tiles = (end + KT - 1) / KT;
+    const LastTwiceLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
+    RowOperand<DP> row_operand(lane);
+    ColumnOperand<DP> column_operand(lane);
+    row_operand.move(row_at<DP>((uint32_t)(KEYS * shared)));
+    column_operand.move(row_at<DP>((uint32_t)(KEYS * shared)));
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+    if (a.dim < DP) {
+#pragma unroll 1
+        for (uint32_t at = 0; at < 2 * SH::kRowStage; at += SH::kRowStage) {
+            k_loads.clear(lane, lds0 + at);
+            v_loads.clear(lane, lds0 + at + SH::kKeysTile);
+        }
+    }
+    auto issue = [&](int32_t t, uint32_t at) {
+        k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, a.dim, end - t * KT, lds0 + at);
+        v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, a.dim, end - t * KT, lds0 + at + SH::kKeysTile);
+    };
+    if (tiles > 0)
+        issue(0, 0);
     u32x4 q[NS], o[NS];
     {
         const uint64_t q_at = a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head));
@@ -382,10 +468,6 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
             o[st] = gload16(loaded ? o_at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
     }
-    // keys: of the workgroup up to its last row's, of the wavefront all below `from`, none from `to` on
-    const int32_t last = (int32_t)((uint32_t)begin + SH::kOwn - 1 < (uint32_t)all ? (uint32_t)begin + SH::kOwn - 1 : (uint32_t)all - 1) / a.group;
-    const int32_t end = s.none ? 0 : last + 1;
-    const int32_t from = (int32_t)(row0 / group) + 1, to = (int32_t)((row0 + 31u) / group) + 1, query = (int32_t)(row / group);
     const float c = a.c;
     const int64_t place = packed_row(a, s, row);
     float up = 1.0f; // of the row
@@ -399,13 +481,13 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
             for (int j = 0; j < 4; ++j)
                 largest = fmaxf(largest, fmaxf(fabsf(MM::first(o[st][j])), fabsf(MM::second(o[st][j]))));
         up = scale_of(__builtin_bit_cast(uint32_t, halves_max(largest)));
-        const int32_t base = slot_of<SH::kOwn>(s.first, 1, s.index), groups = (end + SH::kOwn - 1) / SH::kOwn;
+        const int32_t base = place_of<kGroup>(s.first, 1, s.index), groups = (end + kGroup - 1) / kGroup;
         uint32_t longest = 0;
         for (int32_t i = lane; i < groups; i += 64) {
-            const f32x4 values = reinterpret_cast<const f32x4 *>(a.value_most)[(int64_t)kvh * a.key_tiles + base + i];
+            const f32x4 values = reinterpret_cast<const f32x4 *>(a.value_most)[(int64_t)kvh * a.value_tiles + base + i];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                longest = greater(longest, values[j]);
+                longest = kGroup * i + 32 * j < s.count ? greater(longest, values[j]) : longest; // (the others are nobody's)
         }
         delta = there && !s.none ? a.row_delta[(int64_t)kvh * a.rows + place] : 0.0f;
         up = lowered(up, __builtin_bit_cast(float, most_of_lanes(longest)), fabsf(delta), a.dim);
@@ -425,7 +507,7 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
             for (int j = 0; j < 4; ++j)
                 delta += MM::first(o[st][j]) * MM::first(y[st][j]) + MM::second(o[st][j]) * MM::second(y[st][j]);
         delta = halves_sum(delta);
-        if (h == 0 && there)
+        if (h == 0 && there && shared == 0)
             a.row_delta[(int64_t)kvh * a.rows + place] = delta;
     }
     f32x16 dq[ND];
@@ -433,44 +515,26 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
     for (int d = 0; d < ND; ++d)
         dq[d] = f32x16{};
 
-    const int32_t tiles = (end + KT - 1) / KT;
-    const LastTwiceLoads<DP, KT, SH::kWaves> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
-    const RowOperand<DP> row_operand(lane);
-    const ColumnOperand<DP> column_operand(lane);
-    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
-    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
-    if (a.dim < DP) {
-#pragma unroll 1
-        for (uint32_t at = 0; at < 2 * SH::kRowStage; at += SH::kRowStage) {
-            k_loads.clear(lane, lds0 + at);
-            v_loads.clear(lane, lds0 + at + SH::kKeysTile);
-        }
-    }
     arrived(q);
     arrived(o);
     arrived(lse);
     arrived(delta);
-    uint32_t at = SH::kRowStage;
+    uint32_t at = 0;
 #pragma unroll 1
-    for (int32_t t = -1; t < tiles; ++t) {
-        if (t >= 0) {
-            wait_loads<0>();
-            barrier();
-        }
-        if (t + 1 < tiles) {
-            const uint32_t next = lds0 + (at ^ SH::kRowStage);
-            const int32_t left = end - (t + 1) * KT;
-            k_loads.issue(k_base + (uint64_t)(t + 1) * KT * (uint64_t)a.k.token, a.k.token, a.dim, left, next);
-            v_loads.issue(v_base + (uint64_t)(t + 1) * KT * (uint64_t)a.v.token, a.v.token, a.dim, left, next + SH::kKeysTile);
-        }
+    for (int32_t t = 0; t < tiles; ++t) {
+        wait_loads<0>();
+        barrier();
+        if (t + 1 < tiles)
+            issue(t + 1, at ^ SH::kRowStage);
         const auto rows = row_operand.moved(lds0 + at);
         const auto columns = column_operand.moved(lds0 + at);
         at ^= SH::kRowStage;
-        if (t < 0 || !works || t * KT >= to)
+        const int32_t key0 = t * KT + KEYS * shared; // the wavefront's first
+        if (!works || key0 >= to)
             continue;
-        const bool crossed = t * KT + KT > from;
+        const bool crossed = key0 + KEYS > from;
 #pragma unroll
-        for (int kb = 0; kb < KT / 32; ++kb) {
+        for (int kb = 0; kb < KEYS / 32; ++kb) {
             fence_schedule(); // (the two halves mixed take more registers than there are)
             f32x16 x = {}, d = {};
 #pragma unroll
@@ -483,7 +547,7 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
             for (int i = 0; i < 16; ++i)
                 x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse)) * fmaf(d[i], up, -delta);
             if (crossed) {
-                const int32_t seen = query - t * KT - 32 * kb - 4 * (int32_t)h;
+                const int32_t seen = query - key0 - 32 * kb - 4 * (int32_t)h;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     x[i] = 8 * (i / 4) + i % 4 <= seen ? x[i] : 0.0f;
@@ -501,6 +565,9 @@ template <class SH> __global__ __launch_bounds__(256, 2) void causal_queries_ker
         }
     }
 
+    if constexpr (PARTS > 1) // the first adds what the second has
+        if (!add_second<ND>(smem, own, shared, lane, [&](int n) -> f32x16 & { return dq[n]; }))
+            return;
     if (!there)
         return;
     const float by = a.scale / up;
@@ -525,24 +592,36 @@ typedef void (*Kernel)(Packed);
 struct CausalBack {
     Kernel rows, keys, queries;
     void (*sum)(Packed, int32_t);
-    int size;    // rows of a stage of the keys' kernel
-    int at_once; // workgroups of it that the device holds
+    int size, own; // of the keys' kernel: rows of a stage, keys of a workgroup
+    int at_once;   // workgroups of it that the device holds
     size_t keys_lds, queries_lds;
+    int64_t keys_slots, queries_slots;
 };
-template <class SH> static CausalBack variant()
+template <class KEYS, int PARTS> static CausalBack variant(const Packed &a)
 {
-    return CausalBack{causal_rows_kernel<typename SH::IO>, causal_keys_kernel<SH>, causal_queries_kernel<SH>, causal_sum_kernel<typename SH::IO>, SH::ROWS,
-                      256 * SH::PER, SH::kKeyLds, SH::kRowLds};
+    using IO = typename KEYS::IO;
+    using QUERIES = BackShape<IO, KEYS::DP, 64, false, 2>;
+    CausalBack v = {causal_rows_kernel<IO>, causal_keys_kernel<KEYS>, causal_queries_kernel<QUERIES, PARTS>, causal_sum_kernel<IO, KEYS::kOwn>, KEYS::ROWS, KEYS::kOwn,
+                    256 * KEYS::PER, KEYS::kKeyLds, QUERIES::kRowLds, slots_of<KEYS::kOwn>(a, 1), slots_of<128 / PARTS>(a, a.group)};
+    return v;
 }
-template <typename IO> static CausalBack pick(int32_t dim)
+template <typename IO> static CausalBack pick(const Packed &a)
 {
-    if (dim <= 32)
-        return variant<BackShape<IO, 32, 64, false, 2>>();
-    if (dim <= 64)
-        return variant<BackShape<IO, 64, 32, true, 3>>();
-    if (dim <= 96)
-        return variant<BackShape<IO, 96, 64, false, 2>>();
-    return variant<BackShape<IO, 128, 32, true, 2>>();
+    // (as for rows.  us of the keys' kernel without and with: twelve heads of 64, sixteen sequences of 90 to 1,500 tokens 59 / 49, 24 of 60 to 1,000 54 / 42, one of 4,096 88 / 77, of
+    // 577 25 / 16; 40 of 60 to 1,000 102 / 106, sixteen of 240 to 4,000 262 / 293)
+    const bool rows = few_rows(a), keys = slots_of<128>(a, 1) * a.kv_heads <= 1024;
+    auto with = [&](auto one, auto two) {
+        using ONE = decltype(one);
+        using TWO = decltype(two);
+        return keys ? rows ? variant<TWO, 2>(a) : variant<TWO, 1>(a) : rows ? variant<ONE, 2>(a) : variant<ONE, 1>(a);
+    };
+    if (a.dim <= 32)
+        return with(CausalBackShape<IO, 32, 64, false, 2, 1>{}, CausalBackShape<IO, 32, 64, false, 2, 2>{});
+    if (a.dim <= 64)
+        return with(CausalBackShape<IO, 64, 32, true, 3, 1>{}, CausalBackShape<IO, 64, 64, true, 3, 2>{});
+    if (a.dim <= 96)
+        return with(CausalBackShape<IO, 96, 64, false, 2, 1>{}, CausalBackShape<IO, 96, 64, false, 2, 1>{});
+    return with(CausalBackShape<IO, 128, 32, true, 2, 1>{}, CausalBackShape<IO, 128, 32, true, 2, 1>{});
 }
 
 struct CausalPlan {
@@ -554,27 +633,29 @@ struct CausalPlan {
 static CausalPlan plan(const Packed &given, grkan_dtype_t io)
 {
     CausalPlan p;
-    p.v = io == GRKAN_BF16 ? pick<__bf16>(given.dim) : pick<_Float16>(given.dim);
+    p.v = io == GRKAN_BF16 ? pick<__bf16>(given) : pick<_Float16>(given);
     Packed &a = p.a;
     a = given;
     a.row_tiles = (int32_t)slots_of<kRowTile>(a, a.group);
-    a.key_tiles = (int32_t)slots_of<kGroup>(a, 1);
-    a.slots = (int32_t)slots_of<kGroup>(a, a.group);
-    // Slabs: as if the sequences were all of one length, which the host does not know; where one is longer its parts are the more.
+    a.value_tiles = (int32_t)slots_of<kGroup>(a, 1);
+    a.key_tiles = (int32_t)p.v.keys_slots;
+    a.slots = (int32_t)p.v.queries_slots;
+    // Slabs, of 1.4 times what each workgroup has to do on the average, if the sequences were all of one length, which the host does not know: so many that the device holds them
+    // all at once.  Where a sequence is longer its parts are the more, and then the longer (Walk).  There is a workgroup for each part that there may be, and most are not there:
+    // not so many that these take time themselves, 1.5 us each, nor more than a GB of sums.  us of the keys' kernel + the sum, with slabs of 1.4, 1.0 and 0.5 of the average:
+    // 4,001 and 2,852 tokens, 16 heads of 128 on four 261 + 13, 304 + 16, 289 + 22; one of 4,096, twelve of 64 80 + 10, 87 + 12, 83 + 14.  1,024 and 512 rows at least: one of 1,000,
+    // 32 heads of 128 on eight 67 + 8, 46 + 11; of 577, twelve of 64 15.8 + 0, 14.9 + 3.9.
     const int64_t each = a.sequences > 0 ? ((int64_t)a.tokens + a.sequences - 1) / a.sequences : 0;
     const int64_t walk = (each * a.group + p.v.size - 1) / p.v.size, longest = (a.rows + p.v.size - 1) / p.v.size; // tiles of rows: of a first key, at most
-    const int64_t share = (int64_t)a.kv_heads * ((a.tokens + kGroup - 1) / kGroup) * walk / 2 / p.v.at_once;        // of all, of each workgroup at once
-    const int64_t slab = share * 3 / 5 > 32 ? share * 3 / 5 : 32;
-    // (of a GB at most: where that is less than the parts wanted, there are tiles of keys enough)
-    const int64_t part = 2 * (int64_t)a.tokens * a.kv_heads * a.dim, held = ((int64_t)1 << 28) / (part > 0 ? part : 1), most = held < 16 ? held : 16;
-    const int64_t parts = (longest + slab - 1) / slab;
+    const int64_t share = (int64_t)a.kv_heads * ((a.tokens + p.v.own - 1) / p.v.own) * walk / 2 / p.v.at_once;
+    const int64_t slab = std::max<int64_t>(share * 7 / 5, (a.dim <= 64 ? 1024 : 512) / p.v.size), wanted = (longest + slab - 1) / slab;
+    const int64_t turns = 1 + 2 * (int64_t)p.v.at_once / ((int64_t)a.key_tiles * a.kv_heads);
+    const int64_t part = 2 * (int64_t)a.tokens * a.kv_heads * a.dim, held = ((int64_t)1 << 28) / (part > 0 ? part : 1);
     a.slab = (int32_t)slab;
-    a.parts = (int32_t)(parts < most ? parts : most);
-    if (a.parts < 1)
-        a.parts = 1;
+    a.parts = (int32_t)std::max<int64_t>(1, std::min({wanted, turns, held, (int64_t)16}));
     p.row_most = ((size_t)a.kv_heads * (size_t)a.rows + 3) & ~(size_t)3;
     p.value_most = p.row_most + ((2 * (size_t)a.kv_heads * (size_t)a.row_tiles + 3) & ~(size_t)3);
-    p.stats = p.value_most + 4 * (size_t)a.kv_heads * (size_t)a.key_tiles;
+    p.stats = p.value_most + 4 * (size_t)a.kv_heads * (size_t)a.value_tiles;
     p.partial = a.parts > 1 ? (size_t)a.parts * (size_t)part : 0;
     return p;
 }
@@ -616,7 +697,7 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
     if (!workspace || workspace_bytes < need || address(workspace) % 16 != 0)
         return GRKAN_ERR_WORKSPACE;
     attention::Packed &a = p.a;
-    const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts, sum_grid = 8 * heads * a.key_tiles;
+    const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts, sum_grid = 4 * heads * a.key_tiles;
     const int64_t queries_grid = heads * a.slots;
     if (rows_grid > attention::kMostBlocks || keys_grid > attention::kMostBlocks || queries_grid > attention::kMostBlocks ||
         (a.parts > 1 && sum_grid > attention::kMostBlocks))

@@ -1,10 +1,12 @@
 // Sequences packed one behind the other, each attending to its own earlier tokens: what the forward and the backward kernels share.
 //
 // The buffer's tokens fall into segments: those in front of the first sequence, the sequences, those behind the last.  A workgroup has a tile of one segment,
-// `size` rows that begin with the segment's.  Tile t of a segment that begins with row r (of all rows of a key head) and is number i has slot
-// floor(r / size) + i + t: the segments' slots do not overlap (floor(x + y) >= floor(x) + floor(y)), there are at most floor(rows / size) + segments of them,
-// and which segment a slot belongs to is found by a search in the offsets, without sums over the lengths, a launch in front or the host's knowing them.
-// A slot without rows has nothing to do.
+// `size` rows that begin with the segment's.  Tile t of a segment that begins with row r (of all rows of a key head) and is number i has place
+// floor(r / size) + i + t: the segments' places do not overlap (floor(x + y) >= floor(x) + floor(y)), there are at most floor(rows / size) + segments of them, and
+// so the host, which does not know the lengths, knows how many workgroups it takes, and nothing needs a sum over the lengths or a launch in front.
+//
+// Which tile a workgroup has: of 64 segments, whose places are those of their first one on, the tiles with the longest walks first, found by a search for the length
+// that as many tiles have as there are workgroups in front (24 sequences of 60 to 1,000 tokens, 12 heads of 64: . us in the place of . with the places' order).
 #ifndef GRKAN_PACKED_H_
 #define GRKAN_PACKED_H_
 
@@ -17,7 +19,8 @@ struct Packed : Args { // rows: of all tokens; batch and the operands' batch str
     const void *offsets;
     int32_t offsets_64, sequences;
     int32_t tokens, each; // each: of a sequence, where there are no offsets
-    int32_t slots;        // workgroups of a key head
+    int32_t slots;        // places, and so workgroups, of a key head
+    int32_t value_tiles;  // places of tiles of 128 keys, whose values' lengths are kept
     int32_t parts, slab;  // keys' gradients: over how many workgroups the rows of a tile of keys are split at most, and tiles of rows of each
 };
 
@@ -41,34 +44,66 @@ struct Segment {
     bool none; // of no sequence
 };
 
-// unit: rows of a token.  Offsets that fall give slots whose tokens are unspecified, but within the buffer.
-template <int SIZE> __device__ __forceinline__ int32_t slot_of(int32_t token, int32_t unit, int32_t i)
+// unit: rows of a token.  Offsets that fall give tiles whose tokens are unspecified, but within the buffer.
+template <int SIZE> __device__ __forceinline__ int32_t place_of(int32_t token, int32_t unit, int32_t i)
 {
     return (int32_t)((uint32_t)token * (uint32_t)unit / (uint32_t)SIZE) + i;
 }
-template <int SIZE> __device__ __forceinline__ Segment segment_of(const Packed &a, int32_t slot, int32_t unit)
+
+// The wavefront's sum of numbers that are not negative.
+__device__ __forceinline__ int32_t sum_of_lanes(int32_t v)
 {
-    const int32_t lane = (int32_t)threadIdx.x & 63;
-    int32_t lo = 0, len = a.sequences + 2, begin = 0, end = 0;
-    for (;;) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);
+    const auto rows = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = (int32_t)(rows[0] + rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return __builtin_amdgcn_readfirstlane((int32_t)(halves[0] + halves[1]));
+}
+
+// The tile of workgroup `slot`: of 64 segments the tiles in falling order of their number, `forward`, or of how many follow, where the first ones' walks are the longest.
+// A workgroup without one gets a segment of no tokens.
+template <int SIZE> __device__ __forceinline__ Segment segment_of(const Packed &a, int32_t slot, int32_t unit, bool forward)
+{
+    const int32_t lane = (int32_t)threadIdx.x & 63, segments = a.sequences + 2;
+    int32_t lo = 0, len = (segments + 63) / 64; // of 64 segments each: the last that begins at or in front of the slot
+    while (len > 1) {
         const int32_t step = (len + 63) / 64, i = lo + lane * step;
-        const int32_t at = boundary(a, i < lo + len ? i : lo + len);
-        const uint64_t found = __ballot(lane * step < len && slot_of<SIZE>(at, unit, i) <= slot) | 1u;
+        const uint64_t found = __ballot(lane * step < len && place_of<SIZE>(boundary(a, 64 * i), unit, 64 * i) <= slot) | 1u;
         const int32_t j = 63 - __builtin_clzll(found);
         lo += j * step;
         len = len - j * step < step ? len - j * step : step;
-        if (len > 1)
-            continue;
-        begin = __builtin_amdgcn_readlane(at, j);
-        end = j < 63 ? __builtin_amdgcn_readlane(at, j + 1) : __builtin_amdgcn_readfirstlane(boundary(a, lo + 1));
-        break;
     }
+    const int32_t mine = 64 * lo + lane, begin = boundary(a, mine), end = boundary(a, mine + 1);
+    const int32_t count = mine < segments && end > begin ? end - begin : 0, tiles = (int32_t)(((int64_t)count * unit + SIZE - 1) / SIZE);
+    const int32_t rank = slot - place_of<SIZE>(__builtin_amdgcn_readfirstlane(begin), unit, 64 * lo);
+    // the largest number that more than `rank` tiles have or exceed
+    int32_t number = 0;
+    auto from = [&](int32_t n) { return sum_of_lanes(tiles > n ? tiles - n : 0); };
+    const bool there = rank >= 0 && from(0) > rank;
+    if (there) {
+        int32_t above = __builtin_amdgcn_readfirstlane((int32_t)((int64_t)a.tokens * unit / SIZE)) + 1;
+        while (above - number > 1) {
+            const int32_t n = number + (above - number) / 2;
+            if (from(n) > rank)
+                number = n;
+            else
+                above = n;
+        }
+    }
+    const int32_t turn = rank - from(number + 1);
+    const uint64_t have = __ballot(tiles > number);
+    const uint64_t below = have & (((uint64_t)1 << lane) - 1u);
+    const uint64_t found = __ballot(tiles > number && __popcll(below) == turn);
+    const int32_t at = found ? __builtin_ctzll(found) : 0;
     Segment s;
-    s.first = begin;
-    s.count = end > begin ? end - begin : 0;
-    s.tile = slot - slot_of<SIZE>(begin, unit, lo);
-    s.index = lo;
-    s.none = lo == 0 || lo == a.sequences + 1;
+    s.first = __builtin_amdgcn_readlane(begin, at);
+    s.count = there ? __builtin_amdgcn_readlane(count, at) : 0;
+    s.tile = !there ? 0 : forward ? number : __builtin_amdgcn_readlane(tiles, at) - 1 - number;
+    s.index = 64 * lo + at;
+    s.none = s.index == 0 || s.index == segments - 1;
     return s;
 }
 
@@ -178,6 +213,7 @@ template <int DP, int ROWS, int WAVES> struct RowsTwiceLoads {
 
 // host
 grkan_status_t fill(const grkan_causal_attention_t *a, grkan_dtype_t io, Packed *to); // checks and arguments (grkan_causal.hip)
+bool few_rows(const Packed &a); // whether two wavefronts share the keys of 32 rows (grkan_causal.hip)
 template <int SIZE> inline int64_t slots_of(const Packed &a, int64_t unit) { return (int64_t)a.tokens * unit / SIZE + a.sequences + 2; }
 
 } // namespace attention
