@@ -156,6 +156,7 @@ grkan_status_t grkan_attention_bwd(const grkan_attention_t *attention, const voi
  *      past 0 .. tokens is clamped to it; where offsets fall, what comes out for the tokens between is unspecified.
  *      NULL: `sequences` of the same length, tokens / sequences (else GRKAN_ERR_SHAPE).
  *   out [tokens, heads, dim] of io, contiguous, 16-byte aligned
+ *   rest NULL, or as out, for the backward pass: what out's rounding took away, rounded itself
  *   lse NULL, or float32 [kv_heads, tokens, heads / kv_heads] (grkan_causal_attention_lse_count() elements), for the backward pass: log2 of the sum of
  *      exp(scale q k^T); an infinity for tokens of no sequence
  * No sequence has any influence on another one, and no later token on an earlier one's output, NaN and infinities included.
@@ -173,17 +174,18 @@ typedef struct {
     float scale;
 } grkan_causal_attention_t;
 size_t grkan_causal_attention_lse_count(const grkan_causal_attention_t *attention);
-grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *attention, void *out, float *lse, grkan_dtype_t io, void *hip_stream);
+grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *attention, void *out, void *rest, float *lse, grkan_dtype_t io,
+                                          void *hip_stream);
 
 /*
- * Its backward pass: P is recomputed from lse.  out as the forward pass left it; dout [tokens, heads, dim] strided as q is; dq as out, dk and dv
+ * Its backward pass: P is recomputed from lse.  out and rest as the forward pass left them (rest may be NULL: the gradients are then less exact); dout [tokens, heads, dim] strided as q is; dq as out, dk and dv
  * [tokens, kv_heads, dim], contiguous, 16-byte aligned, overwritten.  What a sequence's tokens hold reaches its own gradients alone (a NaN or an
  * infinity in one token may reach those of all its sequence).
  * workspace: grkan_causal_attention_bwd_workspace_bytes() bytes of scratch (host-only query; 0 for arguments that are refused), 16-byte aligned, untouched until the
  * enqueued work has finished.
  */
 size_t grkan_causal_attention_bwd_workspace_bytes(const grkan_causal_attention_t *attention);
-grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *attention, const void *out, const float *lse, const void *dout,
+grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *attention, const void *out, const void *rest, const float *lse, const void *dout,
                                           int64_t dout_token_stride, int64_t dout_head_stride, void *dq, void *dk, void *dv, void *workspace,
                                           size_t workspace_bytes, grkan_dtype_t io, void *hip_stream);
 

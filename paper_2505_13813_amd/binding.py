@@ -270,11 +270,11 @@ def load_library():
     causal, cache, queries = (ctypes.POINTER(c) for c in (CausalAttention, PagedCacheOperand, PagedQueries))
     lib.grkan_causal_attention_lse_count.argtypes = [causal]
     lib.grkan_causal_attention_lse_count.restype = sz
-    lib.grkan_causal_attention_fwd.argtypes = [causal, vp, vp, ctypes.c_int, vp]
+    lib.grkan_causal_attention_fwd.argtypes = [causal, vp, vp, vp, ctypes.c_int, vp]
     lib.grkan_causal_attention_fwd.restype = ctypes.c_int
     lib.grkan_causal_attention_bwd_workspace_bytes.argtypes = [causal]
     lib.grkan_causal_attention_bwd_workspace_bytes.restype = sz
-    lib.grkan_causal_attention_bwd.argtypes = [causal, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, ctypes.c_int, vp]
+    lib.grkan_causal_attention_bwd.argtypes = [causal, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, ctypes.c_int, vp]
     lib.grkan_causal_attention_bwd.restype = ctypes.c_int
     lib.grkan_paged_write.argtypes = [cache, vp, vp, vp, i32, i64, i64, i64, i64, i64, ctypes.c_int, vp]
     lib.grkan_paged_write.restype = ctypes.c_int

@@ -46,12 +46,6 @@ template <typename IO, int DP, int KT> struct Rows {
     __device__ __forceinline__ void take(const Addresses<NS> &k_from, const Addresses<ND> &v_from, uint64_t word, uint32_t cover, float c, uint32_t h)
     {
         f32x16 s[KB];
-        scores_under(k_from, word, cover, h, s);
-        weigh(s, v_from, c);
-    }
-
-    __device__ __forceinline__ void scores_under(const Addresses<NS> &k_from, uint64_t word, uint32_t cover, uint32_t h, f32x16 (&s)[KB])
-    {
         if (word != kAll) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -64,6 +58,9 @@ template <typename IO, int DP, int KT> struct Rows {
         } else {
             scores(k_from, s);
         }
+        uint32_t p[KB][8];
+        probabilities(s, c, p);
+        add(p, v_from);
     }
 
     // The scores without a mask.
@@ -122,13 +119,6 @@ template <typename IO, int DP, int KT> struct Rows {
                 p[kb][i / 2] = MM::two(x, y);
             }
         sum += part;
-    }
-
-    __device__ __forceinline__ void weigh(const f32x16 (&s)[KB], const Addresses<ND> &v_from, float c)
-    {
-        uint32_t p[KB][8];
-        probabilities(s, c, p);
-        add(p, v_from);
     }
 
     static __device__ __forceinline__ u32x4 operand(const uint32_t (&p)[8], int t)
@@ -246,23 +236,15 @@ template <typename IO_, int DP_> struct TokenShape {
     static_assert(((DP + 4) * 32 * kWaves + 64 * kWaves) * sizeof(float) <= kLds, ""); // what the wavefronts join
 };
 
-// Rows that may not see all the keys of their tiles: `last` is the last valid key of the lane's row, `first` the least of the rows' last ones.
-struct Later {
-    int32_t last, first;
-};
-struct NoLater {
-};
-
 // A wavefront's way through tiles t0, t0 + kWaves, .. (t0 its own first), below t1, without a barrier: the loads of the next are in flight while one is computed
 // with.  word_of(t): which keys of a tile are valid (asked in rising order); load(t, word, whole, to): K of the tile to `to`, V behind it.  Returns whether there
 // was a valid key.
 // (Each part of the loop is in the code once, the first tile's loads too.)
-template <class SH, class Word, class Load, class Limit = NoLater>
+template <class SH, class Word, class Load>
 __device__ __forceinline__ bool walk_alone(Rows<typename SH::IO, SH::DP, SH::KT> &rows, int32_t t0, int32_t t1, uint32_t lds0, int wave, int lane, float c,
-                                           int32_t dim, Word &&word_of, Load &&load, Limit limit = Limit{}, bool each = false)
+                                           int32_t dim, Word &&word_of, Load &&load)
 {
     constexpr int DP = SH::DP, KT = SH::KT, kStep = SH::kWaves;
-    constexpr bool kLater = !__is_same(Limit, NoLater);
     constexpr int kAhead = 2 * TileLoads<DP, KT, 1>::kMine;
     const RowOperand<DP> k_operand(lane);
     const ColumnOperand<DP> v_operand(lane);
@@ -285,24 +267,7 @@ __device__ __forceinline__ bool walk_alone(Rows<typename SH::IO, SH::DP, SH::KT>
                 wait_loads<kAhead>();
             else
                 wait_loads<0>();
-            const auto k_from = k_operand.moved(stages + at);
-            const auto v_from = v_operand.moved(stages + at + SH::kTile);
-            const uint32_t cover = covers + (at ? KT * 4u : 0u);
-            if constexpr (kLater) {
-                f32x16 s[SH::KT / 32];
-                rows.scores_under(k_from, word, cover, h, s);
-                const bool some_later = t * KT + KT - 1 > limit.first;
-                if (some_later)
-                    rows.cut(s, limit.last - t * KT, h);
-                uint32_t p[KT / 32][8];
-                rows.probabilities(s, c, p);
-                if (some_later && each)
-                    rows.add_each(p, v_from, limit.last - t * KT, (uint32_t)lane & 31u, h);
-                else
-                    rows.add(p, v_from);
-            } else {
-                rows.take(k_from, v_from, word, cover, c, h);
-            }
+            rows.take(k_operand.moved(stages + at), v_operand.moved(stages + at + SH::kTile), word, covers + (at ? KT * 4u : 0u), c, h);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (the tile's buffer is loaded into next)
         }
         at ^= SH::kStage;

@@ -26,9 +26,12 @@ template <int DP> __device__ __forceinline__ void clear_rows(const Packed &a, co
     const uint32_t row = row0 + ((uint32_t)lane & 31u), h = (uint32_t)lane >> 5;
     if ((int32_t)row >= rows)
         return;
-    char *const out = a.out + packed_at(a, s, kvh, row);
-    for (int32_t channel = 8 * (int32_t)h; channel < a.dim; channel += 16)
-        *reinterpret_cast<u32x4 *>(out + 2 * channel) = u32x4{};
+    const int64_t at = packed_at(a, s, kvh, row);
+    for (int32_t channel = 8 * (int32_t)h; channel < a.dim; channel += 16) {
+        *reinterpret_cast<u32x4 *>(a.out + at + 2 * channel) = u32x4{};
+        if (a.rest)
+            *reinterpret_cast<u32x4 *>(a.rest + at + 2 * channel) = u32x4{};
+    }
     if (h == 0 && a.lse)
         a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = __builtin_inff();
 }
@@ -180,10 +183,24 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
     if ((int32_t)row >= all)
         return;
     const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    char *const out = a.out + packed_at(a, s, kvh, row);
+    const int64_t at = packed_at(a, s, kvh, row);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
-        store_channels<typename SH::IO>(rows.acc[d], d, inv, a, out, false, h);
+        store_channels<typename SH::IO>(rows.acc[d], d, inv, a, a.out + at, false, h);
+    if (a.rest) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            f32x16 left;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = rows.acc[d][i] * inv, y = rows.acc[d][i + 1] * inv;
+                const uint32_t w = Matrix<typename SH::IO>::two(x, y);
+                left[i] = x - Matrix<typename SH::IO>::first(w);
+                left[i + 1] = y - Matrix<typename SH::IO>::second(w);
+            }
+            store_channels<typename SH::IO>(left, d, 1.0f, a, a.rest + at, false, h);
+        }
+    }
     if (h == 0 && a.lse)
         a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = lse_of(log2_sum(rows.top, sum, a.c));
 }
@@ -272,7 +289,8 @@ extern "C" size_t grkan_causal_attention_lse_count(const grkan_causal_attention_
     return !at || at->tokens < 0 || at->heads < 0 ? 0 : (size_t)at->tokens * (size_t)at->heads;
 }
 
-extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *at, void *out, float *lse, grkan_dtype_t io, void *hip_stream)
+extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *at, void *out, void *rest, float *lse, grkan_dtype_t io,
+                                                     void *hip_stream)
 {
     attention::Packed a;
     const grkan_status_t bad = attention::fill(at, io, &a);
@@ -282,7 +300,7 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
         return GRKAN_OK;
     if (!out)
         return GRKAN_ERR_NULL;
-    if (reinterpret_cast<uintptr_t>(out) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
+    if ((reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(rest)) % 16 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
         return GRKAN_ERR_ALIGN;
     const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a) : attention::pick<_Float16>(a);
     const int64_t grid = v.slots * a.kv_heads;
@@ -290,6 +308,7 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
         return GRKAN_ERR_UNSUPPORTED;
     a.slots = (int32_t)v.slots;
     a.out = static_cast<char *>(out);
+    a.rest = static_cast<char *>(rest);
     a.lse = lse;
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;

@@ -1,4 +1,5 @@
-// Causal attention over packed sequences on gfx950 (MI355X), backward.  With P recomputed from the rows' lse, D = dO V^T and delta = the row's sum of dO O,
+// Causal attention over packed sequences on gfx950 (MI355X), backward.  With P recomputed from the rows' lse, D = dO V^T and delta = the row's sum of dO O, of what out was
+// before it was rounded (out and the rest: an error of delta goes into all of a row's S', and with out alone it is a third of the gradients' own rounding in a sequence of 60 tokens),
 //
 //     dV_j = sum_{i >= j} P_ij dO_i      S'_ij = P_ij (D_ij - delta_i)      dQ_i = scale sum_{j <= i} S'_ij K_j      dK_j = scale sum_{i >= j} S'_ij Q_i
 //
@@ -31,10 +32,10 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
         return;
     const uint32_t lane16 = threadIdx.x & 15u;
     const int64_t heads_dim = (int64_t)a.kv_heads * a.group * a.dim;
-    const uint64_t out = a.forward_out + (uint64_t)packed_at(a, s, kvh, 0);
+    const uint64_t out = a.forward_out + (uint64_t)packed_at(a, s, kvh, 0), rest = reinterpret_cast<uint64_t>(a.rest) + (uint64_t)packed_at(a, s, kvh, 0);
     const uint64_t dout = a.dout.at + (uint64_t)((int64_t)s.first * a.dout.token + (int64_t)kvh * a.group * a.dout.head);
     const uint32_t row0 = (uint32_t)s.tile * kRowTile + (threadIdx.x >> 4);
-    u32x4 o[4], d[4];
+    u32x4 o[4], d[4], left[4];
     float largest = 0.0f, sums = 0.0f;
     // (all loads in front, without a branch: they wait for one another otherwise)
 #pragma unroll
@@ -42,7 +43,9 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
         const uint32_t row = row0 + 16u * k;
         const bool there = (int32_t)row < all, loaded = there && 8u * lane16 < (uint32_t)a.dim;
         const uint64_t zeros = reinterpret_cast<uint64_t>(kZeros);
-        o[k] = gload16(loaded ? out + 2u * (uint64_t)row_offset(row, (uint32_t)a.group, heads_dim, a.dim) + 16u * lane16 : zeros, 0);
+        const uint64_t at = 2u * (uint64_t)row_offset(row, (uint32_t)a.group, heads_dim, a.dim) + 16u * lane16;
+        o[k] = gload16(loaded ? out + at : zeros, 0);
+        left[k] = gload16(loaded && a.rest ? rest + at : zeros, 0);
         d[k] = gload16(loaded ? dout + (uint64_t)row_offset(row, (uint32_t)a.group, a.dout.token, a.dout.head) + 16u * lane16 : zeros, 0);
     }
 #pragma unroll
@@ -52,7 +55,7 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float x = MM::first(d[k][j]), y = MM::second(d[k][j]);
-            sum += x * MM::first(o[k][j]) + y * MM::second(o[k][j]);
+            sum += x * (MM::first(o[k][j]) + MM::first(left[k][j])) + y * (MM::second(o[k][j]) + MM::second(left[k][j]));
             largest = fmaxf(largest, fmaxf(fabsf(x), fabsf(y)));
         }
 #pragma unroll
@@ -494,18 +497,20 @@ template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_
         delta *= up;
     } else {
         // for the keys' kernel too
-        const uint64_t at = a.forward_out + (uint64_t)packed_at(a, s, kvh, row);
-        u32x4 y[NS];
+        const uint64_t at = a.forward_out + (uint64_t)packed_at(a, s, kvh, row), rest = reinterpret_cast<uint64_t>(a.rest) + (uint64_t)packed_at(a, s, kvh, row);
+        u32x4 y[NS], z[NS];
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
             const uint32_t channel = 16u * st + 8u * h;
-            y[st] = gload16(there && channel < (uint32_t)a.dim ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            const bool loaded = there && channel < (uint32_t)a.dim;
+            y[st] = gload16(loaded ? at + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
+            z[st] = gload16(loaded && a.rest ? rest + channel * 2u : reinterpret_cast<uint64_t>(kZeros), 0);
         }
 #pragma unroll
         for (int st = 0; st < NS; ++st)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                delta += MM::first(o[st][j]) * MM::first(y[st][j]) + MM::second(o[st][j]) * MM::second(y[st][j]);
+                delta += MM::first(o[st][j]) * (MM::first(y[st][j]) + MM::first(z[st][j])) + MM::second(o[st][j]) * (MM::second(y[st][j]) + MM::second(z[st][j]));
         delta = halves_sum(delta);
         if (h == 0 && there && shared == 0)
             a.row_delta[(int64_t)kvh * a.rows + place] = delta;
@@ -674,7 +679,7 @@ extern "C" size_t grkan_causal_attention_bwd_workspace_bytes(const grkan_causal_
     return (p.stats + p.partial) * sizeof(float);
 }
 
-extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *at, const void *out, const float *lse, const void *dout,
+extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attention_t *at, const void *out, const void *rest, const float *lse, const void *dout,
                                                      int64_t dout_token_stride, int64_t dout_head_stride, void *dq, void *dk, void *dv, void *workspace,
                                                      size_t workspace_bytes, grkan_dtype_t io, void *hip_stream)
 {
@@ -687,7 +692,7 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
     if (!out || !lse || !dout || !dq || !dk || !dv)
         return GRKAN_ERR_NULL;
     auto address = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
-    if ((address(out) | address(dout) | address(dq) | address(dk) | address(dv)) % 16 != 0 || address(lse) % 4 != 0 ||
+    if ((address(out) | address(rest) | address(dout) | address(dq) | address(dk) | address(dv)) % 16 != 0 || address(lse) % 4 != 0 ||
         (dout_token_stride | dout_head_stride) % 8 != 0)
         return GRKAN_ERR_ALIGN;
     if (!attention::in_offsets(dout_token_stride, dout_head_stride, given.group))
@@ -711,6 +716,7 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
     a.dk = static_cast<char *>(dk);
     a.dv = static_cast<char *>(dv);
     a.forward_out = address(out);
+    a.rest = static_cast<char *>(const_cast<void *>(rest));
     a.out = static_cast<char *>(dq);
     if (!attention::allow_lds(reinterpret_cast<const void *>(p.v.keys), p.v.keys_lds) ||
         !attention::allow_lds(reinterpret_cast<const void *>(p.v.queries), p.v.queries_lds))

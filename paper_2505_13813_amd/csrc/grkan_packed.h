@@ -16,6 +16,7 @@ namespace grkan {
 namespace attention {
 
 struct Packed : Args { // rows: of all tokens; batch and the operands' batch strides: not used
+    char *rest; // what the rounding of `out` left, or null
     const void *offsets;
     int32_t offsets_64, sequences;
     int32_t tokens, each; // each: of a sequence, where there are no offsets

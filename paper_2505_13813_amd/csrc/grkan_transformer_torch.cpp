@@ -638,36 +638,38 @@ struct Causal {
     }
 };
 
-// {out, lse}; lse only where a backward pass may follow
-variable_list causal_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, double scale, bool with_lse)
+// {out, lse, rest}; the last two only where a backward pass may follow
+variable_list causal_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, double scale, bool for_backward)
 {
     check_gpu(q, "q");
     const c10::DeviceGuard guard(q.device());
     const Causal d(q, k, v, offsets, scale);
     const Tensor out = at::empty(q.sizes(), q.options());
-    Tensor lse;
-    if (with_lse)
+    Tensor lse, rest;
+    if (for_backward) {
         lse = at::empty({(int64_t)grkan_causal_attention_lse_count(&d.a)}, q.options().dtype(at::kFloat));
-    check(grkan_causal_attention_fwd(&d.a, out.data_ptr(), with_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, d.io, stream_of(q)),
-          "grkan_causal_attention_fwd");
-    return {out, lse};
+        rest = at::empty(q.sizes(), q.options());
+    }
+    check(grkan_causal_attention_fwd(&d.a, out.data_ptr(), data_of(rest), static_cast<float *>(data_of(lse)), d.io, stream_of(q)), "grkan_causal_attention_fwd");
+    return {out, lse, rest};
 }
 
 variable_list causal_backward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, double scale, const Tensor &out, const Tensor &lse,
-                              const Tensor &dout_)
+                              const Tensor &rest, const Tensor &dout_)
 {
     check_gpu(q, "q");
     const c10::DeviceGuard guard(q.device());
     const Causal d(q, k, v, offsets, scale);
     check_like(out, q, "the saved output", "q");
+    check_like(rest, q, "the saved rest", "q");
     check_like(dout_, q, "the gradient of the output", "q");
-    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.is_contiguous() && dout_.sizes() == q.sizes() && lse.scalar_type() == at::kFloat &&
+    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.is_contiguous() && rest.sizes() == q.sizes() && rest.is_contiguous() && dout_.sizes() == q.sizes() && lse.scalar_type() == at::kFloat &&
                           lse.device() == q.device() && lse.is_contiguous() && lse.numel() == (int64_t)grkan_causal_attention_lse_count(&d.a),
                       "what the forward pass saved must match q");
     const Tensor dout = in_rows(dout_, d.group);
     const Tensor ws = at::empty({(int64_t)grkan_causal_attention_bwd_workspace_bytes(&d.a)}, q.options().dtype(at::kByte));
     const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(v.sizes(), v.options());
-    check(grkan_causal_attention_bwd(&d.a, out.data_ptr(), static_cast<const float *>(lse.data_ptr()), dout.data_ptr(),
+    check(grkan_causal_attention_bwd(&d.a, out.data_ptr(), rest.data_ptr(), static_cast<const float *>(lse.data_ptr()), dout.data_ptr(),
                                      dout.size(0) > 1 ? dout.stride(0) : 0, dout.size(1) > 1 ? dout.stride(1) : 0, dq.data_ptr(), dk.data_ptr(),
                                      dv.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), d.io, stream_of(q)),
           "grkan_causal_attention_bwd");
@@ -680,7 +682,7 @@ struct CausalAttention : public torch::autograd::Function<CausalAttention> {
         ctx->set_materialize_grads(false);
         ctx->saved_data["scale"] = scale;
         const variable_list out = causal_forward(q, k, v, of_optional(offsets), scale, true);
-        ctx->save_for_backward({q, k, v, of_optional(offsets), out[0], out[1]});
+        ctx->save_for_backward({q, k, v, of_optional(offsets), out[0], out[1], out[2]});
         return out[0];
     }
 
@@ -692,7 +694,7 @@ struct CausalAttention : public torch::autograd::Function<CausalAttention> {
             return out;
         const double scale = ctx->saved_data["scale"].toDouble();
         const variable_list found =
-            gradients({s[0], s[1], s[2], grads[0]}, [&] { return causal_backward(s[0], s[1], s[2], s[3], scale, s[4], s[5], grads[0]); });
+            gradients({s[0], s[1], s[2], grads[0]}, [&] { return causal_backward(s[0], s[1], s[2], s[3], scale, s[4], s[5], s[6], grads[0]); });
         for (int i = 0; i < 3; ++i)
             out[i] = found[i];
         return out;

@@ -53,32 +53,34 @@ BAD_CAUSAL = [({"q": None}, NULL), ({"k": None}, NULL), ({"v": None}, NULL), ({"
 @pytest.mark.parametrize("fields,status", BAD_CAUSAL)
 def test_causal_refusals(lib, fields, status):
     a = _causal(**fields)
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, BF16, None) == status
-    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 40, BF16, None) == status
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, 16, None, BF16, None) == status
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 40, BF16, None) == status
     assert lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a)) == 0
 
 
 def test_causal_refusals_of_outputs(lib):
     a = _causal()
-    assert lib.grkan_causal_attention_fwd(None, 16, None, BF16, None) == NULL
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), None, None, BF16, None) == NULL
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 24, None, BF16, None) == ALIGN
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, 18, BF16, None) == ALIGN
+    assert lib.grkan_causal_attention_fwd(None, 16, None, None, BF16, None) == NULL
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), None, None, None, BF16, None) == NULL
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 24, None, None, BF16, None) == ALIGN
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, 24, None, BF16, None) == ALIGN
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, 18, BF16, None) == ALIGN
     for io in (F32, 9):
-        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, io, None) == DTYPE
+        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, None, io, None) == DTYPE
     need = lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a))
 
-    def bwd(out=16, lse=16, dout=16, strides=(256, 64), dq=16, dk=16, dv=16, ws=16, size=need):
-        return lib.grkan_causal_attention_bwd(ctypes.byref(a), out, lse, dout, *strides, dq, dk, dv, ws, size, BF16, None)
+    def bwd(out=16, rest=16, lse=16, dout=16, strides=(256, 64), dq=16, dk=16, dv=16, ws=16, size=need):
+        return lib.grkan_causal_attention_bwd(ctypes.byref(a), out, rest, lse, dout, *strides, dq, dk, dv, ws, size, BF16, None)
 
     for name in ("out", "lse", "dout", "dq", "dk", "dv"):
         assert bwd(**{name: None}) == NULL, name
         assert bwd(**{name: 18}) == ALIGN, name
+    assert bwd(rest=24) == ALIGN
     assert bwd(strides=(257, 64)) == ALIGN and bwd(strides=(1 << 25, 64)) == UNSUPPORTED and bwd(strides=(-256, 64)) == UNSUPPORTED
     assert need > 0 and bwd(size=need - 1) == WORKSPACE and bwd(ws=None) == WORKSPACE and bwd(ws=24) == WORKSPACE
     none = _causal(tokens=0, q=None, k=None, v=None)
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(none), None, None, BF16, None) == OK
-    assert lib.grkan_causal_attention_bwd(ctypes.byref(none), None, None, None, 0, 0, None, None, None, None, 0, BF16, None) == OK
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(none), None, None, None, BF16, None) == OK
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(none), None, None, None, None, 0, 0, None, None, None, None, 0, BF16, None) == OK
     assert lib.grkan_causal_attention_lse_count(ctypes.byref(a)) == 40 * 4
 
 
@@ -95,8 +97,8 @@ def test_causal_workspaces(lib):
 
 def test_more_workgroups_than_a_launch_takes(lib):
     a = _causal(tokens=1 << 24, heads=64, kv_heads=64, sequences=1 << 24)
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, BF16, None) == UNSUPPORTED
-    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 60, BF16, None) == UNSUPPORTED
+    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, None, BF16, None) == UNSUPPORTED
+    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 60, BF16, None) == UNSUPPORTED
 
 
 def _cache(**fields):
