@@ -1,14 +1,16 @@
 """What stands around the KAT MLP in a transformer block: root-mean-square norm with the residual's addition (forward, backward,
-and in inference to 8 bits), rotary positions with several axes for tokens of images and video, and cross attention to an
+and in inference to 8 bits), rotary positions with several axes for tokens of images and video, cross attention to an
 encoder's states of another length (forward, backward, and split over the keys where there are few queries, single tokens
-among them).
+among them), causal attention over packed sequences (forward, backward), and a cache of keys and values in pages with the attention
+of the newest tokens over it.
 
 The functions run hand-written kernels (C ABI: include/grkan_transformer.h) through native autograd functions; there is no other
 route, and nothing falls back.  They take plain tensors on the GPU, outside of function transforms, tracing and
 forward-mode differentiation; under torch.compile they are calls that break the graph.  Work is enqueued on the current stream;
 results are the same bits from run to run.
 
-KATCrossBlock and KATCrossDecoder run them together with KATMlp, as a decoder of image or video tokens does.
+KATCrossBlock and KATCrossDecoder run them together with KATMlp, as a decoder of image or video tokens does; KATDecoderBlock and
+KATDecoder as one that answers token by token, with a PagedCache.
 """
 from __future__ import annotations
 
@@ -259,3 +261,135 @@ class KATCrossDecoder(nn.Module):
             x, stream = block(x, context, stream, positions, context_positions, key_lengths, key_mask,
                               None if cache is None else cache[i])
         return self.norm(x) if stream is None else self.norm(x.to(stream.dtype), stream)[0]
+
+
+class PagedCache:
+    """Pages of keys and values for a KATDecoder, or another caller of paged_write and paged_attention: `depth` blocks' k_pages[i] and
+    v_pages[i] [pages, page_size, kv_heads, dim], and for `sequences` rows a table and lengths, int32 on the device, which the blocks share and
+    whose addresses stay (a captured step reads what grow() wrote).  Which pages are free is kept on the host.
+
+    `longest`: positions that a sequence may have at most."""
+
+    def __init__(self, depth: int, pages: int, page_size: int, kv_heads: int, dim: int, sequences: int, longest: int,
+                 dtype=torch.bfloat16, device="cuda"):
+        if min(depth, pages, page_size, kv_heads, dim, sequences, longest) < 1:
+            raise ValueError("a cache needs a block, a page, a position, a head, a channel and a sequence at least")
+        pools = torch.zeros(2, depth, pages, page_size, kv_heads, dim, dtype=dtype, device=device)
+        self.k_pages, self.v_pages = list(pools[0].unbind(0)), list(pools[1].unbind(0))
+        self.page_size, self.longest = page_size, longest
+        self.table = torch.full((sequences, -(-longest // page_size)), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self.counts = [0] * sequences
+        self._pages = [[] for _ in range(sequences)]
+        self._free = list(range(pages - 1, -1, -1))
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def _written(self):
+        table = torch.full(self.table.shape, -1, dtype=torch.int32)
+        for row, held in zip(table, self._pages):
+            row[:len(held)] = torch.tensor(held, dtype=torch.int32)
+        self.table.copy_(table)
+        self.lengths.copy_(torch.tensor(self.counts, dtype=torch.int32))
+
+    def grow(self, counts: Sequence[int]) -> None:
+        """Makes room for counts[s] new positions of each sequence and adds them to the lengths, before the step that writes them.  Refused as
+        a whole where the pages do not suffice."""
+        counts = [int(n) for n in counts]
+        if len(counts) != len(self.counts) or min(counts) < 0:
+            raise ValueError("counts must be a number of new positions, not negative, for each of the cache's sequences")
+        after = [a + b for a, b in zip(self.counts, counts)]
+        if max(after) > self.longest:
+            raise ValueError("a sequence would have %d positions, and %d is the most" % (max(after), self.longest))
+        wanted = [-(-n // self.page_size) - len(held) for n, held in zip(after, self._pages)]
+        if sum(wanted) > len(self._free):
+            raise RuntimeError("%d more pages are needed, and %d are free" % (sum(wanted), len(self._free)))
+        for held, n in zip(self._pages, wanted):
+            held += [self._free.pop() for _ in range(n)]
+        self.counts = after
+        self._written()
+
+    def release(self, sequence: int) -> None:
+        """Takes a sequence's pages back: its row, of length 0, is free for another one."""
+        self._free += reversed(self._pages[sequence])
+        self._pages[sequence] = []
+        self.counts[sequence] = 0
+        self._written()
+
+
+class KATDecoderBlock(nn.Module):
+    """A decoder block with a KAT MLP: x + attention(norm(x)) within the token's sequence, then x + KATMlp(norm(x)).
+
+    As KATCrossBlock it takes and returns (branch, stream).  Parameters and inputs are bfloat16 or float16, or float32 under autocast to one
+    of the two, which keeps the stream in float32.  `rotary_pairs`: rotated channel pairs of each head for each axis of the positions, which are
+    then needed; none: no rotation."""
+
+    def __init__(self, dim: int, heads: int, kv_heads: Optional[int] = None, rotary_pairs: Sequence[int] = (), groups: int = 8,
+                 hidden: Optional[int] = None, eps: float = 1e-6):
+        super().__init__()
+        kv_heads = heads if kv_heads is None else kv_heads
+        if dim % heads or heads % kv_heads:
+            raise ValueError("dim must be a multiple of heads, and heads of kv_heads")
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, dim // heads
+        self.norm1 = RMSNorm(dim, eps)
+        self.to_qkv = nn.Linear(dim, (heads + 2 * kv_heads) * self.head_dim)
+        self.rotary = RotaryAxes(rotary_pairs) if len(rotary_pairs) else None
+        self.proj = nn.Linear(dim, dim)
+        self.norm2 = RMSNorm(dim, eps)
+        self.mlp = KATMlp(dim, hidden, groups)
+
+    def forward(self, branch, stream=None, offsets=None, positions=None, cache: Optional[PagedCache] = None, index: int = 0,
+                newest: bool = False):
+        """branch [tokens, dim] with offsets, or [batch, tokens, dim].  cache: keys and values go to its pages number `index`, too.  `newest`: the
+        tokens are the last of the cache's sequences, [sequences, tokens, dim], and see all that those hold."""
+        if self.rotary is not None and positions is None:
+            raise ValueError("a block with rotation needs positions")
+        y, x = (self.norm1(branch), branch) if stream is None else self.norm1(branch.to(stream.dtype), stream)
+        qkv = self.to_qkv(y).unflatten(-1, (-1, self.head_dim))
+        q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), -2)
+        if self.rotary is not None:
+            packed = branch.dim() == 2  # one batch entry
+            q, k = self.rotary(q[None] if packed else q, positions, k[None] if packed else k)
+            q, k = (q[0], k[0]) if packed else (q, k)
+        if cache is not None:
+            k_pages, v_pages = cache.k_pages[index], cache.v_pages[index]
+            paged_write(k, v, k_pages, v_pages, cache.table, cache.lengths, offsets)
+        if newest:
+            out = paged_attention(q, k_pages, v_pages, cache.table, cache.lengths)
+        else:
+            out = causal_attention(q, k, v, offsets)
+        y, x = self.norm2(self.proj(out.flatten(-2)).to(x.dtype), x)
+        return self.mlp(y), x
+
+
+class KATDecoder(nn.Module):
+    """KATDecoderBlocks one behind the other, and a norm.  `eps` is that of every norm."""
+
+    def __init__(self, depth: int, dim: int, heads: int, *, eps: float = 1e-6, **block):
+        super().__init__()
+        self.blocks = nn.ModuleList(KATDecoderBlock(dim, heads, eps=eps, **block) for _ in range(depth))
+        self.norm = RMSNorm(dim, eps)
+
+    def cache(self, pages: int, page_size: int, sequences: int, longest: int, dtype=None) -> PagedCache:
+        """An empty PagedCache on the parameters' device, of their type or (under autocast) `dtype`."""
+        block, weight = self.blocks[0], self.norm.weight
+        return PagedCache(len(self.blocks), pages, page_size, block.kv_heads, block.head_dim, sequences, longest, dtype or weight.dtype,
+                          weight.device)
+
+    def _run(self, x, **given):
+        stream = None
+        for i, block in enumerate(self.blocks):
+            x, stream = block(x, stream, index=i, **given)
+        return self.norm(x) if stream is None else self.norm(x.to(stream.dtype), stream)[0]
+
+    def forward(self, x, offsets=None, positions=None, cache: Optional[PagedCache] = None):
+        """Whole sequences: x [tokens, dim] packed, offsets as in causal_attention, positions [tokens, axes]; or [batch, tokens, dim].  With a
+        cache, whose rows held nothing before they grew by these sequences, their keys and values are left there; without gradients."""
+        return self._run(x, offsets=offsets, positions=positions, cache=cache)
+
+    def step(self, x, cache: PagedCache, positions=None):
+        """The newest tokens [sequences, tokens, dim] of the cache's sequences, by which each has grown, or has been released; positions
+        [sequences, tokens, axes]."""
+        return self._run(x, positions=positions, cache=cache, newest=True)

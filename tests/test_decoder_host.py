@@ -193,3 +193,60 @@ def test_tensors_on_the_cpu_and_missing_ones_are_refused():
                        (lambda: T.paged_write(q, q, None, pool, table, lengths), "k_pages")):
         with pytest.raises(TypeError, match=r"^%s must be a tensor" % name):
             call()
+
+
+def _host_cache(**given):
+    import torch
+
+    from paper_2505_13813_amd.transformer import PagedCache
+
+    return PagedCache(**{**dict(depth=2, pages=6, page_size=4, kv_heads=2, dim=8, sequences=3, longest=14, dtype=torch.bfloat16, device="cpu"), **given})
+
+
+def test_pages_are_given_out_and_taken_back():
+    c = _host_cache()
+    assert [t.shape for t in (*c.k_pages, *c.v_pages)] == [(6, 4, 2, 8)] * 4 and c.table.shape == (3, 4) and c.free_pages == 6
+    at = c.table.data_ptr(), c.lengths.data_ptr()
+    c.grow([5, 0, 4])
+    assert c.counts == c.lengths.tolist() == [5, 0, 4] and c.free_pages == 3
+    c.grow([3, 1, 0])
+    assert c.counts == c.lengths.tolist() == [8, 1, 4] and c.free_pages == 2
+    held = [[p for p in row if p >= 0] for row in c.table.tolist()]
+    assert [len(h) for h in held] == [2, 1, 1] and len(set(sum(held, []))) == 4
+    before = c.table.clone()
+    with pytest.raises(RuntimeError, match="pages"):
+        c.grow([1, 4, 8])
+    with pytest.raises(ValueError, match="most"):
+        c.grow([7, 0, 0])
+    for bad in ([1, 1], [1, 1, -1]):
+        with pytest.raises(ValueError):
+            c.grow(bad)
+    assert c.counts == [8, 1, 4] and c.free_pages == 2 and (c.table == before).all()
+    c.release(0)
+    assert c.free_pages == 4 and c.lengths.tolist() == [0, 1, 4] and (c.table[0] == -1).all() and (c.table[1:] == before[1:]).all()
+    c.grow([14, 0, 0])
+    assert c.free_pages == 0 and sorted(sum(([p for p in row if p >= 0] for row in c.table.tolist()), [])) == list(range(6))
+    assert (c.table.data_ptr(), c.lengths.data_ptr()) == at
+    for bad in (dict(pages=0), dict(page_size=0), dict(sequences=0), dict(longest=0), dict(depth=0)):
+        with pytest.raises(ValueError):
+            _host_cache(**bad)
+
+
+def test_a_decoder_wants_positions_and_heads_that_divide():
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    m = T.KATDecoder(1, 64, 2, groups=4, rotary_pairs=(8,))
+    x = torch.zeros(4, 64)
+    for call in (lambda: m(x), lambda: m.step(x[None], _host_cache())):
+        with pytest.raises(ValueError, match="positions"):
+            call()
+    for bad in (dict(heads=5), dict(heads=6, kv_heads=4)):
+        with pytest.raises(ValueError):
+            T.KATDecoderBlock(192, **bad)
+    for given, eps in (({}, 1e-6), ({"eps": 1e-3}, 1e-3)):
+        m = T.KATDecoder(2, 64, 2, groups=4, **given)
+        assert [n.eps for b in m.blocks for n in (b.norm1, b.norm2)] + [m.norm.eps] == [eps] * 5
+    c = T.KATDecoder(3, 64, 4, kv_heads=2, groups=4).bfloat16().cache(5, 16, 2, 40)
+    assert len(c.k_pages) == 3 and c.k_pages[0].shape == (5, 16, 2, 16) and c.k_pages[0].dtype == torch.bfloat16 and c.table.shape == (2, 3)
