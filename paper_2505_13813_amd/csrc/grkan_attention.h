@@ -54,6 +54,9 @@ struct Args {
     int32_t work, run; // work items, and how many of them in a row one XCD gets
 };
 
+// Instruction kinds of __builtin_amdgcn_sched_group_barrier.
+constexpr int kProducts = 0x8, kLdsReads = 0x100;
+
 template <typename IO> struct Matrix;
 template <> struct Matrix<__bf16> {
     static __device__ __forceinline__ f32x16 multiply(const u32x4 &a, const u32x4 &b, const f32x16 &c)

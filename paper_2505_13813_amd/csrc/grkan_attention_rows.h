@@ -76,6 +76,19 @@ template <typename IO, int DP, int KT> struct Rows {
                 s[kb] = MM::multiply(RowOperand<DP>::read(k_from, kb, st), q[st], s[kb]);
     }
 
+    // As scores, with the operands of AHEAD products read in front of the one that is computed.
+    template <int AHEAD> __device__ __forceinline__ void scores_ahead(const Addresses<NS> &k_from, f32x16 (&s)[KB])
+    {
+        scores(k_from, s);
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, AHEAD * KB, 0);
+#pragma unroll
+        for (int st = AHEAD; st < NS; ++st) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, KB, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, KB, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, AHEAD * KB, 0);
+    }
+
     // Keys behind `last` (of the tile, the lane's row's last valid one; below 0: none) are not valid.
     static __device__ __forceinline__ void cut(f32x16 (&s)[KB], int32_t last, uint32_t h)
     {

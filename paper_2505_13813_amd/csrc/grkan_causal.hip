@@ -103,7 +103,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         v_from.move(lds0 + row_at<DP>((uint32_t)(KEYS * part)) + 2 * SH::kTile);
         uint32_t at = 0;
 #pragma unroll 1
-        for (int32_t t = 0; t < tiles; ++t) {
+        for (int32_t t = 0;;) { // (there is a tile: with a way past the loop it would copy the sums in every turn)
             wait_loads<0>();
             barrier(); // all wavefronts' loads of this tile are there, and all are done with the tile before
             if (t + 1 < tiles)
@@ -114,22 +114,24 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
                 v_from.move(at ? 0u - SH::kTile : SH::kTile);
             }
             const int32_t key0 = t * KT + KEYS * part; // the wavefront's first
-            if (!works || key0 >= to)
-                continue;
-            f32x16 x[KEYS / 32];
-            rows.scores(k_from, x);
-            const bool crossed = key0 + KEYS > from;
-            if (crossed)
-                rows.cut(x, (int32_t)query - key0, h);
-            uint32_t p[KEYS / 32][8];
-            rows.probabilities(x, a.c, p);
-            if constexpr (decltype(each)::value) {
-                if (crossed) {
+            if (works && key0 < to) {
+                f32x16 x[KEYS / 32];
+                rows.template scores_ahead<2>(k_from, x);
+                const bool crossed = key0 + KEYS > from;
+                if (crossed)
+                    rows.cut(x, (int32_t)query - key0, h);
+                uint32_t p[KEYS / 32][8];
+                rows.probabilities(x, a.c, p);
+                bool apart = false;
+                if constexpr (decltype(each)::value)
+                    apart = crossed;
+                if (apart)
                     rows.add_each(p, v_from, (int32_t)query - key0, col, h);
-                    continue;
-                }
+                else
+                    rows.add(p, v_from);
             }
-            rows.add(p, v_from);
+            if (++t == tiles)
+                break;
         }
     };
     walk(std::false_type{});
@@ -139,7 +141,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         flag[wave] = works && rows.not_finite();
     wait_loads<0>();
     barrier();
-    if (__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0) {
+    if (__builtin_expect_with_probability(__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0, 0, 1.0)) { // (its loops are not what registers go to)
         issue(0, 0);
         walk(std::true_type{});
         barrier();

@@ -150,15 +150,17 @@ template <int DP, int ROWS, int WAVES> struct LastTwiceLoads {
     __device__ __forceinline__ void issue(uint64_t base, int64_t token_stride, int32_t dim, int32_t rows, uint32_t lds_at) const
     {
         const uint64_t from = uniform_u64(base);
+        if (dim == DP && rows >= ROWS) { // (apart, without a branch between them)
+#pragma unroll
+            for (int q = 0; q < kMine; ++q)
+                load_to_lds(from, offset[q], lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kMine; ++q) {
-            uint32_t o = offset[q];
-            if (rows < ROWS) {
-                const uint32_t l = lane_here();
-                const uint32_t r = row(q, l);
-                o = (r < (uint32_t)rows ? r : (uint32_t)rows - 1) * (uint32_t)token_stride + chunk(q, l) * 16u;
-            }
-            if (dim == DP || (there >> q & 1u))
+            const uint32_t l = lane_here();
+            const uint32_t r = row(q, l), o = (r < (uint32_t)rows ? r : (uint32_t)rows - 1) * (uint32_t)token_stride + chunk(q, l) * 16u;
+            if (there >> q & 1u)
                 load_to_lds(from, o, lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
         }
     }
@@ -197,16 +199,18 @@ template <int DP, int ROWS, int WAVES> struct RowsTwiceLoads {
     {
         const uint32_t group = (uint32_t)a.group, row0 = (uint32_t)t * ROWS, query0 = row0 / group;
         const uint64_t from = uniform_u64(base + (uint64_t)query0 * (uint64_t)o.token);
-        const bool whole = ROWS % group == 0 && row0 + ROWS <= (uint32_t)rows;
+        if (a.dim == DP && ROWS % group == 0 && row0 + ROWS <= (uint32_t)rows) {
+#pragma unroll
+            for (int q = 0; q < kMine; ++q)
+                load_to_lds(from, offset[q], lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kMine; ++q) {
-            uint32_t place = offset[q];
-            if (!whole) {
-                const uint32_t l = lane_here();
-                const uint32_t r = row0 + row(q, l), mine = r < (uint32_t)rows ? r : (uint32_t)rows - 1, query = mine / group;
-                place = (query - query0) * (uint32_t)o.token + (mine - query * group) * (uint32_t)o.head + chunk(q, l) * 16u;
-            }
-            if (a.dim == DP || (there >> q & 1u))
+            const uint32_t l = lane_here();
+            const uint32_t r = row0 + row(q, l), mine = r < (uint32_t)rows ? r : (uint32_t)rows - 1, query = mine / group;
+            const uint32_t place = (query - query0) * (uint32_t)o.token + (mine - query * group) * (uint32_t)o.head + chunk(q, l) * 16u;
+            if (there >> q & 1u)
                 load_to_lds(from, place, lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
         }
     }
