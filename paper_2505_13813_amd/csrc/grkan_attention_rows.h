@@ -9,6 +9,7 @@ namespace attention {
 
 // 32 rows of a wavefront: their queries, the running maximum and sum, and the sum of the weighted values.
 template <typename IO, int DP, int KT> struct Rows {
+    typedef IO Type;
     using MM = Matrix<IO>;
     static constexpr int KB = KT / 32, ND = DP / 32, NS = DP / 16;
     static constexpr uint64_t kAll = KT == 64 ? ~(uint64_t)0 : 0xffffffffu;
@@ -154,6 +155,37 @@ template <typename IO, int DP, int KT> struct Rows {
                 for (int d = 0; d < ND; ++d)
                     acc[d] = MM::multiply(ColumnOperand<DP>::read(v_from, kb, t, d), w, acc[d]);
             }
+    }
+
+    // scores of a tile and add of another, in the order that is written: operands are read four products ahead, and between(n), n from 0 to 3, goes between the products.
+    template <class Between>
+    __device__ __forceinline__ void scores_and_add(const Addresses<NS> &k_from, f32x16 (&s)[KB], const uint32_t (&p)[KB][8], const Addresses<ND> &v_from, Between &&between)
+    {
+        constexpr int kScores = NS * KB, kAll = kScores + 2 * KB * ND, kAhead = 4;
+        auto operand = [&](int n) {
+            const int i = n - kScores;
+            return n < kScores ? RowOperand<DP>::read(k_from, n % KB, n / KB) : ColumnOperand<DP>::read(v_from, i / (2 * ND), i / ND % 2, i % ND);
+        };
+        u32x4 next[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n)
+            next[n] = operand(n);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+            s[kb] = f32x16{};
+#pragma unroll
+        for (int n = 0; n < kAll; ++n) {
+            const int i = n - kScores;
+            if (n < kScores)
+                s[n % KB] = MM::multiply(next[n % kAhead], q[n / KB], s[n % KB]);
+            else
+                acc[i % ND] = MM::multiply(next[n % kAhead], this->operand(p[i / (2 * ND)], i / ND % 2), acc[i % ND]);
+            if (n + kAhead < kAll)
+                next[n % kAhead] = operand(n + kAhead);
+            if (n % (kAll / 4) == kAll / 8)
+                between(n / (kAll / 4));
+            fence_schedule();
+        }
     }
 
     // As add, for scores that were cut: a row at a time, with zeros in place of the values behind its last key.  (Zero times a NaN or an infinity

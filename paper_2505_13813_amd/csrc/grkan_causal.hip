@@ -38,6 +38,76 @@ template <int DP> __device__ __forceinline__ void clear_rows(const Packed &a, co
 
 // ------------------------------------------------------------------------------------------------ 32 rows a wavefront, tiles of 64 keys for all
 
+// Two wavefronts' sums of the same rows (`pairs` of them, this is number `own`): the second leaves its own in LDS (and is done: false), the first adds them, relative to a
+// common maximum.
+template <class R> __device__ __forceinline__ bool join_two(R &rows, char *smem, int pairs, int own, int second, int lane, float c)
+{
+    constexpr int ND = R::ND;
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(smem) + own * ND * 4 * 64 + lane;
+    float *const stats = reinterpret_cast<float *>(smem + pairs * ND * 4 * 64 * 16) + own * 2 * 64 + lane;
+    if (second) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = rows.acc[d][4 * g + j];
+                sums[(4 * d + g) * 64] = o;
+            }
+        stats[0] = rows.top;
+        stats[64] = rows.sum;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    if (second)
+        return false;
+    const float other = stats[0], top = fmaxf(rows.top, other), low = top > -__builtin_inff() ? top : 0.0f;
+    const float mine = __builtin_amdgcn_exp2f((rows.top - low) * c), its = __builtin_amdgcn_exp2f((other - low) * c);
+    rows.top = top;
+    rows.sum = rows.sum * mine + stats[64] * its;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 o = sums[(4 * d + g) * 64];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                rows.acc[d][4 * g + j] = rows.acc[d][4 * g + j] * mine + o[j] * its;
+        }
+    return true;
+}
+
+// The lane's row: of the output, what its rounding left, and the row's lse.
+template <class R> __device__ __forceinline__ void store_rows(const R &rows, const Packed &a, const Segment &s, int32_t kvh, uint32_t row, int32_t all, uint32_t h)
+{
+    using MM = typename R::MM;
+    if ((int32_t)row >= all)
+        return;
+    const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t at = packed_at(a, s, kvh, row);
+#pragma unroll
+    for (int d = 0; d < R::ND; ++d)
+        store_channels<typename R::Type>(rows.acc[d], d, inv, a, a.out + at, false, h);
+    if (a.rest) {
+#pragma unroll
+        for (int d = 0; d < R::ND; ++d) {
+            f32x16 left;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = rows.acc[d][i] * inv, y = rows.acc[d][i + 1] * inv;
+                const uint32_t w = MM::two(x, y);
+                left[i] = x - MM::first(w);
+                left[i + 1] = y - MM::second(w);
+            }
+            store_channels<typename R::Type>(left, d, 1.0f, a, a.rest + at, false, h);
+        }
+    }
+    if (h == 0 && a.lse)
+        a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = lse_of(log2_sum(rows.top, sum, a.c));
+}
+
 // PARTS: wavefronts that share the keys of a tile, of 32 rows each; the others have rows of their own.
 template <typename IO_, int DP_, int PARTS_> struct CausalShape {
     typedef IO_ IO;
@@ -146,65 +216,155 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         walk(std::true_type{});
         barrier();
     }
-    if constexpr (SH::PARTS > 1) { // the first adds the second's, relative to a common maximum
-        static_assert(SH::PARTS == 2, "");
-        f32x4 *const sums = reinterpret_cast<f32x4 *>(smem) + rows_of * ND * 4 * 64 + lane;
-        float *const stats = reinterpret_cast<float *>(smem + SH::kWaves / 2 * ND * 4 * 64 * 16) + rows_of * 2 * 64 + lane;
-        if (part == 1) {
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    f32x4 o;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        o[j] = rows.acc[d][4 * g + j];
-                    sums[(4 * d + g) * 64] = o;
-                }
-            stats[0] = rows.top;
-            stats[64] = rows.sum;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        barrier();
-        if (part == 1)
+    if constexpr (SH::PARTS > 1)
+        if (!join_two(rows, smem, SH::kWaves / 2, rows_of, part, lane, a.c))
             return;
-        const float other = stats[0], top = fmaxf(rows.top, other), low = top > -__builtin_inff() ? top : 0.0f;
-        const float mine = __builtin_amdgcn_exp2f((rows.top - low) * a.c), its = __builtin_amdgcn_exp2f((other - low) * a.c);
-        rows.top = top;
-        rows.sum = rows.sum * mine + stats[64] * its;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 o = sums[(4 * d + g) * 64];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    rows.acc[d][4 * g + j] = rows.acc[d][4 * g + j] * mine + o[j] * its;
-            }
-    }
-    if ((int32_t)row >= all)
+    store_rows(rows, a, s, kvh, row, all, h);
+}
+
+// The same with 256 rows and eight wavefronts, for heads of 128 channels, where the device holds two wavefronts of a SIMD: two groups of four take turns.  While the matrix units
+// compute the products of one (the scores of a tile, and the values of the tile before: 1,160 cycles), the vector unit has the probabilities of the other (1,000).  A barrier ends
+// each turn; the second group is a turn behind, on the same tiles, which are loaded once for both, into the third place behind the two that are read from.
+// Left to themselves the wavefronts of two workgroups come to do the same at the same time: 4,500 cycles for a tile of each, here 3,500, and a clock that falls from
+// 1.95 to 1.88 GHz.
+template <typename IO_, int DP_> struct TurnsShape {
+    typedef IO_ IO;
+    static constexpr int DP = DP_, KT = 64, kRows = 256, kThreads = 512;
+    static constexpr uint32_t kTile = kTileBytes<DP, KT>;
+    static constexpr uint32_t kFlag = 6 * kTile; // behind K and V, three of each
+    static constexpr size_t kLds = kFlag + 32;
+};
+
+template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kernel(const Packed a)
+{
+    constexpr int DP = SH::DP, KT = SH::KT;
+    extern __shared__ __align__(256) char smem[];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool second = wave >= 4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const uint32_t col = (uint32_t)lane & 31u, h = (uint32_t)lane >> 5, group = (uint32_t)a.group;
+
+    const int32_t turn = (int32_t)blockIdx.x / a.kv_heads, kvh = (int32_t)blockIdx.x - turn * a.kv_heads;
+    const Segment s = segment_of<SH::kRows>(a, turn, a.group, true);
+    const int32_t all = s.count * a.group; // rows of the segment
+    const int64_t begin = (int64_t)s.tile * SH::kRows;
+    if (begin >= all)
         return;
-    const float sum = halves_sum(rows.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int64_t at = packed_at(a, s, kvh, row);
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-        store_channels<typename SH::IO>(rows.acc[d], d, inv, a, a.out + at, false, h);
-    if (a.rest) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-            f32x16 left;
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float x = rows.acc[d][i] * inv, y = rows.acc[d][i + 1] * inv;
-                const uint32_t w = Matrix<typename SH::IO>::two(x, y);
-                left[i] = x - Matrix<typename SH::IO>::first(w);
-                left[i + 1] = y - Matrix<typename SH::IO>::second(w);
-            }
-            store_channels<typename SH::IO>(left, d, 1.0f, a, a.rest + at, false, h);
-        }
+    const uint32_t row0 = (uint32_t)begin + (uint32_t)wave * 32u, row = row0 + col;
+    if (s.none) {
+        clear_rows<DP>(a, s, kvh, row0, all, lane);
+        return;
     }
-    if (h == 0 && a.lse)
-        a.lse[(int64_t)kvh * a.rows + packed_row(a, s, row)] = lse_of(log2_sum(rows.top, sum, a.c));
+    // keys: of the workgroup up to its last row's, of the wavefront all below `from`
+    const int32_t end = (int32_t)((uint32_t)begin + SH::kRows - 1 < (uint32_t)all ? (uint32_t)begin + SH::kRows - 1 : (uint32_t)all - 1) / a.group + 1;
+    const int32_t from = (int32_t)(row0 / group) + 1, tiles = (end + KT - 1) / KT;
+    const LastTwiceLoads<DP, KT, 8> k_loads(wave, lane, a.k.token, a.dim), v_loads(wave, lane, a.v.token, a.dim);
+    const uint64_t k_base = a.k.at + (uint64_t)((int64_t)s.first * a.k.token + kvh * a.k.head);
+    const uint64_t v_base = a.v.at + (uint64_t)((int64_t)s.first * a.v.token + kvh * a.v.head);
+    // tile t, to its place
+    auto load_keys = [&](int32_t t, uint32_t at) {
+        if (t < tiles)
+            k_loads.issue(k_base + (uint64_t)t * KT * (uint64_t)a.k.token, a.k.token, a.dim, end - t * KT, lds0 + at);
+    };
+    auto load_values = [&](int32_t t, uint32_t at) {
+        if (t < tiles)
+            v_loads.issue(v_base + (uint64_t)t * KT * (uint64_t)a.v.token, a.v.token, a.dim, end - t * KT, lds0 + at + 3 * SH::kTile);
+    };
+    load_keys(0, 0);
+    Rows<typename SH::IO, DP, KT> rows;
+    const uint32_t query = row / group;
+    rows.load(a.q.at + (uint64_t)((int64_t)s.first * a.q.token + (int64_t)kvh * a.group * a.q.head + row_offset(row, group, a.q.token, a.q.head)),
+              (int32_t)row < all, a.dim, h);
+    arrived(rows.q);
+    auto walk = [&](auto each) {
+        rows.clear();
+        RowOperand<DP> k_from(lane);
+        ColumnOperand<DP> v_from(lane);
+        k_from.move(lds0);
+        v_from.move(lds0 + 3 * SH::kTile);
+        wait_loads<0>();
+        barrier();
+        load_keys(1, SH::kTile);
+        load_values(0, 0);
+        load_keys(2, 2 * SH::kTile);
+        load_values(1, SH::kTile);
+        if (second)
+            barrier();
+        f32x16 x[KT / 32];
+        rows.template scores_ahead<2>(k_from, x);
+        fence_schedule();
+        barrier();
+        uint32_t at = 0; // of tile t
+#pragma unroll 1
+        for (int32_t t = 0;;) { // (without conditions that would copy the sums: a wavefront's last tiles may be cut off as a whole, and the last scores are nobody's)
+            const int32_t key0 = t * KT;
+            uint32_t p[KT / 32][8];
+            const bool crossed = key0 + KT > from;
+            if (crossed)
+                rows.cut(x, (int32_t)query - key0, h);
+            rows.probabilities(x, a.c, p);
+            // (here, and not where they are used first, in the other group's time)
+#pragma unroll
+            for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    asm volatile("" : "+v"(p[kb][j]));
+            asm volatile("" : "+v"(rows.sum));
+            const uint32_t next = at == 2 * SH::kTile ? 0u : at + SH::kTile, last = 3 * SH::kTile - at - next;
+            k_from.move(next - at);
+            wait_loads<0>();
+            fence_schedule();
+            barrier();
+            // scores of tile t + 1, values of tile t; to where the keys of tile t and the values of tile t - 1 were, those of t + 3 and t + 2: a load between eight products, as
+            // one waits for 100 cycles behind the others'
+            const bool spread = end - (t + 3) * KT >= KT && !decltype(each)::value;
+            const uint64_t keys = uniform_u64(k_base + (uint64_t)(t + 3) * KT * (uint64_t)a.k.token), values = uniform_u64(v_base + (uint64_t)(t + 2) * KT * (uint64_t)a.v.token);
+            if (!spread) {
+                load_keys(t + 3, at);
+                load_values(t + 2, last);
+            }
+            bool apart = false;
+            if constexpr (decltype(each)::value)
+                apart = crossed;
+            if (apart) {
+                rows.scores(k_from, x);
+                rows.add_each(p, v_from, (int32_t)query - key0, col, h);
+            } else {
+                rows.scores_and_add(k_from, x, p, v_from, [&](int n) {
+                    if (spread) {
+                        if (n < 2)
+                            k_loads.one(n, keys, lds0 + at);
+                        else
+                            v_loads.one(n - 2, values, lds0 + last + 3 * SH::kTile);
+                    }
+                });
+            }
+            v_from.move(next - at);
+            at = next;
+            fence_schedule();
+            barrier();
+            if (++t == tiles)
+                break;
+        }
+        if (!second)
+            barrier();
+    };
+    walk(std::false_type{});
+    // (by all wavefronts, which load for one another)
+    uint32_t *const flag = reinterpret_cast<uint32_t *>(smem + SH::kFlag);
+    if (lane == 0)
+        flag[wave] = (int32_t)row0 < all && rows.not_finite();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    uint32_t some = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w)
+        some |= flag[w];
+    if (__builtin_expect_with_probability(__builtin_amdgcn_readfirstlane((int)some) != 0, 0, 1.0)) {
+        load_keys(0, 0);
+        walk(std::true_type{});
+    }
+    store_rows(rows, a, s, kvh, row, all, h);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -261,14 +421,21 @@ struct CausalVariant {
     Kernel kernel;
     size_t lds;
     int64_t slots;
+    int threads;
 };
-template <class SH> static CausalVariant shared(const Packed &a) { return CausalVariant{causal_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group)}; }
+template <class SH> static CausalVariant four(const Packed &a) { return CausalVariant{causal_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), 256}; }
+template <class SH> static CausalVariant turns(const Packed &a) { return CausalVariant{causal_turns_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), SH::kThreads}; }
 template <typename IO, int DP> static CausalVariant pick(const Packed &a)
 {
-    return few_rows(a) ? shared<CausalShape<IO, DP, 2>>(a) : shared<CausalShape<IO, DP, 1>>(a);
+    return few_rows(a) ? four<CausalShape<IO, DP, 2>>(a) : four<CausalShape<IO, DP, 1>>(a);
 }
 template <typename IO> static CausalVariant pick(const Packed &a)
 {
+    // (turns: longer walks and fewer of them.  us without and with, query heads / key heads: one of 16,384 tokens, 8/2 537 / 466, of 4,096, 32/32 148 / 139, 32/8 145 / 133, of 3,000, 32/8
+    // 83.2 / 81.8, four of 500 to 2,000, 32/8 59.7 / 56.2; too few workgroups: one of 8,192, 8/8 165 / 175, of 2,048, 32/8 49 / 54; too short: four of 800 to 3,000, 16/16 61 / 69,
+    // eight of 60 to 1,000, 32/8 32 / 35)
+    if (a.dim == 128 && a.sequences > 0 && a.rows / a.sequences >= 4096 && slots_of<256>(a, a.group) * a.kv_heads >= 384)
+        return turns<TurnsShape<IO, 128>>(a);
     return a.dim <= 32 ? pick<IO, 32>(a) : a.dim <= 64 ? pick<IO, 64>(a) : a.dim <= 96 ? pick<IO, 96>(a) : pick<IO, 128>(a);
 }
 
@@ -306,7 +473,7 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
         return GRKAN_ERR_ALIGN;
     const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a) : attention::pick<_Float16>(a);
     const int64_t grid = v.slots * a.kv_heads;
-    if (grid > attention::kMostBlocks)
+    if (grid > attention::kMostBlocks * 256 / v.threads)
         return GRKAN_ERR_UNSUPPORTED;
     a.slots = (int32_t)v.slots;
     a.out = static_cast<char *>(out);
@@ -315,7 +482,7 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3(256), args, v.lds, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3((unsigned)v.threads), args, v.lds, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     return GRKAN_OK;
 }

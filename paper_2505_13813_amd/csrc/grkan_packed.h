@@ -146,6 +146,11 @@ template <int DP, int ROWS, int WAVES> struct LastTwiceLoads {
             if (!(there >> q & 1u))
                 lds_write16(lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP> + 16u * (uint32_t)lane, u32x4{});
     }
+    // load q of a tile that is there as a whole, from `base`, in scalar registers
+    __device__ __forceinline__ void one(int q, uint64_t base, uint32_t lds_at) const
+    {
+        load_to_lds(base, offset[q], lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
+    }
     // base: the tile's first token; rows: tokens that are there, from 1 on
     __device__ __forceinline__ void issue(uint64_t base, int64_t token_stride, int32_t dim, int32_t rows, uint32_t lds_at) const
     {
@@ -153,7 +158,7 @@ template <int DP, int ROWS, int WAVES> struct LastTwiceLoads {
         if (dim == DP && rows >= ROWS) { // (apart, without a branch between them)
 #pragma unroll
             for (int q = 0; q < kMine; ++q)
-                load_to_lds(from, offset[q], lds_at + (first + (uint32_t)(q * WAVES)) * kBlock<DP>);
+                one(q, from, lds_at);
             return;
         }
 #pragma unroll

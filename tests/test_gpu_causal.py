@@ -10,7 +10,9 @@ pytestmark = pytest.mark.gpu
 CASES = [([1], 0, 0, 1, 1, 8), ([16], 0, 0, 3, 3, 64), ([5, 0, 1, 30], 0, 3, 2, 1, 64), ([33, 31, 32], 2, 0, 2, 2, 32), ([129], 0, 1, 6, 2, 128),
          ([64, 65, 63, 1, 0, 0, 127], 0, 40, 3, 1, 96), ([197, 100], 1, 1, 12, 3, 72), ([700], 0, 0, 1, 1, 40), ([300, 2, 513], 5, 0, 8, 8, 64),
          ([1100, 90], 0, 0, 8, 2, 128), ([3] * 70, 0, 2, 4, 2, 64), ([0, 0], 3, 4, 2, 2, 64), ([], 0, 9, 2, 1, 64), ([250, 60], 0, 0, 5, 1, 104),
-         ([17] * 200, 7, 0, 6, 6, 24), ([1500, 640], 0, 0, 16, 8, 80), ([600], 0, 0, 40, 1, 64), ([2000, 900], 0, 100, 10, 10, 64)]
+         ([17] * 200, 7, 0, 6, 6, 24), ([1500, 640], 0, 0, 16, 8, 80), ([600], 0, 0, 40, 1, 64), ([2000, 900], 0, 100, 10, 10, 64),
+         ([300, 65, 1], 1, 0, 200, 100, 128), ([129, 0, 40], 2, 3, 1100, 550, 96), ([400, 200], 0, 1, 128, 64, 104),
+         ([300], 0, 0, 294, 21, 128), ([1100], 2, 0, 80, 20, 128), ([1500, 0, 730], 0, 40, 42, 7, 128), ([64], 0, 0, 512, 8, 128)]
 
 
 def _type(torch, dtype):
@@ -108,7 +110,8 @@ def test_scales(scale):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("shape", [([40], 2, 2, 64), ([300, 80], 4, 1, 128), ([1000, 60], 60, 20, 64), ([700, 300], 64, 16, 72), ([1000], 64, 64, 32),
-                                   ([900], 64, 64, 96)])
+                                   ([900], 64, 64, 96), ([900], 64, 64, 128), ([200, 30], 420, 420, 88), ([1100], 80, 20, 128),
+                                   ([700, 300], 72, 8, 128)])
 def test_later_tokens_have_no_influence(shape, dtype):
     """NaN and infinities in the keys and values of later tokens: the bits of the earlier ones' outputs as with ordinary numbers there, also where they share
     a tile; the tokens behind see them."""
