@@ -279,9 +279,30 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
 #pragma unroll
         for (int rb = 0; rb < ROWS / 32 / SH::PARTS; ++rb) {
             f32x16 p = {}, d = {};
+            // (both at once, in the order that is written, and operands read two steps ahead: each product waits for its own LDS reads otherwise, for four times its own time)
+            {
+                constexpr int kAhead = 2;
+                u32x4 x[kAhead], y[kAhead], z[kAhead];
+                auto read = [&](int st) {
+                    x[st % kAhead] = RowOperand<DP>::read(rows, rb, st);
+                    y[st % kAhead] = RowOperand<DP>::read(rows, rb, st, SH::kRowsTile);
+                    if constexpr (SH::V_LDS)
+                        z[st % kAhead] = RowOperand<DP>::read(v_rows, 0, st);
+                    else
+                        z[st % kAhead] = v[st];
+                };
 #pragma unroll
-            for (int st = 0; st < NS; ++st)
-                p = MM::multiply(RowOperand<DP>::read(rows, rb, st), k[st], p);
+                for (int st = 0; st < kAhead; ++st)
+                    read(st);
+#pragma unroll
+                for (int st = 0; st < NS; ++st) {
+                    p = MM::multiply(x[st % kAhead], k[st], p);
+                    d = MM::multiply(y[st % kAhead], z[st % kAhead], d);
+                    if (st + kAhead < NS)
+                        read(st + kAhead);
+                    fence_schedule();
+                }
+            }
             u32x4 w[2];
 #pragma unroll
             for (int quad = 0; quad < 4; ++quad) {
@@ -302,15 +323,6 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
             for (int i = 0; i < 8; ++i)
                 w[i / 4][i % 4] = MM::two(p[2 * i], p[2 * i + 1]);
 #pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                u32x4 value;
-                if constexpr (SH::V_LDS)
-                    value = RowOperand<DP>::read(v_rows, 0, st);
-                else
-                    value = v[st];
-                d = MM::multiply(RowOperand<DP>::read(rows, rb, st, SH::kRowsTile), value, d);
-            }
-#pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int n = 0; n < ND; ++n)
@@ -330,6 +342,14 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
 #pragma unroll
                 for (int n = 0; n < ND; ++n)
                     dk[n] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, n), w[half], dk[n]);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
+#pragma unroll
+            for (int n = 0; n < 4 * ND - 4; ++n) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, 4, 0);
         }
     }
 
@@ -542,12 +562,25 @@ template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_
         for (int kb = 0; kb < KEYS / 32; ++kb) {
             fence_schedule(); // (the two halves mixed take more registers than there are)
             f32x16 x = {}, d = {};
+            {
+                constexpr int kAhead = 2;
+                u32x4 y[kAhead], z[kAhead];
+                auto read = [&](int st) {
+                    y[st % kAhead] = RowOperand<DP>::read(rows, kb, st);
+                    z[st % kAhead] = RowOperand<DP>::read(rows, kb, st, SH::kKeysTile);
+                };
 #pragma unroll
-            for (int st = 0; st < NS; ++st)
-                x = MM::multiply(RowOperand<DP>::read(rows, kb, st), q[st], x);
+                for (int st = 0; st < kAhead; ++st)
+                    read(st);
 #pragma unroll
-            for (int st = 0; st < NS; ++st)
-                d = MM::multiply(RowOperand<DP>::read(rows, kb, st, SH::kKeysTile), o[st], d);
+                for (int st = 0; st < NS; ++st) {
+                    x = MM::multiply(y[st % kAhead], q[st], x);
+                    d = MM::multiply(z[st % kAhead], o[st], d);
+                    if (st + kAhead < NS)
+                        read(st + kAhead);
+                    fence_schedule();
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse)) * fmaf(d[i], up, -delta);
@@ -567,6 +600,13 @@ template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_
                 for (int n = 0; n < ND; ++n)
                     dq[n] = MM::multiply(ColumnOperand<DP>::read(columns, kb, half, n), w, dq[n]);
             }
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
+#pragma unroll
+            for (int n = 0; n < 2 * ND - 4; ++n) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kProducts, 4, 0);
         }
     }
 
