@@ -161,7 +161,8 @@ grkan_status_t grkan_attention_bwd(const grkan_attention_t *attention, const voi
  *      exp(scale q k^T); an infinity for tokens of no sequence
  * No sequence has any influence on another one, and no later token on an earlier one's output, NaN and infinities included.
  * io, precision, dim and scale as for cross attention.  tokens x heads / kv_heads and sequences below 2^30, heads / kv_heads below 2^20; token strides that are
- * not negative and below 2^24, head strides of q that are not negative and below 2^29 / (heads / kv_heads); kv_heads x (tokens x heads / kv_heads / 32 + sequences + 2) below 2^24: else GRKAN_ERR_UNSUPPORTED.
+ * not negative and below 2^24, head strides of q that are not negative and below 2^29 / (heads / kv_heads);
+ * kv_heads x (tokens x heads / kv_heads / 32 + sequences + 2) below 2^24: else GRKAN_ERR_UNSUPPORTED.
  */
 typedef struct {
     const void *q, *k, *v;
@@ -178,8 +179,8 @@ grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attention_t *attent
                                           void *hip_stream);
 
 /*
- * Its backward pass: P is recomputed from lse.  out and rest as the forward pass left them (rest may be NULL: the gradients are then less exact); dout [tokens, heads, dim] strided as q is; dq as out, dk and dv
- * [tokens, kv_heads, dim], contiguous, 16-byte aligned, overwritten.  What a sequence's tokens hold reaches its own gradients alone (a NaN or an
+ * Its backward pass: P is recomputed from lse.  out and rest as the forward pass left them (rest may be NULL: the gradients are then less exact);
+ * dout [tokens, heads, dim] strided as q is; dq as out, dk and dv [tokens, kv_heads, dim], contiguous, 16-byte aligned, overwritten.  What a sequence's tokens hold reaches its own gradients alone (a NaN or an
  * infinity in one token may reach those of all its sequence).
  * workspace: grkan_causal_attention_bwd_workspace_bytes() bytes of scratch (host-only query; 0 for arguments that are refused), 16-byte aligned, untouched until the
  * enqueued work has finished.
@@ -217,7 +218,7 @@ typedef struct {
  * packed one behind the other as for causal attention (offsets as there; NULL: tokens / sequences of each).  The last of sequence s goes to position
  * lengths[s] - 1, the others in front of it.  Tokens of no sequence are left out, and so are those of a sequence that has more tokens than length, where their
  * positions would be below 0, and all of one whose length is more than its row of the table has place for.
- * Where two tokens have the same place (a page in two sequences' rows), which one it holds afterwards is unspecified.
+ * Where two tokens have the same place (a page in two sequences' rows), which one it holds afterwards is unspecified.  k and v do not overlap the pages.
  * tokens below 2^30, kv_heads x dim below 2^24: else GRKAN_ERR_UNSUPPORTED.
  */
 grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, const void *k, const void *v, const void *offsets, int32_t offsets_64, int64_t tokens,
@@ -229,7 +230,8 @@ grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, const void *k
  * which sees the positions up to its own (the new tokens' keys and values have been written).  Strides as k's above, of sequence, token and head.
  * out [sequences, tokens, heads, dim] of io, contiguous, 16-byte aligned; zeros for a token that sees nothing (below position 0, or no page).  What the
  * pages hold elsewhere has no influence, NaN and infinities included, and neither has a later token on an earlier one.  Precision and scale as for cross attention.
- * tokens x heads / kv_heads below 2^30 and kv_heads x tiles of 32 of them too, sequences x that up to 2^24 - 1: else GRKAN_ERR_UNSUPPORTED.
+ * tokens x heads / kv_heads below 2^30 and kv_heads x tiles of 16 of them too; sequences x kv_heads x tiles of 32 (16 where there is one) below
+ * 2^23: else GRKAN_ERR_UNSUPPORTED.
  * workspace: grkan_paged_attention_workspace_bytes() bytes of scratch (host-only query; 0: none is needed and it may be NULL), 16-byte aligned, untouched until the
  * enqueued work has finished.
  */

@@ -388,6 +388,9 @@ grkan_status_t fill(const grkan_causal_attention_t *at, grkan_dtype_t io, Packed
     const int64_t most = (int64_t)1 << 30;
     if (group >= 1 << 20 || at->tokens >= most || at->tokens * group >= most || at->sequences >= most)
         return GRKAN_ERR_UNSUPPORTED;
+    // every launch below 2^32 threads: tiles are of 64 rows or keys at least
+    if ((at->tokens * group / 32 + at->sequences + 2) * at->kv_heads > kMostBlocks)
+        return GRKAN_ERR_UNSUPPORTED;
     if (!in_offsets(at->q_token_stride, at->q_head_stride, group) || !in_offsets(at->k_token_stride, 0, 1) || !in_offsets(at->v_token_stride, 0, 1))
         return GRKAN_ERR_UNSUPPORTED;
     if (at->tokens > 0 && (!at->q || !at->k || !at->v))
@@ -473,8 +476,6 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
         return GRKAN_ERR_ALIGN;
     const attention::CausalVariant v = io == GRKAN_BF16 ? attention::pick<__bf16>(a) : attention::pick<_Float16>(a);
     const int64_t grid = v.slots * a.kv_heads;
-    if (grid > attention::kMostBlocks * 256 / v.threads)
-        return GRKAN_ERR_UNSUPPORTED;
     a.slots = (int32_t)v.slots;
     a.out = static_cast<char *>(out);
     a.rest = static_cast<char *>(rest);

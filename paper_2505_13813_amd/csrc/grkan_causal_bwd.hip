@@ -744,9 +744,6 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
     attention::Packed &a = p.a;
     const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts, sum_grid = 4 * heads * a.key_tiles;
     const int64_t queries_grid = heads * a.slots;
-    if (rows_grid > attention::kMostBlocks || keys_grid > attention::kMostBlocks || queries_grid > attention::kMostBlocks ||
-        (a.parts > 1 && sum_grid > attention::kMostBlocks))
-        return GRKAN_ERR_UNSUPPORTED;
     a.dout = attention::Operand{address(dout), 0, dout_token_stride * 2, dout_head_stride * 2};
     a.lse = const_cast<float *>(lse);
     a.row_delta = static_cast<float *>(workspace);

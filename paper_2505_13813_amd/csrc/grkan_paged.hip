@@ -726,7 +726,7 @@ extern "C" grkan_status_t grkan_paged_attention(const grkan_paged_cache_t *cache
         return GRKAN_ERR_WORKSPACE;
     const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, work = a.splits > 0 ? (int64_t)a.splits * a.bundle / attention::kWaves : walks;
     const int64_t each = need ? 256 / a.join_lanes : 1, join = need ? walks * ((a.unit_rows * (a.dim / 8) + each - 1) / each) : 0;
-    if (work > attention::kMostBlocks || join > attention::kMostBlocks)
+    if (work > attention::kMostBlocks * 4 / attention::kWaves) // (the second launch's are far fewer)
         return GRKAN_ERR_UNSUPPORTED;
     a.out = static_cast<char *>(out);
     a.partial = static_cast<float *>(workspace);
@@ -790,8 +790,6 @@ extern "C" grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, co
     const int64_t per = (tokens + 1023) / 1024;
     a.per = (int32_t)(per < 64 ? per : 64);
     const int64_t grid = (tokens + a.per - 1) / a.per;
-    if (grid > attention::kMostBlocks)
-        return GRKAN_ERR_UNSUPPORTED;
     attention::paged_write_kernel<<<dim3((unsigned)grid), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a);
     return hipGetLastError() == hipSuccess ? GRKAN_OK : GRKAN_ERR_LAUNCH;
 }

@@ -663,8 +663,8 @@ variable_list causal_backward(const Tensor &q, const Tensor &k, const Tensor &v,
     check_like(out, q, "the saved output", "q");
     check_like(rest, q, "the saved rest", "q");
     check_like(dout_, q, "the gradient of the output", "q");
-    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.is_contiguous() && rest.sizes() == q.sizes() && rest.is_contiguous() && dout_.sizes() == q.sizes() && lse.scalar_type() == at::kFloat &&
-                          lse.device() == q.device() && lse.is_contiguous() && lse.numel() == (int64_t)grkan_causal_attention_lse_count(&d.a),
+    TORCH_CHECK_VALUE(out.sizes() == q.sizes() && out.is_contiguous() && rest.sizes() == q.sizes() && rest.is_contiguous() &&
+                          dout_.sizes() == q.sizes() && lse.scalar_type() == at::kFloat && lse.device() == q.device() && lse.is_contiguous() && lse.numel() == (int64_t)grkan_causal_attention_lse_count(&d.a),
                       "what the forward pass saved must match q");
     const Tensor dout = in_rows(dout_, d.group);
     const Tensor ws = at::empty({(int64_t)grkan_causal_attention_bwd_workspace_bytes(&d.a)}, q.options().dtype(at::kByte));
@@ -775,8 +775,6 @@ std::optional<bool> paged_write(const Tensor &k, const Tensor &v, const Tensor &
     check_gpu(k_pages, "k_pages");
     const c10::DeviceGuard guard(k_pages.device());
     const Cache d(k_pages, v_pages, table, lengths);
-    at::assert_no_internal_overlap(k_pages);
-    at::assert_no_internal_overlap(v_pages);
     check_like(k, k_pages, "k", "k_pages");
     check_like(v, k_pages, "v", "k_pages");
     const int64_t n = k.dim();
@@ -788,6 +786,13 @@ std::optional<bool> paged_write(const Tensor &k, const Tensor &v, const Tensor &
         offsets = check_offsets(offsets, k_pages, "the pages");
         TORCH_CHECK_VALUE(offsets.size(0) == table.size(0) + 1, "offsets must be [sequences + 1], sequences being the rows of the table");
     }
+    at::assert_no_internal_overlap(k_pages);
+    at::assert_no_internal_overlap(v_pages);
+    if (!k_pages.is_same(v_pages) || !k.is_same(v)) // (one pool whose keys are the values too)
+        at::assert_no_overlap(k_pages, v_pages);
+    for (const Tensor *from : {&k, &v})
+        for (const Tensor *to : {&k_pages, &v_pages})
+            at::assert_no_overlap(*to, *from);
     const Tensor kr = in_rows(k, 1), vr = in_rows(v, 1);
     check(grkan_paged_write(&d.c, kr.data_ptr(), vr.data_ptr(), data_of(offsets), offsets.defined() && offsets.scalar_type() == at::kLong, kr.size(0),
                             kr.size(0) > 1 ? kr.stride(0) : 0, kr.size(1) > 1 ? kr.stride(1) : 0, vr.size(0) > 1 ? vr.stride(0) : 0,

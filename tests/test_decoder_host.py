@@ -96,9 +96,12 @@ def test_causal_workspaces(lib):
 
 
 def test_more_workgroups_than_a_launch_takes(lib):
-    a = _causal(tokens=1 << 24, heads=64, kv_heads=64, sequences=1 << 24)
-    assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, None, BF16, None) == UNSUPPORTED
-    assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 60, BF16, None) == UNSUPPORTED
+    for fields in (dict(tokens=1 << 24, heads=64, kv_heads=64, sequences=1 << 24), dict(tokens=1000, heads=1 << 20, kv_heads=1 << 20),
+                   dict(tokens=(1 << 30) - 1, heads=2147483647, kv_heads=2147483647), dict(tokens=1 << 29, heads=4, kv_heads=2)):
+        a = _causal(**fields)
+        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), 16, None, None, BF16, None) == UNSUPPORTED
+        assert lib.grkan_causal_attention_bwd(ctypes.byref(a), 16, 16, 16, 16, 256, 64, 16, 16, 16, 16, 1 << 60, BF16, None) == UNSUPPORTED
+        assert lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a)) == 0
 
 
 def _cache(**fields):
@@ -152,8 +155,8 @@ def test_other_refusals_of_pages(lib):
     need = lib.grkan_paged_attention_workspace_bytes(ctypes.byref(long), ctypes.byref(q))
     assert need > 0 and attend(long, size=need - 1) == WORKSPACE and attend(long, ws=None, size=need) == WORKSPACE and attend(long, ws=24, size=need) == WORKSPACE
     assert attend(_cache(sequences=0), out=None) == OK and attend(queries=_queries(tokens=0, q=None), out=None) == OK
-    many = _cache(sequences=1 << 24)
-    assert attend(many) == UNSUPPORTED
+    for many in (1 << 24, 1 << 23):  # 512 threads each
+        assert attend(_cache(sequences=many)) == UNSUPPORTED
 
     def write(cache=c, k=16, v=16, offsets=16, wide=0, tokens=5, strides=(128, 64, 128, 64)):
         return lib.grkan_paged_write(ctypes.byref(cache) if cache else None, k, v, offsets, wide, tokens, *strides, BF16, None)

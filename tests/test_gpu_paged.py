@@ -312,6 +312,14 @@ def test_refusals():
         with pytest.raises(ValueError):
             paged_attention(q, pool, pool, table, lengths, scale)
     offsets = torch.tensor([0, 1, 2, 3], device="cuda:0")
+    pools = t(2, 4, 16, 2, 64)
+    part = pools.view(2, 64, 2, 64)[0, 5:8].unsqueeze(1)
+    for bad in ((k, k + 1, pool, pool), (part, k, *pools), (k, part, *pools), (k, k, *(pools.view(128, 2, 64)[i:i + 64].view(4, 16, 2, 64) for i in (0, 32))),
+                (k, k, pools[0][:1].expand(4, 16, 2, 64), pools[1])):
+        with pytest.raises(RuntimeError, match="memory location|overlap"):
+            paged_write(*bad, table, lengths)
+    both = t(4, 2, 16, 2, 64).unbind(1)  # keys and values of a page side by side
+    paged_write(k, k, *both, table, lengths)
     for bad in ((k[0], k[0], pool, pool, table, lengths), (k[:, 0], k[:, 0], pool, pool, table, lengths, offsets[:3]), (k, k, pool, pool, table, lengths, offsets),
                 (k[:2], k[:2], pool, pool, table, lengths), (t(3, 1, 1, 64), t(3, 1, 1, 64), pool, pool, table, lengths), (k, t(3, 2, 2, 64), pool, pool, table, lengths),
                 (k, k, odd, odd, table, lengths), (k, k, off, off, table, lengths), (k.cpu(), k, pool, pool, table, lengths)):
@@ -321,7 +329,7 @@ def test_refusals():
         paged_write(k.half(), k.half(), pool, pool, table, lengths)
     with pytest.raises(RuntimeError):
         paged_write(k, k, pool[:1].expand(4, 16, 2, 64), pool, table, lengths)
-    for call in (lambda x: paged_attention(x, pool, pool, table, lengths), lambda x: paged_write(x[:, :, :2], k, pool, pool, table, lengths)):
+    for call in (lambda x: paged_attention(x, pool, pool, table, lengths), lambda x: paged_write(x[:, :, :2], k, *pools, table, lengths)):
         with pytest.raises(RuntimeError, match="no gradient"):
             call(q.clone().requires_grad_())
         with torch.no_grad():
@@ -329,7 +337,7 @@ def test_refusals():
     assert paged_attention(q[:0], pool, pool, table[:0], lengths[:0]).shape == (0, 1, 4, 64)
     assert (paged_attention(q, pool[:0], pool[:0], table, lengths + 5) == 0).all()
     assert (paged_attention(q, pool, pool, table[:, :0], lengths + 5) == 0).all()
-    paged_write(k[:, :0], k[:, :0], pool, pool, table, lengths)
+    paged_write(k[:, :0], k[:, :0], *pools, table, lengths)
 
 
 def test_on_another_stream_and_in_graphs():
