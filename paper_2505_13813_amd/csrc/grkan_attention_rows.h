@@ -157,7 +157,8 @@ template <typename IO, int DP, int KT> struct Rows {
             }
     }
 
-    // scores of a tile and add of another, in the order that is written: operands are read four products ahead, and between(n), n from 0 to 3, goes between the products.
+    // scores of a tile and add of another, in the order that is written: operands are read four products ahead, and between(n), n from 0 to
+    // 3, goes between the products.
     template <class Between>
     __device__ __forceinline__ void scores_and_add(const Addresses<NS> &k_from, f32x16 (&s)[KB], const uint32_t (&p)[KB][8], const Addresses<ND> &v_from, Between &&between)
     {
@@ -281,10 +282,9 @@ template <typename IO_, int DP_> struct TokenShape {
     static_assert(((DP + 4) * 32 * kWaves + 64 * kWaves) * sizeof(float) <= kLds, ""); // what the wavefronts join
 };
 
-// A wavefront's way through tiles t0, t0 + kWaves, .. (t0 its own first), below t1, without a barrier: the loads of the next are in flight while one is computed
-// with.  word_of(t): which keys of a tile are valid (asked in rising order); load(t, word, whole, to): K of the tile to `to`, V behind it.  Returns whether there
-// was a valid key.
-// (Each part of the loop is in the code once, the first tile's loads too.)
+// A wavefront's way through tiles t0, t0 + kWaves, .. (t0 its own first), below t1, without a barrier: the loads of the next are in flight
+// while one is computed with.  word_of(t): which keys of a tile are valid (asked in rising order); load(t, word, whole, to): K of the tile
+// to `to`, V behind it.  Returns whether there was a valid key. (Each part of the loop is in the code once, the first tile's loads too.)
 template <class SH, class Word, class Load>
 __device__ __forceinline__ bool walk_alone(Rows<typename SH::IO, SH::DP, SH::KT> &rows, int32_t t0, int32_t t1, uint32_t lds0, int wave, int lane, float c,
                                            int32_t dim, Word &&word_of, Load &&load)
@@ -322,7 +322,8 @@ __device__ __forceinline__ bool walk_alone(Rows<typename SH::IO, SH::DP, SH::KT>
     return some != 0;
 }
 
-// The wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order.  out, lse: the lane's row's; wide: as parts to be joined are kept.
+// The wavefronts' parts of each row: sums relative to a common maximum, added in wavefront order.  out, lse: the lane's row's; wide: as
+// parts to be joined are kept.
 template <class SH>
 __device__ __forceinline__ void join_wavefronts(const Rows<typename SH::IO, SH::DP, SH::KT> &rows, char *smem, int wave, int lane, bool there, const Args &a, char *out,
                                                 float *lse, bool wide)
@@ -394,10 +395,10 @@ __device__ __forceinline__ void join_wavefronts(const Rows<typename SH::IO, SH::
     barrier(); // (the next part's tiles come where the joined rows were)
 }
 
-// A row's parts p of `parts`, each the mean over its own keys, by the share of the sum that each has: eight channels of it, rounded to `out`, and the row's lse.
-// values(p), stats(p): a part's channels and log2 of its sum.  `lanes` adjacent lanes, of which this is number `lane`, have every lanes-th part each and then add
-// up; the first writes.  Eight parts' loads are out at once: it is their latency that all this takes (23 parts of twelve key heads with 64 channels and two rows:
-// 10.2 us with a lane for all parts, 6.0 with sixteen).
+// A row's parts p of `parts`, each the mean over its own keys, by the share of the sum that each has: eight channels of it, rounded to
+// `out`, and the row's lse. values(p), stats(p): a part's channels and log2 of its sum.  `lanes` adjacent lanes, of which this is number
+// `lane`, have every lanes-th part each and then add up; the first writes.  Eight parts' loads are out at once: it is their latency that
+// all this takes (23 parts of twelve key heads with 64 channels and two rows: 10.2 us with a lane for all parts, 6.0 with sixteen).
 template <typename IO, typename Values, typename Stats>
 __device__ __forceinline__ float join_parts(int32_t parts, int32_t lane, int32_t lanes, Values &&values, Stats &&stats, char *out)
 {

@@ -1,15 +1,22 @@
-// Causal attention over packed sequences on gfx950 (MI355X), forward: row r of a sequence (a token's query of one head) sees the sequence's keys up to its
-// own token's,
+// Causal attention over packed sequences on gfx950 (MI355X), forward: row r of a sequence (a token's query of one head) sees the sequence's
+// keys up to its own token's,
 //
 //     out_r = sum_{j <= r} exp(scale q_r k_j - m_r) v_j / sum_{j <= r} exp(scale q_r k_j - m_r)
 //
-// in one pass with the running maximum and sum, as cross attention does it (grkan_attention.hip), from the same parts: the queries of the heads that
-// share a key head are one list of rows, and the probabilities go from the products of the scores to those of the values in registers.
-// Products and masks stop at the diagonal: a workgroup ends at its last row's key, a wavefront leaves out tiles behind its own, and only the tiles that the
-// diagonal crosses take comparisons.  The longest walks are launched first.
+// in one pass with the running maximum and sum, as cross attention does it (grkan_attention.hip), from the same parts: the queries of the
+// heads that share a key head are one list of rows, and the probabilities go from the products of the scores to those of the values in
+// registers. Products and masks stop at the diagonal: a workgroup ends at its last row's key, a wavefront leaves out tiles behind its own,
+// and only the tiles that the diagonal crosses take comparisons.  The longest walks are launched first.
 //
-// A later token has no influence on an earlier one, NaN and infinities included: in the tiles on the diagonal its weight is zero, but zero times NaN is
-// NaN.  Rows whose sums are not finite at the end are gone through a second time with those tiles row by row (Rows::add_each).
+// What bounds it: the products and the exponentials of long sequences, which overlap little, and the card's clock, which falls under them
+// (4,096 tokens, 32 heads of 128 on eight, float16: 139 us, 0.99 PFLOP/s, where a product of 8,192 has 1.37); of short ones the longest
+// walk, a tile after the other, behind 5 us of launch, search and first loads (24 sequences of 60 to 1,000 tokens, twelve heads of 64: 21
+// us, and 19 where both products are left out).
+//
+// A later token has no influence on an earlier one, NaN and infinities included: in the tiles on the diagonal its weight is zero, but zero
+// times NaN is NaN.  Rows whose sums are not finite at the end are gone through a second time with those tiles row by row (Rows::add_each).
+//
+// The output is rounded once.  For the backward pass what that took away is kept, rounded too (`rest`).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -38,8 +45,8 @@ template <int DP> __device__ __forceinline__ void clear_rows(const Packed &a, co
 
 // ------------------------------------------------------------------------------------------------ 32 rows a wavefront, tiles of 64 keys for all
 
-// Two wavefronts' sums of the same rows (`pairs` of them, this is number `own`): the second leaves its own in LDS (and is done: false), the first adds them, relative to a
-// common maximum.
+// Two wavefronts' sums of the same rows (`pairs` of them, this is number `own`): the second leaves its own in LDS (and is done: false), the
+// first adds them, relative to a common maximum.
 template <class R> __device__ __forceinline__ bool join_two(R &rows, char *smem, int pairs, int own, int second, int lane, float c)
 {
     constexpr int ND = R::ND;
@@ -211,7 +218,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
         flag[wave] = works && rows.not_finite();
     wait_loads<0>();
     barrier();
-    if (__builtin_expect_with_probability(__builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3])) != 0, 0, 1.0)) { // (its loops are not what registers go to)
+    const int some = __builtin_amdgcn_readfirstlane((int)(flag[0] | flag[1] | flag[2] | flag[3]));
+    if (__builtin_expect_with_probability(some != 0, 0, 1.0)) { // (its loops are not what registers go to)
         issue(0, 0);
         walk(std::true_type{});
         barrier();
@@ -222,11 +230,12 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
     store_rows(rows, a, s, kvh, row, all, h);
 }
 
-// The same with 256 rows and eight wavefronts, for heads of 128 channels, where the device holds two wavefronts of a SIMD: two groups of four take turns.  While the matrix units
-// compute the products of one (the scores of a tile, and the values of the tile before: 1,160 cycles), the vector unit has the probabilities of the other (1,000).  A barrier ends
-// each turn; the second group is a turn behind, on the same tiles, which are loaded once for both, into the third place behind the two that are read from.
-// Left to themselves the wavefronts of two workgroups come to do the same at the same time: 4,500 cycles for a tile of each, here 3,500, and a clock that falls from
-// 1.95 to 1.88 GHz.
+// The same with 256 rows and eight wavefronts, for heads of 128 channels, where the device holds two wavefronts of a SIMD: two groups of
+// four take turns.  While the matrix units compute the products of one (the scores of a tile, and the values of the tile before: 1,160
+// cycles), the vector unit has the probabilities of the other (1,000).  A barrier ends each turn; the second group is a turn behind, on the
+// same tiles, which are loaded once for both, into the third place behind the two that are read from. Left to themselves the wavefronts of
+// two workgroups come to do the same at the same time: 4,500 cycles for a tile of each, here 3,500, and a clock that falls from 1.95 to
+// 1.88 GHz.
 template <typename IO_, int DP_> struct TurnsShape {
     typedef IO_ IO;
     static constexpr int DP = DP_, KT = 64, kRows = 256, kThreads = 512;
@@ -295,8 +304,9 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
         fence_schedule();
         barrier();
         uint32_t at = 0; // of tile t
+        // (without conditions that would copy the sums: a wavefront's last tiles may be cut off as a whole, and the last scores are nobody's)
 #pragma unroll 1
-        for (int32_t t = 0;;) { // (without conditions that would copy the sums: a wavefront's last tiles may be cut off as a whole, and the last scores are nobody's)
+        for (int32_t t = 0;;) {
             const int32_t key0 = t * KT;
             uint32_t p[KT / 32][8];
             const bool crossed = key0 + KT > from;
@@ -315,10 +325,11 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
             wait_loads<0>();
             fence_schedule();
             barrier();
-            // scores of tile t + 1, values of tile t; to where the keys of tile t and the values of tile t - 1 were, those of t + 3 and t + 2: a load between eight products, as
-            // one waits for 100 cycles behind the others'
+            // scores of tile t + 1, values of tile t; to where the keys of tile t and the values of tile t - 1 were, those of t + 3 and t +
+            // 2: a load between eight products, as one waits for 100 cycles behind the others'
             const bool spread = end - (t + 3) * KT >= KT && !decltype(each)::value;
-            const uint64_t keys = uniform_u64(k_base + (uint64_t)(t + 3) * KT * (uint64_t)a.k.token), values = uniform_u64(v_base + (uint64_t)(t + 2) * KT * (uint64_t)a.v.token);
+            const uint64_t keys = uniform_u64(k_base + (uint64_t)(t + 3) * KT * (uint64_t)a.k.token);
+            const uint64_t values = uniform_u64(v_base + (uint64_t)(t + 2) * KT * (uint64_t)a.v.token);
             if (!spread) {
                 load_keys(t + 3, at);
                 load_values(t + 2, last);
@@ -426,26 +437,33 @@ struct CausalVariant {
     int64_t slots;
     int threads;
 };
-template <class SH> static CausalVariant four(const Packed &a) { return CausalVariant{causal_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), 256}; }
-template <class SH> static CausalVariant turns(const Packed &a) { return CausalVariant{causal_turns_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), SH::kThreads}; }
+template <class SH> static CausalVariant four(const Packed &a)
+{
+    return CausalVariant{causal_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), 256};
+}
+template <class SH> static CausalVariant turns(const Packed &a)
+{
+    return CausalVariant{causal_turns_kernel<SH>, SH::kLds, slots_of<SH::kRows>(a, a.group), SH::kThreads};
+}
 template <typename IO, int DP> static CausalVariant pick(const Packed &a)
 {
     return few_rows(a) ? four<CausalShape<IO, DP, 2>>(a) : four<CausalShape<IO, DP, 1>>(a);
 }
 template <typename IO> static CausalVariant pick(const Packed &a)
 {
-    // (turns: longer walks and fewer of them.  us without and with, query heads / key heads: one of 16,384 tokens, 8/2 537 / 466, of 4,096, 32/32 148 / 139, 32/8 145 / 133, of 3,000, 32/8
-    // 83.2 / 81.8, four of 500 to 2,000, 32/8 59.7 / 56.2; too few workgroups: one of 8,192, 8/8 165 / 175, of 2,048, 32/8 49 / 54; too short: four of 800 to 3,000, 16/16 61 / 69,
-    // eight of 60 to 1,000, 32/8 32 / 35)
+    // (turns: longer walks and fewer of them.  us without and with, query heads / key heads: one of 16,384 tokens, 8/2 537 / 466, of 4,096,
+    // 32/32 148 / 139, 32/8 145 / 133, of 3,000, 32/8 83.2 / 81.8, four of 500 to 2,000, 32/8 59.7 / 56.2; too few workgroups: one of
+    // 8,192, 8/8 165 / 175, of 2,048, 32/8 49 / 54; too short: four of 800 to 3,000, 16/16 61 / 69, eight of 60 to 1,000, 32/8 32 / 35)
     if (a.dim == 128 && a.sequences > 0 && a.rows / a.sequences >= 4096 && slots_of<256>(a, a.group) * a.kv_heads >= 384)
         return turns<TurnsShape<IO, 128>>(a);
     return a.dim <= 32 ? pick<IO, 32>(a) : a.dim <= 64 ? pick<IO, 64>(a) : a.dim <= 96 ? pick<IO, 96>(a) : pick<IO, 128>(a);
 }
 
-// Two wavefronts on the tiles of 64 keys of the same rows where tiles of 128 rows do not fill the device (four workgroups of a compute unit, with 128 channels two): the
-// longest walk is then what counts, and it is half as long.  us with 128 rows to a workgroup and with 64: twelve heads of 64 channels, 24 sequences of 60 to 1,000 tokens
-// 25.5 / 21.7, eight of 120 to 2,000 39.4 / 30.0, one of 4,096 74 / 55, 40 of 60 to 1,000 36.6 / 39.3, 60 of 12 to 200 13.4 / 14.7, 16 of 240 to 4,000 130 / 161; 32 heads of 128 on
-// eight, one of 1,000 33.1 / 28.6, of 2,000 62.6 / 64.4, eight of 60 to 1,000 38.2 / 50.7; 16 of 96 on four, eight of 120 to 2,000 56.8 / 44.8.
+// Two wavefronts on the tiles of 64 keys of the same rows where tiles of 128 rows do not fill the device (four workgroups of a compute
+// unit, with 128 channels two): the longest walk is then what counts, and it is half as long.  us with 128 rows to a workgroup and with 64:
+// twelve heads of 64 channels, 24 sequences of 60 to 1,000 tokens 25.5 / 21.7, eight of 120 to 2,000 39.4 / 30.0, one of 4,096 74 / 55, 40
+// of 60 to 1,000 36.6 / 39.3, 60 of 12 to 200 13.4 / 14.7, 16 of 240 to 4,000 130 / 161; 32 heads of 128 on eight, one of 1,000 33.1 /
+// 28.6, of 2,000 62.6 / 64.4, eight of 60 to 1,000 38.2 / 50.7; 16 of 96 on four, eight of 120 to 2,000 56.8 / 44.8.
 bool few_rows(const Packed &a)
 {
     return slots_of<128>(a, a.group) * a.kv_heads <= (a.dim <= 64 ? 1024 : a.dim <= 96 ? 2048 : 448);
@@ -483,7 +501,8 @@ extern "C" grkan_status_t grkan_causal_attention_fwd(const grkan_causal_attentio
     if (!attention::allow_lds(reinterpret_cast<const void *>(v.kernel), v.lds))
         return GRKAN_ERR_LAUNCH;
     void *args[] = {&a};
-    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3((unsigned)v.threads), args, v.lds, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    if (hipLaunchKernel(reinterpret_cast<const void *>(v.kernel), dim3((unsigned)grid), dim3((unsigned)v.threads), args, v.lds,
+                        static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return GRKAN_ERR_LAUNCH;
     return GRKAN_OK;
 }

@@ -1,13 +1,18 @@
-// Causal attention over packed sequences on gfx950 (MI355X), backward.  With P recomputed from the rows' lse, D = dO V^T and delta = the row's sum of dO O, of what out was
-// before it was rounded (out and the rest: an error of delta goes into all of a row's S', and with out alone it is a third of the gradients' own rounding in a sequence of 60 tokens),
+// Causal attention over packed sequences on gfx950 (MI355X), backward.  With P recomputed from the rows' lse, D = dO V^T and delta = the
+// row's sum of dO O, of what out was before it was rounded (out and the rest: an error of delta goes into all of a row's S', and with out
+// alone it is a third of the gradients' own rounding in a sequence of 60 tokens),
 //
 //     dV_j = sum_{i >= j} P_ij dO_i      S'_ij = P_ij (D_ij - delta_i)      dQ_i = scale sum_{j <= i} S'_ij K_j      dK_j = scale sum_{i >= j} S'_ij Q_i
 //
-// in two kernels as cross attention has them (grkan_attention_bwd.hip): one owns keys and walks the rows that see them, one owns rows and walks the keys that
-// they see; no atomics, the same bits each time.  Tiles that the diagonal crosses take comparisons, the others none, and what lies behind it is left out.
+// in two kernels as cross attention has them (grkan_attention_bwd.hip): one owns keys and walks the rows that see them, one owns rows and
+// walks the keys that they see; no atomics, the same bits each time.  Tiles that the diagonal crosses take comparisons, the others none,
+// and what lies behind it is left out.
 //
-// A key sees the more rows the earlier it is, so the walks of a long sequence's first keys are cut into slabs of rows, each a workgroup's, whose sums a second launch
-// adds up; the queries' kernel starts its longest walks first.
+// A key sees the more rows the earlier it is, so the walks of a long sequence's first keys are cut into slabs of rows, each a workgroup's,
+// whose sums a second launch adds up; the queries' kernel starts its longest walks first.
+//
+// What bounds it: products and vector operations, as of the forward pass (4,001 and 2,852 tokens, 16 heads of 128 on four: queries 165 us,
+// keys 236, 0.90 and 0.84 PFLOP/s; sixteen sequences of 90 to 1,500 tokens, twelve heads of 64: 35 and 43 us, and 11 for the slabs' sums).
 //
 // float16: scaled as there; the largest upstream gradient is that of the key's own sequence, from the key's tile on.
 #include <hip/hip_runtime.h>
@@ -79,7 +84,8 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
     }
 }
 
-// PARTS: wavefronts that share the rows of a stage, for the same 32 keys, or the keys of a tile, for the same 32 rows; the others have keys or rows of their own.
+// PARTS: wavefronts that share the rows of a stage, for the same 32 keys, or the keys of a tile, for the same 32 rows; the others have keys
+// or rows of their own.
 template <typename IO, int DP, int ROWS, bool V_LDS, int PER, int PARTS_> struct CausalBackShape : BackShape<IO, DP, ROWS, V_LDS, PER> {
     using Base = BackShape<IO, DP, ROWS, V_LDS, PER>;
     static constexpr int PARTS = PARTS_, kOwn = 32 * Base::kWaves / PARTS;
@@ -88,7 +94,8 @@ template <typename IO, int DP, int ROWS, bool V_LDS, int PER, int PARTS_> struct
     static_assert(PARTS == 1 || (ROWS == 64 && (size_t)2 * 2 * (DP / 8) * 64 * 16 <= kKeyLds), ""); // what the wavefronts join
 };
 
-// The rows that tile `tile` of a segment's keys is seen by: tiles [first, tiles) of `size` rows, in `parts` slabs of `per`, the first of what remains.
+// The rows that tile `tile` of a segment's keys is seen by: tiles [first, tiles) of `size` rows, in `parts` slabs of `per`, the first of
+// what remains.
 struct Walk {
     int32_t first, tiles, parts, per;
     __device__ __forceinline__ int32_t begin(int32_t part) const { return part == 0 ? first : tiles - (parts - part) * per; }
@@ -279,7 +286,8 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
 #pragma unroll
         for (int rb = 0; rb < ROWS / 32 / SH::PARTS; ++rb) {
             f32x16 p = {}, d = {};
-            // (both at once, in the order that is written, and operands read two steps ahead: each product waits for its own LDS reads otherwise, for four times its own time)
+            // (both at once, in the order that is written, and operands read two steps ahead: each product waits for its own LDS reads
+            // otherwise, for four times its own time)
             {
                 constexpr int kAhead = 2;
                 u32x4 x[kAhead], y[kAhead], z[kAhead];
@@ -393,10 +401,11 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
         }
 }
 
-// The sum of the slabs' parts of a tile of keys, in their order: block (half of the keys, dK or dV, slot, key head), four times four elements a lane and pass.
-template <typename IO, int OWN> __global__ __launch_bounds__(256) void causal_sum_kernel(const Packed a, int32_t size)
+// The sum of the slabs' parts of a tile of keys, in their order: block (slot, key head), or four of them, one for each half of the keys and each of
+// dK and dV; four times four elements a lane and pass.
+template <typename IO, int OWN> __global__ __launch_bounds__(256) void causal_sum_kernel(const Packed a, int32_t size, int32_t blocks)
 {
-    const int32_t half = (int32_t)blockIdx.x & 1, which = (int32_t)blockIdx.x >> 1 & 1, item = (int32_t)blockIdx.x >> 2;
+    const int32_t item = (int32_t)blockIdx.x / blocks;
     const int32_t slot = item / a.kv_heads, kvh = item - slot * a.kv_heads;
     const Segment s = segment_of<OWN>(a, slot, 1, false);
     const int64_t begin = (int64_t)s.tile * OWN;
@@ -405,30 +414,34 @@ template <typename IO, int OWN> __global__ __launch_bounds__(256) void causal_su
     const Walk walk(a, s, OWN, size);
     if (walk.parts == 1) // written as it should be
         return;
-    const int32_t quads = a.dim / 4, key0 = (int32_t)begin + half * (OWN / 2), left = s.count - key0, keys = left < OWN / 2 ? left : OWN / 2;
     const int64_t lines = (int64_t)a.tokens * a.kv_heads;
-    for (int32_t i0 = (int32_t)threadIdx.x; i0 < keys * quads; i0 += 4 * 256) {
-        f32x4 v[4] = {};
-        int64_t place[4]; // of the four elements, in [tokens, kv_heads, dim]
+    const int32_t quads = a.dim / 4;
+    for (int32_t quarter = (int32_t)blockIdx.x - item * blocks; quarter < 4; quarter += blocks) {
+        const int32_t half = quarter & 1, which = quarter >> 1;
+        const int32_t key0 = (int32_t)begin + half * (OWN / 2), left = s.count - key0, keys = left < OWN / 2 ? left : OWN / 2;
+        for (int32_t i0 = (int32_t)threadIdx.x; i0 < keys * quads; i0 += 4 * 256) {
+            f32x4 v[4] = {};
+            int64_t place[4]; // of the four elements, in [tokens, kv_heads, dim]
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const int32_t i = i0 + 256 * n < keys * quads ? i0 + 256 * n : i0, row = i / quads;
-            place[n] = (((int64_t)s.first + key0 + row) * a.kv_heads + kvh) * a.dim + 4 * (i - row * quads);
-        }
-        for (int32_t p = 0; p < walk.parts; ++p) {
-            const float *const from = a.partial + (2 * p + which) * lines * a.dim;
+            for (int n = 0; n < 4; ++n) {
+                const int32_t i = i0 + 256 * n < keys * quads ? i0 + 256 * n : i0, row = i / quads;
+                place[n] = (((int64_t)s.first + key0 + row) * a.kv_heads + kvh) * a.dim + 4 * (i - row * quads);
+            }
+            for (int32_t p = 0; p < walk.parts; ++p) {
+                const float *const from = a.partial + (2 * p + which) * lines * a.dim;
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                v[n] += *reinterpret_cast<const f32x4 *>(from + place[n]);
-        }
+                for (int n = 0; n < 4; ++n)
+                    v[n] += *reinterpret_cast<const f32x4 *>(from + place[n]);
+            }
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            if (i0 + 256 * n >= keys * quads)
-                break;
-            u32x2 o;
-            o[0] = Matrix<IO>::two(v[n][0], v[n][1]);
-            o[1] = Matrix<IO>::two(v[n][2], v[n][3]);
-            *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + place[n] * 2) = o;
+            for (int n = 0; n < 4; ++n) {
+                if (i0 + 256 * n >= keys * quads)
+                    break;
+                u32x2 o;
+                o[0] = Matrix<IO>::two(v[n][0], v[n][1]);
+                o[1] = Matrix<IO>::two(v[n][2], v[n][3]);
+                *reinterpret_cast<u32x2 *>((which ? a.dv : a.dk) + place[n] * 2) = o;
+            }
         }
     }
 }
@@ -636,7 +649,7 @@ template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_
 typedef void (*Kernel)(Packed);
 struct CausalBack {
     Kernel rows, keys, queries;
-    void (*sum)(Packed, int32_t);
+    void (*sum)(Packed, int32_t, int32_t);
     int size, own; // of the keys' kernel: rows of a stage, keys of a workgroup
     int at_once;   // workgroups of it that the device holds
     size_t keys_lds, queries_lds;
@@ -652,8 +665,8 @@ template <class KEYS, int PARTS> static CausalBack variant(const Packed &a)
 }
 template <typename IO> static CausalBack pick(const Packed &a)
 {
-    // (as for rows.  us of the keys' kernel without and with: twelve heads of 64, sixteen sequences of 90 to 1,500 tokens 59 / 49, 24 of 60 to 1,000 54 / 42, one of 4,096 88 / 77, of
-    // 577 25 / 16; 40 of 60 to 1,000 102 / 106, sixteen of 240 to 4,000 262 / 293)
+    // (as for rows.  us of the keys' kernel without and with: twelve heads of 64, sixteen sequences of 90 to 1,500 tokens 59 / 49, 24 of 60
+    // to 1,000 54 / 42, one of 4,096 88 / 77, of 577 25 / 16; 40 of 60 to 1,000 102 / 106, sixteen of 240 to 4,000 262 / 293)
     const bool rows = few_rows(a), keys = slots_of<128>(a, 1) * a.kv_heads <= 1024;
     auto with = [&](auto one, auto two) {
         using ONE = decltype(one);
@@ -685,11 +698,12 @@ static CausalPlan plan(const Packed &given, grkan_dtype_t io)
     a.value_tiles = (int32_t)slots_of<kGroup>(a, 1);
     a.key_tiles = (int32_t)p.v.keys_slots;
     a.slots = (int32_t)p.v.queries_slots;
-    // Slabs, of 1.4 times what each workgroup has to do on the average, if the sequences were all of one length, which the host does not know: so many that the device holds them
-    // all at once.  Where a sequence is longer its parts are the more, and then the longer (Walk).  There is a workgroup for each part that there may be, and most are not there:
-    // not so many that these take time themselves, 1.5 us each, nor more than a GB of sums.  us of the keys' kernel + the sum, with slabs of 1.4, 1.0 and 0.5 of the average:
-    // 4,001 and 2,852 tokens, 16 heads of 128 on four 261 + 13, 304 + 16, 289 + 22; one of 4,096, twelve of 64 80 + 10, 87 + 12, 83 + 14.  1,024 and 512 rows at least: one of 1,000,
-    // 32 heads of 128 on eight 67 + 8, 46 + 11; of 577, twelve of 64 15.8 + 0, 14.9 + 3.9.
+    // Slabs, of 1.4 times what each workgroup has to do on the average, if the sequences were all of one length, which the host does not
+    // know: so many that the device holds them all at once.  Where a sequence is longer its parts are the more, and then the longer (Walk).
+    // There is a workgroup for each part that there may be, and most are not there: not so many that these take time themselves, 1.5 us
+    // each, nor more than a GB of sums.  us of the keys' kernel + the sum, with slabs of 1.4, 1.0 and 0.5 of the average: 4,001 and 2,852
+    // tokens, 16 heads of 128 on four 261 + 13, 304 + 16, 289 + 22; one of 4,096, twelve of 64 80 + 10, 87 + 12, 83 + 14.  1,024 and 512
+    // rows at least: one of 1,000, 32 heads of 128 on eight 67 + 8, 46 + 11; of 577, twelve of 64 15.8 + 0, 14.9 + 3.9.
     const int64_t each = a.sequences > 0 ? ((int64_t)a.tokens + a.sequences - 1) / a.sequences : 0;
     const int64_t walk = (each * a.group + p.v.size - 1) / p.v.size, longest = (a.rows + p.v.size - 1) / p.v.size; // tiles of rows: of a first key, at most
     const int64_t share = (int64_t)a.kv_heads * ((a.tokens + p.v.own - 1) / p.v.own) * walk / 2 / p.v.at_once;
@@ -742,7 +756,7 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
     if (!workspace || workspace_bytes < need || address(workspace) % 16 != 0)
         return GRKAN_ERR_WORKSPACE;
     attention::Packed &a = p.a;
-    const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts, sum_grid = 4 * heads * a.key_tiles;
+    const int64_t heads = a.kv_heads, rows_grid = heads * a.row_tiles, keys_grid = heads * a.key_tiles * a.parts;
     const int64_t queries_grid = heads * a.slots;
     a.dout = attention::Operand{address(dout), 0, dout_token_stride * 2, dout_head_stride * 2};
     a.lse = const_cast<float *>(lse);
@@ -768,9 +782,12 @@ extern "C" grkan_status_t grkan_causal_attention_bwd(const grkan_causal_attentio
             return false;
         if (a.parts == 1)
             return true;
-        int32_t size = p.v.size;
-        void *args[] = {&a, &size};
-        return hipLaunchKernel(reinterpret_cast<const void *>(p.v.sum), dim3((unsigned)sum_grid), dim3(256), args, 0, stream) == hipSuccess;
+        // four to a tile where the device holds them all (eight on a compute unit; sixteen sequences of 90 to 1,500 tokens, twelve heads of
+        // 64: 11.5 us with four, 8.2 with one)
+        const int64_t tiles = heads * a.key_tiles;
+        int32_t size = p.v.size, blocks = 4 * tiles <= 2048 ? 4 : 1;
+        void *args[] = {&a, &size, &blocks};
+        return hipLaunchKernel(reinterpret_cast<const void *>(p.v.sum), dim3((unsigned)(tiles * blocks)), dim3(256), args, 0, stream) == hipSuccess;
     };
     // each needs what the other leaves: the lengths of the values, or the rows' statistics
     if (io == GRKAN_F16)

@@ -1,16 +1,17 @@
 // A cache of keys and values in pages, on gfx950 (MI355X): new tokens' keys and values into it, and attention of the newest tokens over it.
 //
-// Position p of sequence s lies in row p mod page_size of page table[s][p / page_size].  Of the `queries` newest tokens of a sequence of `length`, token i sees
-// the positions up to length - queries + i: out_i = sum_p softmax_p(scale q_i k_p) v_p.
+// Position p of sequence s lies in row p mod page_size of page table[s][p / page_size].  Of the `queries` newest tokens of a sequence of
+// `length`, token i sees the positions up to length - queries + i: out_i = sum_p softmax_p(scale q_i k_p) v_p.
 //
-// The keys and values are read once, and that bounds it, as there are few rows for each: 32 sequences of 1 to 8,191 positions, 32 heads of 128 on 8, 592 MB, in 111 us =
-// 5.4 TB/s, where reading alone gets 6.0.  A wavefront has tiles of 32 keys and their values by itself, without a barrier.  While it computes it loads little, and
-// so the others must: eight wavefronts on a compute unit with 128 channels, a buffer each, do better than four with two (142 us; with everything in the cache, where only
-// the way through a tile counts, 126, and 56 so: the products have sixteen rows in place of 32, two wavefronts fill one another's waits).  The wavefronts side by side
-// have the heads that lie side by side in memory (116 us with whole heads one behind the other).  Short walks are joined in their workgroup; long ones are dealt
-// out evenly to all wavefronts, whatever the lengths are, and a second launch joins the parts.
-// Where the pages are whole tiles a tile has one address; elsewhere every lane has its key's (pages of 16: 115 us).  The table's entries come to LDS in front of the
-// walk, so that no load waits for another one within it.
+// The keys and values are read once, and that bounds it, as there are few rows for each: 32 sequences of 1 to 8,191 positions, 32 heads of
+// 128 on 8, 592 MB, in 111 us = 5.4 TB/s, where reading alone gets 6.0.  A wavefront has tiles of 32 keys and their values by itself,
+// without a barrier.  While it computes it loads little, and so the others must: eight wavefronts on a compute unit with 128 channels, a
+// buffer each, do better than four with two (142 us; with everything in the cache, where only the way through a tile counts, 126, and 56
+// so: the products have sixteen rows in place of 32, two wavefronts fill one another's waits).  The wavefronts side by side have the heads
+// that lie side by side in memory (116 us with whole heads one behind the other).  Short walks are joined in their workgroup; long ones are
+// dealt out evenly to all wavefronts, whatever the lengths are, and a second launch joins the parts. Where the pages are whole tiles a tile
+// has one address; elsewhere every lane has its key's (pages of 16: 115 us).  The table's entries come to LDS in front of the walk, so that
+// no load waits for another one within it.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -55,7 +56,8 @@ template <typename IO_, int DP_, int BLOCKS_> struct PagedShape {
     static constexpr int kPerUnit = BLOCKS == 1 && 2 * kLds <= 160 * 1024 ? 2 : 1; // workgroups of a compute unit
 };
 
-// A row's way over the pages: which keys of a tile there are, and its loads.  table: of positions from `first` x page on, in LDS, -1 where there is no page.
+// A row's way over the pages: which keys of a tile there are, and its loads.  table: of positions from `first` x page on, in LDS, -1 where
+// there is no page.
 template <class SH> struct Pages {
     static constexpr int KT = kTileKeys, DP = SH::DP;
     using Loads = TileLoads<DP, KT, 1>;
@@ -110,8 +112,8 @@ template <class SH> struct Pages {
 
 __device__ __forceinline__ int32_t page_or_none(const Paged &a, int32_t page) { return page >= 0 && page < a.pages ? page : -1; }
 
-// Sixteen rows for each block, in 16 x 16 x 32 instructions: S^T = K Q^T leaves a lane, of row l mod 16 and with g = l / 16, keys 4 g .. and 16 + 4 g .. of a tile
-// of 32, which in this order are the second operand of V^T P^T; V^T comes by transposing reads, two for each.
+// Sixteen rows for each block, in 16 x 16 x 32 instructions: S^T = K Q^T leaves a lane, of row l mod 16 and with g = l / 16, keys 4 g ..
+// and 16 + 4 g .. of a tile of 32, which in this order are the second operand of V^T P^T; V^T comes by transposing reads, two for each.
 template <class SH> struct PagedRows {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
@@ -266,8 +268,9 @@ template <class SH> struct PagedRows {
         return __ballot(x != x) != 0;
     }
 
-    // A wavefront's way through tiles t0, t0 + STEP, .. below t1 without a barrier.  Keys and values have a buffer each, and each is loaded anew as soon as it has been read:
-    // the next keys are on their way while this tile's probabilities are made, and the other wavefronts' loads while it computes.  Returns whether there was a key.
+    // A wavefront's way through tiles t0, t0 + STEP, .. below t1 without a barrier.  Keys and values have a buffer each, and each is loaded
+    // anew as soon as it has been read: the next keys are on their way while this tile's probabilities are made, and the other wavefronts'
+    // loads while it computes.  Returns whether there was a key.
     template <int STEP> __device__ __forceinline__ bool walk(Pages<SH> &pages, int32_t t0, int32_t t1, uint32_t keys_at, int lane, float c, bool each)
     {
         constexpr int kLoads = TileLoads<DP, kTileKeys, 1>::kMine;
@@ -403,9 +406,10 @@ template <class SH> __global__ __launch_bounds__(64 * kWaves, 2 * SH::kPerUnit) 
     }
 }
 
-// The walks dealt out evenly to the wavefronts, in groups of 32 keys.  Each goes its way by itself, without a barrier, from walk to walk, and leaves
-// what it found of each for the second launch: while one begins or ends a walk, the others' loads keep the memory busy.  `bundle` wavefronts side by side have the
-// same keys of as many heads, which lie side by side in memory, and count as one worker (a.splits of those).
+// The walks dealt out evenly to the wavefronts, in groups of 32 keys.  Each goes its way by itself, without a barrier, from walk to walk,
+// and leaves what it found of each for the second launch: while one begins or ends a walk, the others' loads keep the memory busy.
+// `bundle` wavefronts side by side have the same keys of as many heads, which lie side by side in memory, and count as one worker (a.splits
+// of those).
 typedef DealOf<Paged, kTileKeys> WaveDeal;
 template <class SH> __global__ __launch_bounds__(64 * kWaves, 2 * SH::kPerUnit) void paged_waves_kernel(const Paged a)
 {
@@ -655,9 +659,10 @@ static grkan_status_t fill(const grkan_paged_cache_t *c, const grkan_paged_queri
     a.tile_rows = rows <= 16 ? 16 : 32;
     a.row_tiles = (int32_t)((rows + a.tile_rows - 1) / a.tile_rows);
     a.unit_rows = rows < a.tile_rows ? (int32_t)rows : a.tile_rows;
-    // As many wavefronts as the device holds, or one for each tile of 32 keys; none where a workgroup for each walk does as well: 1,024 of them, or all short (the second
-    // launch takes 4 us, and eight wavefronts on 1,000 keys no more than that in excess.  us without and with, one walk to each of twelve heads of 64 channels: 500 keys
-    // 8.5 / 8.2 + 4.4, 1,000 12.2 / 8.3 + 4.7; 32 walks of 128 channels, 1,000 keys 18.0 / 10.5 + 5.0; 192 of 64, 1,000 keys 12.4 / 11.9 + 4.6).
+    // As many wavefronts as the device holds, or one for each tile of 32 keys; none where a workgroup for each walk does as well: 1,024 of
+    // them, or all short (the second launch takes 4 us, and eight wavefronts on 1,000 keys no more than that in excess.  us without and
+    // with, one walk to each of twelve heads of 64 channels: 500 keys 8.5 / 8.2 + 4.4, 1,000 12.2 / 8.3 + 4.7; 32 walks of 128 channels,
+    // 1,000 keys 18.0 / 10.5 + 5.0; 192 of 64, 1,000 keys 12.4 / 11.9 + 4.6).
     const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, groups = (a.keys + 31) / 32;
     a.bundle = 1;
     a.splits = 0;
