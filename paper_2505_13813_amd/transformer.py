@@ -295,8 +295,8 @@ class PagedCache:
         self.lengths.copy_(torch.tensor(self.counts, dtype=torch.int32))
 
     def grow(self, counts: Sequence[int]) -> None:
-        """Makes room for counts[s] new positions of each sequence and adds them to the lengths, before the step that writes them.  Refused as
-        a whole where the pages do not suffice."""
+        """Makes room for counts[s] new positions of each sequence and adds them to the lengths, before the step that writes them, on the
+        stream that it runs on.  Refused as a whole where the pages do not suffice."""
         counts = [int(n) for n in counts]
         if len(counts) != len(self.counts) or min(counts) < 0:
             raise ValueError("counts must be a number of new positions, not negative, for each of the cache's sequences")

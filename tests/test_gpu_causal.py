@@ -396,7 +396,7 @@ def test_the_same_bits_every_time():
 
     from paper_2505_13813_amd.transformer import causal_attention
 
-    for case in (([1000, 500, 77], 0, 0, 12, 3, 128), ([900, 1000], 0, 0, 12, 12, 64)):
+    for case in (([1000, 500, 77], 0, 0, 12, 3, 128), ([900, 1000], 0, 0, 12, 12, 64), ([1100], 0, 0, 80, 20, 128)):
         q, k, v, dout, offsets = _operands(torch, case, "f16", 30)
         given, first = torch.tensor(offsets, device="cuda:0"), None
         for _ in range(4):
