@@ -86,8 +86,9 @@ template <typename IO> __global__ __launch_bounds__(256) void causal_rows_kernel
 
 // PARTS: wavefronts that share the rows of a stage, for the same 32 keys, or the keys of a tile, for the same 32 rows; the others have keys
 // or rows of their own.
-template <typename IO, int DP, int ROWS, bool V_LDS, int PER, int PARTS_> struct CausalBackShape : BackShape<IO, DP, ROWS, V_LDS, PER> {
+template <typename IO, int DP, int ROWS, bool V_LDS, int PER, int PARTS_, bool FINE_> struct CausalBackShape : BackShape<IO, DP, ROWS, V_LDS, PER> {
     using Base = BackShape<IO, DP, ROWS, V_LDS, PER>;
+    static constexpr bool FINE = FINE_;
     static constexpr int PARTS = PARTS_, kOwn = 32 * Base::kWaves / PARTS;
     static constexpr uint32_t kValues = V_LDS ? kOwn / 64 * Base::kKeysTile : 0; // in front of the stages
     static constexpr size_t kKeyLds = 2 * (size_t)Base::kKeyStage + kValues;
@@ -143,6 +144,11 @@ template <int N, typename Sums> __device__ __forceinline__ bool add_second(char 
         }
     return true;
 }
+
+// What rounding x and y to w took away.  FINE: S' goes into the products in two parts of 16 bits.  Rounded once, its error is as large as
+// that of the gradients' own rounding: dQ and dK are off by 1.41 to 1.47 times that, in sequences of some dozen tokens by up to 1.51; with
+// two parts by 1.02 to 1.09.
+template <class MM> __device__ __forceinline__ uint32_t rest_of(uint32_t w, float x, float y) { return MM::two(x - MM::first(w), y - MM::second(w)); }
 
 // dK and dV of 32 keys a wavefront, from all the rows that see them or a slab of those.  Whole slabs are launched first, what remains of a
 // walk last.
@@ -311,7 +317,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
                     fence_schedule();
                 }
             }
-            u32x4 w[2];
+            u32x4 w[2], left[2];
 #pragma unroll
             for (int quad = 0; quad < 4; ++quad) {
                 const f32x4 lse = __builtin_bit_cast(f32x4, lds_read16(stats + (32u * rb + 8u * quad) * 4u));
@@ -344,20 +350,33 @@ template <class SH> __global__ __launch_bounds__(256, SH::PER) void causal_keys_
                     y[j] = p[4 * quad + j] * fmaf(d[4 * quad + j], up, -delta[j] * up);
                 w[quad / 2][2 * (quad % 2)] = MM::two(y[0], y[1]);
                 w[quad / 2][2 * (quad % 2) + 1] = MM::two(y[2], y[3]);
+                if constexpr (SH::FINE) {
+                    left[quad / 2][2 * (quad % 2)] = rest_of<MM>(w[quad / 2][2 * (quad % 2)], y[0], y[1]);
+                    left[quad / 2][2 * (quad % 2) + 1] = rest_of<MM>(w[quad / 2][2 * (quad % 2) + 1], y[2], y[3]);
+                }
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int n = 0; n < ND; ++n)
-                    dk[n] = MM::multiply(ColumnOperand<DP>::read(columns, rb, half, n), w[half], dk[n]);
+                for (int n = 0; n < ND; ++n) {
+                    const u32x4 column = ColumnOperand<DP>::read(columns, rb, half, n);
+                    dk[n] = MM::multiply(column, w[half], dk[n]);
+                    if constexpr (SH::FINE)
+                        dk[n] = MM::multiply(column, left[half], dk[n]);
+                }
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
 #pragma unroll
-            for (int n = 0; n < 4 * ND - 4; ++n) {
+            for (int n = 0; n < 2 * ND; ++n) {
                 __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
             }
+#pragma unroll
+            for (int n = 4; n < 2 * ND; ++n) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, SH::FINE ? 2 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
+            }
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
-            __builtin_amdgcn_sched_group_barrier(kProducts, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, SH::FINE ? 8 : 4, 0);
         }
     }
 
@@ -447,7 +466,7 @@ template <typename IO, int OWN> __global__ __launch_bounds__(256) void causal_su
 }
 
 // dQ of 32 rows a wavefront.
-template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_queries_kernel(const Packed a)
+template <class SH, int PARTS, bool FINE> __global__ __launch_bounds__(256, 2) void causal_queries_kernel(const Packed a)
 {
     using IO = typename SH::IO;
     using MM = Matrix<IO>;
@@ -605,21 +624,28 @@ template <class SH, int PARTS> __global__ __launch_bounds__(256, 2) void causal_
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                u32x4 w;
+                u32x4 w, left;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j) {
                     w[j] = MM::two(x[8 * half + 2 * j], x[8 * half + 2 * j + 1]);
+                    if constexpr (FINE)
+                        left[j] = rest_of<MM>(w[j], x[8 * half + 2 * j], x[8 * half + 2 * j + 1]);
+                }
 #pragma unroll
-                for (int n = 0; n < ND; ++n)
-                    dq[n] = MM::multiply(ColumnOperand<DP>::read(columns, kb, half, n), w, dq[n]);
+                for (int n = 0; n < ND; ++n) {
+                    const u32x4 column = ColumnOperand<DP>::read(columns, kb, half, n);
+                    dq[n] = MM::multiply(column, w, dq[n]);
+                    if constexpr (FINE)
+                        dq[n] = MM::multiply(column, left, dq[n]);
+                }
             }
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
 #pragma unroll
             for (int n = 0; n < 2 * ND - 4; ++n) {
-                __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kProducts, FINE ? 2 : 1, 0);
                 __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
             }
-            __builtin_amdgcn_sched_group_barrier(kProducts, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, FINE ? 8 : 4, 0);
         }
     }
 
@@ -659,11 +685,11 @@ template <class KEYS, int PARTS> static CausalBack variant(const Packed &a)
 {
     using IO = typename KEYS::IO;
     using QUERIES = BackShape<IO, KEYS::DP, 64, false, 2>;
-    CausalBack v = {causal_rows_kernel<IO>, causal_keys_kernel<KEYS>, causal_queries_kernel<QUERIES, PARTS>, causal_sum_kernel<IO, KEYS::kOwn>, KEYS::ROWS, KEYS::kOwn,
+    CausalBack v = {causal_rows_kernel<IO>, causal_keys_kernel<KEYS>, causal_queries_kernel<QUERIES, PARTS, KEYS::FINE>, causal_sum_kernel<IO, KEYS::kOwn>, KEYS::ROWS, KEYS::kOwn,
                     256 * KEYS::PER, KEYS::kKeyLds, QUERIES::kRowLds, slots_of<KEYS::kOwn>(a, 1), slots_of<128 / PARTS>(a, a.group)};
     return v;
 }
-template <typename IO> static CausalBack pick(const Packed &a)
+template <typename IO, bool FINE> static CausalBack pick(const Packed &a)
 {
     // (as for rows.  us of the keys' kernel without and with: twelve heads of 64, sixteen sequences of 90 to 1,500 tokens 59 / 49, 24 of 60
     // to 1,000 54 / 42, one of 4,096 88 / 77, of 577 25 / 16; 40 of 60 to 1,000 102 / 106, sixteen of 240 to 4,000 262 / 293)
@@ -674,12 +700,20 @@ template <typename IO> static CausalBack pick(const Packed &a)
         return keys ? rows ? variant<TWO, 2>(a) : variant<TWO, 1>(a) : rows ? variant<ONE, 2>(a) : variant<ONE, 1>(a);
     };
     if (a.dim <= 32)
-        return with(CausalBackShape<IO, 32, 64, false, 2, 1>{}, CausalBackShape<IO, 32, 64, false, 2, 2>{});
+        return with(CausalBackShape<IO, 32, 64, false, 2, 1, FINE>{}, CausalBackShape<IO, 32, 64, false, 2, 2, FINE>{});
     if (a.dim <= 64)
-        return with(CausalBackShape<IO, 64, 32, true, 3, 1>{}, CausalBackShape<IO, 64, 64, true, 3, 2>{});
+        return with(CausalBackShape<IO, 64, 32, true, 3, 1, FINE>{}, CausalBackShape<IO, 64, 64, true, 3, 2, FINE>{});
     if (a.dim <= 96)
-        return with(CausalBackShape<IO, 96, 64, false, 2, 1>{}, CausalBackShape<IO, 96, 64, false, 2, 1>{});
-    return with(CausalBackShape<IO, 128, 32, true, 2, 1>{}, CausalBackShape<IO, 128, 32, true, 2, 1>{});
+        return with(CausalBackShape<IO, 96, 64, false, 2, 1, FINE>{}, CausalBackShape<IO, 96, 64, false, 2, 1, FINE>{});
+    return with(CausalBackShape<IO, 128, 32, true, 2, 1, FINE>{}, CausalBackShape<IO, 128, 32, true, 2, 1, FINE>{});
+}
+
+// S' in two parts where sequences are short: longer ones average more, and pay more.  us of forward and backward with one part and with
+// two: 32 sequences of up to 100 tokens, 32 heads of 128 on eight 68.3 / 70.4, ten of up to 100, twelve of 64 66 / 66, sixteen of 90 to
+// 1,500 110.5 / 116, one of 1,000, 32 of 128 on eight 104.5 / 112, 4,001 and 2,852, 16 on four 517 / 591.
+template <typename IO> static CausalBack pick(const Packed &a)
+{
+    return (int64_t)a.tokens < 128 * (int64_t)a.sequences ? pick<IO, true>(a) : pick<IO, false>(a);
 }
 
 struct CausalPlan {

@@ -405,3 +405,27 @@ def test_the_same_bits_every_time():
             got = (out.detach(), *torch.autograd.grad(out, leaves, dout))
             first = first or got
             assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", [([40, 3, 1, 17], 0, 0, 3, 3, 64), ([17], 0, 0, 8, 2, 96), ([38, 100, 12], 0, 2, 6, 3, 128), ([50] * 30, 0, 0, 16, 16, 64),
+                                  ([50] * 30, 0, 0, 12, 12, 32), ([120] * 8, 0, 0, 64, 64, 128)])
+def test_gradients_of_short_sequences_are_rounded_once(case, dtype):
+    """dQ and dK as relative norms: their own rounding alone takes every element by at most u = eps / 2 of itself.  What else there is, the second
+    parts' roundings (u squared) and float32 sums, is below a twentieth of that."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import causal_attention
+
+    print(case, dtype, flush=True)
+    q, k, v, dout, offsets = _operands(torch, case, dtype, 7, poison=False)
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    got = torch.autograd.grad(causal_attention(*leaves, torch.tensor(offsets, device="cuda:0")), leaves, dout)
+    off, whole = [0.0, 0.0], [0.0, 0.0]
+    for at, wanted in _sequences(torch, q, k, v, offsets, case[-1] ** -0.5, dtype, dout):
+        for i in range(2):
+            exact = wanted[1 + i][0]
+            off[i] += float((got[i][at].double() - exact).square().sum())
+            whole[i] += float(exact.square().sum())
+    u = torch.finfo(q.dtype).eps / 2
+    assert all(math.sqrt(a / b) <= 1.05 * u for a, b in zip(off, whole)), [math.sqrt(a / b) / u for a, b in zip(off, whole)]
