@@ -53,17 +53,25 @@ template <int SIZE> __device__ __forceinline__ int32_t place_of(int32_t token, i
     return (int32_t)((uint32_t)token * (uint32_t)unit / (uint32_t)SIZE) + i;
 }
 
-// The wavefront's sum of numbers that are not negative.
+// The wavefront's numbers, none of them negative, put together.
+template <class Op> __device__ __forceinline__ int32_t of_lanes(int32_t v, Op &&op)
+{
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true));
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true));
+    const auto rows = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = op((int32_t)rows[0], (int32_t)rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    return __builtin_amdgcn_readfirstlane(op((int32_t)halves[0], (int32_t)halves[1]));
+}
 __device__ __forceinline__ int32_t sum_of_lanes(int32_t v)
 {
-    v += __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);
-    const auto rows = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
-    v = (int32_t)(rows[0] + rows[1]);
-    const auto halves = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-    return __builtin_amdgcn_readfirstlane((int32_t)(halves[0] + halves[1]));
+    return of_lanes(v, [](int32_t x, int32_t y) { return x + y; });
+}
+__device__ __forceinline__ int32_t largest_of_lanes(int32_t v)
+{
+    return of_lanes(v, [](int32_t x, int32_t y) { return x > y ? x : y; });
 }
 
 // The tile of workgroup `slot`: of 64 segments the tiles in falling order of their number, `forward`, or of how many follow, where the
@@ -87,7 +95,7 @@ template <int SIZE> __device__ __forceinline__ Segment segment_of(const Packed &
     auto from = [&](int32_t n) { return sum_of_lanes(tiles > n ? tiles - n : 0); };
     const bool there = rank >= 0 && from(0) > rank;
     if (there) {
-        int32_t above = __builtin_amdgcn_readfirstlane((int32_t)((int64_t)a.tokens * unit / SIZE)) + 1;
+        int32_t above = largest_of_lanes(tiles); // none has more
         while (above - number > 1) {
             const int32_t n = number + (above - number) / 2;
             if (from(n) > rank)
