@@ -280,19 +280,15 @@ class PagedCache:
         self.table = torch.full((sequences, -(-longest // page_size)), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.counts = [0] * sequences
-        self._pages = [[] for _ in range(sequences)]
+        self._held = torch.full(self.table.shape, -1, dtype=torch.int32)  # the table on the host
         self._free = list(range(pages - 1, -1, -1))
 
     @property
     def free_pages(self) -> int:
         return len(self._free)
 
-    def _written(self):
-        table = torch.full(self.table.shape, -1, dtype=torch.int32)
-        for row, held in zip(table, self._pages):
-            row[:len(held)] = torch.tensor(held, dtype=torch.int32)
-        self.table.copy_(table)
-        self.lengths.copy_(torch.tensor(self.counts, dtype=torch.int32))
+    def _pages(self, count: int) -> int:
+        return -(-count // self.page_size)
 
     def grow(self, counts: Sequence[int]) -> None:
         """Makes room for counts[s] new positions of each sequence and adds them to the lengths, before the step that writes them, on the
@@ -303,20 +299,29 @@ class PagedCache:
         after = [a + b for a, b in zip(self.counts, counts)]
         if max(after) > self.longest:
             raise ValueError("a sequence would have %d positions, and %d is the most" % (max(after), self.longest))
-        wanted = [-(-n // self.page_size) - len(held) for n, held in zip(after, self._pages)]
+        wanted = [self._pages(b) - self._pages(a) for a, b in zip(self.counts, after)]
         if sum(wanted) > len(self._free):
             raise RuntimeError("%d more pages are needed, and %d are free" % (sum(wanted), len(self._free)))
-        for held, n in zip(self._pages, wanted):
-            held += [self._free.pop() for _ in range(n)]
+        for i, n in enumerate(wanted):
+            if n:
+                first = self._pages(self.counts[i])
+                self._held[i, first:first + n] = torch.tensor([self._free.pop() for _ in range(n)], dtype=torch.int32)
         self.counts = after
-        self._written()
+        if any(wanted):
+            self.table.copy_(self._held)
+        if min(counts) == max(counts):
+            self.lengths.add_(counts[0])  # (nothing from the host, which would wait for the device)
+        else:
+            self.lengths.copy_(torch.tensor(after, dtype=torch.int32))
 
     def release(self, sequence: int) -> None:
         """Takes a sequence's pages back: its row, of length 0, is free for another one."""
-        self._free += reversed(self._pages[sequence])
-        self._pages[sequence] = []
+        row = self._held[sequence]
+        self._free += row[:self._pages(self.counts[sequence])].tolist()[::-1]
+        row.fill_(-1)
         self.counts[sequence] = 0
-        self._written()
+        self.table[sequence].fill_(-1)
+        self.lengths[sequence].zero_()
 
 
 class KATDecoderBlock(nn.Module):

@@ -429,3 +429,41 @@ def test_gradients_of_short_sequences_are_rounded_once(case, dtype):
             whole[i] += float(exact.square().sum())
     u = torch.finfo(q.dtype).eps / 2
     assert all(math.sqrt(a / b) <= 1.05 * u for a, b in zip(off, whole)), [math.sqrt(a / b) / u for a, b in zip(off, whole)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", [([200, 77], 0, 3, 6, 2, 64), ([30, 5], 0, 0, 4, 4, 128), ([300], 0, 0, 294, 21, 128)])
+def test_from_c_with_and_without_the_rest(case, dtype):
+    """Without what the output's rounding left the gradients are within the formulas' bounds too, and the outputs, which do not need it, have the same bits."""
+    import ctypes
+
+    import torch
+
+    from paper_2505_13813_amd import binding
+
+    print(case, dtype, flush=True)
+    lib = binding.load_library()
+    q, k, v, dout, offsets = _operands(torch, case, dtype, 8)
+    heads, kv, dim = case[3:]
+    given = torch.tensor(offsets, device="cuda:0", dtype=torch.int32)
+    a = binding.CausalAttention(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), offsets=given.data_ptr(), tokens=q.shape[0], sequences=len(case[0]), heads=heads,
+                                kv_heads=kv, dim=dim, q_token_stride=q.stride(0), q_head_stride=q.stride(1), k_token_stride=k.stride(0), k_head_stride=k.stride(1),
+                                v_token_stride=v.stride(0), v_head_stride=v.stride(1), scale=dim ** -0.5)
+    io, stream = {"bf16": 1, "f16": 2}[dtype], torch.cuda.current_stream().cuda_stream
+    need = lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a))
+    results = []
+    for with_rest in (True, False):
+        out, rest, dq = (torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda:0") for _ in range(3))
+        dk, dv = (torch.full(k.shape, 7.0, dtype=q.dtype, device="cuda:0") for _ in range(2))
+        lse = torch.full((lib.grkan_causal_attention_lse_count(ctypes.byref(a)),), 7.0, device="cuda:0")
+        work = torch.full((need,), 255, dtype=torch.uint8, device="cuda:0")
+        left = rest.data_ptr() if with_rest else None
+        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), out.data_ptr(), left, lse.data_ptr(), io, stream) == 0
+        assert lib.grkan_causal_attention_bwd(ctypes.byref(a), out.data_ptr(), left, lse.data_ptr(), dout.data_ptr(), dout.stride(0), dout.stride(1), dq.data_ptr(),
+                                              dk.data_ptr(), dv.data_ptr(), work.data_ptr(), need, io, stream) == 0
+        torch.cuda.synchronize()
+        for at, wanted in _sequences(torch, q, k, v, offsets, dim ** -0.5, dtype, dout):
+            assert_within([t[at] for t in (out, dq, dk, dv)], wanted, (case, at, with_rest))
+        assert with_rest or bool((rest == 7.0).all())
+        results.append((out, lse, dv))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
