@@ -89,22 +89,35 @@ template <class SH> struct Pages {
     // keys or values (o, loads, head) of the tile that word() was asked for last
     __device__ __forceinline__ void load(const Operand &o, const Loads &loads, uint64_t head, uint64_t word, uint32_t to) const
     {
+        // (every load written out: 1,000 positions, pages of 64, twelve heads of 64 channels 8.6 us in the place of 9.9 with a loop)
         if (even()) {
-            loads.issue(head + (page < 0 ? 0 : (uint64_t)page) * (uint64_t)o.batch + (uint64_t)place * (uint64_t)o.token, o.token, word, word == 0xffffffffu && a.dim == DP,
-                        to);
+            uint64_t base = head + (page < 0 ? 0 : (uint64_t)page) * (uint64_t)o.batch + (uint64_t)place * (uint64_t)o.token;
+            if (word != 0xffffffffu || a.dim != DP) {
+                loads.issue(base, o.token, word, false, to);
+                return;
+            }
+            base = uniform_u64(base);
+#pragma unroll
+            for (int n = 0; n < Loads::kMine; ++n)
+                load_to_lds(base + (uint64_t)(n / Loads::kEach) * Loads::kTokens * (uint64_t)o.token, loads.offset[n % Loads::kEach], to + (uint32_t)n * kBlock<DP>);
             return;
         }
-#pragma unroll 1
-        for (int turn = 0; turn < Loads::kTurns; ++turn)
+        // (all exchanges in front: they wait for one another otherwise.  The same on pages of 16 10.0 us in the place of 11.9, and 700 positions, 32
+        // heads of 128 on eight, four sequences, 12.1 in the place of 14.7)
+        int32_t pages[Loads::kMine], places[Loads::kMine];
 #pragma unroll
-            for (int q = 0; q < Loads::kEach; ++q) {
-                const uint32_t e = (uint32_t)q * 64u + (uint32_t)lane, r0 = e / Loads::kChunks, piece = (e % Loads::kChunks) ^ swizzle<DP>(r0);
-                const int32_t r = (int32_t)(r0 + Loads::kTokens * (uint32_t)turn);
-                const int64_t p = __shfl(page, r), i = __shfl(place, r);
-                const bool there = p >= 0 && (word >> r & 1u) && piece * 8u < (uint32_t)a.dim;
-                load_to_lds_at(there ? head + (uint64_t)(p * o.batch + i * o.token) + piece * 16u : reinterpret_cast<uint64_t>(kZeros),
-                               to + (uint32_t)(turn * Loads::kEach + q) * kBlock<DP>);
-            }
+        for (int n = 0; n < Loads::kMine; ++n) {
+            const int r = ((n % Loads::kEach) * 64 + lane) / Loads::kChunks + Loads::kTokens * (n / Loads::kEach);
+            pages[n] = __shfl(page, r);
+            places[n] = __shfl(place, r);
+        }
+#pragma unroll
+        for (int n = 0; n < Loads::kMine; ++n) {
+            const uint32_t e = (uint32_t)(n % Loads::kEach) * 64u + (uint32_t)lane, piece = (e % Loads::kChunks) ^ swizzle<DP>(e / Loads::kChunks);
+            const bool there = pages[n] >= 0 && piece * 8u < (uint32_t)a.dim; // (none behind the last key)
+            load_to_lds_at(there ? head + (uint64_t)((int64_t)pages[n] * o.batch + (int64_t)places[n] * o.token) + piece * 16u : reinterpret_cast<uint64_t>(kZeros),
+                           to + (uint32_t)n * kBlock<DP>);
+        }
     }
     __device__ __forceinline__ void load_keys(uint64_t word, uint32_t to) const { load(a.k, k_loads, k_head, word, to); }
     __device__ __forceinline__ void load_values(uint64_t word, uint32_t to) const { load(a.v, v_loads, v_head, word, to); }
@@ -660,13 +673,15 @@ static grkan_status_t fill(const grkan_paged_cache_t *c, const grkan_paged_queri
     a.row_tiles = (int32_t)((rows + a.tile_rows - 1) / a.tile_rows);
     a.unit_rows = rows < a.tile_rows ? (int32_t)rows : a.tile_rows;
     // As many wavefronts as the device holds, or one for each tile of 32 keys; none where a workgroup for each walk does as well: 1,024 of
-    // them, or all short (the second launch takes 4 us, and eight wavefronts on 1,000 keys no more than that in excess.  us without and
-    // with, one walk to each of twelve heads of 64 channels: 500 keys 8.5 / 8.2 + 4.4, 1,000 12.2 / 8.3 + 4.7; 32 walks of 128 channels,
-    // 1,000 keys 18.0 / 10.5 + 5.0; 192 of 64, 1,000 keys 12.4 / 11.9 + 4.6).
+    // them, or all short, as the second launch takes 4 to 8 us.  us of a call without and with, one walk to each of twelve heads of 64
+    // channels: 1,300 keys 9.7 / 12.4, 2,000 12.3 / 12.6, 3,000 16.1 / 13.4; 192 of them 1,500 12.1 / 18.5; 768 1,300 34.7 / 38.9.  Eight
+    // of 128 channels: 1,000 11.5 / 13.9, 1,400 13.0 / 14.8, 2,000 16.8 / 14.1, on pages of 16 1,400 17.9 / 15.3; 128 of them 2,000 20.4 /
+    // 23.6, 3,000 34.5 / 28.2.
     const int64_t walks = (int64_t)a.batch * a.kv_heads * a.row_tiles, groups = (a.keys + 31) / 32;
     a.bundle = 1;
     a.splits = 0;
-    if (walks < 1024 && groups > (a.dim <= 64 ? 32 : 24) && walks * groups < most) {
+    const int64_t alone = a.dim <= 64 || (a.page % 32 == 0 && walks >= 64) ? 64 : a.page % 32 == 0 ? 48 : 40; // groups of a workgroup
+    if (walks < 1024 && groups > alone && walks * groups < most) {
         while (a.bundle < kWaves && a.kv_heads * a.row_tiles % (2 * a.bundle) == 0)
             a.bundle *= 2;
         const int64_t waves = a.dim > 64 ? 2048 : 4096, blocks = ((walks * groups < waves ? walks * groups : waves) + kWaves - 1) / kWaves;

@@ -11,7 +11,9 @@ pytestmark = pytest.mark.gpu
 CASES = [([1], 1, 16, 1, 1, 8), ([500], 1, 16, 12, 12, 64), ([40, 0, 1, 129], 1, 32, 8, 2, 128), ([700, 31, 2000], 1, 1, 4, 4, 64),
          ([33, 64, 95, 96], 1, 24, 6, 2, 80), ([3000], 1, 128, 32, 8, 128), ([5, 3, 0, 700], 5, 8, 12, 4, 96), ([9000, 40], 1, 64, 2, 1, 64),
          ([100, 2, 64], 16, 20, 8, 2, 32), ([130] * 90, 1, 16, 2, 2, 64), ([2500, 1], 40, 7, 3, 1, 72), ([4097, 333, 0, 0, 8000], 2, 256, 8, 1, 128),
-         ([60, 61], 33, 1000, 2, 2, 40), ([300] * 300, 1, 64, 4, 4, 24), ([20000], 3, 5, 4, 1, 104), ([6000, 3500], 1, 2, 2, 2, 64)]
+         ([60, 61], 33, 1000, 2, 2, 40), ([300] * 300, 1, 64, 4, 4, 24), ([20000], 3, 5, 4, 1, 104), ([6000, 3500], 1, 2, 2, 2, 64),
+         ([2500], 1, 16, 4, 4, 32), ([2600, 30], 1, 24, 6, 2, 96), ([1900, 5, 1024], 1, 64, 4, 2, 64), ([1400, 7], 1, 64, 16, 4, 128),
+         ([1100, 40], 20, 16, 8, 2, 128), ([3000, 2], 20, 16, 8, 2, 128), ([1000] * 70, 1, 32, 8, 8, 128)]
 
 
 def _type(torch, dtype):
