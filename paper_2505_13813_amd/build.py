@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -52,13 +54,25 @@ def build_library(force: bool = True, verbose: bool = False) -> Path:
     if not force and not is_stale():
         return LIB
     tmp = LIB.with_name("libgrkan.so.tmp%d" % os.getpid())
-    cmd = [hipcc(), *HIPCC_FLAGS, *map(str, SOURCES), "-o", str(tmp)]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        tmp.unlink(missing_ok=True)
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+
+    def run(cmd) -> None:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+
+    # a file at a time on each of up to eight processors, the longest (which come last) first
+    with tempfile.TemporaryDirectory() as folder:
+        objects = [Path(folder) / (p.name + ".o") for p in SOURCES]
+        flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda pair: run([hipcc(), *flags, "-c", str(pair[0]), "-o", str(pair[1])]), reversed(list(zip(SOURCES, objects)))))
+        try:
+            run([hipcc(), *HIPCC_FLAGS, *map(str, objects), "-o", str(tmp)])
+        except RuntimeError:
+            tmp.unlink(missing_ok=True)
+            raise
     os.replace(tmp, LIB)
     return LIB
 
