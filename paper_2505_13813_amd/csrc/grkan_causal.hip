@@ -459,14 +459,14 @@ template <typename IO> static CausalVariant pick(const Packed &a)
     return a.dim <= 32 ? pick<IO, 32>(a) : a.dim <= 64 ? pick<IO, 64>(a) : a.dim <= 96 ? pick<IO, 96>(a) : pick<IO, 128>(a);
 }
 
-// Two wavefronts on the tiles of 64 keys of the same rows where tiles of 128 rows do not fill the device (four workgroups of a compute
-// unit, with 128 channels two): the longest walk is then what counts, and it is half as long.  us with 128 rows to a workgroup and with 64:
-// twelve heads of 64 channels, 24 sequences of 60 to 1,000 tokens 25.5 / 21.7, eight of 120 to 2,000 39.4 / 30.0, one of 4,096 74 / 55, 40
-// of 60 to 1,000 36.6 / 39.3, 60 of 12 to 200 13.4 / 14.7, 16 of 240 to 4,000 130 / 161; 32 heads of 128 on eight, one of 1,000 33.1 /
-// 28.6, of 2,000 62.6 / 64.4, eight of 60 to 1,000 38.2 / 50.7; 16 of 96 on four, eight of 120 to 2,000 56.8 / 44.8.
+// Two wavefronts on the tiles of 64 keys of the same rows where tiles of 128 rows do not fill the device (four workgroups of a compute unit, with
+// more than 64 channels two): the longest walk is then what counts, and it is half as long.  us with 128 rows to a workgroup and with 64: twelve heads
+// of 64 channels, 24 sequences of 60 to 1,000 tokens 21.1 / 19.9, eight of 120 to 2,000 31.5 / 25.1, one of 4,096 57 / 44, 30 of 60 to 1,000
+// 22.4 / 23.6, 60 of 12 to 200 10.9 / 13.1, 16 of 240 to 4,000 110 / 136; 32 heads of 128 on eight, one of 1,500 36.0 / 34.9, of 2,000 46.9 / 51.4, eight of 60
+// to 1,000 31.8 / 41.3; 16 of 96, 14 of 60 to 1,000 27.7 / 25.0, one of 6,000 131 / 143, 18 of 60 to 1,000 29.4 / 35.3.
 bool few_rows(const Packed &a)
 {
-    return slots_of<128>(a, a.group) * a.kv_heads <= (a.dim <= 64 ? 1024 : a.dim <= 96 ? 2048 : 448);
+    return slots_of<128>(a, a.group) * a.kv_heads <= (a.dim <= 64 ? 1024 : a.dim <= 96 ? 720 : 448);
 }
 
 } // namespace attention
