@@ -691,9 +691,9 @@ template <class KEYS, int PARTS> static CausalBack variant(const Packed &a)
 }
 template <typename IO, bool FINE> static CausalBack pick(const Packed &a)
 {
-    // (as for rows.  us of the keys' kernel without and with: twelve heads of 64, sixteen sequences of 90 to 1,500 tokens 59 / 49, 24 of 60
-    // to 1,000 54 / 42, one of 4,096 88 / 77, of 577 25 / 16; 40 of 60 to 1,000 102 / 106, sixteen of 240 to 4,000 262 / 293)
-    const bool rows = few_rows(a), keys = slots_of<128>(a, 1) * a.kv_heads <= 1024;
+    // (as for rows.  us of forward and backward without and with, twelve heads of 64: 24 sequences of 60 to 1,000 tokens 92.7 / 78.2, eight of 240 to
+    // 4,000 256 / 226, one of 4,096 189 / 179, 60 of 18 to 300 71.8 / 67.5, 30 of 60 to 1,000 103.4 / 97.9; 40 136 / 143, sixteen of 240 to 4,000 462 / 485)
+    const bool rows = few_rows(a), keys = slots_of<128>(a, 1) * a.kv_heads <= 1408;
     auto with = [&](auto one, auto two) {
         using ONE = decltype(one);
         using TWO = decltype(two);

@@ -13,7 +13,7 @@ CASES = [([1], 0, 0, 1, 1, 8), ([16], 0, 0, 3, 3, 64), ([5, 0, 1, 30], 0, 3, 2, 
          ([17] * 200, 7, 0, 6, 6, 24), ([1500, 640], 0, 0, 16, 8, 80), ([600], 0, 0, 40, 1, 64), ([2000, 900], 0, 100, 10, 10, 64),
          ([300, 65, 1], 1, 0, 200, 100, 128), ([129, 0, 40], 2, 3, 1100, 550, 96), ([400, 200], 0, 1, 128, 64, 104),
          ([300], 0, 0, 294, 21, 128), ([1100], 2, 0, 80, 20, 128), ([1500, 0, 730], 0, 40, 42, 7, 128), ([64], 0, 0, 512, 8, 128),
-         ([700, 600], 0, 0, 100, 100, 64), ([400], 0, 1, 256, 256, 32), ([300, 200], 0, 0, 130, 130, 80), ([600, 300], 3, 0, 160, 40, 64), ([900], 0, 0, 12, 12, 96)]
+         ([700, 600], 0, 0, 110, 110, 64), ([400], 0, 1, 256, 256, 32), ([300, 200], 0, 0, 130, 130, 80), ([600, 300], 3, 0, 160, 40, 64), ([900], 0, 0, 12, 12, 96)]
 
 
 def _type(torch, dtype):
