@@ -18,7 +18,7 @@ SOURCES = [CSRC / "grkan_kernels.hip", CSRC / "grkan_plan.cpp", CSRC / "grkan_al
            CSRC / "grkan_causal_bwd.hip", CSRC / "grkan_paged.hip"]
 HEADERS = [CSRC / "grkan_walk.h", CSRC / "grkan_plan.h", CSRC / "grkan_elem.h", CSRC / "grkan_tile.h", CSRC / "grkan_stage2.h",
            CSRC / "grkan_vector.h", CSRC / "grkan_attention.h", CSRC / "grkan_attention_rows.h",
-           CSRC / "grkan_attention_back.h", CSRC / "grkan_packed.h",
+           CSRC / "grkan_attention_back.h", CSRC / "grkan_packed.h", CSRC / "grkan_turns.h",
            PKG.parent / "include" / "grkan.h",
            PKG.parent / "include" / "grkan_alg1.h", PKG.parent / "include" / "grkan_transformer.h"]
 

@@ -23,6 +23,7 @@
 
 #include "grkan_attention_rows.h"
 #include "grkan_packed.h"
+#include "grkan_turns.h"
 
 namespace grkan {
 namespace attention {
@@ -291,26 +292,18 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
         ColumnOperand<DP> v_from(lane);
         k_from.move(lds0);
         v_from.move(lds0 + 3 * SH::kTile);
-        wait_loads<0>();
-        barrier();
-        load_keys(1, SH::kTile);
-        load_values(0, 0);
-        load_keys(2, 2 * SH::kTile);
-        load_values(1, SH::kTile);
-        if (second)
-            barrier();
         f32x16 x[KT / 32];
-        rows.template scores_ahead<2>(k_from, x);
-        fence_schedule();
-        barrier();
-        uint32_t at = 0; // of tile t
-        // (without conditions that would copy the sums: a wavefront's last tiles may be cut off as a whole, and the last scores are nobody's)
-#pragma unroll 1
-        for (int32_t t = 0;;) {
+        uint32_t p[KT / 32][8];
+        auto wait = [&] { wait_loads<0>(); };
+        auto meet = [&] {
+            fence_schedule();
+            barrier();
+        };
+        auto scores = [&] { rows.template scores_ahead<2>(k_from, x); };
+        // (without conditions that would copy the sums: a wavefront's last tiles may be cut off as a whole)
+        auto probabilities = [&](int32_t t, uint32_t at, uint32_t next) {
             const int32_t key0 = t * KT;
-            uint32_t p[KT / 32][8];
-            const bool crossed = key0 + KT > from;
-            if (crossed)
+            if (key0 + KT > from)
                 rows.cut(x, (int32_t)query - key0, h);
             rows.probabilities(x, a.c, p);
             // (here, and not where they are used first, in the other group's time)
@@ -320,13 +313,11 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
                 for (int j = 0; j < 8; ++j)
                     asm volatile("" : "+v"(p[kb][j]));
             asm volatile("" : "+v"(rows.sum));
-            const uint32_t next = at == 2 * SH::kTile ? 0u : at + SH::kTile, last = 3 * SH::kTile - at - next;
             k_from.move(next - at);
-            wait_loads<0>();
-            fence_schedule();
-            barrier();
-            // scores of tile t + 1, values of tile t; to where the keys of tile t and the values of tile t - 1 were, those of t + 3 and t +
-            // 2: a load between eight products, as one waits for 100 cycles behind the others'
+        };
+        // (a load between eight products, as one waits for 100 cycles behind the others')
+        auto products = [&](int32_t t, uint32_t at, uint32_t next, uint32_t last) {
+            const int32_t key0 = t * KT;
             const bool spread = end - (t + 3) * KT >= KT && !decltype(each)::value;
             const uint64_t keys = uniform_u64(k_base + (uint64_t)(t + 3) * KT * (uint64_t)a.k.token);
             const uint64_t values = uniform_u64(v_base + (uint64_t)(t + 2) * KT * (uint64_t)a.v.token);
@@ -336,7 +327,7 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
             }
             bool apart = false;
             if constexpr (decltype(each)::value)
-                apart = crossed;
+                apart = key0 + KT > from;
             if (apart) {
                 rows.scores(k_from, x);
                 rows.add_each(p, v_from, (int32_t)query - key0, col, h);
@@ -351,14 +342,8 @@ template <class SH> __global__ __launch_bounds__(512, 2) void causal_turns_kerne
                 });
             }
             v_from.move(next - at);
-            at = next;
-            fence_schedule();
-            barrier();
-            if (++t == tiles)
-                break;
-        }
-        if (!second)
-            barrier();
+        };
+        take_turns<SH::kTile>(tiles, second, wait, meet, load_keys, load_values, scores, probabilities, products);
     };
     walk(std::false_type{});
     // (by all wavefronts, which load for one another)
