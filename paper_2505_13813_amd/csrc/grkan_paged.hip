@@ -681,7 +681,7 @@ static grkan_status_t fill(const grkan_paged_cache_t *c, const grkan_paged_queri
     a.bundle = 1;
     a.splits = 0;
     const int64_t alone = a.dim <= 64 || (a.page % 32 == 0 && walks >= 64) ? 64 : a.page % 32 == 0 ? 48 : 40; // groups of a workgroup
-    if (walks < 1024 && groups > alone && walks * groups < most) {
+    if (walks > 0 && walks < 1024 && groups > alone && walks * groups < most) {
         while (a.bundle < kWaves && a.kv_heads * a.row_tiles % (2 * a.bundle) == 0)
             a.bundle *= 2;
         const int64_t waves = a.dim > 64 ? 2048 : 4096, blocks = ((walks * groups < waves ? walks * groups : waves) + kWaves - 1) / kWaves;

@@ -179,6 +179,28 @@ def test_paged_workspaces(lib):
                         assert need <= 4 * 32 * 129 * (1024 + 4096 + 8)
 
 
+def test_no_tokens_or_no_sequences_over_long_tables():
+    """Nothing to do, whatever the table has place for: no workspace, no error.  (In a process of its own, which a division by zero would end.)"""
+    import subprocess
+    import sys
+
+    text = """
+import ctypes, itertools, sys
+sys.path[:0] = [%r, %r]
+import test_decoder_host as t
+lib = t.binding.load_library()
+for sequences, tokens, entries, dim, page in itertools.product((0, 3), (0, 1), (1, 20, 200, 100000), (64, 128), (16, 32)):
+    if sequences and tokens:
+        continue
+    c, q = t._cache(sequences=sequences, table_entries=entries, dim=dim, page_size=page), t._queries(tokens=tokens)
+    print(sequences, tokens, entries, dim, page, flush=True)
+    assert lib.grkan_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(q)) == 0
+    assert lib.grkan_paged_attention(ctypes.byref(c), ctypes.byref(q), None, None, 0, t.BF16, None) == t.OK
+""" % (str(ROOT), str(ROOT / "tests"))
+    found = subprocess.run([sys.executable, "-c", text], capture_output=True, text=True, timeout=300)
+    assert found.returncode == 0, (found.returncode, found.stdout[-200:], found.stderr[-2000:])
+
+
 def test_tensors_on_the_cpu_and_missing_ones_are_refused():
     import torch
 

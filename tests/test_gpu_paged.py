@@ -342,6 +342,19 @@ def test_refusals():
     paged_write(k[:, :0], k[:, :0], *pools, table, lengths)
 
 
+def test_no_tokens_and_no_sequences():
+    """Nothing to attend with, over tables that have place for many positions."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_attention
+
+    pool = torch.zeros(4, 16, 2, 64, device="cuda:0", dtype=torch.bfloat16)
+    table, lengths = torch.zeros(3, 1000, device="cuda:0", dtype=torch.int32), torch.full((3,), 100, device="cuda:0")
+    q = torch.zeros(3, 1, 4, 64, device="cuda:0", dtype=torch.bfloat16)
+    assert paged_attention(q[:, :0], pool, pool, table, lengths).shape == (3, 0, 4, 64)
+    assert paged_attention(q[:0], pool, pool, table[:0], lengths[:0]).shape == (0, 1, 4, 64)
+
+
 def test_on_another_stream_and_in_graphs():
     """Token by token on a stream of its own and from a captured step that is replayed as the sequences grow, with eager calls on other caches between; two
     graphs that share the allocator's pool."""
