@@ -219,7 +219,7 @@ typedef struct {
  * lengths[s] - 1, the others in front of it.  Tokens of no sequence are left out, and so are those of a sequence that has more tokens than length, where their
  * positions would be below 0, and all of one whose length is more than its row of the table has place for.
  * Where two tokens have the same place (a page in two sequences' rows), which one it holds afterwards is unspecified.  k and v do not overlap the pages.
- * tokens below 2^30, kv_heads x dim below 2^24: else GRKAN_ERR_UNSUPPORTED.
+ * tokens up to 2^30 - 64, sequences below 2^30, kv_heads x dim below 2^24: else GRKAN_ERR_UNSUPPORTED.
  */
 grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, const void *k, const void *v, const void *offsets, int32_t offsets_64, int64_t tokens,
                                  int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, grkan_dtype_t io,

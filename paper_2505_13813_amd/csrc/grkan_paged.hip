@@ -524,6 +524,8 @@ template <typename IO> __global__ __launch_bounds__(256) void join_paged_kernel(
 
 // ------------------------------------------------------------------------------------------------ into the pages
 
+constexpr int kMostTokens = 64; // a lane of a wavefront each
+
 struct PagedWrite : Packed { // k, v: of the new tokens; rows: tokens
     char *k_pages, *v_pages;
     int64_t k_page, k_place, k_place_head, v_page, v_place, v_place_head; // bytes
@@ -531,15 +533,15 @@ struct PagedWrite : Packed { // k, v: of the new tokens; rows: tokens
     const void *lengths;
     int64_t table_stride, pages;
     int32_t lengths_64, page, entries;
-    int32_t per; // tokens of a workgroup, 64 at most
+    int32_t per; // tokens of a workgroup, kMostTokens at most
 };
 
 // A copy, 16 bytes a lane: bound by memory, or for few tokens by the way from the offsets over the lengths and the table to the page.
 __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWrite a)
 {
-    __shared__ int32_t page_of[64], place_of[64];
+    __shared__ int32_t page_of[kMostTokens], place_of[kMostTokens];
     const int32_t token0 = (int32_t)blockIdx.x * a.per, here = a.tokens - token0 < a.per ? a.tokens - token0 : a.per;
-    if (threadIdx.x < 64) {
+    if (threadIdx.x < kMostTokens) {
         const int32_t lane = (int32_t)threadIdx.x, token = token0 + lane;
         // the segment of the workgroup's first token: the last that begins at or in front of it
         int32_t lo = 0, len = a.sequences + 2;
@@ -772,7 +774,7 @@ extern "C" grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, co
         return bad;
     if (tokens < 0 || (!offsets && (cache->sequences == 0 ? tokens != 0 : tokens % cache->sequences != 0)))
         return GRKAN_ERR_SHAPE;
-    if (tokens >= (int64_t)1 << 30 || (int64_t)cache->kv_heads * cache->dim >= (int64_t)1 << 24 || cache->sequences >= 1 << 30)
+    if (tokens > attention::kMostTokens * attention::kMostBlocks || (int64_t)cache->kv_heads * cache->dim >= (int64_t)1 << 24 || cache->sequences >= 1 << 30)
         return GRKAN_ERR_UNSUPPORTED;
     if (tokens == 0 || cache->sequences == 0 || cache->pages == 0)
         return GRKAN_OK;
@@ -808,7 +810,7 @@ extern "C" grkan_status_t grkan_paged_write(const grkan_paged_cache_t *cache, co
     a.page = cache->page_size;
     a.entries = cache->table_entries;
     const int64_t per = (tokens + 1023) / 1024;
-    a.per = (int32_t)(per < 64 ? per : 64);
+    a.per = (int32_t)(per < attention::kMostTokens ? per : attention::kMostTokens);
     const int64_t grid = (tokens + a.per - 1) / a.per;
     attention::paged_write_kernel<<<dim3((unsigned)grid), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a);
     return hipGetLastError() == hipSuccess ? GRKAN_OK : GRKAN_ERR_LAUNCH;

@@ -168,6 +168,13 @@ def test_other_refusals_of_pages(lib):
     assert write(tokens=0, k=None, v=None) == OK and write(cache=_cache(pages=0, k_pages=None, v_pages=None)) == OK
 
 
+def test_writes_of_more_tokens_than_a_launch_takes(lib):
+    """64 tokens of a workgroup of 256: from 2^24 workgroups on there are 2^32 threads."""
+    most = 64 * ((1 << 24) - 1)
+    for tokens in (most + 1, (1 << 30) - 1):
+        assert lib.grkan_paged_write(ctypes.byref(_cache()), 16, 16, 16, 0, tokens, 128, 64, 128, 64, BF16, None) == UNSUPPORTED
+
+
 def test_paged_workspaces(lib):
     for sequences in (1, 7, 300, 5000):
         for entries in (1, 30, 10000):
