@@ -280,6 +280,7 @@ class PagedCache:
         self.table = torch.full((sequences, -(-longest // page_size)), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.counts = [0] * sequences
+        self._grown, self._stepped = [0] * sequences, False  # new positions that no step or prompt has had; since when they are counted anew
         self._held = torch.full(self.table.shape, -1, dtype=torch.int32)  # the table on the host
         self._free = list(range(pages - 1, -1, -1))
 
@@ -307,6 +308,9 @@ class PagedCache:
                 first = self._pages(self.counts[i])
                 self._held[i, first:first + n] = torch.tensor([self._free.pop() for _ in range(n)], dtype=torch.int32)
         self.counts = after
+        if self._stepped:
+            self._grown, self._stepped = [0] * len(counts), False
+        self._grown = [a + b for a, b in zip(self._grown, counts)]
         if any(wanted):
             self.table.copy_(self._held)
         if min(counts) == max(counts):
@@ -319,9 +323,28 @@ class PagedCache:
         row = self._held[sequence]
         self._free += row[:self._pages(self.counts[sequence])].tolist()[::-1]
         row.fill_(-1)
-        self.counts[sequence] = 0
+        self.counts[sequence] = self._grown[sequence] = 0
         self.table[sequence].fill_(-1)
         self.lengths[sequence].zero_()
+
+    def _capturing(self) -> bool:
+        """Whether a call is recorded and not run: then the counts are not those of its replays."""
+        return self.table.is_cuda and torch.cuda.is_current_stream_capturing()
+
+    def _prompts(self) -> None:
+        """Whole sequences go into the rows that held nothing."""
+        if not self._capturing():
+            self._grown = [0 if grown == held else grown for grown, held in zip(self._grown, self.counts)]
+
+    def _newest(self, tokens: int) -> None:
+        """So many tokens go into each row that holds something; once more into the same places, until it grows again."""
+        if self._capturing():
+            return
+        short = [s for s, (grown, held) in enumerate(zip(self._grown, self.counts)) if held and grown < tokens]
+        if short:
+            raise ValueError("a step of %d would overwrite older positions in rows that have not grown by as many since the step or prompt before: row %s"
+                             % (tokens, ", ".join(map(str, short))))
+        self._stepped = True
 
 
 class KATDecoderBlock(nn.Module):
@@ -392,9 +415,13 @@ class KATDecoder(nn.Module):
     def forward(self, x, offsets=None, positions=None, cache: Optional[PagedCache] = None):
         """Whole sequences: x [tokens, dim] packed, offsets as in causal_attention, positions [tokens, axes]; or [batch, tokens, dim].  With a
         cache, whose rows held nothing before they grew by these sequences, their keys and values are left there; without gradients."""
+        if cache is not None:
+            cache._prompts()
         return self._run(x, offsets=offsets, positions=positions, cache=cache)
 
     def step(self, x, cache: PagedCache, positions=None):
         """The newest tokens [sequences, tokens, dim] of the cache's sequences, by which each has grown, or has been released; positions
-        [sequences, tokens, axes]."""
+        [sequences, tokens, axes].  Refused where a row that holds something has not grown since the step or the prompt before; what a captured
+        step is replayed for is not looked at."""
+        cache._newest(x.shape[-2])
         return self._run(x, positions=positions, cache=cache, newest=True)

@@ -282,3 +282,57 @@ def test_a_decoder_wants_positions_and_heads_that_divide():
         assert [n.eps for b in m.blocks for n in (b.norm1, b.norm2)] + [m.norm.eps] == [eps] * 5
     c = T.KATDecoder(3, 64, 4, kv_heads=2, groups=4).bfloat16().cache(5, 16, 2, 40)
     assert len(c.k_pages) == 3 and c.k_pages[0].shape == (5, 16, 2, 16) and c.k_pages[0].dtype == torch.bfloat16 and c.table.shape == (2, 3)
+
+
+def _decoder_without_kernels():
+    """Its blocks return what they are given."""
+    import torch
+
+    from paper_2505_13813_amd import transformer as T
+
+    class Block(torch.nn.Module):
+        def forward(self, x, stream=None, **given):
+            return x, x
+
+    class Norm(torch.nn.Module):
+        def forward(self, x, stream):
+            return x, stream
+
+    m = T.KATDecoder(2, 16, 2, groups=4)
+    m.blocks, m.norm = torch.nn.ModuleList([Block(), Block()]), Norm()
+    return m
+
+
+def test_a_step_of_rows_that_have_not_grown_is_refused():
+    """A row that holds something and has no new position would have its last one's keys and values overwritten."""
+    import torch
+
+    m, c = _decoder_without_kernels(), _host_cache(pages=20, longest=40)
+    one, two = torch.zeros(3, 1, 16), torch.zeros(3, 2, 16)
+    m.step(one, c)  # (nothing is held)
+    c.grow([5, 0, 4])
+    m(torch.zeros(9, 16), torch.tensor([0, 5, 5, 9]), cache=c)
+    with pytest.raises(ValueError, match=r"rows? 0, 2"):  # the prompts have taken what they grew by
+        m.step(one, c)
+    c.grow([1, 0, 0])
+    with pytest.raises(ValueError, match=r"row 2"):
+        m.step(one, c)
+    c.grow([0, 0, 1])
+    m.step(one, c)  # (grown one after the other, and row 1 is free)
+    m.step(one, c)  # the same places once more, as before a capture
+    c.grow([1, 0, 0])
+    with pytest.raises(ValueError, match=r"row 2"):
+        m.step(one, c)
+    c.release(2)
+    m.step(one, c)
+    c.grow([1, 3, 0])
+    m(torch.zeros(3, 16), torch.tensor([0, 0, 3, 3]), cache=c)  # a prompt into a free row, while row 0 has grown for a step
+    c.grow([0, 1, 0])
+    m.step(one, c)
+    with pytest.raises(ValueError, match=r"rows? 0, 1"):
+        m.step(two, c)
+    c.grow([1, 1, 0])
+    c.grow([1, 1, 0])
+    m.step(two, c)
+    c.grow([2, 2, 0])
+    m.step(one, c)  # (what else the rows grew by is the caller's)
