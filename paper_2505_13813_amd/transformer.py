@@ -331,10 +331,14 @@ class PagedCache:
         """Whether a call is recorded and not run: then the counts are not those of its replays."""
         return self.table.is_cuda and torch.cuda.is_current_stream_capturing()
 
-    def _prompts(self) -> None:
-        """Whole sequences go into the rows that held nothing."""
-        if not self._capturing():
-            self._grown = [0 if grown == held else grown for grown, held in zip(self._grown, self.counts)]
+    def _prompts(self, tokens: Optional[int]) -> None:
+        """Whole sequences go into the rows that held nothing before they grew; tokens: of each, where all have as many."""
+        if self._capturing():
+            return
+        other = [s for s, held in enumerate(self.counts) if tokens is not None and held not in (0, tokens)]
+        if other:
+            raise ValueError("whole sequences of %d go into rows that hold nothing else, and have grown by as many: not so row %s" % (tokens, ", ".join(map(str, other))))
+        self._grown = [0 if grown == held else grown for grown, held in zip(self._grown, self.counts)]
 
     def _newest(self, tokens: int) -> None:
         """So many tokens go into each row that holds something; once more into the same places, until it grows again."""
@@ -414,9 +418,10 @@ class KATDecoder(nn.Module):
 
     def forward(self, x, offsets=None, positions=None, cache: Optional[PagedCache] = None):
         """Whole sequences: x [tokens, dim] packed, offsets as in causal_attention, positions [tokens, axes]; or [batch, tokens, dim].  With a
-        cache, whose rows held nothing before they grew by these sequences, their keys and values are left there; without gradients."""
+        cache, whose rows held nothing before they grew by these sequences (a batch is refused where they did), their keys and values are left there;
+        without gradients."""
         if cache is not None:
-            cache._prompts()
+            cache._prompts(x.shape[1] if x.dim() == 3 else None)
         return self._run(x, offsets=offsets, positions=positions, cache=cache)
 
     def step(self, x, cache: PagedCache, positions=None):

@@ -336,3 +336,24 @@ def test_a_step_of_rows_that_have_not_grown_is_refused():
     m.step(two, c)
     c.grow([2, 2, 0])
     m.step(one, c)  # (what else the rows grew by is the caller's)
+
+
+def test_a_batch_into_rows_that_hold_something_else_is_refused():
+    """[batch, tokens, dim] into a cache are whole sequences: behind what a row holds already they would not see it, and of a row with fewer positions the
+    first ones would be lost."""
+    import torch
+
+    m, c = _decoder_without_kernels(), _host_cache(pages=20, longest=40)
+    x = torch.zeros(3, 4, 16)
+    m(x, cache=c)  # (rows of nothing take nothing)
+    c.grow([4, 0, 4])
+    m(x, cache=c)
+    m(x, cache=c)
+    c.grow([4, 4, 0])
+    with pytest.raises(ValueError, match=r"row 0$"):
+        m(x, cache=c)
+    c.release(0)
+    c.grow([3, 0, 0])
+    with pytest.raises(ValueError, match=r"row 0$"):
+        m(x, cache=c)
+    m(x.flatten(0, 1), torch.tensor([0, 3, 3, 3]), cache=c)  # (where the sequences end is on the device)
