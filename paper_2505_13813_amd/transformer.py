@@ -293,7 +293,8 @@ class PagedCache:
 
     def grow(self, counts: Sequence[int]) -> None:
         """Makes room for counts[s] new positions of each sequence and adds them to the lengths, before the step that writes them, on the
-        stream that it runs on.  Refused as a whole where the pages do not suffice."""
+        stream that it runs on.  Refused as a whole where the pages do not suffice, and in a capture."""
+        self._outside_captures()
         counts = [int(n) for n in counts]
         if len(counts) != len(self.counts) or min(counts) < 0:
             raise ValueError("counts must be a number of new positions, not negative, for each of the cache's sequences")
@@ -319,7 +320,8 @@ class PagedCache:
             self.lengths.copy_(torch.tensor(after, dtype=torch.int32))
 
     def release(self, sequence: int) -> None:
-        """Takes a sequence's pages back: its row, of length 0, is free for another one."""
+        """Takes a sequence's pages back: its row, of length 0, is free for another one.  Not in a capture."""
+        self._outside_captures()
         row = self._held[sequence]
         self._free += row[:self._pages(self.counts[sequence])].tolist()[::-1]
         row.fill_(-1)
@@ -330,6 +332,10 @@ class PagedCache:
     def _capturing(self) -> bool:
         """Whether a call is recorded and not run: then the counts are not those of its replays."""
         return self.table.is_cuda and torch.cuda.is_current_stream_capturing()
+
+    def _outside_captures(self) -> None:
+        if self._capturing():
+            raise RuntimeError("a cache grows and releases outside of captured graphs: which pages are free is kept on the host, which has no part in a replay")
 
     def _prompts(self, tokens: Optional[int]) -> None:
         """Whole sequences go into the rows that held nothing before they grew; tokens: of each, where all have as many."""

@@ -264,6 +264,22 @@ def test_pages_are_given_out_and_taken_back():
             _host_cache(**bad)
 
 
+def test_pages_are_not_given_out_in_a_capture(monkeypatch):
+    """The host's part would be done once and the device's at every replay."""
+    c = _host_cache()
+    c.grow([3, 0, 4])
+    state = lambda: (list(c.counts), c.free_pages, c.table.tolist(), c.lengths.tolist())  # noqa: E731
+    before = state()
+    monkeypatch.setattr(type(c), "_capturing", lambda self: True, raising=False)
+    for call in (lambda: c.grow([1, 1, 1]), lambda: c.grow([1, 0, 0]), lambda: c.grow([0, 0, 4]), lambda: c.release(0)):
+        with pytest.raises(RuntimeError, match="captur"):
+            call()
+        assert state() == before
+    monkeypatch.undo()
+    c.grow([1, 1, 1])
+    assert c.counts == c.lengths.tolist() == [4, 1, 5]
+
+
 def test_a_decoder_wants_positions_and_heads_that_divide():
     import torch
 

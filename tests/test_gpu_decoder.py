@@ -204,6 +204,26 @@ def test_prompts_and_then_tokens(page, dtype):
         assert cache.lengths.tolist() == cache.counts == [33 + steps, 1 + steps, 20, 64 + steps]
 
 
+def test_growing_is_no_part_of_a_captured_step():
+    import torch
+
+    m = _decoder(torch, "bf16", kv_heads=1)
+    cache = m.cache(10, 16, 2, 64)
+    x = torch.randn(2, 1, 192, device="cuda:0", dtype=torch.bfloat16)
+    with torch.no_grad():
+        cache.grow([1, 1])
+        want = m.step(x, cache)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for call in (lambda: cache.grow([1, 1]), lambda: cache.grow([16, 0]), lambda: cache.release(0)):
+                with pytest.raises(RuntimeError, match="captur"):
+                    call()
+            got = m.step(x, cache)
+        graph.replay()
+        torch.cuda.synchronize()
+    assert cache.counts == cache.lengths.tolist() == [1, 1] and cache.free_pages == 8 and torch.equal(got, want)
+
+
 def test_saved_tensor_hooks():
     """Operands that come back from hooks in another layout, and of the wrong shape or type."""
     import torch
