@@ -153,7 +153,8 @@ grkan_status_t grkan_attention_bwd(const grkan_attention_t *attention, const voi
  *      pointers (else GRKAN_ERR_ALIGN)
  *   offsets  DEVICE int32 (int64 with offsets_64) [sequences + 1], not falling: sequence s has tokens offsets[s] up to, not with, offsets[s + 1].
  *      Sequences may be empty; tokens in front of the first and behind the last belong to none: zeros come out, and their gradients are zeros.  What lies
- *      past 0 .. tokens is clamped to it; where offsets fall, what comes out for the tokens between is unspecified.
+ *      past 0 .. tokens is clamped to it; where offsets fall, all that comes out is unspecified (parts of it may not be written), but nothing outside of the
+ *      operands is read or written.
  *      NULL: `sequences` of the same length, tokens / sequences (else GRKAN_ERR_SHAPE).
  *   out [tokens, heads, dim] of io, contiguous, 16-byte aligned
  *   rest NULL, or as out, for the backward pass: what out's rounding took away, rounded itself

@@ -47,7 +47,7 @@ struct Segment {
     bool none; // of no sequence
 };
 
-// unit: rows of a token.  Offsets that fall give tiles whose tokens are unspecified, but within the buffer.
+// unit: rows of a token.  Offsets that fall give tiles within the buffer, but there may be more of them than places: some are nobody's then, of any segment.
 template <int SIZE> __device__ __forceinline__ int32_t place_of(int32_t token, int32_t unit, int32_t i)
 {
     return (int32_t)((uint32_t)token * (uint32_t)unit / (uint32_t)SIZE) + i;

@@ -114,7 +114,7 @@ def causal_attention(q, k, v, offsets=None, scale: Optional[float] = None):
     """softmax(scale q k^T) v over the tokens of the same sequence up to the token itself, head h reading key head h // (heads / kv_heads).
 
     q [tokens, heads, dim], k, v [tokens, kv_heads, dim]: sequences packed one behind the other, sequence s being tokens offsets[s] up to, not with,
-    offsets[s + 1] (int [sequences + 1], not falling; one sequence where there are none).  Tokens in front of the first and behind the last belong to no sequence:
+    offsets[s + 1] (int [sequences + 1]; one sequence where there are none; where they fall, all that comes out is unspecified).  Tokens in front of the first and behind the last belong to no sequence:
     zeros, and zeros as their gradients.  Or q [batch, tokens, heads, dim], k and v alike, without offsets: a sequence each.
     bfloat16 or float16, dim a multiple of 8 up to 128, any strides with dense channels; scale: dim ** -0.5.
     No sequence has any influence on another, and no later token on an earlier one's output, NaN and infinities included.  Differentiable (once) with

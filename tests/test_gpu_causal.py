@@ -468,3 +468,38 @@ def test_from_c_with_and_without_the_rest(case, dtype):
         assert with_rest or bool((rest == 7.0).all())
         results.append((out, lse, dv))
     assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+FALLING = [[0, 60, 20, 100], [100, 0], [50, 40, 30, 700], [0] + [1000, 0] * 6 + [1000, 1100], [-5, 900, 3, 3, 1200, 0, 650, 2 ** 31 - 1], [700] * 70 + [10] * 70]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(2, 1, 64), (12, 12, 64), (32, 8, 128), (6, 2, 72)])
+def test_falling_offsets_stay_in_the_buffers(shape, dtype):
+    """What comes out is unspecified, but nothing around the outputs and the workspace is written (that nothing outside is reached: test_packed_host.py)."""
+    import ctypes
+
+    import torch
+
+    from paper_2505_13813_amd import binding
+
+    heads, kv, dim = shape
+    lib, io, stream = binding.load_library(), {"bf16": 1, "f16": 2}[dtype], torch.cuda.current_stream().cuda_stream
+    guard = 4096
+    for offsets in FALLING:
+        print(shape, dtype, offsets[:8], flush=True)
+        tokens = min(1200, max(offsets))
+        q, k, v, dout, _ = _operands(torch, ([tokens], 0, 0, heads, kv, dim), dtype, 9)
+        given = torch.tensor(offsets, device="cuda:0", dtype=torch.int32)
+        a = binding.CausalAttention(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), offsets=given.data_ptr(), tokens=tokens, sequences=len(offsets) - 1, heads=heads,
+                                    kv_heads=kv, dim=dim, q_token_stride=q.stride(0), q_head_stride=q.stride(1), k_token_stride=k.stride(0), k_head_stride=k.stride(1),
+                                    v_token_stride=v.stride(0), v_head_stride=v.stride(1), scale=dim ** -0.5)
+        need = lib.grkan_causal_attention_bwd_workspace_bytes(ctypes.byref(a))
+        sizes = [2 * q.numel(), 2 * q.numel(), 4 * lib.grkan_causal_attention_lse_count(ctypes.byref(a)), 2 * q.numel(), 2 * k.numel(), 2 * v.numel(), need]
+        held = [torch.full((guard + -(-n // 16) * 16 + guard,), 77, dtype=torch.uint8, device="cuda:0") for n in sizes]
+        out, rest, lse, dq, dk, dv, work = (t.data_ptr() + guard for t in held)
+        assert lib.grkan_causal_attention_fwd(ctypes.byref(a), out, rest, lse, io, stream) == 0
+        assert lib.grkan_causal_attention_bwd(ctypes.byref(a), out, rest, lse, dout.data_ptr(), dout.stride(0), dout.stride(1), dq, dk, dv, work, need, io, stream) == 0
+        torch.cuda.synchronize()
+        for t, n in zip(held, sizes):
+            assert bool((t[:guard] == 77).all()) and bool((t[guard + n:] == 77).all()), offsets
