@@ -223,6 +223,7 @@ template <class SH> __global__ __launch_bounds__(256, SH::DP <= 64 ? 4 : 2) void
     if (__builtin_expect_with_probability(some != 0, 0, 1.0)) { // (its loops are not what registers go to)
         issue(0, 0);
         walk(std::true_type{});
+        wait_loads<0>(); // (what is joined lies where the tiles were: all have read them in front of the barrier)
         barrier();
     }
     if constexpr (SH::PARTS > 1)
