@@ -204,6 +204,41 @@ def test_prompts_and_then_tokens(page, dtype):
         assert cache.lengths.tolist() == cache.counts == [33 + steps, 1 + steps, 20, 64 + steps]
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_cache_under_autocast(dtype):
+    """Float32 parameters and streams, the cache of autocast's type: prompts and then tokens as the whole sequences in float32.  A cache of float32 is refused."""
+    import torch
+
+    io = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    m = _decoder(torch, "f32", rotary_pairs=(32,), kv_heads=1)
+    lengths, steps = [40, 1, 23], 5
+    torch.manual_seed(6)
+    whole = [torch.randn(n + steps, 192, device="cuda:0") for n in lengths]
+    ends = lambda counts: [sum(counts[:i]) for i in range(len(counts) + 1)]  # noqa: E731
+    bound = 2 * 14 * UNIT[dtype]
+    with torch.no_grad():
+        every = [n + steps for n in lengths]
+        want = _plain(torch, m, torch.cat(whole), ends(every), _places(torch, every)).split(every)
+        with torch.autocast("cuda", dtype=io):
+            cache = m.cache(20, 16, 3, 64, dtype=io)
+            cache.grow(lengths)
+            out = m(torch.cat([t[:n] for t, n in zip(whole, lengths)]), torch.tensor(ends(lengths), device="cuda:0"), _places(torch, lengths), cache)
+            assert out.dtype == torch.float32 and cache.k_pages[0].dtype == io
+            for got, w, n in zip(out.split(lengths), want, lengths):
+                _near(got, w[:n], bound, ("prompt", n))
+            for i in range(steps):
+                cache.grow([1] * 3)
+                place = torch.tensor([[[n + i]] for n in lengths], dtype=torch.int32, device="cuda:0")
+                out = m.step(torch.stack([t[n + i:n + i + 1] for t, n in zip(whole, lengths)]), cache, place)
+                assert out.dtype == torch.float32
+                for got, w, n in zip(out, want, lengths):
+                    _near(got, w[n + i:n + i + 1], 2 * bound, (n, i))
+            wide = m.cache(20, 16, 3, 64)
+            wide.grow([1] * 3)
+            with pytest.raises(TypeError, match="k_pages"):
+                m.step(torch.stack([t[:1] for t in whole]), wide, torch.zeros(3, 1, 1, dtype=torch.int32, device="cuda:0"))
+
+
 def test_growing_is_no_part_of_a_captured_step():
     import torch
 
@@ -265,3 +300,39 @@ def test_under_compile():
     x = torch.randn(40, 96, device="cuda:0", dtype=torch.bfloat16)
     with torch.no_grad():
         assert all(torch.equal(a, b) for a, b in zip(torch.compile(f, backend="eager")(x), f(x)))
+
+
+def test_transforms_modes_and_forward_differentiation_are_refused():
+    import torch
+    from torch.autograd import forward_ad
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    from paper_2505_13813_amd import transformer as T
+
+    class Mode(TorchDispatchMode):
+        def __torch_dispatch__(self, function, types, args=(), kwargs=None):
+            return function(*args, **(kwargs or {}))
+
+    pool = torch.zeros(2, 4, 16, 2, 32, device="cuda:0", dtype=torch.bfloat16)
+    table, lengths = torch.arange(4, dtype=torch.int32, device="cuda:0").view(2, 2), torch.tensor([20, 20], device="cuda:0")
+    x = torch.randn(2, 3, 2, 32, device="cuda:0", dtype=torch.bfloat16)
+
+    def write(t):
+        T.paged_write(t, t, pool[0], pool[1], table, lengths)
+        return t
+
+    with torch.no_grad():
+        for call in (lambda t: T.causal_attention(t, t, t), write, lambda t: T.paged_attention(t, pool[0], pool[1], table, lengths)):
+            with pytest.raises(NotImplementedError):
+                torch.func.vmap(call)(x[None])
+            with pytest.raises(NotImplementedError):
+                torch.func.jvp(call, (x,), (x,))
+            with pytest.raises(NotImplementedError):
+                torch.func.grad(lambda t: call(t).float().sum())(x)
+            with forward_ad.dual_level(), pytest.raises(NotImplementedError):
+                call(forward_ad.make_dual(x, x))
+            with Mode(), pytest.raises(NotImplementedError):
+                call(x)
+            assert call(x).shape == x.shape
+    torch.cuda.synchronize()
+    assert int(pool.count_nonzero()) == 2 * x.count_nonzero()  # the one write that was not refused
