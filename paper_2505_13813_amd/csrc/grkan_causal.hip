@@ -439,7 +439,8 @@ template <typename IO> static CausalVariant pick(const Packed &a)
 {
     // (turns: longer walks and fewer of them.  us without and with, query heads / key heads: one of 16,384 tokens, 8/2 537 / 466, of 4,096,
     // 32/32 148 / 139, 32/8 145 / 133, of 3,000, 32/8 83.2 / 81.8, four of 500 to 2,000, 32/8 59.7 / 56.2; too few workgroups: one of
-    // 8,192, 8/8 165 / 175, of 2,048, 32/8 49 / 54; too short: four of 800 to 3,000, 16/16 61 / 69, eight of 60 to 1,000, 32/8 32 / 35)
+    // 8,192, 8/8 165 / 175, of 2,048, 32/8 49 / 54; too short: four of 800 to 3,000, 16/16 61 / 69, eight of 60 to 1,000, 32/8 32 / 35.  The
+    // host knows the average alone: long sequences beside many empty ones go without)
     if (a.dim == 128 && a.sequences > 0 && a.rows / a.sequences >= 4096 && slots_of<256>(a, a.group) * a.kv_heads >= 384)
         return turns<TurnsShape<IO, 128>>(a);
     return a.dim <= 32 ? pick<IO, 32>(a) : a.dim <= 64 ? pick<IO, 64>(a) : a.dim <= 96 ? pick<IO, 96>(a) : pick<IO, 128>(a);

@@ -11,8 +11,10 @@
 // A key sees the more rows the earlier it is, so the walks of a long sequence's first keys are cut into slabs of rows, each a workgroup's,
 // whose sums a second launch adds up; the queries' kernel starts its longest walks first.
 //
-// What bounds it: products and vector operations, as of the forward pass (4,001 and 2,852 tokens, 16 heads of 128 on four: queries 165 us,
-// keys 236, 0.90 and 0.84 PFLOP/s; sixteen sequences of 90 to 1,500 tokens, twelve heads of 64: 35 and 43 us, and 11 for the slabs' sums).
+// What bounds it: products and vector operations, as of the forward pass (by the profiler, whose times are 6 to 13 % above those of calls in a
+// row: 4,001 and 2,852 tokens, 16 heads of 128 on four: queries 174 us, keys 255, 0.85 and 0.78 PFLOP/s; sixteen sequences of 90 to 1,500
+// tokens, twelve heads of 64: 36 and 42 us, and 8 for the slabs' sums; the same in float16, with 17 and 9 us for the rows in front: 173 and
+// 282; 32, 48 and 8).
 //
 // float16: scaled as there; the largest upstream gradient is that of the key's own sequence, from the key's tile on.
 #include <hip/hip_runtime.h>
@@ -691,8 +693,9 @@ template <class KEYS, int PARTS> static CausalBack variant(const Packed &a)
 }
 template <typename IO, bool FINE> static CausalBack pick(const Packed &a)
 {
-    // (as for rows.  us of forward and backward without and with, twelve heads of 64: 24 sequences of 60 to 1,000 tokens 92.7 / 78.2, eight of 240 to
-    // 4,000 256 / 226, one of 4,096 189 / 179, 60 of 18 to 300 71.8 / 67.5, 30 of 60 to 1,000 103.4 / 97.9; 40 136 / 143, sixteen of 240 to 4,000 462 / 485)
+    // (as for rows.  us of forward and backward without and with, twelve heads of 64: 24 sequences of 60 to 1,000 tokens 92.7 / 78.2, eight
+    // of 240 to 4,000 256 / 226, one of 4,096 189 / 179, 60 of 18 to 300 71.8 / 67.5, 30 of 60 to 1,000 103.4 / 97.9; 40 136 / 143, sixteen
+    // of 240 to 4,000 462 / 485)
     const bool rows = few_rows(a), keys = slots_of<128>(a, 1) * a.kv_heads <= 1408;
     auto with = [&](auto one, auto two) {
         using ONE = decltype(one);
@@ -710,7 +713,8 @@ template <typename IO, bool FINE> static CausalBack pick(const Packed &a)
 
 // S' in two parts where sequences are short: longer ones average more, and pay more.  us of forward and backward with one part and with
 // two: 32 sequences of up to 100 tokens, 32 heads of 128 on eight 68.3 / 70.4, ten of up to 100, twelve of 64 66 / 66, sixteen of 90 to
-// 1,500 110.5 / 116, one of 1,000, 32 of 128 on eight 104.5 / 112, 4,001 and 2,852, 16 on four 517 / 591.
+// 1,500 110.5 / 116, one of 1,000, 32 of 128 on eight 104.5 / 112, 4,001 and 2,852, 16 on four 517 / 591.  The host knows the average alone,
+// and empty sequences lower it: a short sequence that is packed with a long one has one part, and a long one behind many empty ones two.
 template <typename IO> static CausalBack pick(const Packed &a)
 {
     return (int64_t)a.tokens < 128 * (int64_t)a.sequences ? pick<IO, true>(a) : pick<IO, false>(a);
@@ -733,11 +737,12 @@ static CausalPlan plan(const Packed &given, grkan_dtype_t io)
     a.key_tiles = (int32_t)p.v.keys_slots;
     a.slots = (int32_t)p.v.queries_slots;
     // Slabs, of 1.4 times what each workgroup has to do on the average, if the sequences were all of one length, which the host does not
-    // know: so many that the device holds them all at once.  Where a sequence is longer its parts are the more, and then the longer (Walk).
-    // There is a workgroup for each part that there may be, and most are not there: not so many that these take time themselves, 1.5 us
-    // each, nor more than a GB of sums.  us of the keys' kernel + the sum, with slabs of 1.4, 1.0 and 0.5 of the average: 4,001 and 2,852
-    // tokens, 16 heads of 128 on four 261 + 13, 304 + 16, 289 + 22; one of 4,096, twelve of 64 80 + 10, 87 + 12, 83 + 14.  1,024 and 512
-    // rows at least: one of 1,000, 32 heads of 128 on eight 67 + 8, 46 + 11; of 577, twelve of 64 15.8 + 0, 14.9 + 3.9.
+    // know (empty ones count: 4,001 and 2,852 tokens with 510 empty sequences behind 926 us forward and backward, in the place of 506): so
+    // many that the device holds them all at once.  Where a sequence is longer its parts are the more, and then the longer (Walk). There is
+    // a workgroup for each part that there may be, and most are not there: not so many that these take time themselves, 1.5 us each, nor
+    // more than a GB of sums.  us of the keys' kernel + the sum, with slabs of 1.4, 1.0 and 0.5 of the average: 4,001 and 2,852 tokens, 16
+    // heads of 128 on four 261 + 13, 304 + 16, 289 + 22; one of 4,096, twelve of 64 80 + 10, 87 + 12, 83 + 14.  1,024 and 512 rows at
+    // least: one of 1,000, 32 heads of 128 on eight 67 + 8, 46 + 11; of 577, twelve of 64 15.8 + 0, 14.9 + 3.9.
     const int64_t each = a.sequences > 0 ? ((int64_t)a.tokens + a.sequences - 1) / a.sequences : 0;
     const int64_t walk = (each * a.group + p.v.size - 1) / p.v.size, longest = (a.rows + p.v.size - 1) / p.v.size; // tiles of rows: of a first key, at most
     const int64_t share = (int64_t)a.kv_heads * ((a.tokens + p.v.own - 1) / p.v.own) * walk / 2 / p.v.at_once;
