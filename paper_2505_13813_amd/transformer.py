@@ -337,6 +337,7 @@ class PagedCache:
         if self._capturing():
             raise RuntimeError("a cache grows and releases outside of captured graphs: which pages are free is kept on the host, which has no part in a replay")
 
+    @_outside_graphs
     def _prompts(self, tokens: Optional[int]) -> None:
         """Whole sequences go into the rows that held nothing before they grew; tokens: of each, where all have as many."""
         if self._capturing():
@@ -346,6 +347,7 @@ class PagedCache:
             raise ValueError("whole sequences of %d go into rows that hold nothing else, and have grown by as many: not so row %s" % (tokens, ", ".join(map(str, other))))
         self._grown = [0 if grown == held else grown for grown, held in zip(self._grown, self.counts)]
 
+    @_outside_graphs
     def _newest(self, tokens: int) -> None:
         """So many tokens go into each row that holds something; once more into the same places, until it grows again."""
         if self._capturing():

@@ -373,3 +373,33 @@ def test_a_batch_into_rows_that_hold_something_else_is_refused():
     with pytest.raises(ValueError, match=r"row 0$"):
         m(x, cache=c)
     m(x.flatten(0, 1), torch.tensor([0, 3, 3, 3]), cache=c)  # (where the sequences end is on the device)
+
+
+def test_steps_under_compile_are_compiled_once():
+    """What the host keeps of the cache is no part of a graph: it changes from step to step, and each would be compiled anew."""
+    import torch
+
+    m, c = _decoder_without_kernels(), _host_cache(pages=20, longest=40)
+    graphs = []
+
+    def count(graph, example):
+        graphs.append(graph)
+        return graph.forward
+
+    calls = (lambda run: run(torch.zeros(3, 1, 16), c)), (lambda run: run(torch.zeros(5, 16), torch.tensor([0, 1, 1, 5]), cache=c))
+    for form, call in zip((m.step, m.forward), calls):
+        torch._dynamo.reset()
+        run, first = torch.compile(form, backend=count), None
+        for i in range(1, 6):
+            for row in range(3):
+                c.release(row)
+            c.grow([i, 0, 2])
+            call(run)
+            first = len(graphs) if first is None else first
+        assert len(graphs) == first, form
+    run = torch.compile(m.step, backend=count)
+    c.grow([1, 0, 1])
+    calls[0](run)
+    c.grow([1, 0, 0])
+    with pytest.raises(ValueError, match="row 2"):
+        calls[0](run)
