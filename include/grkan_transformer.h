@@ -1,7 +1,9 @@
 /*
  * grkan_transformer.h - C ABI of the operators that stand around the KAT MLP in a
  * transformer block (gfx950): root-mean-square norm with the residual's addition,
- * rotary positions with several axes, cross attention to an encoder's states.
+ * rotary positions with several axes, cross attention to an encoder's states, causal
+ * attention over packed sequences, a cache of keys and values in pages and attention
+ * over it.
  *
  * Conventions are grkan.h's: DEVICE pointers, caller-owned memory, work enqueued on
  * `hip_stream` without synchronising, argument and launch errors as the status, no

@@ -130,7 +130,8 @@ def paged_write(k, v, k_pages, v_pages, table, lengths, offsets=None) -> None:
     of [pages, kv_heads, page_size, dim]); table int32 [sequences, entries]; lengths int [sequences]: with the new tokens.  k, v [tokens, kv_heads, dim] packed, with
     offsets as in causal_attention, or [sequences, tokens, kv_heads, dim].  A sequence's last new token goes to position lengths[s] - 1, the
     others in front of it.  Tokens of no sequence go nowhere, and neither do those whose entry is no page (below 0, or too large), whose position would be below 0, or
-    whose sequence is longer than its row of the table has place for.  No gradient."""
+    whose sequence is longer than its row of the table has place for.  Where two tokens have one place (a page in two rows), which of them it holds is
+    unspecified.  k and v share no memory with the pages.  No gradient."""
     _taken(binding.load_native().paged_write(k, v, k_pages, v_pages, table, lengths, offsets), "paged_write")
 
 

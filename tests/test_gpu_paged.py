@@ -177,6 +177,26 @@ def test_entries_that_are_no_pages(page):
         assert torch.equal(got.view(torch.int16), w.view(torch.int16))
 
 
+def test_write_with_falling_offsets():
+    """Which tokens go where is unspecified; pages that the table does not name, and places behind the lengths, hold what they held."""
+    import torch
+
+    from paper_2505_13813_amd.transformer import paged_write
+
+    page, lengths = 16, [40, 7, 100, 0]
+    for offsets in ([0, 60, 20, 100, 100], [100, 50, 50, 0, -4], [30, 10, 2 ** 31 - 1, 5, 90]):
+        k_pages, v_pages, table, *_ = _cache(torch, lengths, page, 2, 64, "bf16", 11)
+        before = [t.clone() for t in (k_pages, v_pages)]
+        new = torch.ones(100, 2, 64, dtype=torch.bfloat16, device="cuda:0")
+        paged_write(new, new, k_pages, v_pages, table, torch.tensor(lengths, device="cuda:0"), torch.tensor(offsets, device="cuda:0", dtype=torch.int32))
+        held = torch.zeros(k_pages.shape[:2], dtype=torch.bool, device="cuda:0")
+        for s, n in enumerate(lengths):
+            at = torch.arange(n, device="cuda:0")
+            held[table[s].long()[at // page], at % page] = True
+        for got, w in zip((k_pages, v_pages), before):
+            assert torch.equal(got[~held].view(torch.int16), w[~held].view(torch.int16)), offsets
+
+
 def test_lengths_outside_the_table():
     """A length below 0 is no length, one past the table's places ends there for attention and writes nothing."""
     import torch
